@@ -1,0 +1,397 @@
+"""The operators of quantised transformer blocks whose speed is tracked.
+
+A block served in few bits reads its activations as 8-bit integers with a scale for each token,
+its weights as 8-bit integers with a scale for each output channel, and keeps the keys and
+values of past tokens in 4 bits:
+
+  norm     residual addition, root-mean-square norm and the 8-bit output, row by row
+  matmul   8-bit product, scaled, with bias, residual addition and ReLU in the epilogue
+  cache    the keys and values of new tokens written to the paged 4-bit cache, and tokens read back
+  attend   attention of queries over that cache: single tokens, chunks of a prompt, whole prompts
+
+The 4-bit format: along a head's channels every 32 values share one power of two (a byte, exponent
+plus 127), and each value is a sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6 (two codes to a byte, the
+lower channel in the lower bits).  The exponent is the smallest e with max|x| <= 7 * 2^e.  A cache
+is codes [pages][heads][page size][head size / 2] and exponents [...][head size / 32], for keys and
+for values; a slot is page * page size + place in the page.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+EPS = 1e-6
+E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+# ------------------------------------------------------------------ the cases
+
+def _norm(M, C, dtype, residual):
+    return {"op": "norm", "M": M, "C": C, "dtype": dtype, "residual": residual}
+
+
+def _matmul(M, K, N, out, bias, residual, relu):
+    return {"op": "matmul", "M": M, "K": K, "N": N, "out": out, "bias": bias, "residual": residual, "relu": relu}
+
+
+def _cache(seqs, new, old, heads, D, page):
+    return {"op": "cache", "seqs": seqs, "new": new, "old": old, "heads": heads, "D": D, "page": page}
+
+
+def _attend(seqs, new, longest, heads, kv_heads, D, page, window):
+    return {"op": "attend", "seqs": seqs, "new": new, "longest": longest, "heads": heads, "kv_heads": kv_heads,
+            "D": D, "page": page, "window": window}
+
+
+def listed():
+    return [
+        # One token of one stream through a small block: latency.
+        {"name": "norm_token", **_norm(1, 1024, "bf16", True)},
+        # Odd rows of an fp32 residual stream: a ragged batch of prompts.
+        {"name": "norm_ragged_f32", **_norm(777, 1000, "f32", True)},
+        # A long batch of prompt tokens: bandwidth.
+        {"name": "norm_prompt", **_norm(16384, 4096, "bf16", True)},
+        # The output projection of one token, the residual joined: latency.
+        {"name": "matmul_token", **_matmul(1, 1024, 1024, "bf16", False, True, False)},
+        # A serving batch, one token each: the weights' bandwidth.
+        {"name": "matmul_batch", **_matmul(48, 4096, 4096, "bf16", False, False, False)},
+        # Features of a picture's patches into a thousand classes in fp32: no extent fills a tile.
+        {"name": "matmul_ragged_f32", **_matmul(333, 1999, 1000, "f32", True, False, True)},
+        # The widening projection of a long batch of prompt tokens: the matrix cores' rate.
+        {"name": "matmul_prompt", **_matmul(8192, 4096, 8192, "bf16", True, False, True)},
+        # One new token for each of a few sequences, and a short context read back.
+        {"name": "cache_token", **_cache(4, 1, 60, 8, 128, 64)},
+        # Whole prompts written, and read back for a program that wants them in bf16.
+        {"name": "cache_prompt", **_cache(4, 4000, 0, 8, 128, 64)},
+        # A serving batch, one token each, over caches of ragged lengths: bandwidth.
+        {"name": "attend_tokens", **_attend(16, 1, 32768, 32, 8, 128, 64, 0)},
+        # A short chunk over a window of its context, pages and heads of another size.
+        {"name": "attend_chunk", **_attend(3, 17, 5000, 12, 4, 64, 48, 1000)},
+        # Whole prompts: the matrix cores' rate.
+        {"name": "attend_prompt", **_attend(2, 4096, 4096, 32, 8, 128, 64, 0)},
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """Another case of the same ranges, none dearer than the listed ones of its operator."""
+    while True:
+        op = rng.choice(("norm", "matmul", "matmul", "cache", "attend", "attend"))
+        if op == "norm":
+            C = _log(rng, 64, 8192)
+            C = C if rng.random() < 0.3 else -(-C // 64) * 64
+            c = _norm(_log(rng, 1, 16384), C, rng.choice(("bf16", "bf16", "f32")), rng.random() < 0.7)
+            ok = c["M"] * C * (1 if c["dtype"] == "bf16" else 2) <= 16384 * 4096
+        elif op == "matmul":
+            K, N = _log(rng, 64, 16384), _log(rng, 64, 16384)
+            if rng.random() < 0.7:
+                K, N = -(-K // 64) * 64, -(-N // 64) * 64
+            c = _matmul(_log(rng, 1, 8192), K, N, rng.choice(("bf16", "bf16", "f32")), rng.random() < 0.5,
+                        rng.random() < 0.3, rng.random() < 0.4)
+            ok = c["M"] * K * N <= 8192 * 4096 * 8192 and c["M"] * N <= 8192 * 8192 and K * N <= 1 << 27
+        elif op == "cache":
+            new = 1 if rng.random() < 0.4 else _log(rng, 2, 8000)
+            c = _cache(_log(rng, 1, 64), new, _log(rng, 1, 4000), rng.choice((1, 2, 4, 8, 16)),
+                       rng.choice((64, 64, 96, 128, 128, 128, 256)), rng.choice((16, 32, 48, 64, 64, 128)))
+            ok = c["seqs"] * (2 * new + c["old"]) * c["heads"] * c["D"] <= 4 * 8000 * 8 * 128
+        else:
+            kv = rng.choice((1, 2, 4, 8, 8))
+            new = rng.choice((1, 1, 1, _log(rng, 2, 64), _log(rng, 65, 4096)))
+            c = _attend(_log(rng, 1, 64), new, new + _log(rng, 1, 32768), kv * rng.choice((1, 2, 4, 4, 8)), kv,
+                        rng.choice((64, 64, 96, 128, 128, 128, 256)), rng.choice((16, 32, 48, 64, 64, 128)),
+                        0 if rng.random() < 0.8 else _log(rng, 100, 4000))
+            tokens, scores = c["seqs"] * c["longest"], c["seqs"] * c["heads"] * new * c["longest"]
+            ok = tokens * kv * c["D"] <= 16 * 32768 * 8 * 128 and scores * c["D"] <= 2 * 32 * 4096 * 4096 * 128 and \
+                scores <= 2 * 32 * 4096 * 4096
+        if ok and 3072 not in c.values():
+            return c
+
+
+# ------------------------------------------------------------------ the inputs
+
+def _lengths(case):
+    """Cached tokens of each sequence, the new ones among them: the longest, then ever shorter by a fixed pattern."""
+    n, top, new = case["seqs"], case["longest"], case["new"]
+    return [top if i == 0 else max(new, int(top * (1.0 - 0.6 * ((i * 7) % 11) / 11.0)) - i) for i in range(n)]
+
+
+def _encode(x):
+    """x fp32 [..., D] in the 4-bit format: codes [..., D / 2] and exponent bytes [..., D / 32]."""
+    g = x.reshape(*x.shape[:-1], x.shape[-1] // 32, 32)
+    m, e = torch.frexp(g.abs().amax(-1))
+    e = (torch.where(m > 0.875, e - 2, e - 3)).clamp(-126, 127)
+    e = torch.where(m == 0, torch.full_like(e, -126), e)
+    y = torch.ldexp(g, -e.unsqueeze(-1))
+    a = y.abs()
+    code = (a > 0.25).to(torch.uint8) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0)
+    code = (code + 8 * torch.signbit(y)).to(torch.uint8).reshape(*x.shape[:-1], x.shape[-1] // 2, 2)
+    return code[..., 0] | (code[..., 1] << 4), (e + 127).to(torch.uint8)
+
+
+def _decode(codes, exps):
+    """The values of codes [..., D / 2] with exponent bytes [..., D / 32], fp32 [..., D]."""
+    table = torch.tensor(E2M1 + tuple(-v for v in E2M1), device=codes.device)
+    v = table[torch.stack((codes & 15, codes >> 4), -1).flatten(-2).int()]
+    scale = torch.ldexp(torch.ones((), device=codes.device), exps.int() - 127)
+    return (v.reshape(*exps.shape, 32) * scale.unsqueeze(-1)).reshape(v.shape)
+
+
+def _activations(g, *shape):
+    """Values as hidden states have them: normal, a few channels many times larger than the rest."""
+    x = torch.randn(*shape, generator=g, device="cuda")
+    gain = 1 + 15 * (torch.rand(shape[-1], generator=g, device="cuda") < 0.01)
+    return x * gain
+
+
+def _type(name):
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def _new_cache(g, pages, heads, page, D):
+    """A cache of `pages` pages that hold earlier tokens."""
+    held = _encode(_activations(g, pages * page, heads, D)) + _encode(_activations(g, pages * page, heads, D))
+    return tuple(t.reshape(pages, page, heads, -1).transpose(1, 2).contiguous() for t in held)
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(int(seed))
+    s = dict(case)
+    rand = lambda *shape: torch.rand(*shape, generator=g, device="cuda")  # noqa: E731
+    if case["op"] == "norm":
+        M, C, t = case["M"], case["C"], _type(case["dtype"])
+        s["x"] = (0.2 * _activations(g, M, C)).to(t)
+        s["residual"] = _activations(g, M, C).to(t) if case["residual"] else None
+        s["weight"] = 0.5 + rand(C)
+    elif case["op"] == "matmul":
+        M, K, N = case["M"], case["K"], case["N"]
+        s["a"] = torch.randn(M, K, generator=g, device="cuda").mul_(32).round_().clamp_(-127, 127).to(torch.int8)
+        s["w"] = torch.randn(N, K, generator=g, device="cuda").mul_(32).round_().clamp_(-127, 127).to(torch.int8)
+        s["a_scale"] = 0.01 + 0.03 * rand(M)
+        s["w_scale"] = (0.5 + rand(N)) / (32 * math.sqrt(K))
+        s["bias"] = 0.1 * torch.randn(N, generator=g, device="cuda") if case["bias"] else None
+        s["residual"] = torch.randn(M, N, generator=g, device="cuda").to(_type(case["out"])) if case["residual"] else None
+    elif case["op"] == "cache":
+        n, new, H, D, page = case["seqs"], case["new"], case["heads"], case["D"], case["page"]
+        length = case["old"] + new
+        per = -(-length // page)
+        s["cache"] = _new_cache(g, n * per, H, page, D)
+        table = torch.randperm(n * per, generator=g, device="cuda").reshape(n, per)
+        at = torch.arange(length, device="cuda")
+        slots = (table[:, at // page] * page + at % page).to(torch.int32)
+        s["write"] = slots[:, case["old"]:].reshape(-1).contiguous()
+        s["read"] = slots.reshape(-1).contiguous()
+        kv = _activations(g, n * new, 2 * H * D).to(torch.bfloat16)   # as a fused projection leaves them
+        s["k"], s["v"] = (kv[:, i * H * D:(i + 1) * H * D].unflatten(1, (H, D)) for i in (0, 1))
+    else:
+        n, new, H, KV, D, page = (case[k] for k in ("seqs", "new", "heads", "kv_heads", "D", "page"))
+        lens = _lengths(case)
+        pages = [-(-x // page) for x in lens]
+        s["cache"] = _new_cache(g, sum(pages), KV, page, D)
+        order = torch.randperm(sum(pages), generator=g, device="cuda").to(torch.int32)
+        table = torch.zeros(n, max(pages), dtype=torch.int32, device="cuda")
+        row = torch.repeat_interleave(torch.arange(n), torch.tensor(pages))
+        col = torch.cat([torch.arange(p) for p in pages])
+        table[row.cuda(), col.cuda()] = order
+        s["table"] = table
+        s["lens"] = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        # prompts of one batch differ in length: sequence i brings its own share of the longest's tokens
+        news = [new if i == 0 else max(1, min(lens[i], new - (new * ((i * 5) % 7)) // 16)) for i in range(n)]
+        starts = [0]
+        for x in news:
+            starts.append(starts[-1] + x)
+        s["starts"] = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        s["q"] = (1.5 * torch.randn(starts[-1], H * D, generator=g, device="cuda")).to(torch.bfloat16).unflatten(1, (H, D))
+        s["scale"] = 1.0 / math.sqrt(D) / 2.0
+    return s
+
+
+# ------------------------------------------------------------------ one pass
+
+def _plain_norm(s):
+    x = s["x"].float()
+    h = x if s["residual"] is None else (x + s["residual"].float())
+    h = h.to(s["x"].dtype)
+    f = h.float()
+    t = f * s["weight"]
+    top = t.abs().amax(-1, keepdim=True)
+    r = torch.rsqrt(f.square().mean(-1, keepdim=True) + EPS)
+    q = torch.round(t * torch.div(torch.full_like(top, 127.0), top)).to(torch.int8)
+    out = {"q": q, "scale": (top * r / 127.0).squeeze(-1)}
+    if s["residual"] is not None:
+        out["h"] = h
+    return out
+
+
+def _plain_matmul(s):
+    y = s["a"].float() @ s["w"].float().t()
+    y = y * s["a_scale"].unsqueeze(1) * s["w_scale"]
+    if s["bias"] is not None:
+        y = y + s["bias"]
+    if s["residual"] is not None:
+        y = y + s["residual"].float()
+    if s["relu"]:
+        y = y.clamp_min(0.0)
+    return y.to(_type(s["out"]))
+
+
+def _plain_cache(s):
+    page = s["page"]
+    kc, ke, vc, ve = s["cache"]
+    w, r = s["write"].long(), s["read"].long()
+    kc[w // page, :, w % page], ke[w // page, :, w % page] = _encode(s["k"].float())
+    vc[w // page, :, w % page], ve[w // page, :, w % page] = _encode(s["v"].float())
+    k = _decode(kc[r // page, :, r % page], ke[r // page, :, r % page])
+    v = _decode(vc[r // page, :, r % page], ve[r // page, :, r % page])
+    return {"k": k.to(torch.bfloat16), "v": v.to(torch.bfloat16)}
+
+
+def _plain_attend(s):
+    page, KV, H, D = s["page"], s["kv_heads"], s["heads"], s["D"]
+    kc, ke, vc, ve = s["cache"]
+    table, lens, starts = s["table"].long(), s["lens"].long(), s["starts"].long()
+    n, longest, most = s["seqs"], s["longest"], s["new"]
+    news = starts[1:] - starts[:-1]
+    at = torch.arange(longest, device="cuda")
+    pages, place = table[:, at // page], (at % page).expand(n, -1)
+    # queries as rows of [sequence][key head][token * query head of the group]
+    tok = torch.arange(most, device="cuda")
+    row = (starts[:-1].unsqueeze(1) + tok).clamp_max(s["q"].shape[0] - 1)
+    q = s["q"].float()[row].reshape(n, most, KV, H // KV, D).transpose(1, 2).reshape(n, KV, most * (H // KV), D)
+    k = _decode(kc[pages, :, place], ke[pages, :, place]).transpose(1, 2).contiguous()
+    p = torch.matmul(q, k.transpose(2, 3)).mul_(s["scale"])
+    del k
+    pos = (lens - news).unsqueeze(1) + tok                                  # place of each query in its sequence
+    seen = (at <= pos.unsqueeze(2)) & (at < lens.view(n, 1, 1))
+    if s["window"]:
+        seen &= at > pos.unsqueeze(2) - s["window"]
+    seen = seen.unsqueeze(1).unsqueeze(3)
+    p = p.view(n, KV, most, H // KV, longest).masked_fill_(~seen, float("-inf"))
+    top = p.amax(-1, keepdim=True)
+    p = p.sub_(torch.where(top == float("-inf"), torch.zeros_like(top), top)).exp_()
+    total = p.sum(-1, keepdim=True)
+    v = _decode(vc[pages, :, place], ve[pages, :, place]).transpose(1, 2).contiguous()
+    o = torch.matmul(p.view(n, KV, most * (H // KV), longest), v).view(n, KV, most, H // KV, D)
+    o = torch.where(total > 0, o / total, torch.zeros_like(o))
+    o = o.transpose(1, 2).reshape(n, most, H, D)
+    return o[tok < news.unsqueeze(1)].to(torch.bfloat16)
+
+
+def run(s):
+    if not own:
+        return {"norm": _plain_norm, "matmul": _plain_matmul, "cache": _plain_cache, "attend": _plain_attend}[s["op"]](s)
+    from paper_1907_02154_amd import quant
+    if s["op"] == "norm":
+        q, scale, h = quant.rmsnorm_i8(s["x"], s["weight"], residual=s["residual"], eps=EPS)
+        return {"q": q, "scale": scale} if h is None else {"q": q, "scale": scale, "h": h}
+    if s["op"] == "matmul":
+        return quant.matmul_i8(s["a"], s["a_scale"], s["w"], s["w_scale"], bias=s["bias"], residual=s["residual"],
+                               relu=s["relu"], out_dtype=_type(s["out"]))
+    cache = quant.KV4Cache(*s["cache"])
+    if s["op"] == "cache":
+        quant.kv4_write(s["k"], s["v"], s["write"], cache)
+        k, v = quant.kv4_read(s["read"], cache)
+        return {"k": k, "v": v}
+    return quant.attention_kv4(s["q"], cache, s["table"], s["lens"], starts=s["starts"], max_new=s["new"],
+                               max_len=s["longest"], scale=s["scale"], window=s["window"])
+
+
+# ------------------------------------------------------------------ what a pass cannot do without
+
+def work(case):
+    if case["op"] == "norm":
+        M, C, b = case["M"], case["C"], 2 if case["dtype"] == "bf16" else 4
+        return {"bytes": M * C * (b + 1 + (2 * b if case["residual"] else 0)) + 4 * (M + C), "flops": 6 * M * C}
+    if case["op"] == "matmul":
+        M, K, N, b = case["M"], case["K"], case["N"], 2 if case["out"] == "bf16" else 4
+        return {"bytes": M * K + N * K + M * N * b * (2 if case["residual"] else 1) + 4 * (M + N + (N if case["bias"] else 0)),
+                "flops": 2 * M * K * N}
+    if case["op"] == "cache":
+        H, D = case["heads"], case["D"]
+        held = D // 2 + D // 32
+        new, all_ = case["seqs"] * case["new"], case["seqs"] * (case["new"] + case["old"])
+        return {"bytes": 2 * H * (new * (2 * D + held) + all_ * (2 * D + held)) + 4 * (new + all_), "flops": 2 * H * D * (4 * new + all_)}
+    H, KV, D, win = case["heads"], case["kv_heads"], case["D"], case["window"]
+    lens = _lengths(case)
+    tokens = reads = pairs = 0
+    for i, n in enumerate(lens):
+        new = case["new"] if i == 0 else max(1, min(n, case["new"] - (case["new"] * ((i * 5) % 7)) // 16))
+        tokens += new
+        reads += min(n, win + new - 1) if win else n
+        pairs += sum(min(n - new + j + 1, win) if win else n - new + j + 1 for j in range(new))
+    return {"bytes": tokens * H * D * 4 + reads * KV * 2 * (D // 2 + D // 32), "flops": 4 * pairs * H * D}
+
+
+# ------------------------------------------------------------------ the same in 64 bits
+
+def _values64(codes, exps):
+    """The 4-bit values by the format's fields: sign, two bits of exponent, one of mantissa."""
+    c = torch.stack((codes.to(torch.int64) % 16, codes.to(torch.int64) // 16), -1).flatten(-2)
+    sign, e, m = 1.0 - 2.0 * (c // 8).double(), (c // 2) % 4, (c % 2).double()
+    v = torch.where(e == 0, 0.5 * m, (1 + 0.5 * m) * torch.exp2(e.double() - 1))
+    group = torch.exp2(exps.double() - 127).repeat_interleave(32, -1)
+    return sign * v * group
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "norm":
+        h = s["x"].double()
+        if s["residual"] is not None:
+            h = h + s["residual"].double()
+        kept = h.to(s["x"].dtype).double()          # the stream is held in its own type
+        n = kept.shape[1]
+        rms = (torch.einsum("mc,mc->m", kept, kept) / n + EPS).sqrt()
+        out = {"q": None, "scale": (kept * s["weight"].double()).abs().max(1).values / rms / 127}
+        if s["residual"] is not None:
+            out["h"] = h
+        return out
+    if case["op"] == "matmul":
+        y = torch.mm(s["a"].double() * s["a_scale"].double()[:, None], (s["w"].double() * s["w_scale"].double()[:, None]).t())
+        for extra in (s["bias"], s["residual"]):
+            y = y if extra is None else y + extra.double()
+        return torch.relu(y) if case["relu"] else y
+    page, D = case["page"], case["D"]
+    if case["op"] == "cache":
+        # nearest of the fifteen values, ties to the even code; what was there before is read as it stands
+        out = {}
+        inside = torch.full((s["cache"][0].shape[0] * page,), -1, dtype=torch.int64, device="cuda")
+        inside[s["write"].long()] = torch.arange(len(s["write"]), device="cuda")
+        src = inside[s["read"].long()]
+        slot = s["read"].long()
+        levels = torch.tensor(E2M1, dtype=torch.float64, device="cuda")
+        for name, codes, exps in (("k", *s["cache"][:2]), ("v", *s["cache"][2:])):
+            held = _values64(codes[slot // page, :, slot % page], exps[slot // page, :, slot % page])
+            x = s[name].double().unflatten(-1, (D // 32, 32))
+            top = x.abs().max(-1, keepdim=True).values
+            e = torch.ceil(torch.log2(top.clamp_min(2.0 ** -130) / 7.0)).clamp(-126, 127)
+            u = x.abs() / torch.exp2(e)
+            lo = (torch.searchsorted(levels, u.clamp_max(6.0).contiguous(), right=True) - 1).clamp(0, 6)
+            up = u.clamp_max(6.0) - levels[lo] - (levels[lo + 1] - u.clamp_max(6.0))
+            pick = torch.where(up > 0, lo + 1, torch.where(up < 0, lo, lo + lo % 2))
+            y = (torch.sign(x) * levels[pick] * torch.exp2(e)).flatten(-2)
+            out[name] = torch.where((src >= 0)[:, None, None], y[src.clamp_min(0)], held)
+        return out
+    H, KV = case["heads"], case["kv_heads"]
+    starts, lens, table = s["starts"].tolist(), s["lens"].tolist(), s["table"].long()
+    out = torch.zeros(starts[-1], H, D, dtype=torch.float64, device="cuda")
+    for b, n in enumerate(lens):
+        q = s["q"][starts[b]:starts[b + 1]].double()
+        at = torch.arange(n, device="cuda")
+        pg, place = table[b, at // page], at % page
+        pos = n - q.shape[0] + torch.arange(q.shape[0], device="cuda")
+        bad = at[None, :] > pos[:, None]
+        if case["window"]:
+            bad |= pos[:, None] - at[None, :] >= case["window"]
+        for h in range(KV):
+            k = _values64(s["cache"][0][pg, h, place], s["cache"][1][pg, h, place])
+            v = _values64(s["cache"][2][pg, h, place], s["cache"][3][pg, h, place])
+            for j in range(h * (H // KV), (h + 1) * (H // KV)):
+                score = (q[:, j] @ k.t() * s["scale"]).masked_fill(bad, -math.inf)
+                out[starts[b]:starts[b + 1], j] = torch.softmax(score, -1) @ v
+    return out
