@@ -11,8 +11,8 @@ values of past tokens in 4 bits:
 
 The 4-bit format: along a head's channels every 32 values share one power of two (a byte, exponent
 plus 127), and each value is a sign and one of 0, .5, 1, 1.5, 2, 3, 4, 6 (two codes to a byte, the
-lower channel in the lower bits).  The exponent is the smallest e with max|x| <= 7 * 2^e.  A cache
-is codes [pages][heads][page size][head size / 2] and exponents [...][head size / 32], for keys and
+lower channel in the lower bits).  The exponent is the smallest e with max|x| <= 7 * 2^e, held to
+-126 .. 125.  A cache is codes [pages][heads][page size][head size / 2] and exponents [...][head size / 32], for keys and
 for values; a slot is page * page size + place in the page.
 """
 from __future__ import annotations
@@ -125,7 +125,7 @@ def _encode(x):
     """x fp32 [..., D] in the 4-bit format: codes [..., D / 2] and exponent bytes [..., D / 32]."""
     g = x.reshape(*x.shape[:-1], x.shape[-1] // 32, 32)
     m, e = torch.frexp(g.abs().amax(-1))
-    e = (torch.where(m > 0.875, e - 2, e - 3)).clamp(-126, 127)
+    e = (torch.where(m > 0.875, e - 2, e - 3)).clamp(-126, 125)
     e = torch.where(m == 0, torch.full_like(e, -126), e)
     y = torch.ldexp(g, -e.unsqueeze(-1))
     a = y.abs()
@@ -369,7 +369,7 @@ def exact(case, seed):
             held = _values64(codes[slot // page, :, slot % page], exps[slot // page, :, slot % page])
             x = s[name].double().unflatten(-1, (D // 32, 32))
             top = x.abs().max(-1, keepdim=True).values
-            e = torch.ceil(torch.log2(top.clamp_min(2.0 ** -130) / 7.0)).clamp(-126, 127)
+            e = torch.ceil(torch.log2(top.clamp_min(2.0 ** -130) / 7.0)).clamp(-126, 125)
             u = x.abs() / torch.exp2(e)
             lo = (torch.searchsorted(levels, u.clamp_max(6.0).contiguous(), right=True) - 1).clamp(0, 6)
             up = u.clamp_max(6.0) - levels[lo] - (levels[lo + 1] - u.clamp_max(6.0))
