@@ -1,0 +1,418 @@
+// Attention over the paged 4-bit cache (quant_attention_kv4).
+//
+// Scores are computed transposed, S^T = K Q^T: the cached tokens are the rows
+// of the matrix instruction and the queries its columns, so each lane holds
+// scores of one query, and the probabilities leave the softmax in the very
+// layout in which O^T = V^T P^T reads them as its second operand (the order of
+// the tokens within a product's reduction is free).  One pass over the cache
+// with a running maximum m and sum l: O and l are rescaled by 2^(m - m') when
+// the maximum grows by more than 2^8, which leaves the quotient O / l as it is
+// and the probabilities below 2^8.
+//
+// Queries that share a key head are the rows of one problem: row = token *
+// (heads / key heads) + head within the group.
+#include "quant.h"
+
+namespace miconv {
+namespace quant {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr float kNegInf = -__builtin_inff();
+constexpr float kGrow = 8.0f;   // log2 of how far scores may pass the running maximum before it moves
+
+struct AttArgs {
+    Kv4 c;
+    const uint16_t *q;
+    uint16_t *out;
+    const int32_t *starts, *lens, *table;
+    float *part;           // split partials: [seq][head][max_new][splits] rows of (D sums, m, l), or null
+    long qs, os;           // row strides in elements
+    long tokens;
+    int seqs, heads, group, table_stride;
+    int max_new, max_len;
+    int causal, window;
+    int splits, per_split; // cached tokens a split handles
+    int row_blocks;
+    float scale;           // of the scores, times log2(e)
+    FastDiv dv_group;
+};
+
+// What a work-group works on: a sequence's queries and length, clamped.
+struct Seq {
+    long row0;   // first row of q
+    int news, len;
+};
+
+__device__ __forceinline__ Seq sequence(const AttArgs &a, int s)
+{
+    Seq r;
+    long b = a.starts ? a.starts[s] : s, e = a.starts ? a.starts[s + 1] : s + 1;
+    b = b < 0 ? 0 : b > a.tokens ? a.tokens : b;
+    e = e < b ? b : e > a.tokens ? a.tokens : e;
+    r.row0 = b;
+    r.news = (int)(e - b);
+    const long room = (long)a.table_stride * a.c.page_size;
+    const int most = room < a.max_len ? (int)room : a.max_len;
+    const int n = a.lens[s];
+    r.len = n < 0 ? 0 : n > most ? most : n;
+    return r;
+}
+
+// The places query row i of a sequence sees: lo .. hi - 1.
+__device__ __forceinline__ void seen(const AttArgs &a, const Seq &q, int i, int *lo, int *hi)
+{
+    const int p = q.len - q.news + i;
+    int h = a.causal ? p + 1 : q.len;
+    h = h > q.len ? q.len : h;
+    const int l = a.window > 0 ? p - a.window + 1 : 0;
+    *lo = l < 0 ? 0 : l;
+    *hi = h < 0 ? 0 : h;
+}
+
+__device__ __forceinline__ long cached_row(const AttArgs &a, const int32_t *pages, int kvh, int t)
+{
+    const unsigned p = fdiv((unsigned)t, a.c.dv_page), place = (unsigned)t - p * (unsigned)a.c.page_size;
+    long page = pages[p];
+    const long last = a.c.slots / a.c.page_size - 1;
+    page = page < 0 ? 0 : page > last ? last : page;
+    return (page * a.c.heads + kvh) * a.c.page_size + place;
+}
+
+// Scale bits of an exponent byte; above 252 an infinite scale, which converts to NaN.
+__device__ __forceinline__ float exp_scale(uint32_t e)
+{
+    return __builtin_bit_cast(float, (e > kMaxExp ? 255u : e) << 23);
+}
+
+__device__ __forceinline__ bf16x8 widen8(uint32_t code, float s)
+{
+    u32x4 r = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3))};
+    return __builtin_bit_cast(bf16x8, r);
+}
+
+// Four wavefronts share 16 * NB query rows and take turns at tiles of 32
+// cached tokens; their sums meet in LDS at the end.
+template <int D, int NB>
+__global__ __launch_bounds__(256) void attend_kv4_kernel(AttArgs a)
+{
+    constexpr int NU = D / 32;           // units of 8 channels a lane holds of a cached row
+    constexpr int CB = D / 16;           // blocks of 16 channels
+    constexpr int PITCH = D * 2 + 32;    // bytes of a widened row in LDS
+    constexpr int VBYTES = 32 * PITCH;   // a wavefront's tile of values
+    constexpr int OPITCH = D + 4;        // floats of a query's sums in LDS
+    constexpr int OBYTES = 16 * NB * OPITCH * 4;
+    constexpr int LDS = 4 * VBYTES > OBYTES ? 4 * VBYTES : OBYTES;
+    __shared__ __align__(16) unsigned char lds[LDS];
+    __shared__ float sm[4][16 * NB], sl[4][16 * NB];
+
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int col = lane % 16, quad = lane / 16;
+    const int split = blockIdx.x % a.splits, rb = blockIdx.x / a.splits, kvh = blockIdx.y, s = blockIdx.z;
+    const Seq sq = sequence(a, s);
+    const int rows = (sq.news < a.max_new ? sq.news : a.max_new) * a.group, r0 = rb * 16 * NB;
+    if (r0 >= rows) return;
+    const int r_last = r0 + 16 * NB < rows ? r0 + 16 * NB - 1 : rows - 1;
+
+    // the places any row of the block sees, within this split
+    int lo, hi, x;
+    seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), &lo, &x);
+    seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), &x, &hi);
+    const int s_lo = split * a.per_split;
+    const int s_hi = s_lo + a.per_split;
+    lo = (lo > s_lo ? lo : s_lo) & ~31;   // per_split is a multiple of 32
+    hi = hi < s_hi ? hi : s_hi;
+
+    int q_lo[NB], q_hi[NB];
+    bf16x8 qf[NB][NU];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int r = r0 + 16 * b + col;
+        const bool live = r < rows;
+        const int i = (int)fdiv((unsigned)(live ? r : 0), a.dv_group), h = kvh * a.group + (live ? r : 0) - i * a.group;
+        seen(a, sq, i, &q_lo[b], &q_hi[b]);
+        if (!live) q_hi[b] = 0;
+        const uint16_t *qr = a.q + (sq.row0 + i) * a.qs + (long)h * D + quad * (D / 4);
+#pragma unroll
+        for (int u = 0; u < NU; ++u) memcpy(&qf[b][u], qr + 8 * u, 16);
+    }
+
+    float m[NB], l[NB];
+    f32x4 o[CB][NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        m[b] = kNegInf, l[b] = 0.0f;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) o[cb][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    const int32_t *pages = a.table + (long)s * a.table_stride;
+    unsigned char *vt = lds + wave * VBYTES;
+    for (int t0 = lo + 32 * wave; t0 < hi; t0 += 128) {
+        f32x4 sc[2][NB];
+        u32x4 vw[2][NU];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            int t = t0 + 16 * k + col;
+            t = t < hi ? t : hi - 1;   // past the end: a row that is seen, masked below
+            const long row = cached_row(a, pages, kvh, t);
+            uint32_t kc[NU], vc[NU];
+            memcpy(kc, a.c.kc + row * (D / 2) + quad * (D / 8), 4 * NU);
+            memcpy(vc, a.c.vc + row * (D / 2) + quad * (D / 8), 4 * NU);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sc[k][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                const long at = row * (D / 32) + (quad * NU + u) / 4;
+                uint32_t ke = a.c.ke[at], ve = a.c.ve[at];
+                // A value that is not finite makes the token's score NaN, which reaches
+                // the queries that see it; its own NaN times a probability of 0 would
+                // reach the others too.
+                if (ve > kMaxExp) ve = 127, ke = 255;
+                const bf16x8 kf = widen8(kc[u], exp_scale(ke));
+                vw[k][u] = __builtin_bit_cast(u32x4, widen8(vc[u], exp_scale(ve)));
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    sc[k][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[b][u], sc[k][b], 0, 0, 0);
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+                *(u32x4 *)(vt + (16 * k + col) * PITCH + quad * (D / 2) + 16 * u) = vw[k][u];
+
+        bf16x8 pf[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            float top = kNegInf, p[8];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = t0 + 16 * k + 4 * quad + i;
+                    const float v = t >= q_lo[b] && t < q_hi[b] ? sc[k][b][i] * a.scale : kNegInf;
+                    p[4 * k + i] = v;
+                    top = fmaxf(top, v);
+                }
+            if (__any(top > m[b] + kGrow)) {   // also where m is still -inf
+                top = fmaxf(top, m[b]);
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float f = top == m[b] ? 1.0f : __builtin_amdgcn_exp2f(m[b] - top);
+                m[b] = top;
+                l[b] *= f;
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) o[cb][b] *= f;
+            }
+            const float base = m[b] == kNegInf ? 0.0f : m[b];
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = pack_bf16x2(__builtin_amdgcn_exp2f(p[2 * i] - base), __builtin_amdgcn_exp2f(p[2 * i + 1] - base));
+                l[b] += __builtin_bit_cast(float, w[i] << 16) + __builtin_bit_cast(float, w[i] & 0xFFFF0000u);
+            }
+            pf[b] = __builtin_bit_cast(bf16x8, w);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        // a lane's 8 tokens of the reduction: 4 * quad .. + 3 of each 16, as the scores have them
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            const unsigned char *at = vt + (4 * quad + col / 4) * PITCH + cb * 32 + (col % 4) * 8;
+            s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+            s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 16 * PITCH));
+            const bf16x8 vf = __builtin_shufflevector(__builtin_bit_cast(bf16x4, v0), __builtin_bit_cast(bf16x4, v1), 0, 1, 2,
+                                                      3, 4, 5, 6, 7);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                o[cb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[b], o[cb][b], 0, 0, 0);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+
+    // The four wavefronts' sums: the joint maximum first, then O, one wavefront after another.
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        l[b] += __shfl_xor(l[b], 16);
+        l[b] += __shfl_xor(l[b], 32);
+        if (quad == 0) sm[wave][16 * b + col] = m[b], sl[wave][16 * b + col] = l[b];
+    }
+    __syncthreads();
+    float *sum = (float *)lds;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (wave == w)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const int r = 16 * b + col;
+                const float mm = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
+                const float f = m[b] == mm ? 1.0f : __builtin_amdgcn_exp2f(m[b] - mm);
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    f32x4 *at = (f32x4 *)(sum + r * OPITCH + cb * 16 + 4 * quad);
+                    *at = w == 0 ? o[cb][b] * f : *at + o[cb][b] * f;
+                }
+            }
+        __syncthreads();
+    }
+    // rows out, 8 channels a thread
+    for (int i = threadIdx.x; i < 16 * NB * (D / 8); i += 256) {
+        const int r = i / (D / 8), u = i % (D / 8);
+        if (r0 + r >= rows) break;
+        const float mm = fmaxf(fmaxf(sm[0][r], sm[1][r]), fmaxf(sm[2][r], sm[3][r]));
+        float ll = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) ll += sl[w][r] * (sm[w][r] == mm ? 1.0f : __builtin_amdgcn_exp2f(sm[w][r] - mm));
+        float v[8];
+        memcpy(v, sum + r * OPITCH + 8 * u, 32);
+        const int t = (int)fdiv((unsigned)(r0 + r), a.dv_group), h = kvh * a.group + (r0 + r) - t * a.group;
+        if (a.splits == 1) {
+            const float f = ll == 0.0f ? 0.0f : 1.0f / ll;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= f;
+            store8(a.out + (sq.row0 + t) * a.os + (long)h * D + 8 * u, v);
+        } else {
+            float *part = a.part + ((((long)s * a.heads + h) * a.max_new + t) * a.splits + split) * (D + 4);
+            memcpy(part + 8 * u, v, 32);
+            if (u == 0) part[D] = mm, part[D + 1] = ll;
+        }
+    }
+}
+
+// Joins the splits of one row: a wavefront each.
+template <int D>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttArgs a)
+{
+    const int lane = threadIdx.x % 64, h = blockIdx.y, s = blockIdx.z;
+    const int t = blockIdx.x * 4 + threadIdx.x / 64;
+    const Seq sq = sequence(a, s);
+    if (t >= sq.news || t >= a.max_new) return;
+    const float *part = a.part + (((long)s * a.heads + h) * a.max_new + t) * a.splits * (D + 4);
+    float mm = kNegInf;
+    for (int i = 0; i < a.splits; ++i) mm = fmaxf(mm, part[(long)i * (D + 4) + D]);
+    constexpr int PER = (D + 63) / 64;
+    float l = 0.0f, v[PER] = {};
+    for (int i = 0; i < a.splits; ++i) {
+        const float *p = part + (long)i * (D + 4);
+        const float f = p[D] == mm ? 1.0f : __builtin_amdgcn_exp2f(p[D] - mm);
+        l += p[D + 1] * f;
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (j * 64 + lane < D) v[j] += p[j * 64 + lane] * f;
+    }
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+        if (j * 64 + lane < D) store1(a.out + (sq.row0 + t) * a.os + (long)h * D + j * 64 + lane, v[j] * f);
+}
+
+struct AttPlan {
+    int nb, row_blocks, splits, per_split;
+    size_t bytes;
+};
+
+AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len)
+{
+    AttPlan p;
+    const long rows = (long)max_new * (heads / c.heads);
+    p.nb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    if (c.dim > 128 && p.nb > 2) p.nb = 2;
+    p.row_blocks = (int)((rows + 16 * p.nb - 1) / (16 * p.nb));
+    const long groups = (long)seqs * c.heads * p.row_blocks;
+    const int cus = cu_count() > 0 ? cu_count() : 256;
+    long want = (4L * cus + groups - 1) / groups;                     // work-groups for four on a compute unit
+    const long most = (max_len + 511L) / 512;                         // at least 512 tokens each
+    want = want < 1 ? 1 : want > most ? most : want;
+    p.per_split = (int)(((max_len + want - 1) / want + 31) / 32 * 32);
+    p.splits = (int)((max_len + (long)p.per_split - 1) / p.per_split);
+    p.bytes = p.splits > 1 ? (size_t)seqs * heads * max_new * p.splits * (c.dim + 4) * 4 : 0;
+    return p;
+}
+
+int check_attend(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len, Kv4 *c)
+{
+    const int rc = kv4_view(cache, c);
+    if (rc != MICONV_OK) return rc;
+    if (seqs < 0 || heads < 1 || heads % c->heads || max_new < 1 || max_len < 1) return MICONV_ERR_SHAPE;
+    if ((long)max_new * (heads / c->heads) >= 1L << 30 || max_len >= 1 << 30 || seqs > 65535 || heads > 65535)
+        return MICONV_ERR_TOO_LARGE;
+    return MICONV_OK;
+}
+
+template <int D>
+int launch_attend(const AttArgs &a, const AttPlan &p, hipStream_t st)
+{
+    const dim3 grid((unsigned)((long)p.row_blocks * p.splits), (unsigned)a.c.heads, (unsigned)a.seqs);
+    void (*k)(AttArgs) = p.nb == 1 ? attend_kv4_kernel<D, 1> : attend_kv4_kernel<D, 2>;
+    if constexpr (D <= 128)
+        if (p.nb == 4) k = attend_kv4_kernel<D, 4>;
+    launch_kernel(k, grid, dim3(256), 0, st, a);
+    int rc = launched();
+    if (rc != MICONV_OK || p.splits == 1) return rc;
+    launch_kernel(attend_join_kernel<D>, dim3((unsigned)ceil_div(a.max_new, 4), (unsigned)a.heads, (unsigned)a.seqs),
+                  dim3(256), 0, st, a);
+    return launched();
+}
+
+}  // namespace
+}  // namespace quant
+}  // namespace miconv
+
+extern "C" long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len)
+{
+    miconv::quant::Kv4 c;
+    const int rc = miconv::quant::check_attend(cache, seqs, heads, max_new, max_len, &c);
+    if (rc != MICONV_OK) return rc;
+    return seqs ? (long)miconv::quant::plan_attend(c, seqs, heads, max_new, max_len).bytes : 0;
+}
+
+extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, long tokens, const void *q,
+                                   long q_stride, const int32_t *starts, const int32_t *lens, const int32_t *table,
+                                   int table_stride, int max_new, int max_len, float scale, int causal, int window,
+                                   void *out, long out_stride, void *ws, size_t ws_bytes, void *stream)
+{
+    using namespace miconv;
+    quant::AttArgs a = {};
+    const int rc = quant::check_attend(cache, seqs, heads, max_new, max_len, &a.c);
+    if (rc != MICONV_OK) return rc;
+    const long width = (long)heads * a.c.dim;
+    if (tokens < 0 || q_stride < width || out_stride < width || table_stride < 1) return MICONV_ERR_SHAPE;
+    if (tokens >= 1L << 31) return MICONV_ERR_TOO_LARGE;
+    if (seqs == 0 || tokens == 0) return MICONV_OK;
+    if (!q || !out || !lens || !table) return MICONV_ERR_NULL;
+    if (quant::misaligned(q, 2) || quant::misaligned(out, 2) || quant::misaligned(starts, 4) ||
+        quant::misaligned(lens, 4) || quant::misaligned(table, 4))
+        return MICONV_ERR_ALIGN;
+    const quant::AttPlan p = quant::plan_attend(a.c, seqs, heads, max_new, max_len);
+    if ((long)p.row_blocks * p.splits >= 1L << 31) return MICONV_ERR_TOO_LARGE;
+    if (p.bytes && (!ws || ws_bytes < p.bytes || quant::misaligned(ws, 256))) return MICONV_ERR_WORKSPACE;
+    a.q = (const uint16_t *)q, a.out = (uint16_t *)out;
+    a.starts = starts, a.lens = lens, a.table = table;
+    a.part = (float *)ws;
+    a.qs = q_stride, a.os = out_stride, a.tokens = tokens;
+    a.seqs = seqs, a.heads = heads, a.group = heads / a.c.heads, a.table_stride = table_stride;
+    a.max_new = max_new, a.max_len = max_len;
+    a.causal = causal, a.window = window;
+    a.splits = p.splits, a.per_split = p.per_split, a.row_blocks = p.row_blocks;
+    a.scale = scale * 1.44269504088896340736f;
+    a.dv_group = make_fastdiv((unsigned)a.group);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    switch (a.c.dim) {
+    case 32: return quant::launch_attend<32>(a, p, st);
+    case 64: return quant::launch_attend<64>(a, p, st);
+    case 96: return quant::launch_attend<96>(a, p, st);
+    case 128: return quant::launch_attend<128>(a, p, st);
+    case 192: return quant::launch_attend<192>(a, p, st);
+    default: return quant::launch_attend<256>(a, p, st);
+    }
+}

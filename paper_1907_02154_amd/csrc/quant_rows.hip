@@ -1,0 +1,253 @@
+// Root-mean-square norm with the residual's addition and an 8-bit output, and
+// the 8-bit output alone (quant_rmsnorm_i8, quant_rows_i8).
+//
+// With t = h * w and r = 1 / sqrt(mean(h^2) + eps) the normed row is t * r, its
+// largest magnitude A * r with A = max |t|, and its 8-bit value
+// rint(t * r * 127 / (A * r)) = rint(t * (127 / A)): r cancels.  So q depends
+// on a maximum alone, which no order of evaluation changes, and the sum
+// reaches the scale only.
+//
+// Bound by memory: a row is read once, kept in registers across the one
+// reduction (sum and maximum together), and written once.
+#include "quant.h"
+
+namespace miconv {
+namespace quant {
+namespace {
+
+struct RowArgs {
+    const void *x, *res;
+    const float *w;
+    void *h;
+    int8_t *q;
+    float *scale;
+    long xs, rs, hs, qs;   // row strides in elements
+    long rows;
+    int cols;
+    int norm;              // 0: the 8-bit output alone
+    float eps;
+};
+
+struct RowStat {
+    float sum;       // of h^2
+    uint32_t top;    // largest |t| as its bits: ordered like the magnitudes, infinity and NaN above all
+};
+
+__device__ __forceinline__ RowStat join(RowStat a, RowStat b)
+{
+    return RowStat{a.sum + b.sum, a.top > b.top ? a.top : b.top};
+}
+
+__device__ __forceinline__ RowStat wave_join(RowStat s)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) s = join(s, RowStat{__shfl_xor(s.sum, d), (uint32_t)__shfl_xor((int)s.top, d)});
+    return s;
+}
+
+// 127 / A and the row's scale.
+__device__ __forceinline__ float row_factor(const RowArgs &a, RowStat s, float *scale)
+{
+    const float top = __builtin_bit_cast(float, s.top);
+    if (s.top >= 0x7F800000u) {
+        *scale = __builtin_nanf("");
+        return 0.0f;
+    }
+    if (top < 0x1p-100f) {   // 127 / A would overflow
+        *scale = 0.0f;
+        return 0.0f;
+    }
+    const float r = a.norm ? 1.0f / sqrtf(s.sum / (float)a.cols + a.eps) : 1.0f;
+    *scale = top * r / 127.0f;
+    return 127.0f / top;
+}
+
+__device__ __forceinline__ uint32_t quant4(const float *t, float f)
+{
+    uint32_t v = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v |= ((uint32_t)(int)rintf(t[i] * f) & 255u) << (8 * i);
+    return v;
+}
+
+// One unit of up to 8 elements at p: h (rounded to T) and its part of the statistics.
+template <typename T>
+__device__ __forceinline__ void row_unit(const RowArgs &a, const T *x, const T *res, T *h, int at, int n, float (&t)[8],
+                                         RowStat &s)
+{
+    float w[8];
+    if (n == 8) {
+        load8(x + at, t);
+        if (res) {
+            float r[8];
+            load8(res + at, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = rounded(t[i] + r[i], x);
+            store8(h + at, t);
+        }
+        if (a.w) load8(a.w + at, w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            t[i] = w[i] = 0.0f;
+            if (i < n) {
+                t[i] = load1(x + at + i);
+                if (res) {
+                    t[i] = rounded(t[i] + load1(res + at + i), x);
+                    store1(h + at + i, t[i]);
+                }
+                if (a.w) w[i] = a.w[at + i];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        s.sum += t[i] * t[i];
+        if (a.w) t[i] *= w[i];
+        const uint32_t b = __builtin_bit_cast(uint32_t, t[i]) & 0x7FFFFFFFu;
+        s.top = b > s.top ? b : s.top;
+    }
+}
+
+__device__ __forceinline__ void store_q(int8_t *q, int n, const float (&t)[8], float f)
+{
+    // f is 0 where q is: a NaN or an infinity times 0 must not reach the conversion
+    uint32_t v[2] = {0, 0};
+    if (f != 0.0f) v[0] = quant4(t, f), v[1] = quant4(t + 4, f);
+    if (n == 8) {
+        memcpy(q, v, 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) q[i] = (int8_t)(v[i / 4] >> (8 * (i % 4)));
+    }
+}
+
+// LANES threads (a wavefront, or the whole work-group) share a row, U units of
+// 8 elements each.
+template <typename T, int LANES, int U>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rows_i8_kernel(RowArgs a)
+{
+    constexpr int NT = LANES < 256 ? 256 : LANES, WAVES = LANES / 64;
+    __shared__ RowStat part[WAVES > 1 ? WAVES : 1];
+    const int lane = threadIdx.x % LANES;
+    const long row = (long)blockIdx.x * (NT / LANES) + threadIdx.x / LANES;
+    if (row >= a.rows) return;   // whole wavefronts; with LANES > 64 the grid has no such row
+    const T *x = (const T *)a.x + row * a.xs;
+    const T *res = a.res ? (const T *)a.res + row * a.rs : nullptr;
+    T *h = a.res ? (T *)a.h + row * a.hs : nullptr;
+    float t[U][8];
+    RowStat s = {0.0f, 0u};
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int at = (u * LANES + lane) * 8, n = a.cols - at;
+        if (n > 0) row_unit(a, x, res, h, at, n < 8 ? n : 8, t[u], s);
+    }
+    s = wave_join(s);
+    if (WAVES > 1) {
+        if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = s;
+        __syncthreads();
+        s = part[0];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) s = join(s, part[i]);
+    }
+    float scale;
+    const float f = row_factor(a, s, &scale);
+    int8_t *q = a.q + row * a.qs;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int at = (u * LANES + lane) * 8, n = a.cols - at;
+        if (n > 0) store_q(q + at, n < 8 ? n : 8, t[u], f);
+    }
+    if (lane == 0) a.scale[row] = scale;
+}
+
+// Rows longer than the registers of a work-group hold: h is read again for the
+// second pass (each thread reads back what it wrote itself).
+template <typename T>
+__global__ __launch_bounds__(1024) void rows_i8_long_kernel(RowArgs a)
+{
+    __shared__ RowStat part[16];
+    const long row = blockIdx.x;
+    const T *x = (const T *)a.x + row * a.xs;
+    const T *res = a.res ? (const T *)a.res + row * a.rs : nullptr;
+    T *h = a.res ? (T *)a.h + row * a.hs : nullptr;
+    RowStat s = {0.0f, 0u};
+    float t[8];
+    for (long at = threadIdx.x * 8; at < a.cols; at += 1024 * 8)
+        row_unit(a, x, res, h, (int)at, a.cols - at < 8 ? (int)(a.cols - at) : 8, t, s);
+    s = wave_join(s);
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = s;
+    __syncthreads();
+    s = part[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s = join(s, part[i]);
+    float scale;
+    const float f = row_factor(a, s, &scale);
+    int8_t *q = a.q + row * a.qs;
+    const T *kept = a.res ? h : x;
+    for (long at = threadIdx.x * 8; at < a.cols; at += 1024 * 8) {
+        const int n = a.cols - at < 8 ? (int)(a.cols - at) : 8;
+        row_unit(a, kept, (const T *)nullptr, (T *)nullptr, (int)at, n, t, s);
+        store_q(q + at, n, t, f);
+    }
+    if (threadIdx.x == 0) a.scale[row] = scale;
+}
+
+template <typename T, int LANES, int U>
+void go(const RowArgs &a, hipStream_t st)
+{
+    constexpr int NT = LANES < 256 ? 256 : LANES;
+    const long per = NT / LANES;
+    launch_kernel(rows_i8_kernel<T, LANES, U>, dim3((unsigned)((a.rows + per - 1) / per)), dim3(NT), 0, st, a);
+}
+
+template <typename T>
+int launch_rows(const RowArgs &a, hipStream_t st)
+{
+    const int units = ceil_div(a.cols, 8);
+    if (units <= 64) go<T, 64, 1>(a, st);
+    else if (units <= 128) go<T, 64, 2>(a, st);
+    else if (units <= 256) go<T, 256, 1>(a, st);
+    else if (units <= 512) go<T, 256, 2>(a, st);
+    else if (units <= 1024) go<T, 256, 4>(a, st);
+    else if (units <= 4096) go<T, 1024, 4>(a, st);
+    else launch_kernel(rows_i8_long_kernel<T>, dim3((unsigned)a.rows), dim3(1024), 0, st, a);
+    return launched();
+}
+
+int run_rows(RowArgs a, long cols, int dtype, hipStream_t st)
+{
+    const int b = dtype_bytes(dtype);
+    if (!b) return MICONV_ERR_UNSUPPORTED;
+    if (a.rows < 0 || cols < 1 || a.xs < cols || a.qs < cols || !(a.eps >= 0.0f)) return MICONV_ERR_SHAPE;
+    if (a.rows >= 1L << 31 || cols >= 1L << 31) return MICONV_ERR_TOO_LARGE;
+    if (!a.res != !a.h) return MICONV_ERR_NULL;
+    if (a.res && (a.rs < cols || a.hs < cols)) return MICONV_ERR_SHAPE;
+    if (a.rows == 0) return MICONV_OK;
+    if (!a.x || !a.q || !a.scale) return MICONV_ERR_NULL;
+    if (misaligned(a.x, b) || misaligned(a.res, b) || misaligned(a.h, b) || misaligned(a.w, 4) || misaligned(a.scale, 4))
+        return MICONV_ERR_ALIGN;
+    a.cols = (int)cols;
+    return dtype == kF32 ? launch_rows<float>(a, st) : launch_rows<uint16_t>(a, st);
+}
+
+}  // namespace
+}  // namespace quant
+}  // namespace miconv
+
+extern "C" int quant_rmsnorm_i8(long rows, long cols, int dtype, const void *x, long x_stride, const void *residual,
+                                long residual_stride, const float *weight, float eps, void *h, long h_stride,
+                                int8_t *q, long q_stride, float *scale, void *stream)
+{
+    miconv::quant::RowArgs a = {x, residual, weight, h, q, scale, x_stride, residual_stride, h_stride, q_stride,
+                                rows, 0, 1, eps};
+    return miconv::quant::run_rows(a, cols, dtype, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int quant_rows_i8(long rows, long cols, int dtype, const void *x, long x_stride, int8_t *q,
+                             long q_stride, float *scale, void *stream)
+{
+    miconv::quant::RowArgs a = {x, nullptr, nullptr, nullptr, q, scale, x_stride, 0, 0, q_stride, rows, 0, 0, 0.0f};
+    return miconv::quant::run_rows(a, cols, dtype, static_cast<hipStream_t>(stream));
+}

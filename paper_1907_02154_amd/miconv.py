@@ -18,7 +18,7 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libmiconv.so")
 HEADER = os.path.join(os.path.dirname(_PKG), "include", "miconv.h")
-HEADERS = [HEADER, os.path.join(os.path.dirname(_PKG), "include", "mivision.h")]
+HEADERS = [HEADER, *(os.path.join(os.path.dirname(_PKG), "include", h) for h in ("mivision.h", "miquant.h"))]
 
 OK = 0
 (ERR_NULL, ERR_SHAPE, ERR_GROUPS, ERR_UNSUPPORTED, ERR_TOO_LARGE, ERR_ALIGN, ERR_HIP,
@@ -113,7 +113,7 @@ def lib() -> ctypes.CDLL:
 
 
 def header_functions() -> list:
-    """Names of the functions ``include/miconv.h`` and ``include/mivision.h`` declare."""
+    """Names of the functions ``include/miconv.h``, ``mivision.h`` and ``miquant.h`` declare."""
     names = set()
     for h in HEADERS:
         with open(h) as f:

@@ -1,0 +1,336 @@
+"""Thin Python binding over the operators of quantised transformer blocks in
+libmiconv.so (``include/miquant.h``): the norm with an 8-bit output, the 8-bit
+matrix product, the paged 4-bit cache of keys and values, and attention over it.
+
+Argument marshalling only, as in ``miconv``: dtype / device / shape checks, raw
+device pointers, torch's current HIP stream, and outputs and a workspace
+allocated here when the caller passes none (the C entry points never allocate).
+With ``stream=`` these are allocated on that stream, so that its work may use
+them at once.  All arithmetic runs in the library's HIP kernels.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+
+from . import miconv
+from .miconv import _check, _ptr, _stream
+
+HEAD_DIMS = (32, 64, 96, 128, 192, 256)
+_CODE = {torch.float32: 0, torch.bfloat16: 1}
+
+
+class _Kv4(ctypes.Structure):
+    """quant_kv4"""
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_exps", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_exps", ctypes.c_void_p), ("pages", ctypes.c_long), ("heads", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
+
+_bound: Optional[ctypes.CDLL] = None
+
+
+def lib() -> ctypes.CDLL:
+    """libmiconv.so with the argument types of the quant entry points set."""
+    global _bound
+    if _bound is None:
+        L = miconv.lib()
+        i, p, l, f, sz = ctypes.c_int, ctypes.c_void_p, ctypes.c_long, ctypes.c_float, ctypes.c_size_t
+        c = ctypes.POINTER(_Kv4)
+        L.quant_rmsnorm_i8.argtypes = [l, l, i, p, l, p, l, p, f, p, l, p, l, p, p]
+        L.quant_rows_i8.argtypes = [l, l, i, p, l, p, l, p, p]
+        L.quant_matmul_workspace_bytes.argtypes = [l, l, l]
+        L.quant_matmul_i8.argtypes = [l, l, l, p, l, p, p, l, p, p, p, l, i, p, l, i, p, sz, p]
+        L.quant_kv4_write.argtypes = [c, l, i, p, l, p, l, p, p]
+        L.quant_kv4_read.argtypes = [c, l, p, i, p, l, p, l, p]
+        L.quant_attention_workspace_bytes.argtypes = [c, i, i, i, i]
+        L.quant_attention_kv4.argtypes = [c, i, i, l, p, l, p, p, p, i, i, i, f, i, i, p, l, p, sz, p]
+        L.quant_matmul_workspace_bytes.restype = L.quant_attention_workspace_bytes.restype = l
+        for name in ("rmsnorm_i8", "rows_i8", "matmul_i8", "kv4_write", "kv4_read", "attention_kv4"):
+            getattr(L, "quant_" + name).restype = i
+        _bound = L
+    return _bound
+
+
+# ------------------------------------------------------------------ checks
+
+def _tensor(t, name: str, *dtypes) -> None:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
+
+
+def _matrix(t, name: str, shape, *dtypes) -> int:
+    """A device tensor [rows][cols] with dense rows (cols None: any); returns its row stride."""
+    _tensor(t, name, *dtypes)
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must be {'[rows][cols]' if shape is None else list(shape)}, got {list(t.shape)}")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have dense rows")
+    return _row_stride(t, name, rows, cols)
+
+
+def _row_stride(t, name, rows, width) -> int:
+    s = t.stride(0) if rows > 1 else width
+    if s < width:
+        raise ValueError(f"{name} has overlapping rows")
+    return s
+
+
+def _heads(t, name: str, *dtypes) -> int:
+    """A device tensor [tokens][heads][channels] whose tokens are dense; returns the token stride."""
+    _tensor(t, name, *dtypes)
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens][heads][channels]")
+    n, h, d = t.shape
+    if t.stride(2) != 1 or (h > 1 and t.stride(1) != d):
+        raise ValueError(f"{name} must be dense within each token")
+    return _row_stride(t, name, n, h * d)
+
+
+def _vector(t, name: str, n: int, dtype) -> None:
+    _tensor(t, name, dtype)
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a dense vector of {n}")
+
+
+def _empty(shape, dtype, device, stream):
+    """A tensor for work of `stream`: the current stream when None."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
+    with torch.cuda.stream(s):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(nbytes: int, what: str, ws, device, stream):
+    if nbytes < 0:
+        _check(int(nbytes), what)
+    if nbytes == 0:
+        return None, 0
+    if ws is None:
+        ws = _empty(nbytes, torch.uint8, device, stream)
+    size = ws.numel() * ws.element_size()
+    if not ws.is_cuda or not ws.is_contiguous() or size < nbytes or ws.data_ptr() % 256:
+        raise ValueError(f"workspace must be a 256-byte aligned device tensor of at least {nbytes} bytes")
+    return ws.data_ptr(), size
+
+
+# ------------------------------------------------------------------ rows in 8 bits
+
+def _out_i8(x, q, scale, stream):
+    rows, cols = x.shape
+    if q is None:
+        q = _empty((rows, cols), torch.int8, x.device, stream)
+    if scale is None:
+        scale = _empty((rows,), torch.float32, x.device, stream)
+    _vector(scale, "scale", rows, torch.float32)
+    return q, _matrix(q, "q", (rows, cols), torch.int8), scale
+
+
+def rmsnorm_i8(x, weight=None, residual=None, eps: float = 1e-6, h=None, q=None, scale=None, stream=None):
+    """RMS norm of each row of x [rows][cols] (fp32 or bf16), after the residual's addition, as 8-bit integers:
+    (q int8 [rows][cols], scale fp32 [rows], h) with q * scale the normed row and h = x + residual in x's type,
+    or None without a residual.  h may be residual or x: the addition is then in place."""
+    xs = _matrix(x, "x", None, torch.bfloat16, torch.float32)
+    rows, cols = x.shape
+    if weight is not None:
+        _vector(weight, "weight", cols, torch.float32)
+    rs = hs = 0
+    if residual is not None:
+        rs = _matrix(residual, "residual", (rows, cols), x.dtype)
+        if h is None:
+            h = _empty((rows, cols), x.dtype, x.device, stream)
+        hs = _matrix(h, "h", (rows, cols), x.dtype)
+    elif h is not None:
+        raise ValueError("h is the sum with a residual: there is none")
+    q, qs, scale = _out_i8(x, q, scale, stream)
+    _check(lib().quant_rmsnorm_i8(rows, cols, _CODE[x.dtype], x.data_ptr(), xs, _ptr(residual), rs, _ptr(weight), eps,
+                                  _ptr(h), hs, q.data_ptr(), qs, scale.data_ptr(), _stream(stream)), "quant_rmsnorm_i8")
+    return q, scale, h
+
+
+def rows_i8(x, q=None, scale=None, stream=None):
+    """Each row of x [rows][cols] (fp32 or bf16) as 8-bit integers: (q int8, scale fp32 [rows]), q * scale ~ x."""
+    xs = _matrix(x, "x", None, torch.bfloat16, torch.float32)
+    q, qs, scale = _out_i8(x, q, scale, stream)
+    _check(lib().quant_rows_i8(x.shape[0], x.shape[1], _CODE[x.dtype], x.data_ptr(), xs, q.data_ptr(), qs,
+                               scale.data_ptr(), _stream(stream)), "quant_rows_i8")
+    return q, scale
+
+
+# ------------------------------------------------------------------ product of 8-bit integers
+
+def matmul_workspace_bytes(M: int, N: int, K: int) -> int:
+    n = lib().quant_matmul_workspace_bytes(M, N, K)
+    if n < 0:
+        _check(int(n), "quant_matmul_workspace_bytes")
+    return int(n)
+
+
+def matmul_i8(a, a_scale, w, w_scale, bias=None, residual=None, relu: bool = False, out=None,
+              out_dtype=torch.bfloat16, ws=None, stream=None):
+    """act(a_scale[m] * w_scale[n] * (a w^T)[m][n] + bias[n] + residual[m][n]) of a int8 [M][K] and w int8 [N][K];
+    fp32 scales [M], [N] and bias [N]; residual [M][N] of the output's type (it may be out).  out_dtype: bf16 or
+    fp32, out's where out is given."""
+    sa = _matrix(a, "a", None, torch.int8)
+    sw = _matrix(w, "w", None, torch.int8)
+    (M, K), N = a.shape, w.shape[0]
+    if w.shape[1] != K:
+        raise ValueError(f"w must be [N][{K}], got {list(w.shape)}")
+    _vector(a_scale, "a_scale", M, torch.float32)
+    _vector(w_scale, "w_scale", N, torch.float32)
+    if bias is not None:
+        _vector(bias, "bias", N, torch.float32)
+    if out is None:
+        if out_dtype not in _CODE:
+            raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
+        out = _empty((M, N), out_dtype, a.device, stream)
+    so = _matrix(out, "out", (M, N), torch.bfloat16, torch.float32)
+    sr = 0 if residual is None else _matrix(residual, "residual", (M, N), out.dtype)
+    L = lib()
+    wp, wn = _workspace(L.quant_matmul_workspace_bytes(M, N, K), "quant_matmul_i8", ws, a.device, stream)
+    _check(L.quant_matmul_i8(M, N, K, a.data_ptr(), sa, a_scale.data_ptr(), w.data_ptr(), sw, w_scale.data_ptr(),
+                             _ptr(bias), _ptr(residual), sr, _CODE[out.dtype], out.data_ptr(), so, int(relu), wp, wn,
+                             _stream(stream)), "quant_matmul_i8")
+    return out
+
+
+# ------------------------------------------------------------------ the 4-bit cache
+
+class KV4Cache:
+    """A paged cache of keys and values in 4 bits: codes uint8 [pages][heads][page_size][head_dim / 2] and exponent
+    bytes uint8 [pages][heads][page_size][head_dim / 32] of each (the format: ``include/miquant.h``)."""
+
+    __slots__ = ("k_codes", "k_exps", "v_codes", "v_exps", "pages", "heads", "page_size", "head_dim", "_desc")
+
+    def __init__(self, k_codes, k_exps, v_codes, v_exps):
+        shape = k_codes.shape
+        if len(shape) != 4 or 2 * shape[3] not in HEAD_DIMS:
+            raise ValueError(f"codes must be [pages][heads][page_size][head_dim / 2], head_dim one of {HEAD_DIMS}")
+        for name, t, n in (("k_codes", k_codes, shape[3]), ("k_exps", k_exps, shape[3] // 16),
+                           ("v_codes", v_codes, shape[3]), ("v_exps", v_exps, shape[3] // 16)):
+            _tensor(t, name, torch.uint8)
+            if t.shape[:3] != shape[:3] or t.dim() != 4 or t.shape[3] != n or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous, {[*shape[:3], n]}; got {list(t.shape)}")
+        self.k_codes, self.k_exps, self.v_codes, self.v_exps = k_codes, k_exps, v_codes, v_exps
+        self.pages, self.heads, self.page_size, self.head_dim = shape[0], shape[1], shape[2], 2 * shape[3]
+        self._desc = _Kv4(k_codes.data_ptr(), k_exps.data_ptr(), v_codes.data_ptr(), v_exps.data_ptr(), self.pages,
+                          self.heads, self.page_size, self.head_dim)
+
+    @classmethod
+    def allocate(cls, pages: int, heads: int, page_size: int, head_dim: int, device="cuda") -> "KV4Cache":
+        """An empty cache: every value reads as 0."""
+        if head_dim not in HEAD_DIMS:
+            raise ValueError(f"head_dim must be one of {HEAD_DIMS}")
+        new = lambda n: torch.zeros((pages, heads, page_size, n), dtype=torch.uint8, device=device)  # noqa: E731
+        return cls(new(head_dim // 2), new(head_dim // 32), new(head_dim // 2), new(head_dim // 32))
+
+    def nbytes(self) -> int:
+        return sum(t.numel() for t in (self.k_codes, self.k_exps, self.v_codes, self.v_exps))
+
+
+def _cache(cache) -> KV4Cache:
+    if not isinstance(cache, KV4Cache):
+        raise TypeError("cache must be a KV4Cache")
+    return cache
+
+
+def _token_shape(t, name, n, cache):
+    if tuple(t.shape) != (n, cache.heads, cache.head_dim):
+        raise ValueError(f"{name} must be {[n, cache.heads, cache.head_dim]}, got {list(t.shape)}")
+
+
+def kv4_write(k, v, slots, cache: KV4Cache, stream=None) -> None:
+    """Quantises k and v [tokens][heads][head_dim] (fp32 or bf16; tokens may be strided) into the cache at
+    slots int32 [tokens] (page * page_size + place; outside the cache: skipped)."""
+    c = _cache(cache)
+    ks = _heads(k, "k", torch.bfloat16, torch.float32)
+    vs = _heads(v, "v", k.dtype)
+    n = k.shape[0]
+    _token_shape(k, "k", n, c)
+    _token_shape(v, "v", n, c)
+    _vector(slots, "slots", n, torch.int32)
+    _check(lib().quant_kv4_write(c._desc, n, _CODE[k.dtype], k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(),
+                                 _stream(stream)), "quant_kv4_write")
+
+
+def kv4_read(slots, cache: KV4Cache, k=None, v=None, dtype=torch.bfloat16, stream=None):
+    """The keys and values at slots int32 [tokens] as (k, v) [tokens][heads][head_dim] of dtype (bf16 or fp32; both
+    hold every value exactly), k's where k is given; zeros for slots outside the cache."""
+    c = _cache(cache)
+    n = slots.shape[0] if isinstance(slots, torch.Tensor) and slots.dim() == 1 else -1
+    _vector(slots, "slots", n, torch.int32)
+    if k is not None:
+        dtype = k.dtype
+    if dtype not in _CODE:
+        raise TypeError("dtype must be torch.bfloat16 or torch.float32")
+    k = _empty((n, c.heads, c.head_dim), dtype, slots.device, stream) if k is None else k
+    v = _empty((n, c.heads, c.head_dim), dtype, slots.device, stream) if v is None else v
+    ks, vs = _heads(k, "k", dtype), _heads(v, "v", dtype)
+    _token_shape(k, "k", n, c)
+    _token_shape(v, "v", n, c)
+    _check(lib().quant_kv4_read(c._desc, n, slots.data_ptr(), _CODE[dtype], k.data_ptr(), ks, v.data_ptr(), vs,
+                                _stream(stream)), "quant_kv4_read")
+    return k, v
+
+
+def attention_workspace_bytes(cache: KV4Cache, seqs: int, heads: int, max_new: int, max_len: int) -> int:
+    n = lib().quant_attention_workspace_bytes(_cache(cache)._desc, seqs, heads, max_new, max_len)
+    if n < 0:
+        _check(int(n), "quant_attention_workspace_bytes")
+    return int(n)
+
+
+def attention_kv4(q, cache: KV4Cache, table, lens, starts=None, max_new: Optional[int] = None,
+                  max_len: Optional[int] = None, scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                  out=None, ws=None, stream=None):
+    """Attention of queries q bf16 [tokens][heads][head_dim] (tokens may be strided) over the cache, which holds
+    their own keys and values already.
+
+    table int32 [seqs][pages]: the pages of each sequence in order; lens int32 [seqs]: its cached tokens; starts
+    int32 [seqs + 1]: where its queries begin in q (None: one query each).  max_new and max_len bound the queries and
+    the length of any sequence (None: the bounds that the shapes give); work is laid out for these, so tight bounds
+    are faster.  scale: head_dim ** -0.5 unless given.  window > 0: only the last `window` places, the query's own
+    among them."""
+    c = _cache(cache)
+    qs = _heads(q, "q", torch.bfloat16)
+    n, heads, d = q.shape
+    if d != c.head_dim:
+        raise ValueError(f"q has {d} channels a head, the cache {c.head_dim}")
+    _tensor(table, "table", torch.int32)
+    if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be [seqs][pages] with dense rows")
+    seqs, width = table.shape
+    ts = table.stride(0) if seqs > 1 else width
+    if ts != width:
+        raise ValueError("table must be contiguous")
+    _vector(lens, "lens", seqs, torch.int32)
+    if starts is None:
+        if n != seqs:
+            raise ValueError(f"without starts q holds one token for each of the {seqs} sequences, got {n}")
+    else:
+        _vector(starts, "starts", seqs + 1, torch.int32)
+    if max_new is None:
+        max_new = 1 if starts is None else max(n, 1)
+    if max_len is None:
+        max_len = width * c.page_size
+    if out is None:
+        out = _empty((n, heads, d), torch.bfloat16, q.device, stream)
+    os_ = _heads(out, "out", torch.bfloat16)
+    if out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    L = lib()
+    wp, wn = _workspace(L.quant_attention_workspace_bytes(c._desc, seqs, heads, max_new, max_len),
+                        "quant_attention_kv4", ws, q.device, stream)
+    _check(L.quant_attention_kv4(c._desc, seqs, heads, n, q.data_ptr(), qs, _ptr(starts), lens.data_ptr(),
+                                 table.data_ptr(), ts, max_new, max_len, d ** -0.5 if scale is None else scale,
+                                 int(causal), window, out.data_ptr(), os_, wp, wn, _stream(stream)),
+           "quant_attention_kv4")
+    return out

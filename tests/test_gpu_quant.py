@@ -1,0 +1,497 @@
+"""GPU: the operators of quantised transformer blocks (include/miquant.h)
+against the oracle (oracle/quant.py), through the binding.
+
+8-bit and 4-bit results are unique and compared bit for bit.  The others are
+held to bounds that follow from the kernels' roundings: a row's scale to
+SCALE_TOL (below), a product and an attention row to the bound that the oracle
+computes with them.
+"""
+import math
+
+import pytest
+import torch
+
+from oracle import quant as ref
+from paper_1907_02154_amd import miconv, quant
+
+pytestmark = pytest.mark.gpu
+
+# A row's sum of squares is added in at most 64 steps a thread, 10 across
+# threads; its relative error is halved by the root, four roundings follow.
+SCALE_TOL = (74 / 2 + 4) * 2.0 ** -24
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    quant.lib()
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+# ------------------------------------------------------------------ rows in 8 bits
+
+def check_rows(got, x, weight=None, residual=None, eps=1e-6, norm=True):
+    q, scale, h = ref.rows_i8(x, weight, residual, eps, norm)
+    assert torch.equal(got[0].cpu(), q)
+    s = got[1].cpu().double()
+    fine = torch.isfinite(scale)
+    assert torch.equal(torch.isnan(s), ~fine)
+    assert ((s - scale).abs()[fine] <= SCALE_TOL * scale.abs()[fine]).all()
+    if residual is not None:
+        bits = torch.int16 if x.dtype == BF16 else torch.int32
+        same = (got[2].cpu().view(bits) == h.view(bits)) | (torch.isnan(got[2].cpu()) & torch.isnan(h))
+        assert same.all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (5, 8), (2, 100), (9, 511), (6, 512), (4, 513), (7, 1000), (1, 1024),
+                                       (3, 1031), (2, 2048), (3, 2100), (2, 4096), (2, 4097), (1, 8192), (2, 8200),
+                                       (1, 32768), (2, 32769), (1, 40003)])
+@pytest.mark.parametrize("res", [False, True], ids=["alone", "residual"])
+def test_rmsnorm(dtype, rows, cols, res):
+    g = gen(rows * 7919 + cols)
+    x = (torch.randn(rows, cols, generator=g) * 2).to(dtype)
+    r = torch.randn(rows, cols, generator=g).to(dtype) if res else None
+    w = torch.randn(cols, generator=g)
+    got = quant.rmsnorm_i8(x.cuda(), w.cuda(), None if r is None else r.cuda())
+    assert (got[2] is None) == (not res)
+    check_rows(got, x, w, r)
+    check_rows(quant.rows_i8(x.cuda()), x, norm=False)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_rmsnorm_strides_alignment_and_in_place(dtype):
+    g = gen(5)
+    rows, cols = 6, 203
+    wide = torch.randn(rows, cols + 30, generator=g).to(dtype)
+    r = torch.randn(rows, cols, generator=g).to(dtype)
+    wide_d = wide.cuda()
+    x = wide_d[:, 3:3 + cols]                              # rows start at odd elements, and are not contiguous
+    hold = r.cuda()
+    q = torch.full((rows, cols + 5), 99, dtype=torch.int8, device="cuda")
+    got = quant.rmsnorm_i8(x, None, hold, h=hold, q=q[:, 1:1 + cols])
+    assert got[2] is hold
+    check_rows(got, wide[:, 3:3 + cols], None, r)
+    assert (q[:, 0] == 99).all() and (q[:, 1 + cols:] == 99).all() and torch.equal(wide_d.cpu(), wide)
+    x2 = wide_d[:, 3:3 + cols]
+    got = quant.rmsnorm_i8(x2, None, r.cuda(), h=x2)       # the sum over x itself
+    check_rows(got, wide[:, 3:3 + cols], None, r)
+    assert torch.equal(wide_d.cpu()[:, :3], wide[:, :3]) and torch.equal(wide_d.cpu()[:, 3 + cols:], wide[:, 3 + cols:])
+
+
+def test_rmsnorm_extremes():
+    cols = 300
+    x = torch.zeros(9, cols)
+    x[1] = 1.0
+    x[2, 7] = math.nan
+    x[3, 299] = math.inf
+    x[4, 0] = -math.inf
+    x[5] = 2.0 ** -110                                     # below what 127 / A can take
+    x[6] = 2.0 ** -99
+    x[7, 3] = 3e38                                         # its square overflows
+    x[8, 5] = -1e-3
+    q, scale, _ = quant.rmsnorm_i8(x.cuda(), eps=0.0)
+    scale = scale.cpu()
+    assert q[0].abs().sum() == 0 and scale[0] == 0
+    assert (q[1] == 127).all() and abs(float(scale[1]) * 127 - 1) < 1e-6
+    assert torch.isnan(scale[2:5]).all() and q[2:5].abs().sum() == 0
+    assert scale[5] == 0 and q[5].abs().sum() == 0
+    assert (q[6] == 127).all() and q[7, 3] == 127 and q[8, 5] == -127
+    check_rows(quant.rows_i8(x.cuda()), x, norm=False)
+    for dtype in (BF16, F32):                              # no rows
+        e = quant.rmsnorm_i8(torch.empty(0, 8, dtype=dtype, device="cuda"), residual=torch.empty(0, 8, dtype=dtype, device="cuda"))
+        assert e[0].shape == (0, 8) and e[1].shape == (0,) and e[2].shape == (0, 8)
+
+
+def test_rows_ties():
+    x = torch.arange(-254, 255).float().reshape(1, -1) / 2   # largest 127: halves go to the even side
+    q, scale = quant.rows_i8(x.cuda())
+    assert torch.equal(q.cpu().float(), torch.round(x)) and float(scale) == 1.0
+
+
+# ------------------------------------------------------------------ product of 8-bit integers
+
+def i8(g, *shape):
+    return torch.randint(-128, 128, shape, generator=g, dtype=torch.int8)
+
+
+def check_matmul(M, N, K, dtype, bias, res, relu, seed=0, a=None, w=None):
+    g = gen(seed + M * 31 + N * 17 + K)
+    a, w = i8(g, M, K) if a is None else a, i8(g, N, K) if w is None else w
+    sa, sw = torch.rand(M, generator=g) * 0.02, torch.rand(N, generator=g) * 0.02 - 0.005
+    b = torch.randn(N, generator=g) if bias else None
+    r = torch.randn(M, N, generator=g).to(dtype) if res else None
+    y = quant.matmul_i8(a.cuda(), sa.cuda(), w.cuda(), sw.cuda(), bias=None if b is None else b.cuda(),
+                        residual=None if r is None else r.cuda(), relu=relu, out_dtype=dtype)
+    assert y.dtype == dtype and tuple(y.shape) == (M, N)
+    want, tol = ref.matmul_i8(a, sa, w, sw, b, r, relu, dtype == BF16)
+    off = (y.cpu().double() - want).abs()
+    assert (off <= tol).all(), float((off - tol).max())
+
+
+MATMUL = [(1, 1, 1), (1, 64, 64), (3, 5, 7), (1, 1000, 1024), (16, 16, 16), (17, 33, 65), (2, 130, 4096), (8, 256, 100),
+          (16, 512, 512), (31, 100, 48), (33, 1000, 1999), (48, 512, 4096), (64, 64, 128), (65, 129, 130), (100, 72, 272),
+          (128, 128, 128), (129, 384, 640), (200, 1000, 513), (255, 257, 80), (256, 256, 256), (257, 264, 1040),
+          (300, 520, 2048), (512, 1024, 192)]
+
+
+@pytest.mark.parametrize("M,N,K", MATMUL)
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_matmul(M, N, K, dtype):
+    check_matmul(M, N, K, dtype, bias=(M + N) % 2 == 0, res=K % 2 == 0, relu=N % 3 == 0)
+    check_matmul(M, N, K, dtype, False, False, False, seed=1)
+
+
+@pytest.mark.parametrize("M", [1, 5, 40, 150])
+def test_matmul_largest_sums(M):
+    """Every product 127 * 128 or 128 * 128 and the longest reduction: sums that only 32 bits hold exactly."""
+    for K, lo in ((131071, -128), (131056, 127)):
+        a, w = torch.full((M, K), -128, dtype=torch.int8), torch.full((40, K), lo, dtype=torch.int8)
+        w[::3, ::2] = 1
+        y = quant.matmul_i8(a.cuda(), torch.ones(M, device="cuda"), w.cuda(), torch.ones(40, device="cuda"), out_dtype=F32)
+        want = (a.double() @ w.double().t()).float()          # rounded once, as the kernel's conversion does
+        assert torch.equal(y.cpu(), want)
+
+
+@pytest.mark.parametrize("M", [1, 20, 100, 300])
+def test_matmul_strides_and_residual_in_place(M):
+    g = gen(M)
+    N, K = 200, 320
+    a, w = i8(g, M, K + 13), i8(g, N, K + 32)
+    r = torch.randn(M, N + 3, generator=g)
+    sa, sw = torch.rand(M, generator=g), torch.rand(N, generator=g)
+    for a0, w0 in ((0, 0), (5, 1), (0, 16)):
+        for dtype in (BF16, F32):
+            out = r.to(dtype).cuda()
+            y = quant.matmul_i8(a.cuda()[:, a0:a0 + K], sa.cuda(), w.cuda()[:, w0:w0 + K], sw.cuda(),
+                                residual=out[:, 1:1 + N], out=out[:, 1:1 + N])
+            want, tol = ref.matmul_i8(a[:, a0:a0 + K], sa, w[:, w0:w0 + K], sw, None, r.to(dtype)[:, 1:1 + N], False, dtype == BF16)
+            assert ((y.cpu().double() - want).abs() <= tol).all()
+            assert torch.equal(out[:, 0].cpu(), r.to(dtype)[:, 0]) and torch.equal(out[:, 1 + N:].cpu(), r.to(dtype)[:, 1 + N:])
+
+
+def test_matmul_scales_that_are_not_finite_stay_in_their_row_or_column():
+    for M in (4, 70):
+        g = gen(M)
+        a, w = i8(g, M, 64), i8(g, 48, 64)
+        sa, sw = torch.ones(M), torch.ones(48)
+        sa[2], sw[5] = math.nan, math.inf
+        y = quant.matmul_i8(a.cuda(), sa.cuda(), w.cuda(), sw.cuda(), relu=True, out_dtype=F32).cpu()
+        rest = torch.ones(M, 48, dtype=torch.bool)
+        rest[2], rest[:, 5] = False, False
+        assert torch.isnan(y[2]).all() and torch.isfinite(y[rest]).all()
+        assert torch.equal(y[rest], (a.float() @ w.float().t()).clamp_min(0)[rest])
+
+
+def test_matmul_no_rows():
+    y = quant.matmul_i8(torch.empty(0, 16, dtype=torch.int8, device="cuda"), torch.empty(0, device="cuda"),
+                        torch.zeros(8, 16, dtype=torch.int8, device="cuda"), torch.ones(8, device="cuda"))
+    assert y.shape == (0, 8)
+
+
+# ------------------------------------------------------------------ the 4-bit cache
+
+def empty_cache(pages, heads, page, d):
+    return quant.KV4Cache.allocate(pages, heads, page, d)
+
+
+def rows_of(cache, slots):
+    """The cache's bytes at slots, on the host: (k codes, k exponents, v codes, v exponents) [tokens][heads][...]."""
+    s = slots.long()
+    return [t[(s // cache.page_size).to(t.device), :, (s % cache.page_size).to(t.device)].cpu()
+            for t in (cache.k_codes, cache.k_exps, cache.v_codes, cache.v_exps)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("tokens,heads,page,d", [(1, 1, 1, 32), (5, 2, 16, 64), (33, 3, 7, 96), (70, 8, 64, 128), (9, 1, 48, 192),
+                                                 (130, 5, 100, 256)])
+def test_cache_round_trip(dtype, tokens, heads, page, d):
+    g = gen(tokens + d)
+    pages = tokens // page + 3
+    cache = empty_cache(pages, heads, page, d)
+    x = torch.randn(tokens, 2 * heads * d + 24, generator=g) * torch.exp2(torch.randint(-30, 30, (tokens, 1), generator=g).float())
+    x = x.to(dtype)
+    k, v = (x[:, o:o + heads * d].unflatten(1, (heads, d)) for o in (0, heads * d + 24))
+    xd = x.cuda()
+    kd, vd = (xd[:, o:o + heads * d].unflatten(1, (heads, d)) for o in (0, heads * d + 24))
+    slots = torch.randperm(pages * page, generator=g)[:tokens].to(torch.int32)
+    quant.kv4_write(kd, vd, slots.cuda(), cache)
+    want = [*ref.kv4_encode(k), *ref.kv4_encode(v)]
+    for got, w in zip(rows_of(cache, slots), want):
+        assert torch.equal(got, w)
+    untouched = torch.ones(pages * page, dtype=torch.bool)
+    untouched[slots.long()] = False
+    for t in rows_of(cache, untouched.nonzero()[:, 0]):
+        assert t.sum() == 0
+    for out in (BF16, F32):
+        rk, rv = quant.kv4_read(slots.cuda(), cache, dtype=out)
+        assert torch.equal(rk.cpu().double(), ref.kv4_decode(*want[:2])) and torch.equal(rv.cpu().double(), ref.kv4_decode(*want[2:]))
+
+
+def test_cache_every_exponent_tie_and_special():
+    """Values at and beside every rounding boundary, over the whole range of fp32, signs and specials included."""
+    edges = [0.0, 0.25, 0.5, 0.75, 1.0, 1.25, 1.5, 1.75, 2.0, 2.5, 3.0, 3.5, 4.0, 5.0, 6.0, 7.0]
+    base = torch.tensor(edges + [-e for e in edges])
+    rows = []
+    for e in range(-149, 126, 5):
+        for top in (7.0, 6.0, 4.0, 3.6):
+            m = base.clamp(-top, top).double() * 2.0 ** e
+            for nudge in (-1, 0, 1):
+                f = m.float()
+                rows.append(torch.nextafter(f, f + nudge * float("inf")) if nudge else f)
+    x = torch.stack(rows)
+    x = torch.where(torch.isfinite(x), x, torch.zeros_like(x))
+    special = torch.zeros(6, 32)
+    special[0, 0], special[1, 31], special[2, 5] = math.nan, math.inf, -math.inf
+    special[3], special[4], special[5, 2] = -0.0, 3.4e38, -3.4028234e38
+    x = torch.cat([x, special])
+    n = x.shape[0]
+    x = x.reshape(n, 1, 32)
+    cache = empty_cache(n, 1, 1, 32)
+    slots = torch.arange(n, dtype=torch.int32)
+    quant.kv4_write(x.cuda(), x.cuda(), slots.cuda(), cache)
+    codes, exps = ref.kv4_encode(x)
+    got = rows_of(cache, slots)
+    assert torch.equal(got[1], exps) and torch.equal(got[0], codes) and torch.equal(got[2], codes)
+    k, _ = quant.kv4_read(slots.cuda(), cache, dtype=F32)
+    want = ref.kv4_decode(codes, exps)
+    assert torch.equal(torch.isnan(k.cpu()), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(k.cpu().double()), torch.nan_to_num(want))
+
+
+def test_cache_slots_outside():
+    cache = empty_cache(2, 2, 8, 64)
+    x = torch.ones(5, 2, 64, dtype=BF16, device="cuda")
+    slots = torch.tensor([-1, 16, 3, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda")
+    quant.kv4_write(x, x, slots, cache)
+    assert int((cache.k_codes != 0).sum()) == 2 * 32 and int((cache.v_exps != 0).sum()) == 2 * 2
+    k, v = quant.kv4_read(slots, cache)
+    assert k[2].min() == 1 and k[[0, 1, 3, 4]].abs().max() == 0 and v[[0, 1, 3, 4]].abs().max() == 0
+    quant.kv4_write(x[:0], x[:0], slots[:0], cache)
+    assert quant.kv4_read(slots[:0], cache)[0].shape == (0, 2, 64)
+
+
+# ------------------------------------------------------------------ attention
+
+class Setup:
+    """Sequences in a shuffled paged cache; what no sequence holds is filled with groups that are not finite."""
+
+    def __init__(self, lens, news, heads, kv_heads, d, page, seed=0, spread=1.0, foul=True):
+        g = gen(seed + 1000 * d + sum(lens))
+        self.lens, self.news, self.d = lens, news, d
+        per = [-(-n // page) for n in lens]
+        pages = sum(per) + 2
+        cache = empty_cache(pages, kv_heads, page, d)
+        if foul:
+            for t in (cache.k_exps, cache.v_exps):
+                t.fill_(255)
+            for t in (cache.k_codes, cache.v_codes):
+                t.copy_(torch.randint(0, 256, t.shape, generator=g).to(torch.uint8))
+        order = torch.randperm(pages, generator=g).to(torch.int32)
+        width = max(1, max(per))
+        table = torch.full((len(lens), width), -7, dtype=torch.int32)      # past a sequence's pages: never read
+        at = 0
+        self.k, self.v = [], []
+        for s, n in enumerate(lens):
+            table[s, :per[s]] = order[at:at + per[s]]
+            at += per[s]
+            x = torch.randn(2, n, kv_heads, d, generator=g) * spread
+            if n:
+                p = torch.arange(n)
+                slots = (table[s, p // page] * page + p % page).to(torch.int32).cuda()
+                quant.kv4_write(x[0].cuda(), x[1].cuda(), slots, cache)
+            self.k.append(ref.kv4_decode(*ref.kv4_encode(x[0])))
+            self.v.append(ref.kv4_decode(*ref.kv4_encode(x[1])))
+        self.cache, self.table = cache, table.cuda()
+        self.lens_d = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        starts = [0]
+        for n in news:
+            starts.append(starts[-1] + n)
+        self.starts = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        self.q = (torch.randn(starts[-1], heads, d, generator=g) * 1.5).to(BF16)
+        self.scale = d ** -0.5
+
+    def run(self, **k):
+        k.setdefault("max_new", max(1, max(self.news)))
+        k.setdefault("max_len", max(1, max(self.lens)))
+        return quant.attention_kv4(k.pop("q", None) if "q" in k else self.q.cuda(), self.cache, self.table, self.lens_d,
+                                   starts=k.pop("starts", self.starts), **k)
+
+    def check(self, got, **k):
+        want, tol = ref.attention(self.q, self.k, self.v, self.news, self.lens, self.scale, **k)
+        off = (got.cpu().double() - want).abs()
+        assert not torch.isnan(off).any()
+        assert (off <= tol).all(), (float((off / tol).max()), (off > tol).nonzero()[:4].tolist())
+
+
+TOKENS = [   # lens, heads, kv heads, head dim, page
+    ([1], 1, 1, 32, 1), ([17], 4, 1, 64, 16), ([5, 0, 40], 8, 8, 96, 7), ([100, 33, 64, 31], 32, 8, 128, 16),
+    ([260, 1], 12, 4, 64, 48), ([70, 129], 6, 2, 192, 100), ([90, 257], 16, 2, 256, 64), ([63, 500], 40, 1, 128, 32),
+    ([1500, 700, 2], 16, 1, 64, 64), ([40, 128], 71, 1, 64, 64), ([3000], 8, 2, 128, 64), ([5000, 4100], 2, 1, 32, 128)]
+
+
+@pytest.mark.parametrize("lens,heads,kv,d,page", TOKENS)
+def test_attention_of_single_tokens(lens, heads, kv, d, page):
+    s = Setup(lens, [1] * len(lens), heads, kv, d, page)
+    s.check(s.run())
+    s.check(s.run(starts=None))                            # one query each is what no starts means
+    s.check(s.run(window=20), window=20)
+    s.check(s.run(max_len=None))                           # the table's width as the bound: other splits
+
+
+CHUNKS = [   # lens, news, heads, kv heads, head dim, page
+    ([3], [3], 1, 1, 32, 16), ([40, 9, 77], [7, 9, 0], 4, 2, 64, 16), ([130, 20], [17, 20], 8, 1, 128, 48),
+    ([200, 64, 65], [64, 64, 65], 2, 2, 96, 32), ([300], [129], 6, 2, 128, 64), ([150, 90], [150, 33], 4, 1, 256, 64),
+    ([97], [97], 3, 1, 192, 10), ([700, 3], [5, 3], 3, 3, 64, 64), ([900, 333], [300, 333], 8, 2, 64, 64),
+    ([520], [260], 10, 2, 128, 16)]
+
+
+@pytest.mark.parametrize("lens,news,heads,kv,d,page", CHUNKS)
+def test_attention_of_chunks_and_prompts(lens, news, heads, kv, d, page):
+    s = Setup(lens, news, heads, kv, d, page)
+    s.check(s.run())
+    s.check(s.run(window=13), window=13)
+    s.check(s.run(causal=False), causal=False)
+    s.check(s.run(max_new=None, max_len=None))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_rows_that_see_nothing(d):
+    """Empty sequences, and more queries than cached places: the first ones stand before the start."""
+    s = Setup([0, 2, 5], [3, 6, 5], 4, 2, d, 16)
+    out = s.run()
+    s.check(out)
+    assert out[:7].abs().max() == 0 and out[7].abs().max() > 0
+    s.check(s.run(window=2), window=2)
+    s.check(s.run(causal=False, window=1), causal=False, window=1)
+
+
+@pytest.mark.parametrize("news", [[1, 1], [9, 30], [60, 200]])
+def test_attention_extreme_scores(news):
+    """Scores of several hundred, both signs: one weight takes all, or the running maximum moves often."""
+    s = Setup([250, 400], news, 4, 2, 64, 32, spread=60.0)
+    s.check(s.run())
+    s = Setup([250, 400], news, 4, 2, 64, 32, spread=1e-3)
+    s.check(s.run())
+
+
+@pytest.mark.parametrize("news", [1, 4, 40, 200])
+def test_attention_keys_and_values_that_are_not_finite(news):
+    """A place with a NaN makes NaN of the rows that see it, in its key head, and of no other."""
+    for which in (0, 1):
+        s = Setup([300], [news], 4, 2, 64, 16)
+        bad = 300 - max(1, news // 2)                       # half of the queries stand before it
+        slot = int(s.table[0, bad // 16]) * 16 + bad % 16
+        x = torch.ones(1, 2, 64)
+        x[0, 1, 40] = math.nan
+        fine = torch.ones(1, 2, 64)
+        for t in (s.k, s.v):
+            t[0][bad] = ref.kv4_decode(*ref.kv4_encode(fine))[0]
+        quant.kv4_write(*[(x if i == which else fine).cuda() for i in (0, 1)],
+                        torch.tensor([slot], dtype=torch.int32, device="cuda"), s.cache)
+        out = s.run().cpu()
+        sees = torch.arange(300 - news, 300) >= bad
+        assert torch.isnan(out[sees][:, 2:]).all() and not torch.isnan(out[:, :2]).any() and not torch.isnan(out[~sees]).any()
+        want, tol = ref.attention(s.q, s.k, s.v, [news], [300], s.scale)
+        keep = torch.ones(news, 4, dtype=torch.bool)
+        keep[sees, 2:] = False
+        assert ((out.double() - want).abs() <= tol)[keep].all()
+
+
+@pytest.mark.parametrize("news", [[1, 1, 1], [5, 21, 70]])
+def test_attention_strided_rows(news):
+    s = Setup([200, 64, 90], news, 4, 2, 128, 16)
+    n = sum(news)
+    wide = torch.zeros(n, 4 * 128 + 57, dtype=BF16, device="cuda")
+    q = wide[:, 9:9 + 512].unflatten(1, (4, 128))           # rows at odd elements
+    q.copy_(s.q)
+    hold = torch.full((n, 600), 7.0, dtype=BF16, device="cuda")
+    out = hold[:, 33:33 + 512].unflatten(1, (4, 128))
+    s.check(s.run(q=q, out=out))
+    assert (hold[:, :33] == 7).all() and (hold[:, 33 + 512:] == 7).all()
+
+
+def test_attention_is_the_same_bits_again_and_on_another_stream():
+    s = Setup([2500, 900], [1, 1], 16, 4, 128, 64)
+    first = s.run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    again = [s.run(stream=side) for _ in range(3)]
+    side.synchronize()
+    assert all(torch.equal(first, x) for x in again)
+
+
+def test_bounds_in_device_data_are_clamped():
+    """Lengths past the bound, starts past the queries, pages outside the cache: nothing outside the buffers is touched."""
+    s = Setup([100, 50], [1, 3], 4, 2, 64, 16)
+    lens = torch.tensor([10 ** 9, -5], dtype=torch.int32, device="cuda")
+    table = torch.randint(-2 ** 31, 2 ** 31 - 1, (2, 7), dtype=torch.int32, device="cuda")
+    starts = torch.tensor([-3, 2, 99], dtype=torch.int32, device="cuda")
+    out = quant.attention_kv4(s.q.cuda(), s.cache, table, lens, starts=starts, max_new=4, max_len=112)
+    torch.cuda.synchronize()
+    assert out.shape == s.q.shape
+
+
+def test_cache_beyond_32_bit_offsets():
+    """Codes of more than 2^32 bytes: tokens in the last page, written, read back and attended."""
+    heads, page, d = 8, 64, 128
+    pages = (1 << 32) // (heads * page * d // 2) + 100
+    cache = empty_cache(pages, heads, page, d)
+    assert cache.k_codes.numel() > 1 << 32
+    g = gen(8)
+    n = 40
+    x = torch.randn(2, n, heads, d, generator=g)
+    slots = torch.arange((pages - 1) * page, (pages - 1) * page + n, dtype=torch.int64).to(torch.int32).cuda()
+    quant.kv4_write(x[0].cuda(), x[1].cuda(), slots, cache)
+    k, v = (ref.kv4_decode(*ref.kv4_encode(t)) for t in x)
+    rk, rv = quant.kv4_read(slots, cache)
+    assert torch.equal(rk.cpu().double(), k) and torch.equal(rv.cpu().double(), v)
+    table = torch.tensor([[pages - 1]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    for news in (1, 40):
+        q = torch.randn(news, 16, d, generator=g).to(BF16)
+        starts = torch.tensor([0, news], dtype=torch.int32, device="cuda")
+        out = quant.attention_kv4(q.cuda(), cache, table, lens, starts=starts, max_new=news)
+        want, tol = ref.attention(q, [k], [v], [news], [n], d ** -0.5)
+        assert ((out.cpu().double() - want).abs() <= tol).all()
+
+
+# ------------------------------------------------------------------ refusals through the binding
+
+def test_binding_refusals():
+    x = torch.zeros(4, 64, dtype=BF16, device="cuda")
+    a = torch.zeros(4, 64, dtype=torch.int8, device="cuda")
+    one = torch.ones(4, device="cuda")
+    cache = empty_cache(2, 2, 16, 64)
+    q = torch.zeros(2, 4, 64, dtype=BF16, device="cuda")
+    table = torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    lens = torch.ones(2, dtype=torch.int32, device="cuda")
+    kv = torch.zeros(2, 2, 64, dtype=BF16, device="cuda")
+    bad = [
+        lambda: quant.rmsnorm_i8(x.half()), lambda: quant.rmsnorm_i8(x.t()), lambda: quant.rmsnorm_i8(x, weight=one),
+        lambda: quant.rmsnorm_i8(x, residual=x.float()), lambda: quant.rmsnorm_i8(x, h=x),
+        lambda: quant.rmsnorm_i8(x[:1].expand(4, 64)), lambda: quant.rows_i8(x[0]), lambda: quant.rows_i8(x, q=a[:2]),
+        lambda: quant.matmul_i8(a, one, a[:, :32], one), lambda: quant.matmul_i8(a, one[:2], a, one),
+        lambda: quant.matmul_i8(x, one, a, one), lambda: quant.matmul_i8(a, one, a, one, bias=one[:3]),
+        lambda: quant.matmul_i8(a, one, a, one, residual=torch.zeros(4, 4, device="cuda")),
+        lambda: quant.matmul_i8(a, one, a, one, out_dtype=torch.float16),
+        lambda: quant.KV4Cache(cache.k_codes, cache.k_exps, cache.v_codes[:1], cache.v_exps),
+        lambda: quant.KV4Cache(cache.k_codes, cache.k_codes, cache.v_codes, cache.v_exps),
+        lambda: quant.kv4_write(kv, kv.float(), lens, cache), lambda: quant.kv4_write(kv, kv, lens.long(), cache),
+        lambda: quant.kv4_write(q, q, lens, cache), lambda: quant.kv4_read(lens, cache, dtype=torch.float16),
+        lambda: quant.attention_kv4(q.float(), cache, table, lens), lambda: quant.attention_kv4(q[:1], cache, table, lens),
+        lambda: quant.attention_kv4(q[..., :32], cache, table, lens), lambda: quant.attention_kv4(q, cache, table.long(), lens),
+        lambda: quant.attention_kv4(q, cache, table, lens[:1]), lambda: quant.attention_kv4(q, cache, table, lens, starts=lens),
+        lambda: quant.attention_kv4(q, None, table, lens), lambda: quant.attention_kv4(q[:, :3], cache, table, lens),
+        lambda: quant.attention_kv4(q, cache, table, lens, max_len=0),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises((ValueError, TypeError, miconv.MiconvError)):
+            f()
+            print("case", i)

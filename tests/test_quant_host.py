@@ -1,0 +1,147 @@
+"""Host-side checks of the quantised operators' entry points (no GPU needed):
+every call here fails validation, or has nothing to do, before any launch."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_1907_02154_amd import miconv, quant
+
+FAKE = 4096   # aligned, non-null, never touched
+NAN = float("nan")
+
+
+@pytest.fixture(scope="module")
+def L():
+    return quant.lib()
+
+
+def cache(pages=4, heads=2, page_size=16, head_dim=64, kc=FAKE, ke=FAKE, vc=FAKE, ve=FAKE):
+    return quant._Kv4(kc, ke, vc, ve, pages, heads, page_size, head_dim)
+
+
+def call(f, defaults, **k):
+    assert set(k) <= set(dict(defaults)), k
+    return f(*[k.get(n, d) for n, d in defaults])
+
+
+def test_declared_and_exported(L):
+    names = miconv.header_functions()
+    for n in ("quant_rmsnorm_i8", "quant_rows_i8", "quant_matmul_i8", "quant_matmul_workspace_bytes", "quant_kv4_write",
+              "quant_kv4_read", "quant_attention_kv4", "quant_attention_workspace_bytes"):
+        assert n in names and hasattr(L, n), n
+
+
+def test_rmsnorm_refusals(L):
+    d = [("rows", 2), ("cols", 8), ("dtype", 1), ("x", FAKE), ("xs", 8), ("res", FAKE), ("rs", 8), ("w", FAKE),
+         ("eps", 1e-6), ("h", FAKE), ("hs", 8), ("q", FAKE), ("qs", 8), ("scale", FAKE), ("st", None)]
+    f = lambda **k: call(L.quant_rmsnorm_i8, d, **k)  # noqa: E731
+    for k in (dict(rows=-1), dict(cols=0), dict(xs=7), dict(rs=7), dict(hs=7), dict(qs=7), dict(eps=-1.0), dict(eps=NAN)):
+        assert f(**k) == miconv.ERR_SHAPE, k
+    for k in (dict(x=None), dict(q=None), dict(scale=None), dict(h=None), dict(res=None)):
+        assert f(**k) == miconv.ERR_NULL, k
+    for k in (dict(x=FAKE + 1), dict(res=FAKE + 1), dict(h=FAKE + 1), dict(w=FAKE + 2), dict(scale=FAKE + 2),
+              dict(dtype=0, x=FAKE + 2)):
+        assert f(**k) == miconv.ERR_ALIGN, k
+    assert f(dtype=2) == miconv.ERR_UNSUPPORTED
+    assert f(rows=1 << 31) == miconv.ERR_TOO_LARGE
+    assert f(cols=1 << 31, xs=1 << 31, rs=1 << 31, hs=1 << 31, qs=1 << 31) == miconv.ERR_TOO_LARGE
+    assert f(rows=0, x=None, q=None, scale=None) == miconv.OK
+
+
+def test_rows_refusals(L):
+    d = [("rows", 2), ("cols", 8), ("dtype", 1), ("x", FAKE), ("xs", 8), ("q", FAKE), ("qs", 8), ("scale", FAKE), ("st", None)]
+    f = lambda **k: call(L.quant_rows_i8, d, **k)  # noqa: E731
+    assert f(x=None) == f(q=None) == f(scale=None) == miconv.ERR_NULL
+    assert f(cols=0) == f(xs=4) == f(qs=4) == miconv.ERR_SHAPE
+    assert f(dtype=3) == miconv.ERR_UNSUPPORTED
+    assert f(rows=0) == miconv.OK
+
+
+def test_matmul_refusals(L):
+    d = [("M", 4), ("N", 8), ("K", 16), ("a", FAKE), ("as", 16), ("sa", FAKE), ("w", FAKE), ("ws_", 16), ("sw", FAKE),
+         ("bias", None), ("res", None), ("rs", 0), ("dtype", 1), ("y", FAKE), ("ys", 8), ("relu", 0), ("ws", None),
+         ("wsb", 0), ("st", None)]
+    f = lambda **k: call(L.quant_matmul_i8, d, **k)  # noqa: E731
+    for k in (dict(M=-1), dict(N=0), dict(K=0), {"as": 15}, dict(ws_=15), dict(ys=7), dict(res=FAKE, rs=7)):
+        assert f(**k) == miconv.ERR_SHAPE, k
+    for n in ("a", "sa", "w", "sw", "y"):
+        assert f(**{n: None}) == miconv.ERR_NULL, n
+    for k in (dict(sa=FAKE + 2), dict(sw=FAKE + 1), dict(bias=FAKE + 2), dict(res=FAKE + 1, rs=8), dict(y=FAKE + 1),
+              dict(dtype=0, y=FAKE + 2)):
+        assert f(**k) == miconv.ERR_ALIGN, k
+    assert f(dtype=7) == miconv.ERR_UNSUPPORTED
+    assert f(K=131072, **{"as": 131072, "ws_": 131072}) == miconv.ERR_TOO_LARGE
+    assert f(M=1 << 31) == miconv.ERR_TOO_LARGE
+    assert f(M=0, a=None, y=None) == miconv.OK
+    w = L.quant_matmul_workspace_bytes
+    assert w(-1, 8, 16) == w(4, 0, 16) == w(4, 8, 0) == miconv.ERR_SHAPE
+    assert w(4, 8, 131072) == miconv.ERR_TOO_LARGE
+    assert w(0, 8, 16) == 0
+
+
+@pytest.mark.parametrize("write", [True, False])
+def test_cache_refusals(L, write):
+    d = [("c", cache()), ("tokens", 3), ("dtype", 1), ("k", FAKE), ("ks", 128), ("v", FAKE), ("vs", 128), ("slots", FAKE),
+         ("st", None)]
+    if not write:
+        d = d[:2] + [d[7], d[2]] + d[3:7] + d[8:]
+    f = lambda **k: call(L.quant_kv4_write if write else L.quant_kv4_read, d, **k)  # noqa: E731
+    assert f(c=None) == f(k=None) == f(v=None) == f(slots=None) == miconv.ERR_NULL
+    for n in ("kc", "ke", "vc", "ve"):
+        assert f(c=cache(**{n: None})) == miconv.ERR_NULL, n
+    for k in (dict(tokens=-1), dict(ks=127), dict(vs=127), dict(c=cache(pages=0)), dict(c=cache(heads=0)),
+              dict(c=cache(page_size=0))):
+        assert f(**k) == miconv.ERR_SHAPE, k
+    for D in (0, 16, 48, 160, 512):
+        assert f(c=cache(head_dim=D)) == miconv.ERR_UNSUPPORTED, D
+    assert f(dtype=2) == miconv.ERR_UNSUPPORTED
+    assert f(c=cache(kc=FAKE + 8)) == f(c=cache(vc=FAKE + 4)) == f(k=FAKE + 1) == f(slots=FAKE + 2) == miconv.ERR_ALIGN
+    assert f(c=cache(pages=1 << 20, page_size=1 << 11)) == miconv.ERR_TOO_LARGE
+    assert f(tokens=1 << 31) == miconv.ERR_TOO_LARGE
+    assert f(tokens=0, k=None, v=None, slots=None) == miconv.OK
+
+
+def test_attention_refusals(L):
+    big = 1 << 30
+    d = [("c", cache()), ("seqs", 2), ("heads", 4), ("tokens", 2), ("q", FAKE), ("qs", 256), ("starts", None),
+         ("lens", FAKE), ("table", FAKE), ("ts", 3), ("max_new", 1), ("max_len", 48), ("scale", 1.0), ("causal", 1),
+         ("window", 0), ("out", FAKE), ("os", 256), ("ws", FAKE), ("wsb", big), ("st", None)]
+    f = lambda **k: call(L.quant_attention_kv4, d, **k)  # noqa: E731
+    for n in ("c", "q", "lens", "table", "out"):
+        assert f(**{n: None}) == miconv.ERR_NULL, n
+    for k in (dict(seqs=-1), dict(heads=3), dict(heads=0), dict(tokens=-1), dict(qs=255), dict(os=255), dict(ts=0),
+              dict(max_new=0), dict(max_len=0)):
+        assert f(**k) == miconv.ERR_SHAPE, k
+    for k in (dict(q=FAKE + 1), dict(out=FAKE + 1), dict(starts=FAKE + 2), dict(lens=FAKE + 2), dict(table=FAKE + 1)):
+        assert f(**k) == miconv.ERR_ALIGN, k
+    assert f(c=cache(head_dim=48), qs=192, os=192) == miconv.ERR_UNSUPPORTED
+    assert f(seqs=70000) == f(max_new=1 << 30) == f(max_len=1 << 30) == f(tokens=1 << 31) == miconv.ERR_TOO_LARGE
+    assert f(seqs=0) == f(tokens=0) == miconv.OK
+    w = L.quant_attention_workspace_bytes
+    c = cache(pages=4096, page_size=64)
+    assert w(c, 1, 4, 1, 16) == 0                       # one split: nothing to join
+    need = w(c, 1, 4, 1, 65536)
+    assert need > 0                                     # one sequence, many places: split over the work-groups
+    assert f(c=c, seqs=1, tokens=1, ts=1024, max_len=65536, wsb=need - 1) == miconv.ERR_WORKSPACE
+    assert f(c=c, seqs=1, tokens=1, ts=1024, max_len=65536, ws=None) == miconv.ERR_WORKSPACE
+    assert f(c=c, seqs=1, tokens=1, ts=1024, max_len=65536, ws=FAKE + 16) == miconv.ERR_WORKSPACE
+    assert w(None, 1, 4, 1, 16) == miconv.ERR_NULL
+    assert w(c, 1, 3, 1, 16) == miconv.ERR_SHAPE
+
+
+def test_binding_refuses_host_tensors_and_wrong_types():
+    x = torch.zeros(2, 8)
+    with pytest.raises(ValueError, match="device"):
+        quant.rmsnorm_i8(x)
+    with pytest.raises(TypeError):
+        quant.rows_i8([1.0])
+    with pytest.raises(ValueError, match="device"):
+        quant.matmul_i8(x.to(torch.int8), x[:, 0], x.to(torch.int8), x[:, 0])
+    with pytest.raises(ValueError):
+        quant.KV4Cache.allocate(1, 1, 16, 48)
+    with pytest.raises(ValueError, match="device"):
+        quant.KV4Cache.allocate(1, 1, 16, 64, device="cpu")
+    with pytest.raises(TypeError, match="KV4Cache"):
+        quant.kv4_read(x, None)
+    assert ctypes.sizeof(quant._Kv4) == 56
