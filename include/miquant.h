@@ -66,11 +66,16 @@ int quant_rows_i8(long rows, long cols, int dtype, const void *x, long x_stride,
  * fp32 scales, fp32 bias [N] or NULL, residual [M][N] of y's type or NULL (it
  * may be y itself), y [M][N] of out_dtype, act = ReLU when relu != 0.  The sum
  * is an exact 32-bit integer; the rest is fp32, rounded once to out_dtype.
+ * An operand whose rows are not 16-byte aligned (pointer, stride and K all
+ * multiples of 16) is first copied to the workspace in rows that are; without
+ * one that needs it, no workspace is used.  Weights kept in aligned rows save
+ * their copy.
  * Errors: MICONV_ERR_NULL, MICONV_ERR_SHAPE (M < 0, N or K < 1, a stride below
  * its row), MICONV_ERR_UNSUPPORTED (out_dtype), MICONV_ERR_ALIGN,
  * MICONV_ERR_TOO_LARGE (K > 131071, where the sum could pass 32 bits; M or
  * N >= 2^31), MICONV_ERR_WORKSPACE. */
-long quant_matmul_workspace_bytes(long M, long N, long K);
+long quant_matmul_workspace_bytes(long M, long N, long K, const int8_t *a, long a_stride, const int8_t *w,
+                                  long w_stride);
 int quant_matmul_i8(long M, long N, long K, const int8_t *a, long a_stride, const float *a_scale, const int8_t *w,
                     long w_stride, const float *w_scale, const float *bias, const void *residual,
                     long residual_stride, int out_dtype, void *y, long y_stride, int relu, void *ws,

@@ -34,6 +34,23 @@ __device__ __forceinline__ void load8(const uint16_t *p, float (&v)[8])
         v[2 * i + 1] = __builtin_bit_cast(float, raw[i] & 0xFFFF0000u);
     }
 }
+__device__ __forceinline__ void load4(const float *p, float (&v)[4]) { memcpy(v, p, 16); }
+__device__ __forceinline__ void load4(const uint16_t *p, float (&v)[4])
+{
+    uint32_t raw[2];
+    memcpy(raw, p, 8);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        v[2 * i] = __builtin_bit_cast(float, raw[i] << 16);
+        v[2 * i + 1] = __builtin_bit_cast(float, raw[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void store4(float *p, const float (&v)[4]) { memcpy(p, v, 16); }
+__device__ __forceinline__ void store4(uint16_t *p, const float (&v)[4])
+{
+    const uint32_t raw[2] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    memcpy(p, raw, 8);
+}
 __device__ __forceinline__ float load1(const float *p) { return *p; }
 __device__ __forceinline__ float load1(const uint16_t *p) { return bf16_to_f32(*p); }
 __device__ __forceinline__ void store8(float *p, const float (&v)[8]) { memcpy(p, v, 32); }

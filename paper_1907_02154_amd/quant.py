@@ -41,7 +41,7 @@ def lib() -> ctypes.CDLL:
         c = ctypes.POINTER(_Kv4)
         L.quant_rmsnorm_i8.argtypes = [l, l, i, p, l, p, l, p, f, p, l, p, l, p, p]
         L.quant_rows_i8.argtypes = [l, l, i, p, l, p, l, p, p]
-        L.quant_matmul_workspace_bytes.argtypes = [l, l, l]
+        L.quant_matmul_workspace_bytes.argtypes = [l, l, l, p, l, p, l]
         L.quant_matmul_i8.argtypes = [l, l, l, p, l, p, p, l, p, p, p, l, i, p, l, i, p, sz, p]
         L.quant_kv4_write.argtypes = [c, l, i, p, l, p, l, p, p]
         L.quant_kv4_read.argtypes = [c, l, p, i, p, l, p, l, p]
@@ -167,8 +167,10 @@ def rows_i8(x, q=None, scale=None, stream=None):
 
 # ------------------------------------------------------------------ product of 8-bit integers
 
-def matmul_workspace_bytes(M: int, N: int, K: int) -> int:
-    n = lib().quant_matmul_workspace_bytes(M, N, K)
+def matmul_workspace_bytes(a, w) -> int:
+    """Bytes of workspace that matmul_i8 needs for these operands: 0 unless rows are not 16-byte aligned."""
+    sa, sw = _matrix(a, "a", None, torch.int8), _matrix(w, "w", None, torch.int8)
+    n = lib().quant_matmul_workspace_bytes(a.shape[0], w.shape[0], a.shape[1], a.data_ptr(), sa, w.data_ptr(), sw)
     if n < 0:
         _check(int(n), "quant_matmul_workspace_bytes")
     return int(n)
@@ -195,7 +197,8 @@ def matmul_i8(a, a_scale, w, w_scale, bias=None, residual=None, relu: bool = Fal
     so = _matrix(out, "out", (M, N), torch.bfloat16, torch.float32)
     sr = 0 if residual is None else _matrix(residual, "residual", (M, N), out.dtype)
     L = lib()
-    wp, wn = _workspace(L.quant_matmul_workspace_bytes(M, N, K), "quant_matmul_i8", ws, a.device, stream)
+    wp, wn = _workspace(L.quant_matmul_workspace_bytes(M, N, K, a.data_ptr(), sa, w.data_ptr(), sw), "quant_matmul_i8",
+                        ws, a.device, stream)
     _check(L.quant_matmul_i8(M, N, K, a.data_ptr(), sa, a_scale.data_ptr(), w.data_ptr(), sw, w_scale.data_ptr(),
                              _ptr(bias), _ptr(residual), sr, _CODE[out.dtype], out.data_ptr(), so, int(relu), wp, wn,
                              _stream(stream)), "quant_matmul_i8")

@@ -74,10 +74,15 @@ def test_matmul_refusals(L):
     assert f(K=131072, **{"as": 131072, "ws_": 131072}) == miconv.ERR_TOO_LARGE
     assert f(M=1 << 31) == miconv.ERR_TOO_LARGE
     assert f(M=0, a=None, y=None) == miconv.OK
-    w = L.quant_matmul_workspace_bytes
-    assert w(-1, 8, 16) == w(4, 0, 16) == w(4, 8, 0) == miconv.ERR_SHAPE
+    w = lambda M, N, K, a=FAKE, sa=None, p=FAKE, sw=None: L.quant_matmul_workspace_bytes(  # noqa: E731
+        M, N, K, a, K if sa is None else sa, p, K if sw is None else sw)
+    assert w(-1, 8, 16) == w(4, 0, 16) == w(4, 8, 0) == w(4, 8, 16, sa=15) == w(4, 8, 16, sw=0) == miconv.ERR_SHAPE
     assert w(4, 8, 131072) == miconv.ERR_TOO_LARGE
-    assert w(0, 8, 16) == 0
+    assert w(0, 8, 17) == w(4, 8, 16) == w(4, 8, 32, sa=48) == 0      # rows that can be read as they are
+    assert w(4, 8, 17) == 2 * 256                                     # both copied: 4 and 8 rows of 32 bytes
+    assert w(4, 8, 16, a=FAKE + 1) == w(4, 8, 16, sw=17) == 256       # one of them
+    for k in (dict(ws=None), dict(wsb=255), dict(ws=FAKE + 16)):
+        assert f(**{"a": FAKE + 1, "ws": FAKE, "wsb": 256, **k}) == miconv.ERR_WORKSPACE, k
 
 
 @pytest.mark.parametrize("write", [True, False])
