@@ -18,6 +18,8 @@ namespace quant {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -289,6 +291,218 @@ __global__ __launch_bounds__(256) void attend_kv4_kernel(AttArgs a)
     }
 }
 
+// Many rows: 32 a wavefront, 32 * NW a work-group, over tiles of 64 cached
+// tokens that the work-group widens to bf16 once, into LDS.
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void attend_kv4_wide_kernel(AttArgs a)
+{
+    constexpr int NT = 64 * NW, TILE = 64;
+    constexpr int KP = D * 2 + 16;               // bytes between rows in LDS: keys are read by rows of 16 bytes,
+    constexpr int VP = (D / 32 | 1) * 64;        // values by blocks of 4 rows: an odd number of 64-byte steps
+    constexpr int STAGE = TILE * (KP + VP);
+    constexpr int PARTS = D / 32, UNITS = 2 * TILE * PARTS;   // groups of 32 channels: of a row, of a tile's keys and values
+    constexpr int PER = (UNITS + NT - 1) / NT;
+    __shared__ __align__(16) unsigned char lds[2 * STAGE];
+
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 32, half = lane / 32;
+    const int split = blockIdx.x % a.splits, kvh = blockIdx.y, s = blockIdx.z;
+    const int rb = a.row_blocks - 1 - blockIdx.x / a.splits;   // with a causal mask the last rows see most: they go first
+    const Seq sq = sequence(a, s);
+    const int rows = (sq.news < a.max_new ? sq.news : a.max_new) * a.group, r0 = rb * 32 * NW;
+    if (r0 >= rows) return;
+    const int r_last = r0 + 32 * NW < rows ? r0 + 32 * NW - 1 : rows - 1;
+
+    // the places any row of the block sees, within this split
+    int lo, hi, x;
+    seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), &lo, &x);
+    seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), &x, &hi);
+    const int s_lo = split * a.per_split, s_hi = s_lo + a.per_split;
+    lo = (lo > s_lo ? lo : s_lo) & ~(TILE - 1);   // per_split is a multiple of the tile
+    hi = hi < s_hi ? hi : s_hi;
+    const int tiles = hi > lo ? (hi - lo + TILE - 1) / TILE : 0;
+
+    // this lane's query row, and its part of it
+    const int r = r0 + 32 * wave + col;
+    const bool live = r < rows;
+    const int qi = (int)fdiv((unsigned)(live ? r : 0), a.dv_group), qh = kvh * a.group + (live ? r : 0) - qi * a.group;
+    int q_lo, q_hi;
+    seen(a, sq, qi, &q_lo, &q_hi);
+    if (!live) q_lo = 0, q_hi = 0;
+    int w_lo = live ? q_lo : 0x7FFFFFFF, w_hi = q_hi, w_all = live ? q_hi : 0x7FFFFFFF, w_from = q_lo;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {   // the wavefront sees w_lo .. w_hi - 1, every row of it w_from .. w_all - 1
+        w_lo = min(w_lo, __shfl_xor(w_lo, d));
+        w_hi = max(w_hi, __shfl_xor(w_hi, d));
+        w_all = min(w_all, __shfl_xor(w_all, d));
+        w_from = max(w_from, __shfl_xor(w_from, d));
+    }
+    w_lo = __builtin_amdgcn_readfirstlane(w_lo), w_hi = __builtin_amdgcn_readfirstlane(w_hi);
+    w_all = __builtin_amdgcn_readfirstlane(w_all), w_from = __builtin_amdgcn_readfirstlane(w_from);
+    bf16x8 qf[D / 16];
+    {
+        const uint16_t *qr = a.q + (sq.row0 + qi) * a.qs + (long)qh * D + 8 * half;
+        const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;   // a negative factor is taken into the query
+#pragma unroll
+        for (int u = 0; u < D / 16; ++u) {
+            u32x4 v;
+            memcpy(&v, qr + 16 * u, 16);
+            qf[u] = __builtin_bit_cast(bf16x8, v ^ flip);
+        }
+    }
+    const float c = fmaxf(fabsf(a.scale), 0x1p-120f);   // not 0, so that a masked score stays -inf
+
+    const int32_t *pages = a.table + (long)s * a.table_stride;
+    // group i of this thread: keys, then values, by tokens
+    u32x4 code[PER];
+    uint32_t exp[PER];
+    const auto fetch = [&](int t0) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int idx = i * NT + tid;
+            if (UNITS % NT == 0 || idx < UNITS) {
+                const bool val = idx >= UNITS / 2;
+                const int in = idx - (val ? UNITS / 2 : 0), part = in % PARTS;
+                int t = t0 + in / PARTS;
+                t = t < hi ? t : hi - 1;   // past the end: a row that is seen, masked below
+                const long row = cached_row(a, pages, kvh, t);
+                const long at = row * PARTS + part;
+                code[i] = *(const u32x4 *)((val ? a.c.vc : a.c.kc) + at * 16);
+                // A value that is not finite makes the token's score NaN, which reaches the queries that see it;
+                // its own NaN times a probability of 0 would reach the others too.
+                const uint32_t ve = a.c.ve[at], ke = a.c.ke[at];
+                exp[i] = val ? (ve > kMaxExp ? 127u : ve) : (ve > kMaxExp ? 255u : ke);
+            }
+        }
+    };
+    const auto widen = [&](unsigned char *st) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int idx = i * NT + tid;
+            if (UNITS % NT == 0 || idx < UNITS) {
+                const bool val = idx >= UNITS / 2;
+                const int in = idx - (val ? UNITS / 2 : 0), part = in % PARTS, t = in / PARTS;
+                unsigned char *to = st + (val ? TILE * KP + t * VP : t * KP) + part * 64;
+                const float f = exp_scale(exp[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *(bf16x8 *)(to + 16 * j) = widen8(code[i][j], f);
+            }
+        }
+    };
+
+    float m = kNegInf, l = 0.0f;   // m: the running maximum times c
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[cb][i] = 0.0f;
+    const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
+
+    if (tiles > 0) {
+        fetch(lo);
+        widen(lds);
+        if (tiles > 1) fetch(lo + TILE);
+        __syncthreads();
+    }
+    for (int t = 0; t < tiles; ++t) {
+        const int t0 = lo + t * TILE;
+        if (t + 1 < tiles) {
+            widen(lds + (t + 1 & 1) * STAGE);   // read last before the previous barrier
+            if (t + 2 < tiles) fetch(t0 + 2 * TILE);
+        }
+        if (t0 < w_hi && t0 + TILE > w_lo) {
+            const unsigned char *kt = lds + (t & 1) * STAGE, *vt = kt + TILE * KP;
+            f32x16 sc[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[b][i] = 0.0f;
+#pragma unroll
+                for (int u = 0; u < D / 16; ++u) {
+                    const bf16x8 kf = *(const bf16x8 *)(kt + (32 * b + col) * KP + 32 * u + 16 * half);
+                    sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[u], sc[b], 0, 0, 0);
+                }
+            }
+            if (t0 < w_from || t0 + TILE > w_all) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int at = t0 + 32 * b + i % 4 + 8 * (i / 4) + 4 * half;
+                        sc[b][i] = at >= q_lo && at < q_hi ? sc[b][i] : kNegInf;
+                    }
+            }
+            float top = kNegInf;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
+            top *= c;
+            if (__any(top > m + kGrow)) {   // also where m is still -inf
+                top = fmaxf(top, m);
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float f = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+                m = top;
+                l *= f;
+#pragma unroll
+                for (int cb = 0; cb < D / 32; ++cb) o[cb] *= f;
+            }
+            const float base = m == kNegInf ? 0.0f : m;
+            bf16x8 pf[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                u32x4 w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = 8 * (k % 2) + 2 * i;
+                    const uint32_t two = pack_bf16x2(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][at], c, -base)),
+                                                     __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][at + 1], c, -base)));
+                    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), ones, l, false);
+                    w[i] = two;
+                }
+                pf[k] = __builtin_bit_cast(bf16x8, w);
+            }
+            // a lane's 8 tokens of the reduction: 4 * half .. + 3 and 8 later, as the scores have them
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const unsigned char *at =
+                        vt + (16 * k + 4 * half + lane % 16 / 4) * VP + cb * 64 + lane / 16 % 2 * 32 + lane % 4 * 8;
+                    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+                    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * VP));
+                    const bf16x8 vf = __builtin_shufflevector(__builtin_bit_cast(bf16x4, v0), __builtin_bit_cast(bf16x4, v1), 0,
+                                                              1, 2, 3, 4, 5, 6, 7);
+                    o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[k], o[cb], 0, 0, 0);
+                }
+        }
+        __syncthreads();
+    }
+
+    l += __shfl_xor(l, 32);
+    if (!live) return;
+    if (a.splits == 1) {
+        const float f = l == 0.0f ? 0.0f : 1.0f / l;
+        uint16_t *out = a.out + (sq.row0 + qi) * a.os + (long)qh * D + 4 * half;
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v[4] = {o[cb][4 * i] * f, o[cb][4 * i + 1] * f, o[cb][4 * i + 2] * f, o[cb][4 * i + 3] * f};
+                store4(out + 32 * cb + 8 * i, v);
+            }
+    } else {
+        float *part = a.part + ((((long)s * a.heads + qh) * a.max_new + qi) * a.splits + split) * (D + 4);
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v[4] = {o[cb][4 * i], o[cb][4 * i + 1], o[cb][4 * i + 2], o[cb][4 * i + 3]};
+                store4(part + 32 * cb + 8 * i + 4 * half, v);
+            }
+        if (half == 0) part[D] = m, part[D + 1] = l;
+    }
+}
+
 // Joins the splits of one row: a wavefront each.
 template <int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttArgs a)
@@ -317,23 +531,27 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttArgs a)
 }
 
 struct AttPlan {
+    bool wide;
     int nb, row_blocks, splits, per_split;
     size_t bytes;
 };
+
+constexpr int wide_waves(int dim) { return dim <= 128 ? 8 : 4; }
 
 AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len)
 {
     AttPlan p;
     const long rows = (long)max_new * (heads / c.heads);
+    p.wide = rows > 64;
     p.nb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     if (c.dim > 128 && p.nb > 2) p.nb = 2;
-    p.row_blocks = (int)((rows + 16 * p.nb - 1) / (16 * p.nb));
+    const long block = p.wide ? 32 * wide_waves(c.dim) : 16 * p.nb;
+    p.row_blocks = (int)((rows + block - 1) / block);
     const long groups = (long)seqs * c.heads * p.row_blocks;
-    const int cus = cu_count() > 0 ? cu_count() : 256;
-    long want = (4L * cus + groups - 1) / groups;                     // work-groups for four on a compute unit
+    long want = (4L * cu_count() + groups - 1) / groups;              // work-groups for four on a compute unit
     const long most = (max_len + 511L) / 512;                         // at least 512 tokens each
     want = want < 1 ? 1 : want > most ? most : want;
-    p.per_split = (int)(((max_len + want - 1) / want + 31) / 32 * 32);
+    p.per_split = (int)(((max_len + want - 1) / want + 63) / 64 * 64);
     p.splits = (int)((max_len + (long)p.per_split - 1) / p.per_split);
     p.bytes = p.splits > 1 ? (size_t)seqs * heads * max_new * p.splits * (c.dim + 4) * 4 : 0;
     return p;
@@ -353,10 +571,15 @@ template <int D>
 int launch_attend(const AttArgs &a, const AttPlan &p, hipStream_t st)
 {
     const dim3 grid((unsigned)((long)p.row_blocks * p.splits), (unsigned)a.c.heads, (unsigned)a.seqs);
-    void (*k)(AttArgs) = p.nb == 1 ? attend_kv4_kernel<D, 1> : attend_kv4_kernel<D, 2>;
-    if constexpr (D <= 128)
-        if (p.nb == 4) k = attend_kv4_kernel<D, 4>;
-    launch_kernel(k, grid, dim3(256), 0, st, a);
+    if (p.wide) {
+        constexpr int NW = wide_waves(D);
+        launch_kernel(attend_kv4_wide_kernel<D, NW>, grid, dim3(64 * NW), 0, st, a);
+    } else {
+        void (*k)(AttArgs) = p.nb == 1 ? attend_kv4_kernel<D, 1> : attend_kv4_kernel<D, 2>;
+        if constexpr (D <= 128)
+            if (p.nb == 4) k = attend_kv4_kernel<D, 4>;
+        launch_kernel(k, grid, dim3(256), 0, st, a);
+    }
     int rc = launched();
     if (rc != MICONV_OK || p.splits == 1) return rc;
     launch_kernel(attend_join_kernel<D>, dim3((unsigned)ceil_div(a.max_new, 4), (unsigned)a.heads, (unsigned)a.seqs),
