@@ -134,7 +134,8 @@ int quant_kv4_read(const quant_kv4 *cache, long tokens, const int32_t *slots, in
  * a stride below its row, max_new or max_len < 1, table_stride < 1),
  * MICONV_ERR_UNSUPPORTED (head_dim), MICONV_ERR_ALIGN, MICONV_ERR_TOO_LARGE
  * (2^31 rows or slots), MICONV_ERR_WORKSPACE. */
-long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len);
+long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len,
+                                     int causal, int window);
 int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, long tokens, const void *q, long q_stride,
                         const int32_t *starts, const int32_t *lens, const int32_t *table, int table_stride,
                         int max_new, int max_len, float scale, int causal, int window, void *out, long out_stride,

@@ -102,10 +102,47 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t code, float s)
     return __builtin_bit_cast(bf16x8, r);
 }
 
+// N words from p on, which is aligned to the widest access that divides them.
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t *p, uint32_t (&w)[N])
+{
+    constexpr int V = N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 1;
+    typedef uint32_t words __attribute__((ext_vector_type(V)));
+#pragma unroll
+    for (int i = 0; i < N / V; ++i) {
+        const words v = ((const words *)p)[i];
+#pragma unroll
+        for (int j = 0; j < V; ++j) w[i * V + j] = v[j];
+    }
+}
+
+// The factor of the scores as the kernels take it: positive, its sign in the
+// queries' sign bits, and not 0, so that a masked score stays -inf.
+__device__ __forceinline__ float factor(const AttArgs &a) { return fmaxf(fabsf(a.scale), 0x1p-120f); }
+__device__ __forceinline__ bf16x8 query8(const AttArgs &a, const uint16_t *q)
+{
+    uint32_t raw[4];
+    memcpy(raw, q, 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(raw[i]));   // or it is loaded again by halves for the exclusive or
+    const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+    const u32x4 v = {raw[0] ^ flip, raw[1] ^ flip, raw[2] ^ flip, raw[3] ^ flip};
+    return __builtin_bit_cast(bf16x8, v);
+}
+
+// Two probabilities 2^(s c - base) as bf16, added to l as rounded.
+__device__ __forceinline__ uint32_t weights2(float s0, float s1, float c, float base, float &l)
+{
+    const uint32_t w = pack_bf16x2(__builtin_amdgcn_exp2f(__builtin_fmaf(s0, c, -base)),
+                                   __builtin_amdgcn_exp2f(__builtin_fmaf(s1, c, -base)));
+    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3F803F80u), l, false);
+    return w;
+}
+
 // Four wavefronts share 16 * NB query rows and take turns at tiles of 32
 // cached tokens; their sums meet in LDS at the end.
 template <int D, int NB>
-__global__ __launch_bounds__(256) void attend_kv4_kernel(AttArgs a)
+__global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
 {
     constexpr int NU = D / 32;           // units of 8 channels a lane holds of a cached row
     constexpr int CB = D / 16;           // blocks of 16 channels
@@ -117,7 +154,7 @@ __global__ __launch_bounds__(256) void attend_kv4_kernel(AttArgs a)
     __shared__ __align__(16) unsigned char lds[LDS];
     __shared__ float sm[4][16 * NB], sl[4][16 * NB];
 
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int col = lane % 16, quad = lane / 16;
     const int split = blockIdx.x % a.splits, rb = blockIdx.x / a.splits, kvh = blockIdx.y, s = blockIdx.z;
     const Seq sq = sequence(a, s);
@@ -125,14 +162,12 @@ __global__ __launch_bounds__(256) void attend_kv4_kernel(AttArgs a)
     if (r0 >= rows) return;
     const int r_last = r0 + 16 * NB < rows ? r0 + 16 * NB - 1 : rows - 1;
 
-    // the places any row of the block sees, within this split
-    int lo, hi, x;
-    seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), &lo, &x);
-    seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), &x, &hi);
-    const int s_lo = split * a.per_split;
-    const int s_hi = s_lo + a.per_split;
-    lo = (lo > s_lo ? lo : s_lo) & ~31;   // per_split is a multiple of 32
-    hi = hi < s_hi ? hi : s_hi;
+    // the places that any row of the block sees, lo .. hi - 1, and that every row does, from .. all - 1; within this split
+    int lo, hi, from, all;
+    seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), &lo, &all);
+    seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), &from, &hi);
+    lo = (lo & ~31) + split * a.per_split;   // per_split is a multiple of 64
+    hi = min(hi, lo + a.per_split);
 
     int q_lo[NB], q_hi[NB];
     bf16x8 qf[NB][NU];
@@ -145,10 +180,11 @@ __global__ __launch_bounds__(256) void attend_kv4_kernel(AttArgs a)
         if (!live) q_hi[b] = 0;
         const uint16_t *qr = a.q + (sq.row0 + i) * a.qs + (long)h * D + quad * (D / 4);
 #pragma unroll
-        for (int u = 0; u < NU; ++u) memcpy(&qf[b][u], qr + 8 * u, 16);
+        for (int u = 0; u < NU; ++u) qf[b][u] = query8(a, qr + 8 * u);
     }
+    const float c = factor(a);
 
-    float m[NB], l[NB];
+    float m[NB], l[NB];   // m: the running maximum times c
     f32x4 o[CB][NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -158,55 +194,93 @@ __global__ __launch_bounds__(256) void attend_kv4_kernel(AttArgs a)
     }
 
     const int32_t *pages = a.table + (long)s * a.table_stride;
+    const int last_page = (int)(a.c.slots / a.c.page_size) - 1;
+    const int page_rows = a.c.heads * a.c.page_size, head_row = kvh * a.c.page_size;
     unsigned char *vt = lds + wave * VBYTES;
-    for (int t0 = lo + 32 * wave; t0 < hi; t0 += 128) {
-        f32x4 sc[2][NB];
-        u32x4 vw[2][NU];
+    // What a lane holds of a tile: of token 16 k + col the units quad * NU .. + NU - 1 and the exponents of their groups.
+    constexpr int NE = D == 96 || D > 128 ? 2 : 1;
+    const int g0 = quad * NU / 4, g1 = min(g0 + 1, D / 32 - 1);
+    struct Held {
+        uint32_t kc[2][NU], vc[2][NU], ke[2][NE], ve[2][NE];
+    };
+    int page[2], place[2];
+    const auto look = [&](int t0) {   // the pages of a tile's tokens
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             int t = t0 + 16 * k + col;
             t = t < hi ? t : hi - 1;   // past the end: a row that is seen, masked below
-            const long row = cached_row(a, pages, kvh, t);
-            uint32_t kc[NU], vc[NU];
-            memcpy(kc, a.c.kc + row * (D / 2) + quad * (D / 8), 4 * NU);
-            memcpy(vc, a.c.vc + row * (D / 2) + quad * (D / 8), 4 * NU);
+            const unsigned p = fdiv((unsigned)t, a.c.dv_page);
+            place[k] = t - (int)p * a.c.page_size;
+            page[k] = pages[p];
+        }
+    };
+    const auto fetch = [&](Held &to) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const unsigned pg = (unsigned)min(max(page[k], 0), last_page);
+            const uint64_t row = (uint64_t)pg * (unsigned)page_rows + (unsigned)(head_row + place[k]);
+            load_words<NU>(a.c.kc + row * (D / 2) + quad * (D / 8), to.kc[k]);
+            load_words<NU>(a.c.vc + row * (D / 2) + quad * (D / 8), to.vc[k]);
+            to.ke[k][0] = a.c.ke[row * (D / 32) + g0];
+            to.ve[k][0] = a.c.ve[row * (D / 32) + g0];
+            if constexpr (NE == 2) {
+                to.ke[k][1] = a.c.ke[row * (D / 32) + g1];
+                to.ve[k][1] = a.c.ve[row * (D / 32) + g1];
+            }
+        }
+    };
+    const auto tile = [&](const Held &cur, Held &next, int t0) {
+        if (t0 + 128 < hi) {
+            fetch(next);
+            if (t0 + 256 < hi) look(t0 + 256);
+        }
+        f32x4 sc[2][NB];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float ks[NE], vs[NE];
+#pragma unroll
+            for (int e = 0; e < NE; ++e) {
+                // A value that is not finite makes the token's score NaN, which reaches
+                // the queries that see it; its own NaN times a probability of 0 would
+                // reach the others too.
+                const bool bad = cur.ve[k][e] > kMaxExp;
+                ks[e] = exp_scale(bad ? 255u : cur.ke[k][e]);
+                vs[e] = exp_scale(bad ? 127u : cur.ve[k][e]);
+            }
 #pragma unroll
             for (int b = 0; b < NB; ++b) sc[k][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
-                const long at = row * (D / 32) + (quad * NU + u) / 4;
-                uint32_t ke = a.c.ke[at], ve = a.c.ve[at];
-                // A value that is not finite makes the token's score NaN, which reaches
-                // the queries that see it; its own NaN times a probability of 0 would
-                // reach the others too.
-                if (ve > kMaxExp) ve = 127, ke = 255;
-                const bf16x8 kf = widen8(kc[u], exp_scale(ke));
-                vw[k][u] = __builtin_bit_cast(u32x4, widen8(vc[u], exp_scale(ve)));
+                const int e = NE == 1 ? 0 : (quad * NU + u) / 4 - g0;
+                const bf16x8 kf = widen8(cur.kc[k][u], e == 0 ? ks[0] : ks[NE - 1]);
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
                     sc[k][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[b][u], sc[k][b], 0, 0, 0);
+                *(bf16x8 *)(vt + (16 * k + col) * PITCH + quad * (D / 2) + 16 * u) =
+                    widen8(cur.vc[k][u], e == 0 ? vs[0] : vs[NE - 1]);
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        if (t0 < from || t0 + 32 > all) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int u = 0; u < NU; ++u)
-                *(u32x4 *)(vt + (16 * k + col) * PITCH + quad * (D / 2) + 16 * u) = vw[k][u];
-
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int t = t0 + 16 * k + 4 * quad + i;
+                        sc[k][b][i] = t >= q_lo[b] && t < q_hi[b] ? sc[k][b][i] : kNegInf;
+                    }
+        }
         bf16x8 pf[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            float top = kNegInf, p[8];
+            float top = kNegInf;
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = t0 + 16 * k + 4 * quad + i;
-                    const float v = t >= q_lo[b] && t < q_hi[b] ? sc[k][b][i] * a.scale : kNegInf;
-                    p[4 * k + i] = v;
-                    top = fmaxf(top, v);
-                }
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[k][b][i]);
+            top *= c;
             if (__any(top > m[b] + kGrow)) {   // also where m is still -inf
                 top = fmaxf(top, m[b]);
                 top = fmaxf(top, __shfl_xor(top, 16));
@@ -220,10 +294,8 @@ __global__ __launch_bounds__(256) void attend_kv4_kernel(AttArgs a)
             const float base = m[b] == kNegInf ? 0.0f : m[b];
             u32x4 w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = pack_bf16x2(__builtin_amdgcn_exp2f(p[2 * i] - base), __builtin_amdgcn_exp2f(p[2 * i + 1] - base));
-                l[b] += __builtin_bit_cast(float, w[i] << 16) + __builtin_bit_cast(float, w[i] & 0xFFFF0000u);
-            }
+            for (int i = 0; i < 4; ++i)
+                w[i] = weights2(sc[i / 2][b][i % 2 * 2], sc[i / 2][b][i % 2 * 2 + 1], c, base, l[b]);
             pf[b] = __builtin_bit_cast(bf16x8, w);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -231,8 +303,8 @@ __global__ __launch_bounds__(256) void attend_kv4_kernel(AttArgs a)
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
             const unsigned char *at = vt + (4 * quad + col / 4) * PITCH + cb * 32 + (col % 4) * 8;
-            s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
-            s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 16 * PITCH));
+            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+            const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 16 * PITCH));
             const bf16x8 vf = __builtin_shufflevector(__builtin_bit_cast(bf16x4, v0), __builtin_bit_cast(bf16x4, v1), 0, 1, 2,
                                                       3, 4, 5, 6, 7);
 #pragma unroll
@@ -240,6 +312,18 @@ __global__ __launch_bounds__(256) void attend_kv4_kernel(AttArgs a)
                 o[cb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[b], o[cb][b], 0, 0, 0);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    // Loads run a tile ahead of the arithmetic, the page table's two.
+    int t0 = lo + 32 * wave;
+    Held even, odd;
+    if (t0 < hi) {
+        look(t0);
+        fetch(even);
+        if (t0 + 128 < hi) look(t0 + 128);
+    }
+    for (; t0 < hi; t0 += 256) {
+        tile(even, odd, t0);
+        if (t0 + 128 < hi) tile(odd, even, t0 + 128);
     }
 
     // The four wavefronts' sums: the joint maximum first, then O, one wavefront after another.
@@ -316,9 +400,8 @@ __global__ __launch_bounds__(64 * NW) void attend_kv4_wide_kernel(AttArgs a)
     int lo, hi, x;
     seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), &lo, &x);
     seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), &x, &hi);
-    const int s_lo = split * a.per_split, s_hi = s_lo + a.per_split;
-    lo = (lo > s_lo ? lo : s_lo) & ~(TILE - 1);   // per_split is a multiple of the tile
-    hi = hi < s_hi ? hi : s_hi;
+    lo = (lo & ~(TILE - 1)) + split * a.per_split;   // per_split is a multiple of the tile
+    hi = min(hi, lo + a.per_split);
     const int tiles = hi > lo ? (hi - lo + TILE - 1) / TILE : 0;
 
     // this lane's query row, and its part of it
@@ -339,17 +422,9 @@ __global__ __launch_bounds__(64 * NW) void attend_kv4_wide_kernel(AttArgs a)
     w_lo = __builtin_amdgcn_readfirstlane(w_lo), w_hi = __builtin_amdgcn_readfirstlane(w_hi);
     w_all = __builtin_amdgcn_readfirstlane(w_all), w_from = __builtin_amdgcn_readfirstlane(w_from);
     bf16x8 qf[D / 16];
-    {
-        const uint16_t *qr = a.q + (sq.row0 + qi) * a.qs + (long)qh * D + 8 * half;
-        const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;   // a negative factor is taken into the query
 #pragma unroll
-        for (int u = 0; u < D / 16; ++u) {
-            u32x4 v;
-            memcpy(&v, qr + 16 * u, 16);
-            qf[u] = __builtin_bit_cast(bf16x8, v ^ flip);
-        }
-    }
-    const float c = fmaxf(fabsf(a.scale), 0x1p-120f);   // not 0, so that a masked score stays -inf
+    for (int u = 0; u < D / 16; ++u) qf[u] = query8(a, a.q + (sq.row0 + qi) * a.qs + (long)qh * D + 8 * half + 16 * u);
+    const float c = factor(a);
 
     const int32_t *pages = a.table + (long)s * a.table_stride;
     // group i of this thread: keys, then values, by tokens
@@ -395,7 +470,6 @@ __global__ __launch_bounds__(64 * NW) void attend_kv4_wide_kernel(AttArgs a)
     for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[cb][i] = 0.0f;
-    const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
 
     if (tiles > 0) {
         fetch(lo);
@@ -454,10 +528,7 @@ __global__ __launch_bounds__(64 * NW) void attend_kv4_wide_kernel(AttArgs a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int at = 8 * (k % 2) + 2 * i;
-                    const uint32_t two = pack_bf16x2(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][at], c, -base)),
-                                                     __builtin_amdgcn_exp2f(__builtin_fmaf(sc[k / 2][at + 1], c, -base)));
-                    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), ones, l, false);
-                    w[i] = two;
+                    w[i] = weights2(sc[k / 2][at], sc[k / 2][at + 1], c, base, l);
                 }
                 pf[k] = __builtin_bit_cast(bf16x8, w);
             }
@@ -503,20 +574,23 @@ __global__ __launch_bounds__(64 * NW) void attend_kv4_wide_kernel(AttArgs a)
     }
 }
 
-// Joins the splits of one row: a wavefront each.
+// Joins the splits of a row of a head: four wavefronts take turns at them.
 template <int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttArgs a)
 {
-    const int lane = threadIdx.x % 64, h = blockIdx.y, s = blockIdx.z;
-    const int t = blockIdx.x * 4 + threadIdx.x / 64;
+    constexpr int PER = (D + 63) / 64;
+    __shared__ float sum[4][D], den[4];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, h = blockIdx.y, s = blockIdx.z, t = blockIdx.x;
     const Seq sq = sequence(a, s);
-    if (t >= sq.news || t >= a.max_new) return;
+    if (t >= sq.news) return;
     const float *part = a.part + (((long)s * a.heads + h) * a.max_new + t) * a.splits * (D + 4);
     float mm = kNegInf;
-    for (int i = 0; i < a.splits; ++i) mm = fmaxf(mm, part[(long)i * (D + 4) + D]);
-    constexpr int PER = (D + 63) / 64;
+    for (int i = lane; i < a.splits; i += 64) mm = fmaxf(mm, part[(long)i * (D + 4) + D]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) mm = fmaxf(mm, __shfl_xor(mm, d));
     float l = 0.0f, v[PER] = {};
-    for (int i = 0; i < a.splits; ++i) {
+#pragma unroll 4
+    for (int i = wave; i < a.splits; i += 4) {
         const float *p = part + (long)i * (D + 4);
         const float f = p[D] == mm ? 1.0f : __builtin_amdgcn_exp2f(p[D] - mm);
         l += p[D + 1] * f;
@@ -524,10 +598,15 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttArgs a)
         for (int j = 0; j < PER; ++j)
             if (j * 64 + lane < D) v[j] += p[j * 64 + lane] * f;
     }
-    const float f = l == 0.0f ? 0.0f : 1.0f / l;
+    if (lane == 0) den[wave] = l;
 #pragma unroll
     for (int j = 0; j < PER; ++j)
-        if (j * 64 + lane < D) store1(a.out + (sq.row0 + t) * a.os + (long)h * D + j * 64 + lane, v[j] * f);
+        if (j * 64 + lane < D) sum[wave][j * 64 + lane] = v[j];
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    l = den[0] + den[1] + den[2] + den[3];
+    const float x = sum[0][threadIdx.x] + sum[1][threadIdx.x] + sum[2][threadIdx.x] + sum[3][threadIdx.x];
+    store1(a.out + (sq.row0 + t) * a.os + (long)h * D + threadIdx.x, l == 0.0f ? 0.0f : x / l);
 }
 
 struct AttPlan {
@@ -538,21 +617,28 @@ struct AttPlan {
 
 constexpr int wide_waves(int dim) { return dim <= 128 ? 8 : 4; }
 
-AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len)
+AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len, int causal, int window)
 {
     AttPlan p;
-    const long rows = (long)max_new * (heads / c.heads);
-    p.wide = rows > 64;
+    const long group = heads / c.heads, rows = (long)max_new * group;
+    // The kernel for few rows holds up to 64 of them in registers, fewer of wide heads.
+    p.wide = rows > (c.dim <= 64 ? 64 : c.dim <= 128 ? 32 : 16);
     p.nb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    if (c.dim > 128 && p.nb > 2) p.nb = 2;
     const long block = p.wide ? 32 * wide_waves(c.dim) : 16 * p.nb;
     p.row_blocks = (int)((rows + block - 1) / block);
-    const long groups = (long)seqs * c.heads * p.row_blocks;
-    long want = (4L * cu_count() + groups - 1) / groups;              // work-groups for four on a compute unit
-    const long most = (max_len + 511L) / 512;                         // at least 512 tokens each
-    want = want < 1 ? 1 : want > most ? most : want;
-    p.per_split = (int)(((max_len + want - 1) / want + 63) / 64 * 64);
-    p.splits = (int)((max_len + (long)p.per_split - 1) / p.per_split);
+    // Places that a block of rows sees: with a window behind each, its own and those of the block's tokens.
+    long len = max_len;
+    if (causal && window > 0) len = min(len, (long)window + block / group + 1 + 64);
+    // The places are split until work-groups fill the card once, three on a
+    // compute unit (one, with many rows): 16 sequences of up to 32768 places, 8 key
+    // heads of 128, take 95 us so, 109 with four and 101 with six or eight.  A split
+    // has 256 places at least: one sequence of 1000 takes 8.7 us so, 8.2 with 128 and
+    // 10.1 with 512, one of 30000 18.2, 21 and 16.5.
+    const long least = p.wide ? 512 : 256, groups = (long)seqs * c.heads * p.row_blocks;
+    long want = ((p.wide ? 1L : 3L) * cu_count() + groups - 1) / groups;
+    want = max(1L, min(want, (len + least - 1) / least));
+    p.per_split = (int)(((len + want - 1) / want + 63) / 64 * 64);
+    p.splits = (int)((len + (long)p.per_split - 1) / p.per_split);
     p.bytes = p.splits > 1 ? (size_t)seqs * heads * max_new * p.splits * (c.dim + 4) * 4 : 0;
     return p;
 }
@@ -575,15 +661,16 @@ int launch_attend(const AttArgs &a, const AttPlan &p, hipStream_t st)
         constexpr int NW = wide_waves(D);
         launch_kernel(attend_kv4_wide_kernel<D, NW>, grid, dim3(64 * NW), 0, st, a);
     } else {
-        void (*k)(AttArgs) = p.nb == 1 ? attend_kv4_kernel<D, 1> : attend_kv4_kernel<D, 2>;
+        void (*k)(AttArgs) = attend_kv4_kernel<D, 1>;
         if constexpr (D <= 128)
+            if (p.nb == 2) k = attend_kv4_kernel<D, 2>;
+        if constexpr (D <= 64)
             if (p.nb == 4) k = attend_kv4_kernel<D, 4>;
         launch_kernel(k, grid, dim3(256), 0, st, a);
     }
     int rc = launched();
     if (rc != MICONV_OK || p.splits == 1) return rc;
-    launch_kernel(attend_join_kernel<D>, dim3((unsigned)ceil_div(a.max_new, 4), (unsigned)a.heads, (unsigned)a.seqs),
-                  dim3(256), 0, st, a);
+    launch_kernel(attend_join_kernel<D>, dim3((unsigned)a.max_new, (unsigned)a.heads, (unsigned)a.seqs), dim3(256), 0, st, a);
     return launched();
 }
 
@@ -591,12 +678,13 @@ int launch_attend(const AttArgs &a, const AttPlan &p, hipStream_t st)
 }  // namespace quant
 }  // namespace miconv
 
-extern "C" long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len)
+extern "C" long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len,
+                                                int causal, int window)
 {
     miconv::quant::Kv4 c;
     const int rc = miconv::quant::check_attend(cache, seqs, heads, max_new, max_len, &c);
     if (rc != MICONV_OK) return rc;
-    return seqs ? (long)miconv::quant::plan_attend(c, seqs, heads, max_new, max_len).bytes : 0;
+    return seqs ? (long)miconv::quant::plan_attend(c, seqs, heads, max_new, max_len, causal, window).bytes : 0;
 }
 
 extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, long tokens, const void *q,
@@ -616,7 +704,7 @@ extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, 
     if (quant::misaligned(q, 2) || quant::misaligned(out, 2) || quant::misaligned(starts, 4) ||
         quant::misaligned(lens, 4) || quant::misaligned(table, 4))
         return MICONV_ERR_ALIGN;
-    const quant::AttPlan p = quant::plan_attend(a.c, seqs, heads, max_new, max_len);
+    const quant::AttPlan p = quant::plan_attend(a.c, seqs, heads, max_new, max_len, causal, window);
     if ((long)p.row_blocks * p.splits >= 1L << 31) return MICONV_ERR_TOO_LARGE;
     if (p.bytes && (!ws || ws_bytes < p.bytes || quant::misaligned(ws, 256))) return MICONV_ERR_WORKSPACE;
     a.q = (const uint16_t *)q, a.out = (uint16_t *)out;

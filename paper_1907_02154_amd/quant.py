@@ -45,7 +45,7 @@ def lib() -> ctypes.CDLL:
         L.quant_matmul_i8.argtypes = [l, l, l, p, l, p, p, l, p, p, p, l, i, p, l, i, p, sz, p]
         L.quant_kv4_write.argtypes = [c, l, i, p, l, p, l, p, p]
         L.quant_kv4_read.argtypes = [c, l, p, i, p, l, p, l, p]
-        L.quant_attention_workspace_bytes.argtypes = [c, i, i, i, i]
+        L.quant_attention_workspace_bytes.argtypes = [c, i, i, i, i, i, i]
         L.quant_attention_kv4.argtypes = [c, i, i, l, p, l, p, p, p, i, i, i, f, i, i, p, l, p, sz, p]
         L.quant_matmul_workspace_bytes.restype = L.quant_attention_workspace_bytes.restype = l
         for name in ("rmsnorm_i8", "rows_i8", "matmul_i8", "kv4_write", "kv4_read", "attention_kv4"):
@@ -55,32 +55,35 @@ def lib() -> ctypes.CDLL:
 
 
 # ------------------------------------------------------------------ checks
+#
+# A call's own time on the host matters where one token is in flight, so each
+# check is one test in the good case.
+
+_Tensor, _getdevice = torch.Tensor, torch.cuda.current_device
+_rawstream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
 
 def _tensor(t, name: str, *dtypes) -> None:
-    if not isinstance(t, torch.Tensor):
+    if isinstance(t, _Tensor) and t.is_cuda and t.dtype in dtypes:
+        return
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
 
 
-def _matrix(t, name: str, shape, *dtypes) -> int:
-    """A device tensor [rows][cols] with dense rows (cols None: any); returns its row stride."""
+def _matrix(t, name: str, rows, cols, *dtypes) -> int:
+    """A device tensor [rows][cols] (None: any) with dense rows; returns its row stride."""
     _tensor(t, name, *dtypes)
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{name} must be {'[rows][cols]' if shape is None else list(shape)}, got {list(t.shape)}")
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must have dense rows")
-    return _row_stride(t, name, rows, cols)
-
-
-def _row_stride(t, name, rows, width) -> int:
-    s = t.stride(0) if rows > 1 else width
-    if s < width:
-        raise ValueError(f"{name} has overlapping rows")
-    return s
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape != (rows, cols)):
+        raise ValueError(f"{name} must be {'[rows][cols]' if rows is None else [rows, cols]}, got {list(shape)}")
+    s0, s1 = t.stride()
+    n, width = shape
+    if (width > 1 and s1 != 1) or (n > 1 and s0 < width):
+        raise ValueError(f"{name} must have dense rows that do not overlap")
+    return s0 if n > 1 else width
 
 
 def _heads(t, name: str, *dtypes) -> int:
@@ -89,33 +92,44 @@ def _heads(t, name: str, *dtypes) -> int:
     if t.dim() != 3:
         raise ValueError(f"{name} must be [tokens][heads][channels]")
     n, h, d = t.shape
-    if t.stride(2) != 1 or (h > 1 and t.stride(1) != d):
-        raise ValueError(f"{name} must be dense within each token")
-    return _row_stride(t, name, n, h * d)
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or (h > 1 and s1 != d) or (n > 1 and s0 < h * d):
+        raise ValueError(f"{name} must be dense within each token, and tokens must not overlap")
+    return s0 if n > 1 else h * d
 
 
 def _vector(t, name: str, n: int, dtype) -> None:
     _tensor(t, name, dtype)
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{name} must be a dense vector of {n}")
 
 
-def _empty(shape, dtype, device, stream):
-    """A tensor for work of `stream`: the current stream when None."""
+def _where(t, stream):
+    """The stream for work on t: the current one when None.  t has to be on the current device."""
+    i = t.get_device()
+    if i != _getdevice():
+        raise ValueError(f"tensors are on device {i}, the current device is {_getdevice()}")
+    if stream is not None:
+        return _stream(stream)
+    return _rawstream(i) if _rawstream else _stream(None)
+
+
+def _empty(like, shape, dtype, stream):
+    """A tensor on like's device for work of `stream` (None: the current one), so that its memory is free there."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
     with torch.cuda.stream(s):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _workspace(nbytes: int, what: str, ws, device, stream):
-    if nbytes < 0:
-        _check(int(nbytes), what)
+def _workspace(nbytes: int, what: str, ws, like, stream):
     if nbytes == 0:
         return None, 0
+    if nbytes < 0:
+        _check(int(nbytes), what)
     if ws is None:
-        ws = _empty(nbytes, torch.uint8, device, stream)
+        ws = _empty(like, nbytes, torch.uint8, stream)
     size = ws.numel() * ws.element_size()
     if not ws.is_cuda or not ws.is_contiguous() or size < nbytes or ws.data_ptr() % 256:
         raise ValueError(f"workspace must be a 256-byte aligned device tensor of at least {nbytes} bytes")
@@ -124,44 +138,55 @@ def _workspace(nbytes: int, what: str, ws, device, stream):
 
 # ------------------------------------------------------------------ rows in 8 bits
 
-def _out_i8(x, q, scale, stream):
-    rows, cols = x.shape
+def _out_i8(x, rows, cols, q, scale, stream):
     if q is None:
-        q = _empty((rows, cols), torch.int8, x.device, stream)
+        q, qs = _empty(x, (rows, cols), torch.int8, stream), cols
+    else:
+        qs = _matrix(q, "q", rows, cols, torch.int8)
     if scale is None:
-        scale = _empty((rows,), torch.float32, x.device, stream)
-    _vector(scale, "scale", rows, torch.float32)
-    return q, _matrix(q, "q", (rows, cols), torch.int8), scale
+        scale = _empty(x, rows, torch.float32, stream)
+    else:
+        _vector(scale, "scale", rows, torch.float32)
+    return q, qs, scale
 
 
 def rmsnorm_i8(x, weight=None, residual=None, eps: float = 1e-6, h=None, q=None, scale=None, stream=None):
     """RMS norm of each row of x [rows][cols] (fp32 or bf16), after the residual's addition, as 8-bit integers:
     (q int8 [rows][cols], scale fp32 [rows], h) with q * scale the normed row and h = x + residual in x's type,
     or None without a residual.  h may be residual or x: the addition is then in place."""
-    xs = _matrix(x, "x", None, torch.bfloat16, torch.float32)
+    xs = _matrix(x, "x", None, None, torch.bfloat16, torch.float32)
     rows, cols = x.shape
+    t = x.dtype
     if weight is not None:
         _vector(weight, "weight", cols, torch.float32)
+    rp = hp = None
     rs = hs = 0
     if residual is not None:
-        rs = _matrix(residual, "residual", (rows, cols), x.dtype)
+        rs = _matrix(residual, "residual", rows, cols, t)
         if h is None:
-            h = _empty((rows, cols), x.dtype, x.device, stream)
-        hs = _matrix(h, "h", (rows, cols), x.dtype)
+            h, hs = _empty(x, (rows, cols), t, stream), cols
+        else:
+            hs = _matrix(h, "h", rows, cols, t)
+        rp, hp = residual.data_ptr(), h.data_ptr()
     elif h is not None:
         raise ValueError("h is the sum with a residual: there is none")
-    q, qs, scale = _out_i8(x, q, scale, stream)
-    _check(lib().quant_rmsnorm_i8(rows, cols, _CODE[x.dtype], x.data_ptr(), xs, _ptr(residual), rs, _ptr(weight), eps,
-                                  _ptr(h), hs, q.data_ptr(), qs, scale.data_ptr(), _stream(stream)), "quant_rmsnorm_i8")
+    q, qs, scale = _out_i8(x, rows, cols, q, scale, stream)
+    rc = lib().quant_rmsnorm_i8(rows, cols, _CODE[t], x.data_ptr(), xs, rp, rs, _ptr(weight), eps, hp, hs, q.data_ptr(),
+                                qs, scale.data_ptr(), _where(x, stream))
+    if rc:
+        _check(rc, "quant_rmsnorm_i8")
     return q, scale, h
 
 
 def rows_i8(x, q=None, scale=None, stream=None):
     """Each row of x [rows][cols] (fp32 or bf16) as 8-bit integers: (q int8, scale fp32 [rows]), q * scale ~ x."""
-    xs = _matrix(x, "x", None, torch.bfloat16, torch.float32)
-    q, qs, scale = _out_i8(x, q, scale, stream)
-    _check(lib().quant_rows_i8(x.shape[0], x.shape[1], _CODE[x.dtype], x.data_ptr(), xs, q.data_ptr(), qs,
-                               scale.data_ptr(), _stream(stream)), "quant_rows_i8")
+    xs = _matrix(x, "x", None, None, torch.bfloat16, torch.float32)
+    rows, cols = x.shape
+    q, qs, scale = _out_i8(x, rows, cols, q, scale, stream)
+    rc = lib().quant_rows_i8(rows, cols, _CODE[x.dtype], x.data_ptr(), xs, q.data_ptr(), qs, scale.data_ptr(),
+                             _where(x, stream))
+    if rc:
+        _check(rc, "quant_rows_i8")
     return q, scale
 
 
@@ -169,7 +194,7 @@ def rows_i8(x, q=None, scale=None, stream=None):
 
 def matmul_workspace_bytes(a, w) -> int:
     """Bytes of workspace that matmul_i8 needs for these operands: 0 unless rows are not 16-byte aligned."""
-    sa, sw = _matrix(a, "a", None, torch.int8), _matrix(w, "w", None, torch.int8)
+    sa, sw = _matrix(a, "a", None, None, torch.int8), _matrix(w, "w", None, None, torch.int8)
     n = lib().quant_matmul_workspace_bytes(a.shape[0], w.shape[0], a.shape[1], a.data_ptr(), sa, w.data_ptr(), sw)
     if n < 0:
         _check(int(n), "quant_matmul_workspace_bytes")
@@ -181,10 +206,11 @@ def matmul_i8(a, a_scale, w, w_scale, bias=None, residual=None, relu: bool = Fal
     """act(a_scale[m] * w_scale[n] * (a w^T)[m][n] + bias[n] + residual[m][n]) of a int8 [M][K] and w int8 [N][K];
     fp32 scales [M], [N] and bias [N]; residual [M][N] of the output's type (it may be out).  out_dtype: bf16 or
     fp32, out's where out is given."""
-    sa = _matrix(a, "a", None, torch.int8)
-    sw = _matrix(w, "w", None, torch.int8)
-    (M, K), N = a.shape, w.shape[0]
-    if w.shape[1] != K:
+    sa = _matrix(a, "a", None, None, torch.int8)
+    sw = _matrix(w, "w", None, None, torch.int8)
+    M, K = a.shape
+    N, wk = w.shape
+    if wk != K:
         raise ValueError(f"w must be [N][{K}], got {list(w.shape)}")
     _vector(a_scale, "a_scale", M, torch.float32)
     _vector(w_scale, "w_scale", N, torch.float32)
@@ -193,15 +219,22 @@ def matmul_i8(a, a_scale, w, w_scale, bias=None, residual=None, relu: bool = Fal
     if out is None:
         if out_dtype not in _CODE:
             raise TypeError("out_dtype must be torch.bfloat16 or torch.float32")
-        out = _empty((M, N), out_dtype, a.device, stream)
-    so = _matrix(out, "out", (M, N), torch.bfloat16, torch.float32)
-    sr = 0 if residual is None else _matrix(residual, "residual", (M, N), out.dtype)
+        out, so = _empty(a, (M, N), out_dtype, stream), N
+    else:
+        so = _matrix(out, "out", M, N, torch.bfloat16, torch.float32)
+        out_dtype = out.dtype
+    rp, sr = None, 0
+    if residual is not None:
+        rp, sr = residual.data_ptr(), _matrix(residual, "residual", M, N, out_dtype)
     L = lib()
-    wp, wn = _workspace(L.quant_matmul_workspace_bytes(M, N, K, a.data_ptr(), sa, w.data_ptr(), sw), "quant_matmul_i8",
-                        ws, a.device, stream)
-    _check(L.quant_matmul_i8(M, N, K, a.data_ptr(), sa, a_scale.data_ptr(), w.data_ptr(), sw, w_scale.data_ptr(),
-                             _ptr(bias), _ptr(residual), sr, _CODE[out.dtype], out.data_ptr(), so, int(relu), wp, wn,
-                             _stream(stream)), "quant_matmul_i8")
+    ap, wp = a.data_ptr(), w.data_ptr()
+    sp, sn = None, 0
+    if (K | sa | sw | ap | wp) % 16:   # else no workspace is needed
+        sp, sn = _workspace(L.quant_matmul_workspace_bytes(M, N, K, ap, sa, wp, sw), "quant_matmul_i8", ws, a, stream)
+    rc = L.quant_matmul_i8(M, N, K, ap, sa, a_scale.data_ptr(), wp, sw, w_scale.data_ptr(), _ptr(bias), rp, sr,
+                           _CODE[out_dtype], out.data_ptr(), so, relu, sp, sn, _where(a, stream))
+    if rc:
+        _check(rc, "quant_matmul_i8")
     return out
 
 
@@ -214,18 +247,20 @@ class KV4Cache:
     __slots__ = ("k_codes", "k_exps", "v_codes", "v_exps", "pages", "heads", "page_size", "head_dim", "_desc")
 
     def __init__(self, k_codes, k_exps, v_codes, v_exps):
-        shape = k_codes.shape
-        if len(shape) != 4 or 2 * shape[3] not in HEAD_DIMS:
+        _tensor(k_codes, "k_codes", torch.uint8)
+        if k_codes.dim() != 4 or 2 * k_codes.shape[3] not in HEAD_DIMS:
             raise ValueError(f"codes must be [pages][heads][page_size][head_dim / 2], head_dim one of {HEAD_DIMS}")
-        for name, t, n in (("k_codes", k_codes, shape[3]), ("k_exps", k_exps, shape[3] // 16),
-                           ("v_codes", v_codes, shape[3]), ("v_exps", v_exps, shape[3] // 16)):
+        pages, heads, page_size, half = codes = tuple(k_codes.shape)
+        exps = (pages, heads, page_size, half // 16)
+        for name, t, shape in (("k_codes", k_codes, codes), ("k_exps", k_exps, exps), ("v_codes", v_codes, codes),
+                               ("v_exps", v_exps, exps)):
             _tensor(t, name, torch.uint8)
-            if t.shape[:3] != shape[:3] or t.dim() != 4 or t.shape[3] != n or not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous, {[*shape[:3], n]}; got {list(t.shape)}")
+            if t.shape != shape or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous, {list(shape)}; got {list(t.shape)}")
         self.k_codes, self.k_exps, self.v_codes, self.v_exps = k_codes, k_exps, v_codes, v_exps
-        self.pages, self.heads, self.page_size, self.head_dim = shape[0], shape[1], shape[2], 2 * shape[3]
-        self._desc = _Kv4(k_codes.data_ptr(), k_exps.data_ptr(), v_codes.data_ptr(), v_exps.data_ptr(), self.pages,
-                          self.heads, self.page_size, self.head_dim)
+        self.pages, self.heads, self.page_size, self.head_dim = pages, heads, page_size, 2 * half
+        self._desc = _Kv4(k_codes.data_ptr(), k_exps.data_ptr(), v_codes.data_ptr(), v_exps.data_ptr(), pages, heads,
+                          page_size, 2 * half)
 
     @classmethod
     def allocate(cls, pages: int, heads: int, page_size: int, head_dim: int, device="cuda") -> "KV4Cache":
@@ -245,47 +280,57 @@ def _cache(cache) -> KV4Cache:
     return cache
 
 
-def _token_shape(t, name, n, cache):
-    if tuple(t.shape) != (n, cache.heads, cache.head_dim):
+def _tokens(t, name, n, cache, *dtypes) -> int:
+    s = _heads(t, name, *dtypes)
+    if t.shape != (n, cache.heads, cache.head_dim):
         raise ValueError(f"{name} must be {[n, cache.heads, cache.head_dim]}, got {list(t.shape)}")
+    return s
 
 
 def kv4_write(k, v, slots, cache: KV4Cache, stream=None) -> None:
     """Quantises k and v [tokens][heads][head_dim] (fp32 or bf16; tokens may be strided) into the cache at
     slots int32 [tokens] (page * page_size + place; outside the cache: skipped)."""
     c = _cache(cache)
-    ks = _heads(k, "k", torch.bfloat16, torch.float32)
-    vs = _heads(v, "v", k.dtype)
-    n = k.shape[0]
-    _token_shape(k, "k", n, c)
-    _token_shape(v, "v", n, c)
+    n = k.shape[0] if isinstance(k, _Tensor) and k.dim() == 3 else -1
+    ks = _tokens(k, "k", n, c, torch.bfloat16, torch.float32)
+    vs = _tokens(v, "v", n, c, k.dtype)
     _vector(slots, "slots", n, torch.int32)
-    _check(lib().quant_kv4_write(c._desc, n, _CODE[k.dtype], k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(),
-                                 _stream(stream)), "quant_kv4_write")
+    rc = lib().quant_kv4_write(c._desc, n, _CODE[k.dtype], k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(),
+                               _where(k, stream))
+    if rc:
+        _check(rc, "quant_kv4_write")
 
 
 def kv4_read(slots, cache: KV4Cache, k=None, v=None, dtype=torch.bfloat16, stream=None):
     """The keys and values at slots int32 [tokens] as (k, v) [tokens][heads][head_dim] of dtype (bf16 or fp32; both
     hold every value exactly), k's where k is given; zeros for slots outside the cache."""
     c = _cache(cache)
-    n = slots.shape[0] if isinstance(slots, torch.Tensor) and slots.dim() == 1 else -1
+    n = slots.shape[0] if isinstance(slots, _Tensor) and slots.dim() == 1 else -1
     _vector(slots, "slots", n, torch.int32)
     if k is not None:
         dtype = k.dtype
     if dtype not in _CODE:
         raise TypeError("dtype must be torch.bfloat16 or torch.float32")
-    k = _empty((n, c.heads, c.head_dim), dtype, slots.device, stream) if k is None else k
-    v = _empty((n, c.heads, c.head_dim), dtype, slots.device, stream) if v is None else v
-    ks, vs = _heads(k, "k", dtype), _heads(v, "v", dtype)
-    _token_shape(k, "k", n, c)
-    _token_shape(v, "v", n, c)
-    _check(lib().quant_kv4_read(c._desc, n, slots.data_ptr(), _CODE[dtype], k.data_ptr(), ks, v.data_ptr(), vs,
-                                _stream(stream)), "quant_kv4_read")
+    shape = (n, c.heads, c.head_dim)
+    ks = vs = c.heads * c.head_dim
+    if k is None:
+        k = _empty(slots, shape, dtype, stream)
+    else:
+        ks = _tokens(k, "k", n, c, dtype)
+    if v is None:
+        v = _empty(slots, shape, dtype, stream)
+    else:
+        vs = _tokens(v, "v", n, c, dtype)
+    rc = lib().quant_kv4_read(c._desc, n, slots.data_ptr(), _CODE[dtype], k.data_ptr(), ks, v.data_ptr(), vs,
+                              _where(slots, stream))
+    if rc:
+        _check(rc, "quant_kv4_read")
     return k, v
 
 
-def attention_workspace_bytes(cache: KV4Cache, seqs: int, heads: int, max_new: int, max_len: int) -> int:
-    n = lib().quant_attention_workspace_bytes(_cache(cache)._desc, seqs, heads, max_new, max_len)
+def attention_workspace_bytes(cache: KV4Cache, seqs: int, heads: int, max_new: int, max_len: int, causal: bool = True,
+                              window: int = 0) -> int:
+    n = lib().quant_attention_workspace_bytes(_cache(cache)._desc, seqs, heads, max_new, max_len, causal, window)
     if n < 0:
         _check(int(n), "quant_attention_workspace_bytes")
     return int(n)
@@ -297,43 +342,43 @@ def attention_kv4(q, cache: KV4Cache, table, lens, starts=None, max_new: Optiona
     """Attention of queries q bf16 [tokens][heads][head_dim] (tokens may be strided) over the cache, which holds
     their own keys and values already.
 
-    table int32 [seqs][pages]: the pages of each sequence in order; lens int32 [seqs]: its cached tokens; starts
-    int32 [seqs + 1]: where its queries begin in q (None: one query each).  max_new and max_len bound the queries and
-    the length of any sequence (None: the bounds that the shapes give); work is laid out for these, so tight bounds
-    are faster.  scale: head_dim ** -0.5 unless given.  window > 0: only the last `window` places, the query's own
-    among them."""
+    table int32 [seqs][pages], contiguous: the pages of each sequence in order; lens int32 [seqs]: its cached tokens;
+    starts int32 [seqs + 1]: where its queries begin in q (None: one query each).  max_new and max_len bound the
+    queries and the length of any sequence (None: the bounds that the shapes give); work is laid out for these, so
+    tight bounds are faster.  scale: head_dim ** -0.5 unless given.  window > 0: only the last `window` places, the
+    query's own among them."""
     c = _cache(cache)
     qs = _heads(q, "q", torch.bfloat16)
     n, heads, d = q.shape
     if d != c.head_dim:
         raise ValueError(f"q has {d} channels a head, the cache {c.head_dim}")
     _tensor(table, "table", torch.int32)
-    if table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
-        raise ValueError("table must be [seqs][pages] with dense rows")
+    if table.dim() != 2 or not table.is_contiguous():
+        raise ValueError("table must be [seqs][pages], contiguous")
     seqs, width = table.shape
-    ts = table.stride(0) if seqs > 1 else width
-    if ts != width:
-        raise ValueError("table must be contiguous")
     _vector(lens, "lens", seqs, torch.int32)
-    if starts is None:
-        if n != seqs:
-            raise ValueError(f"without starts q holds one token for each of the {seqs} sequences, got {n}")
-    else:
+    sp = None
+    if starts is not None:
         _vector(starts, "starts", seqs + 1, torch.int32)
+        sp = starts.data_ptr()
+    elif n != seqs:
+        raise ValueError(f"without starts q holds one token for each of the {seqs} sequences, got {n}")
     if max_new is None:
         max_new = 1 if starts is None else max(n, 1)
     if max_len is None:
         max_len = width * c.page_size
     if out is None:
-        out = _empty((n, heads, d), torch.bfloat16, q.device, stream)
-    os_ = _heads(out, "out", torch.bfloat16)
-    if out.shape != q.shape:
-        raise ValueError("out must have q's shape")
+        out, outs = _empty(q, (n, heads, d), torch.bfloat16, stream), heads * d
+    else:
+        outs = _heads(out, "out", torch.bfloat16)
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
     L = lib()
-    wp, wn = _workspace(L.quant_attention_workspace_bytes(c._desc, seqs, heads, max_new, max_len),
-                        "quant_attention_kv4", ws, q.device, stream)
-    _check(L.quant_attention_kv4(c._desc, seqs, heads, n, q.data_ptr(), qs, _ptr(starts), lens.data_ptr(),
-                                 table.data_ptr(), ts, max_new, max_len, d ** -0.5 if scale is None else scale,
-                                 int(causal), window, out.data_ptr(), os_, wp, wn, _stream(stream)),
-           "quant_attention_kv4")
+    wp, wn = _workspace(L.quant_attention_workspace_bytes(c._desc, seqs, heads, max_new, max_len, causal, window),
+                        "quant_attention_kv4", ws, q, stream)
+    rc = L.quant_attention_kv4(c._desc, seqs, heads, n, q.data_ptr(), qs, sp, lens.data_ptr(), table.data_ptr(), width,
+                               max_new, max_len, d ** -0.5 if scale is None else scale, causal, window, out.data_ptr(),
+                               outs, wp, wn, _where(q, stream))
+    if rc:
+        _check(rc, "quant_attention_kv4")
     return out

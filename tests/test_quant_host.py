@@ -125,14 +125,16 @@ def test_attention_refusals(L):
     assert f(seqs=0) == f(tokens=0) == miconv.OK
     w = L.quant_attention_workspace_bytes
     c = cache(pages=4096, page_size=64)
-    assert w(c, 1, 4, 1, 16) == 0                       # one split: nothing to join
-    need = w(c, 1, 4, 1, 65536)
+    assert w(c, 1, 4, 1, 16, 1, 0) == 0                 # one split: nothing to join
+    need = w(c, 1, 4, 1, 65536, 1, 0)
     assert need > 0                                     # one sequence, many places: split over the work-groups
     assert f(c=c, seqs=1, tokens=1, ts=1024, max_len=65536, wsb=need - 1) == miconv.ERR_WORKSPACE
     assert f(c=c, seqs=1, tokens=1, ts=1024, max_len=65536, ws=None) == miconv.ERR_WORKSPACE
     assert f(c=c, seqs=1, tokens=1, ts=1024, max_len=65536, ws=FAKE + 16) == miconv.ERR_WORKSPACE
-    assert w(None, 1, 4, 1, 16) == miconv.ERR_NULL
-    assert w(c, 1, 3, 1, 16) == miconv.ERR_SHAPE
+    assert w(c, 1, 4, 1, 65536, 1, 100) == 0            # a short window: nothing to split
+    assert w(c, 1, 4, 1, 65536, 0, 100) == need         # which bounds nothing ahead of the query
+    assert w(None, 1, 4, 1, 16, 1, 0) == miconv.ERR_NULL
+    assert w(c, 1, 3, 1, 16, 1, 0) == miconv.ERR_SHAPE
 
 
 def test_binding_refuses_host_tensors_and_wrong_types():
