@@ -375,203 +375,350 @@ __global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
     }
 }
 
-// Many rows: 32 a wavefront, 32 * NW a work-group, over tiles of 64 cached
-// tokens that the work-group widens to bf16 once, into LDS.
-template <int D, int NW>
-__global__ __launch_bounds__(64 * NW) void attend_kv4_wide_kernel(AttArgs a)
-{
-    constexpr int NT = 64 * NW, TILE = 64;
-    constexpr int KP = D * 2 + 16;               // bytes between rows in LDS: keys are read by rows of 16 bytes,
-    constexpr int VP = (D / 32 | 1) * 64;        // values by blocks of 4 rows: an odd number of 64-byte steps
-    constexpr int STAGE = TILE * (KP + VP);
-    constexpr int PARTS = D / 32, UNITS = 2 * TILE * PARTS;   // groups of 32 channels: of a row, of a tile's keys and values
-    constexpr int PER = (UNITS + NT - 1) / NT;
-    __shared__ __align__(16) unsigned char lds[2 * STAGE];
+// What the kernels for many rows share: 32 rows a wavefront, tiles of 64 cached
+// tokens that a work-group widens to bf16 once, into LDS.
+template <int D>
+struct Wide {
+    static constexpr int TILE = 64;
+    static constexpr int KP = D * 2 + 16;              // bytes between rows in LDS: keys are read by rows of 16 bytes,
+    static constexpr int VP = (D / 32 | 1) * 64;       // values by blocks of 4 rows: an odd number of 64-byte steps
+    static constexpr int KBYTES = TILE * KP, VBYTES = TILE * VP;
+    static constexpr int PARTS = D / 32, UNITS = TILE * PARTS;   // groups of 32 channels: of a row, of a tile's keys (or values)
 
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64, col = lane % 32, half = lane / 32;
-    const int split = blockIdx.x % a.splits, kvh = blockIdx.y, s = blockIdx.z;
-    const int rb = a.row_blocks - 1 - blockIdx.x / a.splits;   // with a causal mask the last rows see most: they go first
-    const Seq sq = sequence(a, s);
-    const int rows = (sq.news < a.max_new ? sq.news : a.max_new) * a.group, r0 = rb * 32 * NW;
-    if (r0 >= rows) return;
-    const int r_last = r0 + 32 * NW < rows ? r0 + 32 * NW - 1 : rows - 1;
-
-    // the places any row of the block sees, within this split
-    int lo, hi, x;
-    seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), &lo, &x);
-    seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), &x, &hi);
-    lo = (lo & ~(TILE - 1)) + split * a.per_split;   // per_split is a multiple of the tile
-    hi = min(hi, lo + a.per_split);
-    const int tiles = hi > lo ? (hi - lo + TILE - 1) / TILE : 0;
-
-    // this lane's query row, and its part of it
-    const int r = r0 + 32 * wave + col;
-    const bool live = r < rows;
-    const int qi = (int)fdiv((unsigned)(live ? r : 0), a.dv_group), qh = kvh * a.group + (live ? r : 0) - qi * a.group;
-    int q_lo, q_hi;
-    seen(a, sq, qi, &q_lo, &q_hi);
-    if (!live) q_lo = 0, q_hi = 0;
-    int w_lo = live ? q_lo : 0x7FFFFFFF, w_hi = q_hi, w_all = live ? q_hi : 0x7FFFFFFF, w_from = q_lo;
+    // Where a lane stands: its query row, what that sees, and what any row (lo, hi) or every row (from, all) of the
+    // wavefront sees.
+    int qi, qh, q_lo, q_hi, lo, hi, from, all;
+    bool live;
+    __device__ __forceinline__ void place(const AttArgs &a, const Seq &sq, int kvh, int r, int rows)
+    {
+        live = r < rows;
+        qi = (int)fdiv((unsigned)(live ? r : 0), a.dv_group);
+        qh = kvh * a.group + (live ? r : 0) - qi * a.group;
+        seen(a, sq, qi, &q_lo, &q_hi);
+        lo = live ? q_lo : 0x7FFFFFFF, hi = live ? q_hi : 0, from = live ? q_lo : 0, all = live ? q_hi : 0x7FFFFFFF;
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) {   // the wavefront sees w_lo .. w_hi - 1, every row of it w_from .. w_all - 1
-        w_lo = min(w_lo, __shfl_xor(w_lo, d));
-        w_hi = max(w_hi, __shfl_xor(w_hi, d));
-        w_all = min(w_all, __shfl_xor(w_all, d));
-        w_from = max(w_from, __shfl_xor(w_from, d));
+        for (int d = 1; d < 32; d *= 2) {
+            lo = min(lo, __shfl_xor(lo, d));
+            hi = max(hi, __shfl_xor(hi, d));
+            from = max(from, __shfl_xor(from, d));
+            all = min(all, __shfl_xor(all, d));
+        }
+        lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
+        from = __builtin_amdgcn_readfirstlane(from), all = __builtin_amdgcn_readfirstlane(all);
     }
-    w_lo = __builtin_amdgcn_readfirstlane(w_lo), w_hi = __builtin_amdgcn_readfirstlane(w_hi);
-    w_all = __builtin_amdgcn_readfirstlane(w_all), w_from = __builtin_amdgcn_readfirstlane(w_from);
+
     bf16x8 qf[D / 16];
+    f32x16 sc[2], o[D / 32];
+    bf16x8 pf[4];
+    float m, l, c;   // m: the running maximum times c
+    __device__ __forceinline__ void start(const AttArgs &a, const Seq &sq, int half)
+    {
 #pragma unroll
-    for (int u = 0; u < D / 16; ++u) qf[u] = query8(a, a.q + (sq.row0 + qi) * a.qs + (long)qh * D + 8 * half + 16 * u);
-    const float c = factor(a);
-
-    const int32_t *pages = a.table + (long)s * a.table_stride;
-    // group i of this thread: keys, then values, by tokens
-    u32x4 code[PER];
-    uint32_t exp[PER];
-    const auto fetch = [&](int t0) {
+        for (int u = 0; u < D / 16; ++u) qf[u] = query8(a, a.q + (sq.row0 + qi) * a.qs + (long)qh * D + 8 * half + 16 * u);
+        c = factor(a);
+        m = kNegInf, l = 0.0f;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int idx = i * NT + tid;
-            if (UNITS % NT == 0 || idx < UNITS) {
-                const bool val = idx >= UNITS / 2;
-                const int in = idx - (val ? UNITS / 2 : 0), part = in % PARTS;
-                int t = t0 + in / PARTS;
-                t = t < hi ? t : hi - 1;   // past the end: a row that is seen, masked below
-                const long row = cached_row(a, pages, kvh, t);
-                const long at = row * PARTS + part;
-                code[i] = *(const u32x4 *)((val ? a.c.vc : a.c.kc) + at * 16);
-                // A value that is not finite makes the token's score NaN, which reaches the queries that see it;
-                // its own NaN times a probability of 0 would reach the others too.
-                const uint32_t ve = a.c.ve[at], ke = a.c.ke[at];
-                exp[i] = val ? (ve > kMaxExp ? 127u : ve) : (ve > kMaxExp ? 255u : ke);
-            }
-        }
-    };
-    const auto widen = [&](unsigned char *st) {
+        for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int idx = i * NT + tid;
-            if (UNITS % NT == 0 || idx < UNITS) {
-                const bool val = idx >= UNITS / 2;
-                const int in = idx - (val ? UNITS / 2 : 0), part = in % PARTS, t = in / PARTS;
-                unsigned char *to = st + (val ? TILE * KP + t * VP : t * KP) + part * 64;
-                const float f = exp_scale(exp[i]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) *(bf16x8 *)(to + 16 * j) = widen8(code[i][j], f);
-            }
-        }
-    };
-
-    float m = kNegInf, l = 0.0f;   // m: the running maximum times c
-    f32x16 o[D / 32];
-#pragma unroll
-    for (int cb = 0; cb < D / 32; ++cb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[cb][i] = 0.0f;
-
-    if (tiles > 0) {
-        fetch(lo);
-        widen(lds);
-        if (tiles > 1) fetch(lo + TILE);
-        __syncthreads();
+            for (int i = 0; i < 16; ++i) o[cb][i] = 0.0f;
     }
-    for (int t = 0; t < tiles; ++t) {
-        const int t0 = lo + t * TILE;
-        if (t + 1 < tiles) {
-            widen(lds + (t + 1 & 1) * STAGE);   // read last before the previous barrier
-            if (t + 2 < tiles) fetch(t0 + 2 * TILE);
-        }
-        if (t0 < w_hi && t0 + TILE > w_lo) {
-            const unsigned char *kt = lds + (t & 1) * STAGE, *vt = kt + TILE * KP;
-            f32x16 sc[2];
+
+    // A lane's operand of the scores: row 32 b + lane % 32 of the keys, 16 bytes of step u.
+    static __device__ __forceinline__ bf16x8 key(const unsigned char *kt, int lane, int b, int u)
+    {
+        return *(const bf16x8 *)(kt + (32 * b + lane % 32) * KP + 32 * u + 16 * (lane / 32));
+    }
+    __device__ __forceinline__ void no_scores()
+    {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sc[b][i] = 0.0f;
-#pragma unroll
-                for (int u = 0; u < D / 16; ++u) {
-                    const bf16x8 kf = *(const bf16x8 *)(kt + (32 * b + col) * KP + 32 * u + 16 * half);
-                    sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[u], sc[b], 0, 0, 0);
-                }
-            }
-            if (t0 < w_from || t0 + TILE > w_all) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int at = t0 + 32 * b + i % 4 + 8 * (i / 4) + 4 * half;
-                        sc[b][i] = at >= q_lo && at < q_hi ? sc[b][i] : kNegInf;
-                    }
-            }
-            float top = kNegInf;
+            for (int i = 0; i < 16; ++i) sc[b][i] = 0.0f;
+    }
+
+    // Of the values: channel 32 cb + lane % 32 of the lane's 8 tokens of a step of 16, 4 * half .. + 3 and 8 later, as
+    // the scores have them.
+    static __device__ __forceinline__ bf16x8 value(const unsigned char *vt, int lane, int cb, int k)
+    {
+        const unsigned char *at =
+            vt + (16 * k + 4 * (lane / 32) + lane % 16 / 4) * VP + cb * 64 + lane / 16 % 2 * 32 + lane % 4 * 8;
+        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
+        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * VP));
+        return __builtin_shufflevector(__builtin_bit_cast(bf16x4, v0), __builtin_bit_cast(bf16x4, v1), 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+
+    // The scores of the tile at t0 become probabilities in pf; m, l and o follow.
+    __device__ __forceinline__ void soften(int t0, int half)
+    {
+        if (t0 < from || t0 + TILE > all) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
-            top *= c;
-            if (__any(top > m + kGrow)) {   // also where m is still -inf
-                top = fmaxf(top, m);
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float f = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-                m = top;
-                l *= f;
-#pragma unroll
-                for (int cb = 0; cb < D / 32; ++cb) o[cb] *= f;
-            }
-            const float base = m == kNegInf ? 0.0f : m;
-            bf16x8 pf[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                u32x4 w;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int at = 8 * (k % 2) + 2 * i;
-                    w[i] = weights2(sc[k / 2][at], sc[k / 2][at + 1], c, base, l);
+                for (int i = 0; i < 16; ++i) {
+                    const int at = t0 + 32 * b + i % 4 + 8 * (i / 4) + 4 * half;
+                    sc[b][i] = at >= q_lo && at < q_hi ? sc[b][i] : kNegInf;
                 }
-                pf[k] = __builtin_bit_cast(bf16x8, w);
+        }
+        float top = kNegInf;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
+        top *= c;
+        if (__any(top > m + kGrow)) {   // also where m is still -inf
+            top = fmaxf(top, m);
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float f = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            l *= f;
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb) o[cb] *= f;
+        }
+        const float base = m == kNegInf ? 0.0f : m;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = 8 * (k % 2) + 2 * i;
+                w[i] = weights2(sc[k / 2][at], sc[k / 2][at + 1], c, base, l);
             }
-            // a lane's 8 tokens of the reduction: 4 * half .. + 3 and 8 later, as the scores have them
+            pf[k] = __builtin_bit_cast(bf16x8, w);
+        }
+    }
+
+    // The row's result, or its part of a split.
+    __device__ __forceinline__ void finish(const AttArgs &a, const Seq &sq, int s, int split, int half)
+    {
+        l += __shfl_xor(l, 32);
+        if (!live) return;
+        if (a.splits == 1) {
+            const float f = l == 0.0f ? 0.0f : 1.0f / l;
+            uint16_t *out = a.out + (sq.row0 + qi) * a.os + (long)qh * D + 4 * half;
 #pragma unroll
             for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const unsigned char *at =
-                        vt + (16 * k + 4 * half + lane % 16 / 4) * VP + cb * 64 + lane / 16 % 2 * 32 + lane % 4 * 8;
-                    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
-                    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * VP));
-                    const bf16x8 vf = __builtin_shufflevector(__builtin_bit_cast(bf16x4, v0), __builtin_bit_cast(bf16x4, v1), 0,
-                                                              1, 2, 3, 4, 5, 6, 7);
-                    o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[k], o[cb], 0, 0, 0);
+                for (int i = 0; i < 4; ++i) {
+                    const float v[4] = {o[cb][4 * i] * f, o[cb][4 * i + 1] * f, o[cb][4 * i + 2] * f, o[cb][4 * i + 3] * f};
+                    store4(out + 32 * cb + 8 * i, v);
                 }
+        } else {
+            float *part = a.part + ((((long)s * a.heads + qh) * a.max_new + qi) * a.splits + split) * (D + 4);
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float v[4] = {o[cb][4 * i], o[cb][4 * i + 1], o[cb][4 * i + 2], o[cb][4 * i + 3]};
+                    store4(part + 32 * cb + 8 * i + 4 * half, v);
+                }
+            if (half == 0) part[D] = m, part[D + 1] = l;
         }
-        __syncthreads();
     }
+};
 
-    l += __shfl_xor(l, 32);
-    if (!live) return;
-    if (a.splits == 1) {
-        const float f = l == 0.0f ? 0.0f : 1.0f / l;
-        uint16_t *out = a.out + (sq.row0 + qi) * a.os + (long)qh * D + 4 * half;
+// Keys or values of a tile on their way from the cache to LDS, by NT threads:
+// groups of 32 channels by tokens.  Loads run a tile ahead of the conversion,
+// the page table's two.
+template <int D, int NT>
+struct Mover {
+    static constexpr int PARTS = Wide<D>::PARTS, UNITS = Wide<D>::UNITS, PER = (UNITS + NT - 1) / NT;
+    u32x4 code[PER];
+    uint32_t exp[PER], vexp[PER];
+    int page[PER], place[PER];
+
+    __device__ __forceinline__ void look(const AttArgs &a, const int32_t *pages, int tid, int t0, int hi)
+    {
 #pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float v[4] = {o[cb][4 * i] * f, o[cb][4 * i + 1] * f, o[cb][4 * i + 2] * f, o[cb][4 * i + 3] * f};
-                store4(out + 32 * cb + 8 * i, v);
-            }
-    } else {
-        float *part = a.part + ((((long)s * a.heads + qh) * a.max_new + qi) * a.splits + split) * (D + 4);
-#pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float v[4] = {o[cb][4 * i], o[cb][4 * i + 1], o[cb][4 * i + 2], o[cb][4 * i + 3]};
-                store4(part + 32 * cb + 8 * i + 4 * half, v);
-            }
-        if (half == 0) part[D] = m, part[D + 1] = l;
+        for (int i = 0; i < PER; ++i) {
+            const int t = min(t0 + (i * NT + tid) / PARTS, hi - 1);   // past the end: a row that is seen, masked later
+            const unsigned p = fdiv((unsigned)t, a.c.dv_page);
+            place[i] = t - (int)p * a.c.page_size;
+            page[i] = pages[p];
+        }
     }
+    __device__ __forceinline__ void fetch(const AttArgs &a, bool keys, int tid, int kvh)
+    {
+        const int last_page = (int)(a.c.slots / a.c.page_size) - 1;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const unsigned pg = (unsigned)min(max(page[i], 0), last_page);
+            const uint64_t row = (uint64_t)pg * (unsigned)(a.c.heads * a.c.page_size) + (unsigned)(kvh * a.c.page_size + place[i]);
+            const uint64_t at = row * PARTS + (unsigned)((i * NT + tid) % PARTS);
+            code[i] = *(const u32x4 *)((keys ? a.c.kc : a.c.vc) + at * 16);
+            exp[i] = (keys ? a.c.ke : a.c.ve)[at];
+            vexp[i] = a.c.ve[at];
+        }
+    }
+    // A value that is not finite makes the token's score NaN, which reaches the queries that see it; its own NaN times
+    // a probability of 0 would reach the others too.
+    __device__ __forceinline__ void widen(unsigned char *to, int pitch, bool keys, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int idx = i * NT + tid;
+            if (UNITS % NT == 0 || idx < UNITS) {
+                unsigned char *at = to + idx / PARTS * pitch + idx % PARTS * 64;
+                const float f = exp_scale(vexp[i] <= kMaxExp ? exp[i] : keys ? 255u : 127u);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *(bf16x8 *)(at + 16 * j) = widen8(code[i][j], f);
+            }
+        }
+    }
+};
+
+// The places that any row of a block sees within a split.
+__device__ __forceinline__ void block_range(const AttArgs &a, const Seq &sq, int r0, int r_last, int split, int *lo, int *hi)
+{
+    int x;
+    seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), lo, &x);
+    seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), &x, hi);
+    *lo = (*lo & ~63) + split * a.per_split;   // per_split is a multiple of the tile
+    *hi = min(*hi, *lo + a.per_split);
+}
+
+// A work-group's sequence, key head, split and block of `block` rows, if there
+// is one.  A sequence's last rows see most under a causal mask: they go first,
+// of every sequence and head, and the short work comes last.  Heads follow one
+// another, so where they are a multiple of eight a head's work-groups share a
+// die's L2.
+__device__ __forceinline__ bool wide_place(const AttArgs &a, int block, Seq *sq, int *s, int *kvh, int *split, int *r0, int *rows)
+{
+    const int pairs = a.seqs * a.c.heads, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+    *kvh = pair % a.c.heads, *s = pair / a.c.heads, *split = rest % a.splits;
+    *sq = sequence(a, *s);
+    *rows = min(sq->news, a.max_new) * a.group;
+    *r0 = ((*rows + block - 1) / block - 1 - rest / a.splits) * block;
+    return *r0 >= 0;
+}
+
+// Many rows: NW wavefronts in step, two on a SIMD (heads of up to 128 channels)
+// or one (wider ones: their sums and operands take more registers than two
+// have).  The next tile is widened first, over the tile before, then this one
+// worked on, and one barrier a tile keeps the wavefronts together.
+//
+// Bound by what a barrier's phases do not overlap (LDS reads and products,
+// then the probabilities): at two prompts of 4096 tokens, 32 heads of 128 on 8
+// key heads, 281 us, 930 TFLOP/s; the matrix cores alone would take 105.
+// Measured beside it: the tile widened between the scores and the
+// probabilities 292 us, after these 285; the two wavefronts of a SIMD half a
+// tile apart, one at its products and one at its probabilities, two barriers a
+// tile, 313; work-groups of four wavefronts, two on a compute unit, 8% more;
+// operands read as their products need them, 16% more (heads of 64 take these
+// registers for a third wavefront on a SIMD instead).
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) void attend_kv4_wide_kernel(AttArgs a)
+{
+    typedef Wide<D> W;
+    constexpr int TILE = W::TILE;
+    constexpr bool ASK = D == 96 || D == 128;   // whether registers hold a tile's operands ahead of their products
+    __shared__ __align__(16) unsigned char lds[2 * (W::KBYTES + W::VBYTES)];
+    unsigned char *const keys = lds, *const vals = lds + 2 * W::KBYTES;
+
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    int s, kvh, split, r0, rows, lo, hi;
+    Seq sq;
+    if (!wide_place(a, 32 * NW, &sq, &s, &kvh, &split, &r0, &rows)) return;
+    block_range(a, sq, r0, min(r0 + 32 * NW, rows) - 1, split, &lo, &hi);
+    const int tiles = hi > lo ? (hi - lo + TILE - 1) / TILE : 0;
+    W w;
+    w.place(a, sq, kvh, r0 + 32 * wave + lane % 32, rows);
+    w.start(a, sq, half);
+
+    // Eight wavefronts: the first four move the keys, the others the values; four: both.
+    constexpr int MOVERS = NW == 8 ? 1 : 2;
+    const int tid = threadIdx.x % 256;
+    const int32_t *pages = a.table + (long)s * a.table_stride;
+    Mover<D, 256> mv[MOVERS];
+    const auto moves_keys = [&](int i) { return MOVERS == 2 ? i == 0 : wave < 4; };
+    const auto look = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < MOVERS; ++i) mv[i].look(a, pages, tid, lo + t * TILE, hi);
+    };
+    const auto fetch = [&] {
+#pragma unroll
+        for (int i = 0; i < MOVERS; ++i) mv[i].fetch(a, moves_keys(i), tid, kvh);
+    };
+    const auto widen = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < MOVERS; ++i) {
+            if (moves_keys(i)) mv[i].widen(keys + (t & 1) * W::KBYTES, W::KP, true, tid);
+            else mv[i].widen(vals + (t & 1) * W::VBYTES, W::VP, false, tid);
+        }
+    };
+    if (tiles > 0) {
+        look(0);
+        fetch();
+        if (tiles > 1) look(1);
+        widen(0);
+        if (tiles > 1) fetch();
+        if (tiles > 2) look(2);
+    }
+    // the loads of later tiles stay in flight across it
+    const auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    barrier();
+    for (int t = 0; t < tiles; ++t) {
+        const int t0 = lo + t * TILE;
+        const bool active = t0 < w.hi && t0 + TILE > w.lo;
+        const unsigned char *kt = keys + (t & 1) * W::KBYTES, *vt = vals + (t & 1) * W::VBYTES;
+        if (t + 1 < tiles) {
+            widen(t + 1);   // over a tile that was last read before the previous barrier
+            if (t + 2 < tiles) fetch();
+            if (t + 3 < tiles) look(t + 3);
+        }
+        // Operands are asked for together and before their products: left to itself the compiler waits for each in turn.
+        if (active) {
+            w.no_scores();
+            if constexpr (ASK) {
+                bf16x8 kf[2][D / 16];
+#pragma unroll
+                for (int u = 0; u < D / 16; ++u)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) kf[b][u] = W::key(kt, lane, b, u);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int u = 0; u < D / 16; ++u)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+                        w.sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b][u], w.qf[u], w.sc[b], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int u = 0; u < D / 16; ++u)
+                        w.sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W::key(kt, lane, b, u), w.qf[u], w.sc[b], 0, 0, 0);
+            }
+        }
+        if (active) {
+            w.soften(t0, half);
+            if constexpr (ASK) {
+                bf16x8 vf[2][4];
+#pragma unroll
+                for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) vf[cb][k] = W::value(vt, lane, cb, k);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int cb = 0; cb < D / 32; ++cb) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        w.o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[cb & 1][k], w.pf[k], w.o[cb], 0, 0, 0);
+                    if (cb + 2 < D / 32) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) vf[cb & 1][k] = W::value(vt, lane, cb + 2, k);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        w.o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W::value(vt, lane, cb, k), w.pf[k], w.o[cb], 0, 0, 0);
+            }
+        }
+        barrier();
+    }
+    w.finish(a, sq, s, split, half);
 }
 
 // Joins the splits of a row of a head: four wavefronts take turns at them.
@@ -615,7 +762,7 @@ struct AttPlan {
     size_t bytes;
 };
 
-constexpr int wide_waves(int dim) { return dim <= 128 ? 8 : 4; }
+constexpr int wide_rows(int dim) { return dim <= 128 ? 256 : 128; }   // rows of a work-group
 
 AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len, int causal, int window)
 {
@@ -624,7 +771,7 @@ AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len,
     // The kernel for few rows holds up to 64 of them in registers, fewer of wide heads.
     p.wide = rows > (c.dim <= 64 ? 64 : c.dim <= 128 ? 32 : 16);
     p.nb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const long block = p.wide ? 32 * wide_waves(c.dim) : 16 * p.nb;
+    const long block = p.wide ? wide_rows(c.dim) : 16 * p.nb;
     p.row_blocks = (int)((rows + block - 1) / block);
     // Places that a block of rows sees: with a window behind each, its own and those of the block's tokens.
     long len = max_len;
@@ -658,8 +805,9 @@ int launch_attend(const AttArgs &a, const AttPlan &p, hipStream_t st)
 {
     const dim3 grid((unsigned)((long)p.row_blocks * p.splits), (unsigned)a.c.heads, (unsigned)a.seqs);
     if (p.wide) {
-        constexpr int NW = wide_waves(D);
-        launch_kernel(attend_kv4_wide_kernel<D, NW>, grid, dim3(64 * NW), 0, st, a);
+        const dim3 all(grid.x * grid.y * grid.z);
+        constexpr int NW = wide_rows(D) / 32;
+        launch_kernel(attend_kv4_wide_kernel<D, NW>, all, dim3(64 * NW), 0, st, a);
     } else {
         void (*k)(AttArgs) = attend_kv4_kernel<D, 1>;
         if constexpr (D <= 128)
@@ -705,7 +853,7 @@ extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, 
         quant::misaligned(lens, 4) || quant::misaligned(table, 4))
         return MICONV_ERR_ALIGN;
     const quant::AttPlan p = quant::plan_attend(a.c, seqs, heads, max_new, max_len, causal, window);
-    if ((long)p.row_blocks * p.splits >= 1L << 31) return MICONV_ERR_TOO_LARGE;
+    if ((double)p.row_blocks * p.splits * a.c.heads * seqs >= 0x1p31) return MICONV_ERR_TOO_LARGE;
     if (p.bytes && (!ws || ws_bytes < p.bytes || quant::misaligned(ws, 256))) return MICONV_ERR_WORKSPACE;
     a.q = (const uint16_t *)q, a.out = (uint16_t *)out;
     a.starts = starts, a.lens = lens, a.table = table;
