@@ -127,9 +127,11 @@ int quant_kv4_read(const quant_kv4 *cache, long tokens, const int32_t *slots, in
  * q, out: bf16 [tokens][heads][head_dim], rows q_stride / out_stride elements
  * apart.  max_new and max_len bound the queries and the length of any
  * sequence: rows past max_new are not computed, places past max_len (or the
- * table's end) are not seen.  Scores, softmax statistics and sums are fp32;
- * the probabilities are rounded to bf16 for the matrix cores, and the sum they
- * are divided by is that of the rounded ones.
+ * table's end) are not seen.  Scores, softmax statistics and sums are fp32.
+ * For the matrix cores the probabilities are rounded to bf16, and the sum they
+ * are divided by is that of the rounded ones; where a key head has few query
+ * rows (64, 32 or 16 of head_dim 64, 128 or more) they keep a second bf16
+ * part, 16 bits in all.
  * Errors: MICONV_ERR_NULL, MICONV_ERR_SHAPE (heads no multiple of the cache's,
  * a stride below its row, max_new or max_len < 1, table_stride < 1),
  * MICONV_ERR_UNSUPPORTED (head_dim), MICONV_ERR_ALIGN, MICONV_ERR_TOO_LARGE

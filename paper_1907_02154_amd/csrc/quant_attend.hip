@@ -78,15 +78,6 @@ __device__ __forceinline__ void seen(const AttArgs &a, const Seq &q, int i, int 
     *hi = h < 0 ? 0 : h;
 }
 
-__device__ __forceinline__ long cached_row(const AttArgs &a, const int32_t *pages, int kvh, int t)
-{
-    const unsigned p = fdiv((unsigned)t, a.c.dv_page), place = (unsigned)t - p * (unsigned)a.c.page_size;
-    long page = pages[p];
-    const long last = a.c.slots / a.c.page_size - 1;
-    page = page < 0 ? 0 : page > last ? last : page;
-    return (page * a.c.heads + kvh) * a.c.page_size + place;
-}
-
 // Scale bits of an exponent byte; above 252 an infinite scale, which converts to NaN.
 __device__ __forceinline__ float exp_scale(uint32_t e)
 {
@@ -272,7 +263,7 @@ __global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
                         sc[k][b][i] = t >= q_lo[b] && t < q_hi[b] ? sc[k][b][i] : kNegInf;
                     }
         }
-        bf16x8 pf[NB];
+        bf16x8 pf[NB], pl[NB];   // the probabilities in two bf16 parts: the matrix cores wait for memory here anyway
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             float top = kNegInf;
@@ -292,11 +283,18 @@ __global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
                 for (int cb = 0; cb < CB; ++cb) o[cb][b] *= f;
             }
             const float base = m[b] == kNegInf ? 0.0f : m[b];
-            u32x4 w;
+            u32x4 w, v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w[i] = weights2(sc[i / 2][b][i % 2 * 2], sc[i / 2][b][i % 2 * 2 + 1], c, base, l[b]);
+            for (int i = 0; i < 4; ++i) {
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i / 2][b][i % 2 * 2], c, -base));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i / 2][b][i % 2 * 2 + 1], c, -base));
+                const uint32_t two = pack_bf16x2(p0, p1);
+                w[i] = two;
+                v[i] = pack_bf16x2(p0 - __builtin_bit_cast(float, two << 16), p1 - __builtin_bit_cast(float, two & 0xFFFF0000u));
+                l[b] += p0 + p1;
+            }
             pf[b] = __builtin_bit_cast(bf16x8, w);
+            pl[b] = __builtin_bit_cast(bf16x8, v);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         // a lane's 8 tokens of the reduction: 4 * quad .. + 3 of each 16, as the scores have them
@@ -308,8 +306,10 @@ __global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
             const bf16x8 vf = __builtin_shufflevector(__builtin_bit_cast(bf16x4, v0), __builtin_bit_cast(bf16x4, v1), 0, 1, 2,
                                                       3, 4, 5, 6, 7);
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b) {
                 o[cb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[b], o[cb][b], 0, 0, 0);
+                o[cb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[b], o[cb][b], 0, 0, 0);
+            }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     };
@@ -603,8 +603,8 @@ __device__ __forceinline__ bool wide_place(const AttArgs &a, int block, Seq *sq,
 // probabilities 292 us, after these 285; the two wavefronts of a SIMD half a
 // tile apart, one at its products and one at its probabilities, two barriers a
 // tile, 313; work-groups of four wavefronts, two on a compute unit, 8% more;
-// operands read as their products need them, 16% more (heads of 64 take these
-// registers for a third wavefront on a SIMD instead).
+// operands read as their products need them, 16% more (heads of 64 and less do
+// that, and have room for a second work-group on a compute unit).
 template <int D, int NW>
 __global__ __launch_bounds__(64 * NW) void attend_kv4_wide_kernel(AttArgs a)
 {

@@ -86,24 +86,29 @@ __device__ __forceinline__ void row_unit(const RowArgs &a, const T *x, const T *
             store8(h + at, t);
         }
         if (a.w) load8(a.w + at, w);
-    } else {
+    } else {   // all loads first: the last element stands in past the end
+        float r[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            t[i] = w[i] = 0.0f;
-            if (i < n) {
-                t[i] = load1(x + at + i);
-                if (res) {
-                    t[i] = rounded(t[i] + load1(res + at + i), x);
-                    store1(h + at + i, t[i]);
-                }
-                if (a.w) w[i] = a.w[at + i];
-            }
+            const int k = at + min(i, n - 1);
+            t[i] = load1(x + k);
+            r[i] = res ? load1(res + k) : 0.0f;
+            w[i] = a.w ? a.w[k] : 0.0f;
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (res) t[i] = rounded(t[i] + r[i], x);
+            if (i >= n) t[i] = 0.0f;
+        }
+        if (res)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) store1(h + at + i, t[i]);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         s.sum += t[i] * t[i];
-        if (a.w) t[i] *= w[i];
+        if (a.w) t[i] = i < n ? t[i] * w[i] : 0.0f;
         const uint32_t b = __builtin_bit_cast(uint32_t, t[i]) & 0x7FFFFFFFu;
         s.top = b > s.top ? b : s.top;
     }
