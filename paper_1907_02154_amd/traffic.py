@@ -86,6 +86,15 @@ SOURCES = {
     "scan_upsweep_kernel": "vision.hip",
     "segsort_merge_kernel": "vision.hip",
     "segsort_tile_kernel": "vision.hip",
+    "attend_kv4_kernel": "quant_attend.hip",
+    "attend_kv4_wide_kernel": "quant_attend.hip",
+    "attend_join_kernel": "quant_attend.hip",
+    "kv4_write_kernel": "quant_cache.hip",
+    "kv4_read_kernel": "quant_cache.hip",
+    "matmul_i8_tile_kernel": "quant_matmul.hip",
+    "matmul_i8_align_kernel": "quant_matmul.hip",
+    "rows_i8_kernel": "quant_rows.hip",
+    "rows_i8_long_kernel": "quant_rows.hip",
 }
 
 
