@@ -73,7 +73,8 @@ int quant_rows_i8(long rows, long cols, int dtype, const void *x, long x_stride,
  * Errors: MICONV_ERR_NULL, MICONV_ERR_SHAPE (M < 0, N or K < 1, a stride below
  * its row), MICONV_ERR_UNSUPPORTED (out_dtype), MICONV_ERR_ALIGN,
  * MICONV_ERR_TOO_LARGE (K > 131071, where the sum could pass 32 bits; M or
- * N >= 2^31), MICONV_ERR_WORKSPACE. */
+ * N >= 2^31, or so many outputs that a grid does not hold them),
+ * MICONV_ERR_WORKSPACE. */
 long quant_matmul_workspace_bytes(long M, long N, long K, const int8_t *a, long a_stride, const int8_t *w,
                                   long w_stride);
 int quant_matmul_i8(long M, long N, long K, const int8_t *a, long a_stride, const float *a_scale, const int8_t *w,
@@ -103,7 +104,8 @@ typedef struct quant_kv4 {
  * between 4 and 6 allow), its values the nearest, ties to the even code.  A
  * group that holds a NaN or an infinity gets exponent byte 255 and codes 0.
  * Errors: MICONV_ERR_NULL, MICONV_ERR_SHAPE, MICONV_ERR_UNSUPPORTED (dtype,
- * head_dim), MICONV_ERR_ALIGN, MICONV_ERR_TOO_LARGE (2^31 slots or tokens). */
+ * head_dim), MICONV_ERR_ALIGN, MICONV_ERR_TOO_LARGE (2^31 slots, more than 2^25
+ * tokens). */
 int quant_kv4_write(const quant_kv4 *cache, long tokens, int dtype, const void *k, long k_stride, const void *v,
                     long v_stride, const int32_t *slots, void *stream);
 
@@ -135,7 +137,8 @@ int quant_kv4_read(const quant_kv4 *cache, long tokens, const int32_t *slots, in
  * Errors: MICONV_ERR_NULL, MICONV_ERR_SHAPE (heads no multiple of the cache's,
  * a stride below its row, max_new or max_len < 1, table_stride < 1),
  * MICONV_ERR_UNSUPPORTED (head_dim), MICONV_ERR_ALIGN, MICONV_ERR_TOO_LARGE
- * (2^31 rows or slots), MICONV_ERR_WORKSPACE. */
+ * (2^31 slots, 2^24 query rows of a key head, or so much work that a grid does
+ * not hold it), MICONV_ERR_WORKSPACE. */
 long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len,
                                      int causal, int window);
 int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, long tokens, const void *q, long q_stride,

@@ -795,7 +795,7 @@ int check_attend(const quant_kv4 *cache, int seqs, int heads, int max_new, int m
     const int rc = kv4_view(cache, c);
     if (rc != MICONV_OK) return rc;
     if (seqs < 0 || heads < 1 || heads % c->heads || max_new < 1 || max_len < 1) return MICONV_ERR_SHAPE;
-    if ((long)max_new * (heads / c->heads) >= 1L << 30 || max_len >= 1 << 30 || seqs > 65535 || heads > 65535)
+    if ((long)max_new * (heads / c->heads) >= 1L << 24 || max_len >= 1 << 30 || seqs > 65535 || heads > 65535)
         return MICONV_ERR_TOO_LARGE;
     return MICONV_OK;
 }
@@ -853,7 +853,8 @@ extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, 
         quant::misaligned(lens, 4) || quant::misaligned(table, 4))
         return MICONV_ERR_ALIGN;
     const quant::AttPlan p = quant::plan_attend(a.c, seqs, heads, max_new, max_len, causal, window);
-    if ((double)p.row_blocks * p.splits * a.c.heads * seqs >= 0x1p31) return MICONV_ERR_TOO_LARGE;
+    // a grid holds fewer than 2^32 threads
+    if ((double)p.row_blocks * p.splits * (p.wide ? 512.0 * a.c.heads * seqs : 256.0) >= 0x1p32) return MICONV_ERR_TOO_LARGE;
     if (p.bytes && (!ws || ws_bytes < p.bytes || quant::misaligned(ws, 256))) return MICONV_ERR_WORKSPACE;
     a.q = (const uint16_t *)q, a.out = (uint16_t *)out;
     a.starts = starts, a.lens = lens, a.table = table;

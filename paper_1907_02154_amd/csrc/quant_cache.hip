@@ -157,7 +157,7 @@ int run_cache(const quant_kv4 *cache, long tokens, int dtype, const void *k, lon
     if (!b) return MICONV_ERR_UNSUPPORTED;
     const long width = (long)a.c.heads * a.c.dim;
     if (tokens < 0 || k_stride < width || v_stride < width) return MICONV_ERR_SHAPE;
-    if (tokens >= 1L << 31) return MICONV_ERR_TOO_LARGE;
+    if (tokens > 1L << 25) return MICONV_ERR_TOO_LARGE;   // a grid holds fewer than 2^32 threads
     if (tokens == 0) return MICONV_OK;
     if (!k || !v || !slots) return MICONV_ERR_NULL;
     if (misaligned(k, b) || misaligned(v, b) || misaligned(slots, 4)) return MICONV_ERR_ALIGN;

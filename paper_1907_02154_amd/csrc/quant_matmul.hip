@@ -276,7 +276,8 @@ template <typename T, int BM, int BN, int WM, int WN, int KG, int NST>
 int go_tile(MatArgs a, hipStream_t st)
 {
     a.mt = ceil_div(a.M, BM), a.nt = ceil_div(a.N, BN);
-    if ((long)a.mt * a.nt >= 1L << 31 || (long)kGroup * a.nt >= 1L << 31) return MICONV_ERR_TOO_LARGE;
+    // a grid holds fewer than 2^32 threads
+    if ((long)a.mt * a.nt * (64 * WM * WN * KG) >= 1L << 32 || (long)kGroup * a.nt >= 1L << 31) return MICONV_ERR_TOO_LARGE;
     a.tiles = a.mt * a.nt;
     a.dv_group = make_fastdiv((unsigned)(kGroup * a.nt));
     launch_kernel(matmul_i8_tile_kernel<T, BM, BN, WM, WN, KG, NST>, dim3((unsigned)a.tiles), dim3(64 * WM * WN * KG), 0, st, a);

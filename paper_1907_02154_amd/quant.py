@@ -59,7 +59,8 @@ def lib() -> ctypes.CDLL:
 # A call's own time on the host matters where one token is in flight, so each
 # check is one test in the good case.
 
-_Tensor, _getdevice = torch.Tensor, torch.cuda.current_device
+_Tensor = torch.Tensor
+_getdevice = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _rawstream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -248,15 +249,18 @@ class KV4Cache:
 
     def __init__(self, k_codes, k_exps, v_codes, v_exps):
         _tensor(k_codes, "k_codes", torch.uint8)
-        if k_codes.dim() != 4 or 2 * k_codes.shape[3] not in HEAD_DIMS:
+        codes = k_codes.shape
+        if len(codes) != 4 or 2 * codes[3] not in HEAD_DIMS:
             raise ValueError(f"codes must be [pages][heads][page_size][head_dim / 2], head_dim one of {HEAD_DIMS}")
-        pages, heads, page_size, half = codes = tuple(k_codes.shape)
+        pages, heads, page_size, half = codes
         exps = (pages, heads, page_size, half // 16)
-        for name, t, shape in (("k_codes", k_codes, codes), ("k_exps", k_exps, exps), ("v_codes", v_codes, codes),
-                               ("v_exps", v_exps, exps)):
-            _tensor(t, name, torch.uint8)
-            if t.shape != shape or not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous, {list(shape)}; got {list(t.shape)}")
+        _tensor(k_exps, "k_exps", torch.uint8)
+        _tensor(v_codes, "v_codes", torch.uint8)
+        _tensor(v_exps, "v_exps", torch.uint8)
+        if v_codes.shape != codes or k_exps.shape != exps or v_exps.shape != exps:
+            raise ValueError(f"with k_codes {list(codes)} v_codes must be the same and k_exps and v_exps {list(exps)}")
+        if not (k_codes.is_contiguous() and k_exps.is_contiguous() and v_codes.is_contiguous() and v_exps.is_contiguous()):
+            raise ValueError("codes and exponents must be contiguous")
         self.k_codes, self.k_exps, self.v_codes, self.v_exps = k_codes, k_exps, v_codes, v_exps
         self.pages, self.heads, self.page_size, self.head_dim = pages, heads, page_size, 2 * half
         self._desc = _Kv4(k_codes.data_ptr(), k_exps.data_ptr(), v_codes.data_ptr(), v_exps.data_ptr(), pages, heads,
