@@ -3,8 +3,9 @@
 TEST INFRASTRUCTURE ONLY: the tests, the smoke check and the bench's CPU
 baseline may import this package; the product library never does.  It shares
 no code with the HIP path.  See ``ref_conv.c`` for the operator definition it
-writes out, ``ref.py`` for the numpy-facing wrapper and ``vision.py`` for
-segmented argsort, prefix sum and box_nms.
+writes out, ``ref.py`` for the numpy-facing wrapper, ``vision.py`` for
+segmented argsort, prefix sum and box_nms, and ``quant.py`` (imported by
+itself) for the operators of quantised transformer blocks.
 """
 from .ref import (  # noqa: F401
     build,
