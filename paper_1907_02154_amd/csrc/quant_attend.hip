@@ -375,13 +375,15 @@ __global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
     }
 }
 
-// What the kernels for many rows share: 32 rows a wavefront, tiles of 64 cached
-// tokens that a work-group widens to bf16 once, into LDS.
+// What the kernels for many rows share: eight wavefronts of 32 rows, tiles of 64
+// cached tokens that a work-group widens to bf16 once, into LDS.
+constexpr int kWideRows = 256;
 template <int D>
 struct Wide {
     static constexpr int TILE = 64;
-    static constexpr int KP = D * 2 + 16;              // bytes between rows in LDS: keys are read by rows of 16 bytes,
-    static constexpr int VP = (D / 32 | 1) * 64;       // values by blocks of 4 rows: an odd number of 64-byte steps
+    // Bytes between rows in LDS: keys are read by rows of 16 bytes, values by blocks of 4 rows of 64 (steps of 64 bytes
+    // serve the reads alone, and put the widened rows' writes on the same banks: 272 us in place of 268, below).
+    static constexpr int KP = D * 2 + 16, VP = D * 2 + 32;
     static constexpr int KBYTES = TILE * KP, VBYTES = TILE * VP;
     static constexpr int PARTS = D / 32, UNITS = TILE * PARTS;   // groups of 32 channels: of a row, of a tile's keys (or values)
 
@@ -408,8 +410,7 @@ struct Wide {
     }
 
     bf16x8 qf[D / 16];
-    f32x16 sc[2], o[D / 32];
-    bf16x8 pf[4];
+    f32x16 o[D / 32];
     float m, l, c;   // m: the running maximum times c
     __device__ __forceinline__ void start(const AttArgs &a, const Seq &sq, int half)
     {
@@ -428,14 +429,6 @@ struct Wide {
     {
         return *(const bf16x8 *)(kt + (32 * b + lane % 32) * KP + 32 * u + 16 * (lane / 32));
     }
-    __device__ __forceinline__ void no_scores()
-    {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[b][i] = 0.0f;
-    }
-
     // Of the values: channel 32 cb + lane % 32 of the lane's 8 tokens of a step of 16, 4 * half .. + 3 and 8 later, as
     // the scores have them.
     static __device__ __forceinline__ bf16x8 value(const unsigned char *vt, int lane, int cb, int k)
@@ -447,24 +440,18 @@ struct Wide {
         return __builtin_shufflevector(__builtin_bit_cast(bf16x4, v0), __builtin_bit_cast(bf16x4, v1), 0, 1, 2, 3, 4, 5, 6, 7);
     }
 
-    // The scores of the tile at t0 become probabilities in pf; m, l and o follow.
-    __device__ __forceinline__ void soften(int t0, int half)
+    // Scores of 32 places at t0 that a row does not see become -inf.
+    __device__ __forceinline__ void mask(f32x16 &x, int t0, int half)
     {
-        if (t0 < from || t0 + TILE > all) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int at = t0 + 32 * b + i % 4 + 8 * (i / 4) + 4 * half;
-                    sc[b][i] = at >= q_lo && at < q_hi ? sc[b][i] : kNegInf;
-                }
+        for (int i = 0; i < 16; ++i) {
+            const int at = t0 + i % 4 + 8 * (i / 4) + 4 * half;
+            x[i] = at >= q_lo && at < q_hi ? x[i] : kNegInf;
         }
-        float top = kNegInf;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
-        top *= c;
+    }
+    // The running maximum moves if a lane's scores, times c, pass it by far; l and o follow.
+    __device__ __forceinline__ void grow(float top)
+    {
         if (__any(top > m + kGrow)) {   // also where m is still -inf
             top = fmaxf(top, m);
             top = fmaxf(top, __shfl_xor(top, 32));
@@ -474,18 +461,8 @@ struct Wide {
 #pragma unroll
             for (int cb = 0; cb < D / 32; ++cb) o[cb] *= f;
         }
-        const float base = m == kNegInf ? 0.0f : m;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            u32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = 8 * (k % 2) + 2 * i;
-                w[i] = weights2(sc[k / 2][at], sc[k / 2][at + 1], c, base, l);
-            }
-            pf[k] = __builtin_bit_cast(bf16x8, w);
-        }
     }
+    __device__ __forceinline__ float base() const { return m == kNegInf ? 0.0f : m; }
 
     // The row's result, or its part of a split.
     __device__ __forceinline__ void finish(const AttArgs &a, const Seq &sq, int s, int split, int half)
@@ -526,11 +503,12 @@ struct Mover {
     uint32_t exp[PER], vexp[PER];
     int page[PER], place[PER];
 
-    __device__ __forceinline__ void look(const AttArgs &a, const int32_t *pages, int tid, int t0, int hi)
+    __device__ __forceinline__ void look(const AttArgs &a, const int32_t *pages, int tid, int t0, int lo, int hi)
     {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int t = min(t0 + (i * NT + tid) / PARTS, hi - 1);   // past the end: a row that is seen, masked later
+            // before the start and past the end: a row that is seen, masked later
+            const int t = max(lo, min(t0 + (i * NT + tid) / PARTS, hi - 1));
             const unsigned p = fdiv((unsigned)t, a.c.dv_page);
             place[i] = t - (int)p * a.c.page_size;
             page[i] = pages[p];
@@ -551,6 +529,10 @@ struct Mover {
     }
     // A value that is not finite makes the token's score NaN, which reaches the queries that see it; its own NaN times
     // a probability of 0 would reach the others too.
+    __device__ __forceinline__ float scale(int i, bool keys) const
+    {
+        return exp_scale(vexp[i] <= kMaxExp ? exp[i] : keys ? 255u : 127u);
+    }
     __device__ __forceinline__ void widen(unsigned char *to, int pitch, bool keys, int tid)
     {
 #pragma unroll
@@ -558,7 +540,7 @@ struct Mover {
             const int idx = i * NT + tid;
             if (UNITS % NT == 0 || idx < UNITS) {
                 unsigned char *at = to + idx / PARTS * pitch + idx % PARTS * 64;
-                const float f = exp_scale(vexp[i] <= kMaxExp ? exp[i] : keys ? 255u : 127u);
+                const float f = scale(i, keys);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) *(bf16x8 *)(at + 16 * j) = widen8(code[i][j], f);
             }
@@ -576,147 +558,272 @@ __device__ __forceinline__ void block_range(const AttArgs &a, const Seq &sq, int
     *hi = min(*hi, *lo + a.per_split);
 }
 
-// A work-group's sequence, key head, split and block of `block` rows, if there
-// is one.  A sequence's last rows see most under a causal mask: they go first,
-// of every sequence and head, and the short work comes last.  Heads follow one
-// another, so where they are a multiple of eight a head's work-groups share a
-// die's L2.
-__device__ __forceinline__ bool wide_place(const AttArgs &a, int block, Seq *sq, int *s, int *kvh, int *split, int *r0, int *rows)
+// A work-group's sequence, key head, split and block of rows, if there is one.
+// A sequence's last rows see most under a causal mask: they go first, of every
+// sequence and head, and the short work comes last.  Heads follow one another,
+// so where they are a multiple of eight a head's work-groups share a die's L2.
+__device__ __forceinline__ bool wide_place(const AttArgs &a, Seq *sq, int *s, int *kvh, int *split, int *r0, int *rows)
 {
     const int pairs = a.seqs * a.c.heads, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
     *kvh = pair % a.c.heads, *s = pair / a.c.heads, *split = rest % a.splits;
     *sq = sequence(a, *s);
     *rows = min(sq->news, a.max_new) * a.group;
-    *r0 = ((*rows + block - 1) / block - 1 - rest / a.splits) * block;
+    *r0 = ((*rows + kWideRows - 1) / kWideRows - 1 - rest / a.splits) * kWideRows;
     return *r0 >= 0;
 }
 
-// Many rows: NW wavefronts in step, two on a SIMD (heads of up to 128 channels)
-// or one (wider ones: their sums and operands take more registers than two
-// have).  The next tile is widened first, over the tile before, then this one
-// worked on, and one barrier a tile keeps the wavefronts together.
+// The wavefronts' barrier; loads of later tiles stay in flight across it.
+__device__ __forceinline__ void wide_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Many rows, for heads that leave the registers of a SIMD to four wavefronts (up
+// to 64 channels), where these overlap one another, and for heads whose sums
+// fill those of two (192 and more).  The first four wavefronts move the keys and
+// the others the values: the next tile is widened first, over the tile before,
+// then this one worked on, and one barrier a tile keeps the wavefronts together.
 //
-// Bound by what a barrier's phases do not overlap (LDS reads and products,
-// then the probabilities): at two prompts of 4096 tokens, 32 heads of 128 on 8
-// key heads, 281 us, 930 TFLOP/s; the matrix cores alone would take 105.
-// Measured beside it: the tile widened between the scores and the
-// probabilities 292 us, after these 285; the two wavefronts of a SIMD half a
-// tile apart, one at its products and one at its probabilities, two barriers a
-// tile, 313; work-groups of four wavefronts, two on a compute unit, 8% more;
-// operands read as their products need them, 16% more (heads of 64 and less do
-// that, and have room for a second work-group on a compute unit).
-template <int D, int NW>
-__global__ __launch_bounds__(64 * NW) void attend_kv4_wide_kernel(AttArgs a)
+// Bound by the probabilities' exponentials at few channels, at many by LDS
+// reads and products, which a barrier keeps in phase.  Two prompts of 4096
+// tokens, causal, 32 heads on 8 key heads: of 32 channels 133 us, of 64 173 (755
+// TFLOP/s); 20 heads of 192 on 5, 283 us (870), 16 of 256 on 4, 294 (890).  With
+// four wavefronts in place of eight, and registers for all they hold, the last
+// two took 460 and 482: one wavefront a SIMD has nothing to overlap.
+template <int D>
+__global__ __launch_bounds__(512, 2) void attend_kv4_wide_kernel(AttArgs a)
 {
     typedef Wide<D> W;
     constexpr int TILE = W::TILE;
-    constexpr bool ASK = D == 96 || D == 128;   // whether registers hold a tile's operands ahead of their products
     __shared__ __align__(16) unsigned char lds[2 * (W::KBYTES + W::VBYTES)];
     unsigned char *const keys = lds, *const vals = lds + 2 * W::KBYTES;
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
     int s, kvh, split, r0, rows, lo, hi;
     Seq sq;
-    if (!wide_place(a, 32 * NW, &sq, &s, &kvh, &split, &r0, &rows)) return;
-    block_range(a, sq, r0, min(r0 + 32 * NW, rows) - 1, split, &lo, &hi);
+    if (!wide_place(a, &sq, &s, &kvh, &split, &r0, &rows)) return;
+    block_range(a, sq, r0, min(r0 + kWideRows, rows) - 1, split, &lo, &hi);
     const int tiles = hi > lo ? (hi - lo + TILE - 1) / TILE : 0;
+
+    const int tid = threadIdx.x % 256;
+    const bool mk = wave < 4;   // moves keys
+    const int32_t *pages = a.table + (long)s * a.table_stride;
+    Mover<D, 256> mv;
+    const auto look = [&](int t) { mv.look(a, pages, tid, lo + t * TILE, lo, hi); };
+    const auto widen = [&](int t) {
+        if (mk) mv.widen(keys + (t & 1) * W::KBYTES, W::KP, true, tid);
+        else mv.widen(vals + (t & 1) * W::VBYTES, W::VP, false, tid);
+    };
+    if (tiles > 0) look(0);
     W w;
     w.place(a, sq, kvh, r0 + 32 * wave + lane % 32, rows);
+    if (tiles > 0) mv.fetch(a, mk, tid, kvh);
     w.start(a, sq, half);
-
-    // Eight wavefronts: the first four move the keys, the others the values; four: both.
-    constexpr int MOVERS = NW == 8 ? 1 : 2;
-    const int tid = threadIdx.x % 256;
-    const int32_t *pages = a.table + (long)s * a.table_stride;
-    Mover<D, 256> mv[MOVERS];
-    const auto moves_keys = [&](int i) { return MOVERS == 2 ? i == 0 : wave < 4; };
-    const auto look = [&](int t) {
-#pragma unroll
-        for (int i = 0; i < MOVERS; ++i) mv[i].look(a, pages, tid, lo + t * TILE, hi);
-    };
-    const auto fetch = [&] {
-#pragma unroll
-        for (int i = 0; i < MOVERS; ++i) mv[i].fetch(a, moves_keys(i), tid, kvh);
-    };
-    const auto widen = [&](int t) {
-#pragma unroll
-        for (int i = 0; i < MOVERS; ++i) {
-            if (moves_keys(i)) mv[i].widen(keys + (t & 1) * W::KBYTES, W::KP, true, tid);
-            else mv[i].widen(vals + (t & 1) * W::VBYTES, W::VP, false, tid);
-        }
-    };
     if (tiles > 0) {
-        look(0);
-        fetch();
         if (tiles > 1) look(1);
         widen(0);
-        if (tiles > 1) fetch();
+        if (tiles > 1) mv.fetch(a, mk, tid, kvh);
         if (tiles > 2) look(2);
     }
-    // the loads of later tiles stay in flight across it
-    const auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-    barrier();
+    wide_barrier();
     for (int t = 0; t < tiles; ++t) {
         const int t0 = lo + t * TILE;
-        const bool active = t0 < w.hi && t0 + TILE > w.lo;
         const unsigned char *kt = keys + (t & 1) * W::KBYTES, *vt = vals + (t & 1) * W::VBYTES;
         if (t + 1 < tiles) {
             widen(t + 1);   // over a tile that was last read before the previous barrier
-            if (t + 2 < tiles) fetch();
+            if (t + 2 < tiles) mv.fetch(a, mk, tid, kvh);
             if (t + 3 < tiles) look(t + 3);
         }
-        // Operands are asked for together and before their products: left to itself the compiler waits for each in turn.
-        if (active) {
-            w.no_scores();
-            if constexpr (ASK) {
-                bf16x8 kf[2][D / 16];
+        if (t0 < w.hi && t0 + TILE > w.lo) {
+            f32x16 sc[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[b][i] = 0.0f;
 #pragma unroll
                 for (int u = 0; u < D / 16; ++u)
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) kf[b][u] = W::key(kt, lane, b, u);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int u = 0; u < D / 16; ++u)
-#pragma unroll
-                    for (int b = 0; b < 2; ++b)
-                        w.sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b][u], w.qf[u], w.sc[b], 0, 0, 0);
-            } else {
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int u = 0; u < D / 16; ++u)
-                        w.sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W::key(kt, lane, b, u), w.qf[u], w.sc[b], 0, 0, 0);
+                    sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W::key(kt, lane, b, u), w.qf[u], sc[b], 0, 0, 0);
             }
-        }
-        if (active) {
-            w.soften(t0, half);
-            if constexpr (ASK) {
-                bf16x8 vf[2][4];
+            if (t0 < w.from || t0 + TILE > w.all) w.mask(sc[0], t0, half), w.mask(sc[1], t0 + 32, half);
+            float top = kNegInf;
 #pragma unroll
-                for (int cb = 0; cb < 2; ++cb)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) vf[cb][k] = W::value(vt, lane, cb, k);
-                __builtin_amdgcn_sched_barrier(0);
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
+            w.grow(top * w.c);
+            const float base = w.base();
+            bf16x8 pf[4];
 #pragma unroll
-                for (int cb = 0; cb < D / 32; ++cb) {
+            for (int k = 0; k < 4; ++k) {
+                u32x4 p;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        w.o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[cb & 1][k], w.pf[k], w.o[cb], 0, 0, 0);
-                    if (cb + 2 < D / 32) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) vf[cb & 1][k] = W::value(vt, lane, cb + 2, k);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const int at = 8 * (k % 2) + 2 * i;
+                    p[i] = weights2(sc[k / 2][at], sc[k / 2][at + 1], w.c, base, w.l);
                 }
-            } else {
-#pragma unroll
-                for (int cb = 0; cb < D / 32; ++cb)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        w.o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W::value(vt, lane, cb, k), w.pf[k], w.o[cb], 0, 0, 0);
+                pf[k] = __builtin_bit_cast(bf16x8, p);
             }
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    w.o[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W::value(vt, lane, cb, k), pf[k], w.o[cb], 0, 0, 0);
         }
-        barrier();
+        wide_barrier();
+    }
+    w.finish(a, sq, s, split, half);
+}
+
+// Many rows, heads of 96 and 128 channels: two wavefronts on a SIMD, each of which
+// gives the matrix cores and the vector unit work side by side.  A step takes 32
+// cached tokens in two phases: the products of the NEXT step's scores beside
+// this step's exponentials, then this step's sums of values beside the next
+// step's maximum and a part of the tile that is being widened; operands are read
+// from LDS a phase before their products.  Since scores run a step ahead, a
+// tile's keys are those 32 tokens behind its values, and the keys of the first
+// step come by themselves.
+//
+// Two prompts of 4096 tokens, causal, 32 heads of 128 on 8 key heads: 268 us, 975
+// TFLOP/s (of 96: 229 us, 857).  The matrix cores alone would take 110 at full
+// clock; with what each product has beside it a SIMD's product takes about 43
+// cycles in place of 32 in a loop without memory (measured with four
+// multiply-adds and two exponentials), which is 150, and the rest is barriers, LDS
+// reads and the start of each block of rows.  Measured beside it: a tile's
+// scores, probabilities and sums one after another 288; scores a step ahead,
+// but in the compiler's order, 287, and 296 where it moves exponentials to the
+// phase that needs them; 64 rows a wavefront, one on a SIMD, half the LDS reads,
+// 286 (a lone wavefront's product takes 51 cycles in that loop); two groups of
+// wavefronts half a tile apart 313.  Heads of 64 take 191 so, 173 in the kernel above.
+template <int D>
+__global__ __launch_bounds__(512, 2) void attend_kv4_steps_kernel(AttArgs a)
+{
+    typedef Wide<D> W;
+    constexpr int TILE = W::TILE;
+    constexpr int NQ = D / 16;   // products of a phase
+    __shared__ __align__(16) unsigned char lds[2 * (W::KBYTES + W::VBYTES)];
+    unsigned char *const keys = lds, *const vals = lds + 2 * W::KBYTES;
+
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    int s, kvh, split, r0, rows, lo, hi;
+    Seq sq;
+    if (!wide_place(a, &sq, &s, &kvh, &split, &r0, &rows)) return;
+    block_range(a, sq, r0, min(r0 + kWideRows, rows) - 1, split, &lo, &hi);
+    const int tiles = hi > lo ? (hi - lo + TILE - 1) / TILE : 0;
+
+    const int tid = threadIdx.x % 256;
+    const bool mk = wave < 4;   // moves keys
+    const int32_t *pages = a.table + (long)s * a.table_stride;
+    Mover<D, 256> mv, first;
+    const auto look = [&](int t) { mv.look(a, pages, tid, lo + t * TILE + (mk ? 32 : 0), lo, hi); };
+    if (tiles > 0) {
+        first.look(a, pages, tid, lo - 32, lo, hi);
+        look(0);
+    }
+    W w;
+    w.place(a, sq, kvh, r0 + 32 * wave + lane % 32, rows);
+    // the last step looks one ahead, past the end of a split too
+    w.q_hi = min(w.q_hi, hi), w.all = min(w.all, hi);
+    if (tiles > 0) {
+        if (mk) first.fetch(a, true, tid, kvh);
+        mv.fetch(a, mk, tid, kvh);
+    }
+    w.start(a, sq, half);
+    if (tiles > 0) {
+        if (tiles > 1) look(1);
+        if (mk) {
+            first.widen(keys + W::KBYTES, W::KP, true, tid);
+            mv.widen(keys, W::KP, true, tid);
+        } else {
+            mv.widen(vals, W::VP, false, tid);
+        }
+        if (tiles > 1) mv.fetch(a, mk, tid, kvh);
+        if (tiles > 2) look(2);
+    }
+    wide_barrier();
+
+    bf16x8 kf[NQ], vf[D / 32][2], pf[2];
+    f32x16 even, odd;   // scores of a step, and of the next
+    if (tiles > 0) {
+        float top = kNegInf;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) even[i] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < NQ; ++u)
+            even = __builtin_amdgcn_mfma_f32_32x32x16_bf16(W::key(keys + W::KBYTES, lane, 1, u), w.qf[u], even, 0, 0, 0);
+        if (lo < w.from || lo + 32 > w.all) w.mask(even, lo, half);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, even[i]);
+        w.grow(top * w.c);
+#pragma unroll
+        for (int u = 0; u < NQ; ++u) kf[u] = W::key(keys, lane, 0, u);
+    }
+    wide_barrier();   // the first keys' place is that of the next tile's
+    // The step of the scores x, of the 32 tokens at t0 (block h of the tile vt of values): their sums, and the next
+    // step's scores y.  The barriers to the scheduler keep what stands side by side there.
+    const auto step = [&](f32x16 &x, f32x16 &y, const unsigned char *vt, int h, int t0, auto between, auto beside) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = 0.0f;
+        float f[8][2];
+        u32x4 p[2];
+        const float base = w.base();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 10; ++i) {   // two probabilities go through three turns: product, exponential, rounding
+            if (i < 8) {
+#pragma unroll
+                for (int n = i * NQ / 8; n < (i + 1) * NQ / 8; ++n)
+                    y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[n], w.qf[n], y, 0, 0, 0);
+#pragma unroll
+                for (int n = i * NQ / 8; n < (i + 1) * NQ / 8; ++n) vf[n / 2][n % 2] = W::value(vt, lane, n / 2, 2 * h + n % 2);
+            }
+            if (i >= 2) {
+                const uint32_t two = pack_bf16x2(f[i - 2][0], f[i - 2][1]);
+                w.l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3F803F80u),
+                                                      w.l, false);
+                p[(i - 2) / 4][(i - 2) % 4] = two;
+            }
+            if (i >= 1 && i < 9)
+                f[i - 1][0] = __builtin_amdgcn_exp2f(f[i - 1][0]), f[i - 1][1] = __builtin_amdgcn_exp2f(f[i - 1][1]);
+            if (i < 8)
+                f[i][0] = __builtin_fmaf(x[2 * i], w.c, -base), f[i][1] = __builtin_fmaf(x[2 * i + 1], w.c, -base);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            pf[k] = __builtin_bit_cast(bf16x8, p[k]);
+            asm volatile("" : "+v"(pf[k]));   // or the exponentials move to the next phase
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (t0 + 32 < w.from || t0 + 64 > w.all) w.mask(y, t0 + 32, half);
+        between();
+        __builtin_amdgcn_sched_barrier(0);
+        float top = kNegInf;
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            w.o[i / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i / 2][i % 2], pf[i % 2], w.o[i / 2], 0, 0, 0);
+            beside(i);
+#pragma unroll
+            for (int n = i * 8 / NQ; n < (i + 1) * 8 / NQ; ++n) top = fmaxf(fmaxf(top, y[2 * n]), y[2 * n + 1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        w.grow(top * w.c);
+    };
+    static_assert(W::UNITS <= 256, "a thread moves a group of 32 channels of a tile");
+    unsigned char *const put = (mk ? keys : vals) + tid / W::PARTS * (mk ? W::KP : W::VP) + tid % W::PARTS * 64;
+    const int put_step = mk ? W::KBYTES : W::VBYTES;
+    for (int t = 0; t < tiles; ++t) {
+        const int t0 = lo + t * TILE, b = t & 1;
+        const unsigned char *kt = keys + b * W::KBYTES, *kn = keys + (b ^ 1) * W::KBYTES, *vt = vals + b * W::VBYTES;
+        // The next tile goes where nothing is read since the barrier before; the last one's turn writes what no one reads.
+        unsigned char *const to = put + (b ^ 1) * put_step;
+        const float scale = mv.scale(0, mk);
+        step(even, odd, vt, 0, t0, [] {}, [&](int i) {
+            kf[i] = W::key(kt, lane, 1, i);
+            if (W::UNITS == 256 || tid < W::UNITS)
+#pragma unroll
+                for (int j = i * 4 / NQ; j < (i + 1) * 4 / NQ; ++j) *(bf16x8 *)(to + 16 * j) = widen8(mv.code[0][j], scale);
+        });
+        if (t + 2 < tiles) mv.fetch(a, mk, tid, kvh);
+        if (t + 3 < tiles) look(t + 3);
+        // past the barrier the next tile's keys are there, and this tile's values in registers
+        step(odd, even, vt, 1, t0 + 32, [] { wide_barrier(); }, [&](int i) { kf[i] = W::key(kn, lane, 0, i); });
     }
     w.finish(a, sq, s, split, half);
 }
@@ -762,8 +869,6 @@ struct AttPlan {
     size_t bytes;
 };
 
-constexpr int wide_rows(int dim) { return dim <= 128 ? 256 : 128; }   // rows of a work-group
-
 AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len, int causal, int window)
 {
     AttPlan p;
@@ -771,7 +876,7 @@ AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len,
     // The kernel for few rows holds up to 64 of them in registers, fewer of wide heads.
     p.wide = rows > (c.dim <= 64 ? 64 : c.dim <= 128 ? 32 : 16);
     p.nb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const long block = p.wide ? wide_rows(c.dim) : 16 * p.nb;
+    const long block = p.wide ? kWideRows : 16 * p.nb;
     p.row_blocks = (int)((rows + block - 1) / block);
     // Places that a block of rows sees: with a window behind each, its own and those of the block's tokens.
     long len = max_len;
@@ -806,8 +911,10 @@ int launch_attend(const AttArgs &a, const AttPlan &p, hipStream_t st)
     const dim3 grid((unsigned)((long)p.row_blocks * p.splits), (unsigned)a.c.heads, (unsigned)a.seqs);
     if (p.wide) {
         const dim3 all(grid.x * grid.y * grid.z);
-        constexpr int NW = wide_rows(D) / 32;
-        launch_kernel(attend_kv4_wide_kernel<D, NW>, all, dim3(64 * NW), 0, st, a);
+        void (*k)(AttArgs);
+        if constexpr (D == 96 || D == 128) k = attend_kv4_steps_kernel<D>;
+        else k = attend_kv4_wide_kernel<D>;
+        launch_kernel(k, all, dim3(512), 0, st, a);
     } else {
         void (*k)(AttArgs) = attend_kv4_kernel<D, 1>;
         if constexpr (D <= 128)

@@ -88,6 +88,7 @@ SOURCES = {
     "segsort_tile_kernel": "vision.hip",
     "attend_kv4_kernel": "quant_attend.hip",
     "attend_kv4_wide_kernel": "quant_attend.hip",
+    "attend_kv4_steps_kernel": "quant_attend.hip",
     "attend_join_kernel": "quant_attend.hip",
     "kv4_write_kernel": "quant_cache.hip",
     "kv4_read_kernel": "quant_cache.hip",

@@ -360,6 +360,19 @@ def test_attention_of_chunks_and_prompts(lens, news, heads, kv, d, page):
     s.check(s.run(max_new=None, max_len=None))
 
 
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 192, 256])
+def test_attention_of_many_rows_at_the_edges_of_tiles(d):
+    """Prompts that end at, before and after the 32 and 64 cached tokens that are worked on together, one split in two."""
+    lens = [1, 31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129]
+    s = Setup(lens, lens, 8, 2, d, 24)
+    s.check(s.run())
+    s.check(s.run(window=33), window=33)
+    s.check(s.run(causal=False), causal=False)
+    s = Setup([1100], [70], 4, 1, d, 24)
+    s.check(s.run())
+    s.check(s.run(window=600), window=600)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_attention_rows_that_see_nothing(d):
     """Empty sequences, and more queries than cached places: the first ones stand before the start."""
