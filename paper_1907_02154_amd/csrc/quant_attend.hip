@@ -907,7 +907,7 @@ AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len,
     if (causal && window > 0) len = min(len, (long)window + block / group + 1 + 64);
     // The places are split until work-groups fill the card once, three on a
     // compute unit (one, with many rows): 16 sequences of up to 32768 places, 8 key
-    // heads of 128, take 95 us so, 109 with four and 101 with six or eight.  A split
+    // heads of 128, take 94 us so, 109 with four and 101 with six or eight.  A split
     // has 256 places at least: one sequence of 1000 takes 8.7 us so, 8.2 with 128 and
     // 10.1 with 512, one of 30000 18.2, 21 and 16.5.
     const long least = p.wide ? 512 : 256, groups = (long)seqs * c.heads * p.row_blocks;

@@ -64,6 +64,14 @@ def test_rmsnorm(dtype, rows, cols, res):
     check_rows(quant.rows_i8(x.cuda()), x, norm=False)
 
 
+@pytest.mark.parametrize("cols", [8193, 16384, 16385, 24001])
+def test_rmsnorm_of_long_rows(cols):
+    """Either side of the lengths at which another share of a row starts."""
+    test_rmsnorm(BF16, 2, cols, True)
+    test_rmsnorm(F32, 3, cols, False)
+
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 def test_rmsnorm_strides_alignment_and_in_place(dtype):
     g = gen(5)
