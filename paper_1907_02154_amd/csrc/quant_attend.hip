@@ -137,7 +137,7 @@ __device__ __forceinline__ uint32_t weights2(float s0, float s1, float c, float 
 // key heads, 413 MB: 89 us and 5 more for the join, 4.4 TB/s; while all
 // work-groups run they read at the rate of a large copy (5.2), and the first loads
 // and the last tiles take the rest.  Short calls are latencies in a row: one
-// token over 100 places 4.3 us, 17 tokens each with a window of 1000, 13 us with
+// token over 100 places 4.3 us, 17 tokens each with a window of 1000, 12 us with
 // the join.
 template <int D, int NB>
 __global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
@@ -905,14 +905,24 @@ AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len,
     // Places that a block of rows sees: with a window behind each, its own and those of the block's tokens.
     long len = max_len;
     if (causal && window > 0) len = min(len, (long)window + block / group + 1 + 64);
-    // The places are split until work-groups fill the card once, three on a
-    // compute unit (one, with many rows): 16 sequences of up to 32768 places, 8 key
-    // heads of 128, take 94 us so, 109 with four and 101 with six or eight.  A split
-    // has 256 places at least: one sequence of 1000 takes 8.7 us so, 8.2 with 128 and
-    // 10.1 with 512, one of 30000 18.2, 21 and 16.5.
-    const long least = p.wide ? 512 : 256, groups = (long)seqs * c.heads * p.row_blocks;
-    long want = ((p.wide ? 1L : 3L) * cu_count() + groups - 1) / groups;
-    want = max(1L, min(want, (len + least - 1) / least));
+    // The places are split, at most until work-groups fill the card once, three on
+    // a compute unit (one, with many rows): 16 sequences of up to 32768 places, 8 key
+    // heads of 128, take 94 us so, 109 with four and 101 with six or eight.
+    const long groups = (long)seqs * c.heads * p.row_blocks, fill = ((p.wide ? 1L : 3L) * cu_count() + groups - 1) / groups;
+    long want = 1;
+    if (p.wide) {
+        // In n pieces all / n + 6 + n * part microseconds: the tiles of 64 places, the join,
+        // and the parts, written and read.  16 heads on 4 key heads, causal: 1000 tokens, of
+        // 128, take 33 us in one piece and 42 in two; 2000, of 96, 53 and 64; 100 tokens
+        // behind 900, of 128, 20 in six pieces and 26 in two.
+        const float all = (float)len / 64.0f * c.dim / 64.0f, part = 4e-6f * (float)seqs * (float)heads * (float)max_new * (c.dim + 4);
+        const long n = max(1L, min(min(fill, (len + 127) / 128), (long)(sqrtf(all / part) + 0.5f)));
+        if (all / n + 6.0f + n * part < all) want = n;
+    } else {
+        // 128 places at least, 256 beyond 32 splits: one sequence of 1000 takes 7.5 us so,
+        // 8.5 with 256 and 7.6 with 64; one of 8000 10.0, and 10.9 with 128.
+        want = min(fill, max(min((len + 127) / 128, 32L), (len + 255) / 256));
+    }
     p.per_split = (int)(((len + want - 1) / want + 63) / 64 * 64);
     p.splits = (int)((len + (long)p.per_split - 1) / p.per_split);
     p.bytes = p.splits > 1 ? (size_t)seqs * heads * max_new * p.splits * (c.dim + 4) * 4 : 0;
