@@ -918,9 +918,10 @@ AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len,
         const float all = (float)len / 64.0f * c.dim / 64.0f, part = 4e-6f * (float)seqs * (float)heads * (float)max_new * (c.dim + 4);
         const long n = max(1L, min(min(fill, (len + 127) / 128), (long)(sqrtf(all / part) + 0.5f)));
         if (all / n + 6.0f + n * part < all) want = n;
-    } else {
+    } else if (len > 384) {
         // 128 places at least, 256 beyond 32 splits: one sequence of 1000 takes 7.5 us so,
-        // 8.5 with 256 and 7.6 with 64; one of 8000 10.0, and 10.9 with 128.
+        // 8.5 with 256 and 7.6 with 64; one of 8000 10.0, and 10.9 with 128.  In one piece
+        // 256 take 5.9 us (7.5 in two), 384 6.9 (7.6) and 640 8.4 (7.6).
         want = min(fill, max(min((len + 127) / 128, 32L), (len + 255) / 256));
     }
     p.per_split = (int)(((len + want - 1) / want + 63) / 64 * 64);
