@@ -13,6 +13,8 @@
 // (heads / key heads) + head within the group.
 #include "quant.h"
 
+#include <algorithm>
+
 namespace miconv {
 namespace quant {
 namespace {
@@ -73,8 +75,7 @@ __device__ __forceinline__ void seen(const AttArgs &a, const Seq &q, int i, int 
     const int p = q.len - q.news + i;
     int h = a.causal ? p + 1 : q.len;
     h = h > q.len ? q.len : h;
-    const int l = a.window > 0 ? p - a.window + 1 : 0;
-    *lo = l < 0 ? 0 : l;
+    *lo = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;   // a difference that no window makes pass 32 bits
     *hi = h < 0 ? 0 : h;
 }
 
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
     seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), &lo, &all);
     seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), &from, &hi);
     lo = (lo & ~31) + split * a.per_split;   // per_split is a multiple of 64
-    hi = min(hi, lo + a.per_split);
+    hi = lo + min(hi - lo, a.per_split);
 
     int q_lo[NB], q_hi[NB];
     bf16x8 qf[NB][NU];
@@ -562,7 +563,7 @@ __device__ __forceinline__ void block_range(const AttArgs &a, const Seq &sq, int
     seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), lo, &x);
     seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), &x, hi);
     *lo = (*lo & ~63) + split * a.per_split;   // per_split is a multiple of the tile
-    *hi = min(*hi, *lo + a.per_split);
+    *hi = *lo + min(*hi - *lo, a.per_split);
 }
 
 // A work-group's sequence, key head, split and block of rows, if there is one.
@@ -904,7 +905,8 @@ AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len,
     p.row_blocks = (int)((rows + block - 1) / block);
     // Places that a block of rows sees: with a window behind each, its own and those of the block's tokens.
     long len = max_len;
-    if (causal && window > 0) len = min(len, (long)window + block / group + 1 + 64);
+    // (std::min: HIP's own of two longs is that of their low 32 bits on the host.)
+    if (causal && window > 0) len = std::min(len, (long)window + block / group + 1 + 64);
     // The places are split, at most until work-groups fill the card once, three on
     // a compute unit (one, with many rows): 16 sequences of up to 32768 places, 8 key
     // heads of 128, take 94 us so, 109 with four and 101 with six or eight.
@@ -916,13 +918,13 @@ AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len,
         // 128, take 33 us in one piece and 42 in two; 2000, of 96, 53 and 64; 100 tokens
         // behind 900, of 128, 20 in six pieces and 26 in two.
         const float all = (float)len / 64.0f * c.dim / 64.0f, part = 4e-6f * (float)seqs * (float)heads * (float)max_new * (c.dim + 4);
-        const long n = max(1L, min(min(fill, (len + 127) / 128), (long)(sqrtf(all / part) + 0.5f)));
+        const long n = std::max(1L, std::min({fill, (len + 127) / 128, (long)(sqrtf(all / part) + 0.5f)}));
         if (all / n + 6.0f + n * part < all) want = n;
     } else if (len > 384) {
         // 128 places at least, 256 beyond 32 splits: one sequence of 1000 takes 7.5 us so,
         // 8.5 with 256 and 7.6 with 64; one of 8000 10.0, and 10.9 with 128.  In one piece
         // 256 take 5.9 us (7.5 in two), 384 6.9 (7.6) and 640 8.4 (7.6).
-        want = min(fill, max(min((len + 127) / 128, 32L), (len + 255) / 256));
+        want = std::min(fill, std::max(std::min((len + 127) / 128, 32L), (len + 255) / 256));
     }
     p.per_split = (int)(((len + want - 1) / want + 63) / 64 * 64);
     p.splits = (int)((len + (long)p.per_split - 1) / p.per_split);

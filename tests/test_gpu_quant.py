@@ -483,6 +483,17 @@ def test_cache_beyond_32_bit_offsets():
         assert ((out.cpu().double() - want).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("news", [12, 70])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 30])
+def test_attention_windows_wider_than_any_length(news, window):
+    """Such a window bounds nothing, for queries that stand before the first place and bounds of several splits too."""
+    s = Setup([7, 300], [news, news], 4, 1, 64, 16)
+    for causal in (True, False):
+        for bound in (300, 2000):
+            s.check(s.run(window=window, causal=causal, max_len=bound), window=window, causal=causal)
+            assert torch.equal(s.run(window=window, causal=causal, max_len=bound), s.run(causal=causal, max_len=bound))
+
+
 # ------------------------------------------------------------------ refusals through the binding
 
 def test_binding_refusals():

@@ -137,6 +137,17 @@ def test_attention_refusals(L):
     assert w(c, 1, 3, 1, 16, 1, 0) == miconv.ERR_SHAPE
 
 
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("max_new", [1, 12, 300])
+def test_attention_plans_of_windows_wider_than_any_length(L, head_dim, max_new):
+    """A window that bounds nothing leaves the splits, and so the workspace, as they are without one."""
+    c = cache(pages=40, heads=1, head_dim=head_dim)
+    for max_len in (300, 2000, 30000):
+        want = L.quant_attention_workspace_bytes(c, 2, 4, max_new, max_len, 1, 0)
+        for window in (1 << 30, (1 << 31) - 300, (1 << 31) - 80, (1 << 31) - 2, (1 << 31) - 1):
+            assert L.quant_attention_workspace_bytes(c, 2, 4, max_new, max_len, 1, window) == want, (max_len, window)
+
+
 def test_binding_refuses_host_tensors_and_wrong_types():
     x = torch.zeros(2, 8)
     with pytest.raises(ValueError, match="device"):
