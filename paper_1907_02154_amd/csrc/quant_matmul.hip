@@ -206,10 +206,13 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul_i8_tile_kernel(MatAr
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(i < WL ? wres : ares, (lds_void_t *)(st + i * NT), 16, o, k, 0, 0);
             }
         } else {   // past K the next row begins
+            // A group's part may begin past K: its loads are all outside, and their scalar offset has to stay below the
+            // buffer's size, from which the hardware's range check may subtract it.
+            const int base = k < a.K ? k : 0;
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 const unsigned o = k + at_k[i] < a.K ? off[i] : kOutside;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < WL ? wres : ares, (lds_void_t *)(st + i * NT), 16, o, k, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(i < WL ? wres : ares, (lds_void_t *)(st + i * NT), 16, o, base, 0, 0);
             }
         }
     };

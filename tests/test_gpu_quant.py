@@ -155,6 +155,14 @@ def test_matmul(M, N, K, dtype):
     check_matmul(M, N, K, dtype, False, False, False, seed=1)
 
 
+@pytest.mark.parametrize("K", [16, 32, 112, 128, 144, 272, 400, 528])
+@pytest.mark.parametrize("M,N", [(1, 1), (1, 17), (17, 1), (16, 33), (33, 16)])
+def test_matmul_reductions_shorter_than_the_groups_parts(M, N, K):
+    """Groups of wavefronts whose part of the reduction begins past its end, one row of an operand the shortest buffer."""
+    check_matmul(M, N, K, BF16, True, False, False)
+    check_matmul(M, N, K, F32, False, True, True)
+
+
 @pytest.mark.parametrize("M", [1, 5, 40, 150])
 def test_matmul_largest_sums(M):
     """Every product 127 * 128 or 128 * 128 and the longest reduction: sums that only 32 bits hold exactly."""
