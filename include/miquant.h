@@ -121,7 +121,8 @@ int quant_kv4_read(const quant_kv4 *cache, long tokens, const int32_t *slots, in
  * queries at rows starts[s] .. starts[s + 1] of q (starts NULL: row s alone);
  * query i of n stands at place p = lens[s] - n + i.  It sees the places
  * 0 .. p (0 .. lens[s] - 1 unless causal), of these with window > 0 only those
- * above p - window.  For each of the `heads` query heads, head j reading key
+ * above p - window.  lens[s] may pass what can be seen (max_len and the table's
+ * end, below): the queries keep their places.  For each of the `heads` query heads, head j reading key
  * head j / (heads / cache->heads):
  *   out = softmax(scale * q k^T over the places seen) v
  * zeros where none is seen, NaN where a key or value that is seen is not

@@ -52,6 +52,7 @@ struct AttArgs {
 struct Seq {
     long row0;   // first row of q
     int news, len;
+    int most;    // places that can be seen: what the bound, the table and the sequence hold
 };
 
 __device__ __forceinline__ Seq sequence(const AttArgs &a, int s)
@@ -65,7 +66,8 @@ __device__ __forceinline__ Seq sequence(const AttArgs &a, int s)
     const long room = (long)a.table_stride * a.c.page_size;
     const int most = room < a.max_len ? (int)room : a.max_len;
     const int n = a.lens[s];
-    r.len = n < 0 ? 0 : n > most ? most : n;
+    r.len = n < 0 ? 0 : n;   // where the queries stand, also past what can be seen
+    r.most = r.len > most ? most : r.len;
     return r;
 }
 
@@ -73,9 +75,10 @@ __device__ __forceinline__ Seq sequence(const AttArgs &a, int s)
 __device__ __forceinline__ void seen(const AttArgs &a, const Seq &q, int i, int *lo, int *hi)
 {
     const int p = q.len - q.news + i;
-    int h = a.causal ? p + 1 : q.len;
-    h = h > q.len ? q.len : h;
-    *lo = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;   // a difference that no window makes pass 32 bits
+    int h = a.causal ? p + 1 : q.most;
+    h = h > q.most ? q.most : h;
+    const int l = a.window > 0 && p >= a.window ? p - a.window + 1 : 0;   // a difference that no window makes pass 32 bits
+    *lo = l > q.most ? q.most : l;
     *hi = h < 0 ? 0 : h;
 }
 

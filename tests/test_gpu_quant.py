@@ -502,6 +502,34 @@ def test_attention_windows_wider_than_any_length(news, window):
             assert torch.equal(s.run(window=window, causal=causal, max_len=bound), s.run(causal=causal, max_len=bound))
 
 
+@pytest.mark.parametrize("lens,news,heads,d,page", [([160, 40], [20, 5], 4, 64, 16), ([700, 160], [1, 1], 8, 128, 64),
+                                                    ([400, 170, 149], [90, 40, 9], 4, 96, 32), ([500], [120], 2, 256, 50)])
+@pytest.mark.parametrize("k", [dict(), dict(window=30), dict(causal=False), dict(causal=False, window=30)],
+                         ids=["causal", "window", "all", "all-window"])
+def test_attention_lengths_past_the_bound(lens, news, heads, d, page, k):
+    """Queries stand at their sequence's length, whatever bound or table ends what they see."""
+    s = Setup(lens, news, heads, 2, d, page)
+    most = 150
+    want, tol = torch.zeros(s.q.shape, dtype=torch.float64), torch.zeros(s.q.shape, dtype=torch.float64)
+    row = 0
+    for i, n in enumerate(news):
+        for j in range(n):
+            p = lens[i] - n + j
+            hi = min(lens[i], most, p + 1 if k.get("causal", True) else lens[i])
+            lo = max(0, p - k["window"] + 1) if "window" in k else 0
+            if hi > lo:      # the same row as one that stands at the end of what it sees
+                want[row], tol[row] = (x[0] for x in ref.attention(s.q[row:row + 1], [s.k[i][:hi]], [s.v[i][:hi]], [1], [hi],
+                                                                   s.scale, window=hi - lo))
+            row += 1
+    got = [s.run(max_len=most, **k)]
+    if most % page == 0:
+        width = most // page
+        got.append(quant.attention_kv4(s.q.cuda(), s.cache, s.table[:, :width].contiguous(), s.lens_d, starts=s.starts,
+                                       max_new=max(news), max_len=512, **k))
+    for out in got:
+        assert ((out.cpu().double() - want).abs() <= tol).all()
+
+
 # ------------------------------------------------------------------ refusals through the binding
 
 def test_binding_refusals():
