@@ -48,8 +48,46 @@ __device__ __forceinline__ RowStat wave_join(RowStat s)
     return s;
 }
 
-// 127 / A and the row's scale.
-__device__ __forceinline__ float row_factor(const RowArgs &a, RowStat s, float *scale)
+// The statistics of a row's WAVES wavefronts (of one wavefront: its lanes).
+template <int WAVES>
+__device__ __forceinline__ RowStat row_join(RowStat s, RowStat *part)
+{
+    s = wave_join(s);
+    if (WAVES > 1) {
+        if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = s;
+        __syncthreads();
+        s = part[0];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) s = join(s, part[i]);
+    }
+    return s;
+}
+
+// What fp32 holds of a sum of squares ends at magnitudes of 2^64, and below 2^-63
+// squares lose bits.  Where that reaches the scale (the sum is infinite, or it
+// and eps are below 2^-80) the row is read once more and the sum taken of
+// (h unit^2)^2, which stays inside: rows whose h goes so far are rare, and the
+// test is all that others pay.
+__device__ __forceinline__ float row_unit_of_sum(const RowArgs &a, RowStat s)
+{
+    if (!a.norm || s.top >= 0x7F800000u || s.top < __builtin_bit_cast(uint32_t, 0x1p-100f)) return 1.0f;   // no sum is used
+    return s.sum < 0x1p-80f && a.eps < 0x1p-80f ? 0x1p50f : s.sum == __builtin_inff() ? 0x1p-48f : 1.0f;
+}
+
+template <typename T, int LANES>
+__device__ __forceinline__ float row_sum_again(const T *h, int cols, int lane, float unit)
+{
+    float sum = 0.0f;
+    for (long at = (long)lane * 8; at < cols; at += LANES * 8)   // the elements that this thread wrote, where h was
+        for (int i = 0; i < 8 && at + i < cols; ++i) {
+            const float v = load1(h + at + i) * unit * unit;
+            sum += v * v;
+        }
+    return sum;
+}
+
+// 127 / A and the row's scale; s.sum is that of (h unit^2)^2.
+__device__ __forceinline__ float row_factor(const RowArgs &a, RowStat s, float unit, float *scale)
 {
     const float top = __builtin_bit_cast(float, s.top);
     if (s.top >= 0x7F800000u) {
@@ -60,8 +98,10 @@ __device__ __forceinline__ float row_factor(const RowArgs &a, RowStat s, float *
         *scale = 0.0f;
         return 0.0f;
     }
-    const float r = a.norm ? 1.0f / sqrtf(s.sum / (float)a.cols + a.eps) : 1.0f;
-    *scale = top * r / 127.0f;
+    // in this order no step leaves fp32's range unless the scale itself does
+    const float eps = a.eps * unit * unit * unit * unit;
+    const float r = a.norm ? 1.0f / sqrtf(s.sum / (float)a.cols + eps) * unit : 1.0f;
+    *scale = top * r * unit / 127.0f;
     return 127.0f / top;
 }
 
@@ -151,16 +191,14 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void rows_i8_kernel(RowA
         const int at = (u * LANES + lane) * 8, n = a.cols - at;
         if (n > 0) row_unit(a, x, res, h, at, n < 8 ? n : 8, t[u], s);
     }
-    s = wave_join(s);
-    if (WAVES > 1) {
-        if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = s;
-        __syncthreads();
-        s = part[0];
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i) s = join(s, part[i]);
+    s = row_join<WAVES>(s, part);
+    const float unit = row_unit_of_sum(a, s);   // the same for a row's threads
+    if (unit != 1.0f) {
+        if (WAVES > 1) __syncthreads();
+        s.sum = row_join<WAVES>(RowStat{row_sum_again<T, LANES>(a.res ? h : x, a.cols, lane, unit), 0u}, part).sum;
     }
     float scale;
-    const float f = row_factor(a, s, &scale);
+    const float f = row_factor(a, s, unit, &scale);
     int8_t *q = a.q + row * a.qs;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -185,16 +223,16 @@ __global__ __launch_bounds__(1024) void rows_i8_long_kernel(RowArgs a)
     float t[8];
     for (long at = threadIdx.x * 8; at < a.cols; at += 1024 * 8)
         row_unit(a, x, res, h, (int)at, a.cols - at < 8 ? (int)(a.cols - at) : 8, t, s);
-    s = wave_join(s);
-    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = s;
-    __syncthreads();
-    s = part[0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) s = join(s, part[i]);
-    float scale;
-    const float f = row_factor(a, s, &scale);
-    int8_t *q = a.q + row * a.qs;
+    s = row_join<16>(s, part);
     const T *kept = a.res ? h : x;
+    const float unit = row_unit_of_sum(a, s);
+    if (unit != 1.0f) {
+        __syncthreads();
+        s.sum = row_join<16>(RowStat{row_sum_again<T, 1024>(kept, a.cols, threadIdx.x, unit), 0u}, part).sum;
+    }
+    float scale;
+    const float f = row_factor(a, s, unit, &scale);
+    int8_t *q = a.q + row * a.qs;
     for (long at = threadIdx.x * 8; at < a.cols; at += 1024 * 8) {
         const int n = a.cols - at < 8 ? (int)(a.cols - at) : 8;
         row_unit(a, kept, (const T *)nullptr, (T *)nullptr, (int)at, n, t, s);

@@ -116,6 +116,29 @@ def test_rmsnorm_extremes():
         assert e[0].shape == (0, 8) and e[1].shape == (0,) and e[2].shape == (0, 8)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("cols", [1, 300, 1000, 1500, 5000, 9000, 20000, 40003])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-6, 1e6])
+def test_rmsnorm_scales_over_the_range_of_fp32(dtype, cols, eps):
+    """Rows whose squares pass fp32 at either end, of one magnitude and of all: the scale is the definition's."""
+    g = gen(cols)
+    e = torch.tensor([-126, -99, -90, -80, -75, -64, -63, -50, -41, -40, -39, -20, 0, 40, 56, 60, 62, 63, 64, 70, 100, 124])
+    n = len(e)
+    x = torch.randn(n + 4, cols, generator=g).clamp(-4, 4)
+    x[:n] *= torch.exp2(e.float())[:, None]
+    x[n:] *= torch.exp2(torch.randint(-120, 125, (4, cols), generator=g).float())
+    x = x.to(dtype)
+    for w in (torch.ones(cols), torch.full((cols,), 2.0 ** 40)):      # the second lifts small rows above the cutoff of A
+        t = (x.double() * w.double()).abs().amax(1)
+        keep = t < 2.0 ** 127                                          # t itself stays finite
+        check_rows(quant.rmsnorm_i8(x[keep].cuda(), w.cuda(), eps=eps), x[keep], w, eps=eps)
+    r = (torch.randn(x.shape, generator=g) * x.abs().float()).to(dtype)
+    keep = ((x.double() + r.double()).abs().amax(1) < 2.0 ** 127)
+    hold = r[keep].cuda()
+    got = quant.rmsnorm_i8(x[keep].cuda(), torch.ones(cols, device="cuda"), hold, eps=eps, h=hold)
+    check_rows(got, x[keep], torch.ones(cols), r[keep], eps=eps)
+
+
 def test_rows_ties():
     x = torch.arange(-254, 255).float().reshape(1, -1) / 2   # largest 127: halves go to the even side
     q, scale = quant.rows_i8(x.cuda())
