@@ -136,8 +136,8 @@ int quant_kv4_read(const quant_kv4 *cache, long tokens, const int32_t *slots, in
  * rows (64, 32 or 16 of head_dim 64, 128 or more) they keep a second bf16
  * part, 16 bits in all.
  * Errors: MICONV_ERR_NULL, MICONV_ERR_SHAPE (heads no multiple of the cache's,
- * a stride below its row, max_new or max_len < 1, table_stride < 1),
- * MICONV_ERR_UNSUPPORTED (head_dim), MICONV_ERR_ALIGN, MICONV_ERR_TOO_LARGE
+ * a stride below its row, max_new or max_len < 1, table_stride < 1, a scale that
+ * is not finite, also times log2(e)), MICONV_ERR_UNSUPPORTED (head_dim), MICONV_ERR_ALIGN, MICONV_ERR_TOO_LARGE
  * (2^31 slots, 2^24 query rows of a key head, or so much work that a grid does
  * not hold it), MICONV_ERR_WORKSPACE. */
 long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len,

@@ -992,7 +992,9 @@ extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, 
     const int rc = quant::check_attend(cache, seqs, heads, max_new, max_len, &a.c);
     if (rc != MICONV_OK) return rc;
     const long width = (long)heads * a.c.dim;
-    if (tokens < 0 || q_stride < width || out_stride < width || table_stride < 1) return MICONV_ERR_SHAPE;
+    a.scale = scale * 1.44269504088896340736f;
+    if (tokens < 0 || q_stride < width || out_stride < width || table_stride < 1 || !__builtin_isfinite(a.scale))
+        return MICONV_ERR_SHAPE;
     if (tokens >= 1L << 31) return MICONV_ERR_TOO_LARGE;
     if (seqs == 0 || tokens == 0) return MICONV_OK;
     if (!q || !out || !lens || !table) return MICONV_ERR_NULL;
@@ -1011,7 +1013,6 @@ extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, 
     a.max_new = max_new, a.max_len = max_len;
     a.causal = causal, a.window = window;
     a.splits = p.splits, a.per_split = p.per_split, a.row_blocks = p.row_blocks;
-    a.scale = scale * 1.44269504088896340736f;
     a.dv_group = make_fastdiv((unsigned)a.group);
     hipStream_t st = static_cast<hipStream_t>(stream);
     switch (a.c.dim) {

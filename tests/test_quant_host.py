@@ -137,6 +137,12 @@ def test_attention_refusals(L):
     assert w(c, 1, 3, 1, 16, 1, 0) == miconv.ERR_SHAPE
 
 
+@pytest.mark.parametrize("scale", [NAN, float("inf"), -float("inf"), 3e38, -3e38])
+def test_attention_refuses_scales_that_are_not_finite(L, scale):
+    assert L.quant_attention_kv4(cache(), 2, 4, 2, FAKE, 256, None, FAKE, FAKE, 3, 1, 48, scale, 1, 0, FAKE, 256, None, 0,
+                                 None) == miconv.ERR_SHAPE
+
+
 @pytest.mark.parametrize("head_dim", [64, 128])
 @pytest.mark.parametrize("max_new", [1, 12, 300])
 def test_attention_plans_of_windows_wider_than_any_length(L, head_dim, max_new):
