@@ -303,6 +303,36 @@ def test_cache_every_exponent_tie_and_special():
     assert torch.equal(torch.nan_to_num(k.cpu().double()), torch.nan_to_num(want))
 
 
+@pytest.mark.parametrize("byte", [252, 253, 254, 255])
+def test_cache_exponents_of_groups_that_are_not_finite(byte):
+    """Every code under the last exponent of a finite group and under those above: values, and NaN, read and attended."""
+    cache = empty_cache(1, 2, 4, 64)
+    codes = torch.arange(16, dtype=torch.uint8)
+    codes = (codes + 16 * codes.flip(0)).repeat(2).reshape(1, 32)          # every code in either half of a byte
+    for t in (cache.k_codes, cache.v_codes):
+        t[0, :, 2] = codes.cuda()
+    for t in (cache.k_exps, cache.v_exps):
+        t.fill_(127)
+        t[0, 1, 2, 1] = byte                                               # the second group of the second head
+    slot = torch.tensor([2], dtype=torch.int32, device="cuda")
+    want = ref.kv4_decode(codes.expand(2, 32), torch.tensor([[127, 127], [127, byte]], dtype=torch.uint8))[None]
+    for out in (BF16, F32):
+        for got in quant.kv4_read(slot, cache, dtype=out):
+            got = got.cpu().double()
+            assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
+    assert torch.isnan(want[0, 1, 32:]).all() == (byte > 252) and not torch.isnan(want[0, 0]).any()
+    if byte > 252:
+        table, lens = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.tensor([3], dtype=torch.int32, device="cuda")
+        fine = cache.v_exps.clone().fill_(127)
+        for news in (1, 40):                                               # the kernels for few and for many rows
+            q = torch.ones(news, 8, 64, dtype=BF16, device="cuda")
+            starts = torch.tensor([0, news], dtype=torch.int32, device="cuda")
+            for c in (quant.KV4Cache(cache.k_codes, cache.k_exps, cache.v_codes, fine),
+                      quant.KV4Cache(cache.k_codes, fine, cache.v_codes, cache.v_exps)):
+                o = quant.attention_kv4(q, c, table, lens, starts=starts, causal=False)
+                assert torch.isnan(o[:, 4:]).all() and torch.isfinite(o[:, :4]).all()
+
+
 def test_cache_slots_outside():
     cache = empty_cache(2, 2, 8, 64)
     x = torch.ones(5, 2, 64, dtype=BF16, device="cuda")
