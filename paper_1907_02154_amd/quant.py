@@ -64,14 +64,19 @@ _getdevice = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _rawstream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _tensor(t, name: str, *dtypes) -> None:
-    if isinstance(t, _Tensor) and t.is_cuda and t.dtype in dtypes:
+def _tensor(t, name: str, *dtypes, device: Optional[int] = None) -> None:
+    """t has to be a tensor of one of dtypes on `device` (None: the current one, where a call runs)."""
+    if isinstance(t, _Tensor) and t.is_cuda and t.dtype in dtypes and \
+            t.get_device() == (_getdevice() if device is None else device):
         return
     if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    raise ValueError(f"{name} is on device {t.get_device()}, " + (f"the current device is {_getdevice()}" if device is None
+                                                                  else f"the others are on {device}"))
 
 
 def _matrix(t, name: str, rows, cols, *dtypes) -> int:
@@ -106,13 +111,10 @@ def _vector(t, name: str, n: int, dtype) -> None:
 
 
 def _where(t, stream):
-    """The stream for work on t: the current one when None.  t has to be on the current device."""
-    i = t.get_device()
-    if i != _getdevice():
-        raise ValueError(f"tensors are on device {i}, the current device is {_getdevice()}")
+    """The stream for work on t, which is on the current device: the current one when None."""
     if stream is not None:
         return _stream(stream)
-    return _rawstream(i) if _rawstream else _stream(None)
+    return _rawstream(t.get_device()) if _rawstream else _stream(None)
 
 
 def _empty(like, shape, dtype, stream):
@@ -132,8 +134,8 @@ def _workspace(nbytes: int, what: str, ws, like, stream):
     if ws is None:
         ws = _empty(like, nbytes, torch.uint8, stream)
     size = ws.numel() * ws.element_size()
-    if not ws.is_cuda or not ws.is_contiguous() or size < nbytes or ws.data_ptr() % 256:
-        raise ValueError(f"workspace must be a 256-byte aligned device tensor of at least {nbytes} bytes")
+    if ws.get_device() != like.get_device() or not ws.is_contiguous() or size < nbytes or ws.data_ptr() % 256:
+        raise ValueError(f"workspace must be a 256-byte aligned tensor of at least {nbytes} bytes on the operands' device")
     return ws.data_ptr(), size
 
 
@@ -245,24 +247,26 @@ class KV4Cache:
     """A paged cache of keys and values in 4 bits: codes uint8 [pages][heads][page_size][head_dim / 2] and exponent
     bytes uint8 [pages][heads][page_size][head_dim / 32] of each (the format: ``include/miquant.h``)."""
 
-    __slots__ = ("k_codes", "k_exps", "v_codes", "v_exps", "pages", "heads", "page_size", "head_dim", "_desc")
+    __slots__ = ("k_codes", "k_exps", "v_codes", "v_exps", "pages", "heads", "page_size", "head_dim", "device",
+                 "_desc")
 
     def __init__(self, k_codes, k_exps, v_codes, v_exps):
-        _tensor(k_codes, "k_codes", torch.uint8)
+        i = k_codes.get_device() if isinstance(k_codes, _Tensor) else -1
+        _tensor(k_codes, "k_codes", torch.uint8, device=i)
         codes = k_codes.shape
         if len(codes) != 4 or 2 * codes[3] not in HEAD_DIMS:
             raise ValueError(f"codes must be [pages][heads][page_size][head_dim / 2], head_dim one of {HEAD_DIMS}")
         pages, heads, page_size, half = codes
         exps = (pages, heads, page_size, half // 16)
-        _tensor(k_exps, "k_exps", torch.uint8)
-        _tensor(v_codes, "v_codes", torch.uint8)
-        _tensor(v_exps, "v_exps", torch.uint8)
+        _tensor(k_exps, "k_exps", torch.uint8, device=i)
+        _tensor(v_codes, "v_codes", torch.uint8, device=i)
+        _tensor(v_exps, "v_exps", torch.uint8, device=i)
         if v_codes.shape != codes or k_exps.shape != exps or v_exps.shape != exps:
             raise ValueError(f"with k_codes {list(codes)} v_codes must be the same and k_exps and v_exps {list(exps)}")
         if not (k_codes.is_contiguous() and k_exps.is_contiguous() and v_codes.is_contiguous() and v_exps.is_contiguous()):
             raise ValueError("codes and exponents must be contiguous")
         self.k_codes, self.k_exps, self.v_codes, self.v_exps = k_codes, k_exps, v_codes, v_exps
-        self.pages, self.heads, self.page_size, self.head_dim = pages, heads, page_size, 2 * half
+        self.pages, self.heads, self.page_size, self.head_dim, self.device = pages, heads, page_size, 2 * half, i
         self._desc = _Kv4(k_codes.data_ptr(), k_exps.data_ptr(), v_codes.data_ptr(), v_exps.data_ptr(), pages, heads,
                           page_size, 2 * half)
 
@@ -281,6 +285,8 @@ class KV4Cache:
 def _cache(cache) -> KV4Cache:
     if not isinstance(cache, KV4Cache):
         raise TypeError("cache must be a KV4Cache")
+    if cache.device != _getdevice():
+        raise ValueError(f"the cache is on device {cache.device}, the current device is {_getdevice()}")
     return cache
 
 

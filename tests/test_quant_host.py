@@ -154,6 +154,63 @@ def test_attention_plans_of_windows_wider_than_any_length(L, head_dim, max_new):
             assert L.quant_attention_workspace_bytes(c, 2, 4, max_new, max_len, 1, window) == want, (max_len, window)
 
 
+class Placed(torch.Tensor):
+    """A host tensor that says it is on GPU `at`: what the binding checks before it passes a pointer on."""
+    at = 0
+    is_cuda = property(lambda self: True)
+
+    def get_device(self):
+        return self.at
+
+
+def placed(at, *shape, dtype):
+    t = torch.zeros(*shape, dtype=dtype).as_subclass(Placed)
+    t.at = at
+    return t
+
+
+def test_binding_refuses_operands_on_another_device(monkeypatch):
+    """Each operand in turn on GPU 1 where GPU 0 is the current one: a ValueError, and no call."""
+    monkeypatch.setattr(quant, "_getdevice", lambda: 0)
+
+    class Called(Exception):
+        pass
+
+    class Library:
+        def __getattr__(self, name):
+            if name.endswith("_workspace_bytes"):
+                return lambda *a: 256
+            raise Called(name)
+    monkeypatch.setattr(quant, "lib", Library)
+    f32, i32, i8, u8, bf = torch.float32, torch.int32, torch.int8, torch.uint8, torch.bfloat16
+
+    def kv(at):
+        return quant.KV4Cache(*(placed(at, 2, 2, 16, n, dtype=u8) for n in (32, 2, 32, 2)))
+
+    calls = {
+        "norm": (lambda x, w, r, h, q, s: quant.rmsnorm_i8(x, w, r, h=h, q=q, scale=s, stream=0),
+                 [((4, 64), bf), ((64,), f32), ((4, 64), bf), ((4, 64), bf), ((4, 64), i8), ((4,), f32)]),
+        "rows": (lambda x, q, s: quant.rows_i8(x, q=q, scale=s, stream=0), [((4, 64), bf), ((4, 64), i8), ((4,), f32)]),
+        "product": (lambda a, sa, w, sw, b, r, o: quant.matmul_i8(a, sa, w, sw, bias=b, residual=r, out=o, stream=0),
+                    [((4, 64), i8), ((4,), f32), ((8, 64), i8), ((8,), f32), ((8,), f32), ((4, 8), bf), ((4, 8), bf)]),
+        "write": (lambda k, v, s, c: quant.kv4_write(k, v, s, c, stream=0), [((3, 2, 64), bf), ((3, 2, 64), bf), ((3,), i32), kv]),
+        "read": (lambda s, k, v, c: quant.kv4_read(s, c, k=k, v=v, stream=0), [((3,), i32), ((3, 2, 64), bf), ((3, 2, 64), bf), kv]),
+        "attend": (lambda q, t, n, s, o, w, c: quant.attention_kv4(q, c, t, n, starts=s, out=o, ws=w, stream=0),
+                   [((2, 4, 64), bf), ((2, 2), i32), ((2,), i32), ((3,), i32), ((2, 4, 64), bf), ((512,), u8), kv]),
+    }
+    for name, (f, kinds) in calls.items():
+        make = lambda at: [k(d) if callable(k) else placed(d, *k[0], dtype=k[1]) for k, d in zip(kinds, at)]  # noqa: E731
+        if name != "attend":   # its workspace's address is the host allocator's
+            with pytest.raises(Called):
+                f(*make([0] * len(kinds)))
+        for i in range(len(kinds)):
+            with pytest.raises(ValueError, match="device"):
+                f(*make([int(i == j) for j in range(len(kinds))]))
+    with pytest.raises(ValueError, match="device"):          # a cache on two devices
+        quant.KV4Cache(*(placed(int(i == 2), 2, 2, 16, n, dtype=u8) for i, n in enumerate((32, 2, 32, 2))))
+    assert kv(1).device == 1                                 # kept on another device than the current one: right until used
+
+
 def test_binding_refuses_host_tensors_and_wrong_types():
     x = torch.zeros(2, 8)
     with pytest.raises(ValueError, match="device"):
