@@ -67,9 +67,9 @@ int quant_rows_i8(long rows, long cols, int dtype, const void *x, long x_stride,
  * may be y itself), y [M][N] of out_dtype, act = ReLU when relu != 0.  The sum
  * is an exact 32-bit integer; the rest is fp32, rounded once to out_dtype.
  * An operand whose rows are not 16-byte aligned (pointer, stride and K all
- * multiples of 16) is first copied to the workspace in rows that are; without
- * one that needs it, no workspace is used.  Weights kept in aligned rows save
- * their copy.
+ * multiples of 16), or are 2^23 or more bytes apart, is first copied to the
+ * workspace in rows that are aligned and dense; without one that needs it, no
+ * workspace is used.  Weights kept in aligned rows save their copy.
  * Errors: MICONV_ERR_NULL, MICONV_ERR_SHAPE (M < 0, N or K < 1, a stride below
  * its row), MICONV_ERR_UNSUPPORTED (out_dtype), MICONV_ERR_ALIGN,
  * MICONV_ERR_TOO_LARGE (K > 131071, where the sum could pass 32 bits; M or

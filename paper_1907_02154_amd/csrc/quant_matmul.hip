@@ -344,7 +344,8 @@ int launch_matmul(const MatArgs &a, hipStream_t st)
     }
 }
 
-// Whether an operand's rows can be loaded as they are.
+// Whether an operand's rows can be loaded as they are: 16-byte chunks, and the
+// 256 rows of the largest tile within the 31-bit offsets of a buffer.
 bool rows_aligned(const int8_t *p, long stride, long K)
 {
     return K % 16 == 0 && stride % 16 == 0 && !misaligned(p, 16) && 256 * stride < 1L << 31;

@@ -196,7 +196,8 @@ def rows_i8(x, q=None, scale=None, stream=None):
 # ------------------------------------------------------------------ product of 8-bit integers
 
 def matmul_workspace_bytes(a, w) -> int:
-    """Bytes of workspace that matmul_i8 needs for these operands: 0 unless rows are not 16-byte aligned."""
+    """Bytes of workspace that matmul_i8 needs for these operands: 0 unless rows are not 16-byte aligned, or 2^23 or
+    more bytes apart."""
     sa, sw = _matrix(a, "a", None, None, torch.int8), _matrix(w, "w", None, None, torch.int8)
     n = lib().quant_matmul_workspace_bytes(a.shape[0], w.shape[0], a.shape[1], a.data_ptr(), sa, w.data_ptr(), sw)
     if n < 0:
@@ -232,7 +233,7 @@ def matmul_i8(a, a_scale, w, w_scale, bias=None, residual=None, relu: bool = Fal
     L = lib()
     ap, wp = a.data_ptr(), w.data_ptr()
     sp, sn = None, 0
-    if (K | sa | sw | ap | wp) % 16:   # else no workspace is needed
+    if (K | sa | sw | ap | wp) % 16 or sa >= 1 << 23 or sw >= 1 << 23:   # else no workspace is needed
         sp, sn = _workspace(L.quant_matmul_workspace_bytes(M, N, K, ap, sa, wp, sw), "quant_matmul_i8", ws, a, stream)
     rc = L.quant_matmul_i8(M, N, K, ap, sa, a_scale.data_ptr(), wp, sw, w_scale.data_ptr(), _ptr(bias), rp, sr,
                            _CODE[out_dtype], out.data_ptr(), so, relu, sp, sn, _where(a, stream))

@@ -214,6 +214,22 @@ def test_matmul_strides_and_residual_in_place(M):
             assert torch.equal(out[:, 0].cpu(), r.to(dtype)[:, 0]) and torch.equal(out[:, 1 + N:].cpu(), r.to(dtype)[:, 1 + N:])
 
 
+@pytest.mark.parametrize("far", [(1 << 23) - 16, 1 << 23, (1 << 23) + 16])
+def test_matmul_rows_far_apart(far):
+    """A few columns of a very wide matrix, either side of the stride from which rows are copied."""
+    g = gen(3)
+    for M, N, K in ((5, 40, 96), (40, 3, 96)):
+        a, w = torch.zeros(M, far, dtype=torch.int8, device="cuda")[:, 16:16 + K], torch.zeros(N, far, dtype=torch.int8,
+                                                                                             device="cuda")[:, :K]
+        ha, hw = i8(g, M, K), i8(g, N, K)
+        a.copy_(ha), w.copy_(hw)
+        sa, sw = torch.rand(M, generator=g), torch.rand(N, generator=g)
+        for x, y in ((a, w), (ha.cuda(), w), (a, hw.cuda())):
+            got = quant.matmul_i8(x, sa.cuda(), y, sw.cuda(), out_dtype=F32)
+            want, tol = ref.matmul_i8(ha, sa, hw, sw, bf16=False)
+            assert ((got.cpu().double() - want).abs() <= tol).all()
+
+
 def test_matmul_scales_that_are_not_finite_stay_in_their_row_or_column():
     for M in (4, 70):
         g = gen(M)

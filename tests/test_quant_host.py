@@ -137,6 +137,32 @@ def test_attention_refusals(L):
     assert w(c, 1, 3, 1, 16, 1, 0) == miconv.ERR_SHAPE
 
 
+def test_matmul_workspace_of_rows_far_apart(L, monkeypatch):
+    """Aligned rows 2^23 bytes apart are copied: the query says so, and the binding brings the workspace."""
+    w = L.quant_matmul_workspace_bytes
+    far = 1 << 23
+    assert w(4, 8, 16, FAKE, far - 16, FAKE, far - 16) == 0
+    assert w(4, 8, 16, FAKE, far, FAKE, 16) == w(4, 8, 16, FAKE, 16, FAKE, far) == 256 and w(4, 8, 16, FAKE, far, FAKE, far) == 512
+    given = []
+
+    class Library:
+        quant_matmul_workspace_bytes = staticmethod(w)
+
+        def quant_matmul_i8(self, *a):
+            given.append(a[-2])
+            return 0
+    monkeypatch.setattr(quant, "_getdevice", lambda: 0)
+    monkeypatch.setattr(quant, "lib", Library)
+    i8, f32 = torch.int8, torch.float32
+    for sa, sw in ((far, 16), (16, far), (far, far), (16, 16)):
+        a, b = (placed(0, r, st, dtype=i8)[:, :16] for r, st in ((4, sa), (8, sw)))
+        a.at = b.at = 0
+        ws = placed(0, 1024, dtype=torch.uint8)
+        ws.data_ptr = lambda: FAKE                  # the host allocator aligns to 64 bytes only
+        quant.matmul_i8(a, placed(0, 4, dtype=f32), b, placed(0, 8, dtype=f32), out=placed(0, 4, 8, dtype=f32), ws=ws, stream=0)
+        assert (given[-1] >= w(4, 8, 16, a.data_ptr(), sa, b.data_ptr(), sw)) and (given[-1] > 0) == (max(sa, sw) >= far)
+
+
 @pytest.mark.parametrize("scale", [NAN, float("inf"), -float("inf"), 3e38, -3e38])
 def test_attention_refuses_scales_that_are_not_finite(L, scale):
     assert L.quant_attention_kv4(cache(), 2, 4, 2, FAKE, 256, None, FAKE, FAKE, 3, 1, 48, scale, 1, 0, FAKE, 256, None, 0,
