@@ -138,8 +138,9 @@ int quant_kv4_read(const quant_kv4 *cache, long tokens, const int32_t *slots, in
  * Errors: MICONV_ERR_NULL, MICONV_ERR_SHAPE (heads no multiple of the cache's,
  * a stride below its row, max_new or max_len < 1, table_stride < 1, a scale that
  * is not finite, also times log2(e)), MICONV_ERR_UNSUPPORTED (head_dim), MICONV_ERR_ALIGN, MICONV_ERR_TOO_LARGE
- * (2^31 slots, 2^24 query rows of a key head, or so much work that a grid does
- * not hold it), MICONV_ERR_WORKSPACE. */
+ * (2^31 slots, 2^31 rows of heads in a page, a max_len of 2^30, 2^16 sequences or
+ * heads, 2^24 query rows of a key head, or so much work that a grid does not hold
+ * it), MICONV_ERR_WORKSPACE. */
 long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len,
                                      int causal, int window);
 int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, long tokens, const void *q, long q_stride,

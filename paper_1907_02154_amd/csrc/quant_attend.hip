@@ -942,6 +942,7 @@ int check_attend(const quant_kv4 *cache, int seqs, int heads, int max_new, int m
     if (seqs < 0 || heads < 1 || heads % c->heads || max_new < 1 || max_len < 1) return MICONV_ERR_SHAPE;
     if ((long)max_new * (heads / c->heads) >= 1L << 24 || max_len >= 1 << 30 || seqs > 65535 || heads > 65535)
         return MICONV_ERR_TOO_LARGE;
+    if ((long)c->heads * c->page_size >= 1L << 31) return MICONV_ERR_TOO_LARGE;   // the kernels number a page's rows in 32 bits
     return MICONV_OK;
 }
 

@@ -169,6 +169,19 @@ def test_attention_refuses_scales_that_are_not_finite(L, scale):
                                  None) == miconv.ERR_SHAPE
 
 
+def test_attention_refuses_pages_of_more_rows_than_32_bits_hold(L):
+    """heads * page_size >= 2^31: too many for attention's kernels, though the cache's own take them."""
+    w = L.quant_attention_workspace_bytes
+    assert w(cache(pages=1, heads=8, page_size=(1 << 28) - 1, head_dim=32), 1, 8, 1, 16, 1, 0) == 0
+    for heads, page in ((8, 1 << 28), (65535, 1 << 15 | 1), (16, 1 << 28)):
+        c = cache(pages=1, heads=heads, page_size=page, head_dim=32)
+        assert w(c, 1, heads, 1, 16, 1, 0) == miconv.ERR_TOO_LARGE
+        n = heads * 32
+        assert L.quant_attention_kv4(c, 1, heads, 1, FAKE, n, None, FAKE, FAKE, 1, 1, 16, 1.0, 1, 0, FAKE, n, None, 0,
+                                     None) == miconv.ERR_TOO_LARGE
+        assert L.quant_kv4_read(c, 0, FAKE, 1, FAKE, n, FAKE, n, None) == miconv.OK
+
+
 @pytest.mark.parametrize("head_dim", [64, 128])
 @pytest.mark.parametrize("max_new", [1, 12, 300])
 def test_attention_plans_of_windows_wider_than_any_length(L, head_dim, max_new):
