@@ -273,7 +273,7 @@ void go(const RowArgs &a, hipStream_t st)
 template <typename T>
 int launch_rows(const RowArgs &a, hipStream_t st)
 {
-    const int units = ceil_div(a.cols, 8);
+    const int units = (int)((a.cols + 7L) / 8);
     if (units <= 64) go<T, 64, 1>(a, st);
     else if (units <= 128) go<T, 64, 2>(a, st);
     else if (units <= 256) go<T, 256, 1>(a, st);

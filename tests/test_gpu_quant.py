@@ -139,6 +139,17 @@ def test_rmsnorm_scales_over_the_range_of_fp32(dtype, cols, eps):
     check_rows(got, x[keep], torch.ones(cols), r[keep], eps=eps)
 
 
+@pytest.mark.parametrize("cols", [2 ** 31 - 1, 2 ** 31 - 8, 2 ** 31 - 9])
+def test_rows_of_the_longest_lengths(cols):
+    """The last lengths that an int holds: both ends of the row, and all of it by its sum."""
+    x = torch.ones(1, cols, dtype=BF16, device="cuda")
+    x[0, 1000], x[0, -1], x[0, -1000] = 127.0, -127.0, 5.0
+    q = torch.full((1, cols), 9, dtype=torch.int8, device="cuda")
+    scale = quant.rows_i8(x, q=q)[1]
+    assert float(scale) == 1.0 and int(q.sum(dtype=torch.int64)) == cols - 3 + 5
+    assert q[0, 1000] == 127 and q[0, -1] == -127 and q[0, -1000] == 5 and int(q.max()) == 127 and int(q.min()) == -127
+
+
 def test_rows_ties():
     x = torch.arange(-254, 255).float().reshape(1, -1) / 2   # largest 127: halves go to the even side
     q, scale = quant.rows_i8(x.cuda())
