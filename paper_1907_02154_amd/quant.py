@@ -110,6 +110,12 @@ def _vector(t, name: str, n: int, dtype) -> None:
         raise ValueError(f"{name} must be a dense vector of {n}")
 
 
+def _int32(**values) -> None:
+    """Numbers that the library takes in 32 bits: ctypes would pass the low ones of a larger number on."""
+    if max(values.values()) >= 1 << 31 or min(values.values()) < -1 << 31:
+        raise ValueError("must fit 32 bits: " + ", ".join(f"{k} = {v}" for k, v in values.items()))
+
+
 def _where(t, stream):
     """The stream for work on t, which is on the current device: the current one when None."""
     if stream is not None:
@@ -266,6 +272,7 @@ class KV4Cache:
             raise ValueError(f"with k_codes {list(codes)} v_codes must be the same and k_exps and v_exps {list(exps)}")
         if not (k_codes.is_contiguous() and k_exps.is_contiguous() and v_codes.is_contiguous() and v_exps.is_contiguous()):
             raise ValueError("codes and exponents must be contiguous")
+        _int32(heads=heads, page_size=page_size)
         self.k_codes, self.k_exps, self.v_codes, self.v_exps = k_codes, k_exps, v_codes, v_exps
         self.pages, self.heads, self.page_size, self.head_dim, self.device = pages, heads, page_size, 2 * half, i
         self._desc = _Kv4(k_codes.data_ptr(), k_exps.data_ptr(), v_codes.data_ptr(), v_exps.data_ptr(), pages, heads,
@@ -341,6 +348,7 @@ def kv4_read(slots, cache: KV4Cache, k=None, v=None, dtype=torch.bfloat16, strea
 
 def attention_workspace_bytes(cache: KV4Cache, seqs: int, heads: int, max_new: int, max_len: int, causal: bool = True,
                               window: int = 0) -> int:
+    _int32(seqs=seqs, heads=heads, max_new=max_new, max_len=max_len, window=window)
     n = lib().quant_attention_workspace_bytes(_cache(cache)._desc, seqs, heads, max_new, max_len, causal, window)
     if n < 0:
         _check(int(n), "quant_attention_workspace_bytes")
@@ -378,6 +386,8 @@ def attention_kv4(q, cache: KV4Cache, table, lens, starts=None, max_new: Optiona
         max_new = 1 if starts is None else max(n, 1)
     if max_len is None:
         max_len = width * c.page_size
+    if (seqs | heads | width | max_new | max_len | window) >> 31:   # one of them negative or too large
+        _int32(seqs=seqs, heads=heads, width=width, max_new=max_new, max_len=max_len, window=window)
     if out is None:
         out, outs = _empty(q, (n, heads, d), torch.bfloat16, stream), heads * d
     else:

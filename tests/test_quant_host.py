@@ -250,6 +250,29 @@ def test_binding_refuses_operands_on_another_device(monkeypatch):
     assert kv(1).device == 1                                 # kept on another device than the current one: right until used
 
 
+def test_binding_refuses_numbers_of_more_than_32_bits(monkeypatch):
+    """ctypes takes the low 32 bits of a number: a window of 2^32 + 5 would be one of 5."""
+    monkeypatch.setattr(quant, "_getdevice", lambda: 0)
+    calls = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *a: calls.append(name) or 0
+    monkeypatch.setattr(quant, "lib", Library)
+    c = quant.KV4Cache(*(placed(0, 2, 2, 16, n, dtype=torch.uint8) for n in (32, 2, 32, 2)))
+    q, o = (placed(0, 2, 4, 64, dtype=torch.bfloat16) for _ in range(2))
+    t, n = placed(0, 2, 2, dtype=torch.int32), placed(0, 2, dtype=torch.int32)
+    for k in ("max_new", "max_len", "window"):
+        for v in (1 << 31, (1 << 32) + 5, -(1 << 31) - 1):
+            with pytest.raises(ValueError, match=k):
+                quant.attention_kv4(q, c, t, n, out=o, stream=0, **{k: v})
+            with pytest.raises(ValueError, match=k):
+                quant.attention_workspace_bytes(c, 2, 4, **{"max_new": 1, "max_len": 32, k: v})
+    assert not calls
+    quant.attention_kv4(q, c, t, n, out=o, stream=0, window=(1 << 31) - 1)
+    assert calls == ["quant_attention_workspace_bytes", "quant_attention_kv4"]
+
+
 def test_binding_refuses_host_tensors_and_wrong_types():
     x = torch.zeros(2, 8)
     with pytest.raises(ValueError, match="device"):
