@@ -38,20 +38,34 @@ class Weights:
 
 class State:
     """What `seqs` sequences of up to `max_len` tokens keep between calls: their pages in each block's cache, and their
-    lengths."""
+    lengths, on the device (`lens`) and on the host (`held`: what a call is checked against before it launches anything)."""
 
     def __init__(self, dec: "Decoder", seqs: int, max_len: int, page_size: int = 64, seed: int = 0):
+        if seqs < 1 or max_len < 1 or page_size < 1:
+            raise ValueError("a state holds one sequence of one token at least, in pages of one at least")
         pages = -(-max_len // page_size)
         g = torch.Generator().manual_seed(seed)      # pages in no order, as a server that reuses them has them
         self.table = torch.randperm(seqs * pages, generator=g).reshape(seqs, pages).to(torch.int32).cuda()
         self.caches = [quant.KV4Cache.allocate(seqs * pages, dec.kv_heads, page_size, dec.head_dim) for _ in dec.blocks]
         self.lens = torch.zeros(seqs, dtype=torch.int32, device="cuda")
+        self.held = [0] * seqs
         self.max_len, self.page_size = max_len, page_size
 
+    def take(self, news: List[int]) -> None:
+        """Counts news[s] more tokens of each sequence s, if all have room for theirs."""
+        if len(news) != len(self.held):
+            raise ValueError(f"the state has {len(self.held)} sequences, got tokens of {len(news)}")
+        after = [h + n for h, n in zip(self.held, news)]
+        if max(after) > self.max_len:
+            s = after.index(max(after))
+            raise ValueError(f"sequence {s} holds {self.held[s]} tokens of {self.max_len} at most: no room for {news[s]} more")
+        self.held = after
+
     def slots(self, seq: torch.Tensor, place: torch.Tensor) -> torch.Tensor:
-        """Cache slots of the tokens at `place` of sequences `seq`."""
-        page = self.table[seq, torch.div(place, self.page_size, rounding_mode="floor")]
-        return (page * self.page_size + place % self.page_size).to(torch.int32)
+        """Cache slots of the tokens at `place` of sequences `seq`; -1, which is not written, past max_len."""
+        page = self.table[seq, torch.div(place.clamp(max=self.max_len - 1), self.page_size, rounding_mode="floor")]
+        slot = page * self.page_size + place % self.page_size
+        return torch.where(place < self.max_len, slot, -1).to(torch.int32)
 
 
 class Block:
@@ -99,8 +113,11 @@ class Decoder:
 
     def prompt(self, state: State, xs: List[torch.Tensor], trace=None) -> List[torch.Tensor]:
         """New tokens of every sequence, xs[s] bf16 [tokens][width] behind what the sequence holds: the stream after the
-        last block, a tensor for each sequence."""
+        last block, a tensor for each sequence.  A ValueError, and nothing done, where a sequence has no room for its own."""
+        if any(x.dim() != 2 or x.shape[1] != self.width or x.dtype != torch.bfloat16 for x in xs):
+            raise ValueError(f"tokens must be bf16 [tokens][{self.width}]")
         news = [x.shape[0] for x in xs]
+        state.take(news)
         starts = torch.tensor([0, *torch.tensor(news).cumsum(0).tolist()], dtype=torch.int32).cuda()
         seq = torch.repeat_interleave(torch.arange(len(xs)), torch.tensor(news)).cuda()
         place = torch.arange(sum(news), device="cuda") - starts[seq] + state.lens[seq]
@@ -112,7 +129,14 @@ class Decoder:
         return list(x.split(news))
 
     def step(self, state: State, x: torch.Tensor, trace=None) -> torch.Tensor:
-        """One new token of every sequence, x bf16 [seqs][width]: the stream after the last block."""
+        """One new token of every sequence, x bf16 [seqs][width]: the stream after the last block.  A ValueError, and
+        nothing done, where a sequence has no room for it."""
+        if x.dim() != 2 or x.shape[1] != self.width or x.dtype != torch.bfloat16:
+            raise ValueError(f"tokens must be bf16 [sequences][{self.width}]")
+        state.take([1] * x.shape[0])
+        return self._step(state, x, trace)
+
+    def _step(self, state: State, x: torch.Tensor, trace=None) -> torch.Tensor:
         seq = torch.arange(x.shape[0], device="cuda")
         slots = state.slots(seq, state.lens)
         state.lens += 1
@@ -121,19 +145,32 @@ class Decoder:
         return x
 
 
+class Steps:
+    """A captured step: each replay takes the sequences of its state one token further."""
+
+    def __init__(self, state: State, graph: "torch.cuda.CUDAGraph"):
+        self.state, self.graph = state, graph
+
+    def replay(self) -> None:
+        """A ValueError, and nothing done, where a sequence has no room for a token more."""
+        self.state.take([1] * len(self.state.held))
+        self.graph.replay()
+
+
 def capture_step(dec: Decoder, state: State, x: torch.Tensor):
-    """A step on the tensor x as a HIP graph: (graph, its output).  Each replay takes the sequences one token further."""
-    lens = state.lens.clone()
+    """A step on the tensor x as a HIP graph: (``Steps`` to replay, its output)."""
+    lens, held = state.lens.clone(), state.held
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):      # once outside the graph: kernels are loaded on their first launch
         dec.step(state, x)
     torch.cuda.current_stream().wait_stream(side)
     state.lens.copy_(lens)
+    state.held = held
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        out = dec.step(state, x)
-    return graph, out
+        out = dec._step(state, x)
+    return Steps(state, graph), out
 
 
 def main(seqs: int = 16, prompt: int = 1000, steps: int = 64) -> None:

@@ -108,3 +108,36 @@ def test_weights_hold_a_scale_for_each_channel():
     got = decoder.Weights(w.cuda())
     off = (got.q.cpu().float() * got.scale.cpu()[:, None] - w).abs()
     assert (off <= 0.5001 * got.scale.cpu()[:, None]).all()      # half a step of the channel's own
+
+
+def test_sequences_up_to_their_last_place_and_past_it():
+    """A state whose last page has room past max_len: the last token against the oracle, the next one refused, and a replay
+    that goes round the refusal writes no cache."""
+    dec, state = small()                             # 150 tokens of at most, pages of 16: 160 places
+    held = [[[torch.zeros(0, 2, 64, dtype=torch.float64) for _ in "kv"] for _ in range(3)] for _ in dec.blocks]
+    trace = []
+    out = dec.prompt(state, streams(dec, [148, 140, 3], 30), trace)
+    check_pass(dec, state, trace, [148, 140, 3], held)
+    x = torch.stack([y[-1] for y in out])
+    steps, got = decoder.capture_step(dec, state, x)
+    for _ in range(2):
+        steps.replay()
+    torch.cuda.synchronize()
+    assert state.lens.tolist() == state.held == [150, 142, 5]
+    kept = [t.clone() for c in state.caches for t in (c.k_codes, c.k_exps, c.v_codes, c.v_exps)]
+    for f in (steps.replay, lambda: dec.step(state, x), lambda: decoder.capture_step(dec, state, x),
+              lambda: dec.prompt(state, streams(dec, [1, 0, 0], 31)), lambda: dec.prompt(state, streams(dec, [0, 9, 0], 31))):
+        with pytest.raises(ValueError, match="no room"):
+            f()
+    assert state.lens.tolist() == state.held == [150, 142, 5]
+    dec.prompt(state, streams(dec, [0, 8, 0], 32))
+    for _ in range(12):
+        steps.graph.replay()                         # past 150, and for the first sequence past its pages
+    torch.cuda.synchronize()
+    assert state.lens.tolist() == [162, 162, 17]
+    pages = state.table[:2].flatten().long()         # of the full sequences: only what the prompt wrote has changed
+    wrote = state.slots(torch.ones(8, dtype=torch.long, device="cuda"), torch.arange(142, 150, device="cuda")).long()
+    for old, new in zip(kept, [t for c in state.caches for t in (c.k_codes, c.k_exps, c.v_codes, c.v_exps)]):
+        same = (old == new).all(-1).all(1)           # [pages][place]
+        same[wrote // 16, wrote % 16] = True
+        assert same[pages].all()
