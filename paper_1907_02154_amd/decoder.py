@@ -118,6 +118,8 @@ class Decoder:
             raise ValueError(f"tokens must be bf16 [tokens][{self.width}]")
         news = [x.shape[0] for x in xs]
         state.take(news)
+        if not any(news):
+            return list(xs)
         starts = torch.tensor([0, *torch.tensor(news).cumsum(0).tolist()], dtype=torch.int32).cuda()
         seq = torch.repeat_interleave(torch.arange(len(xs)), torch.tensor(news)).cuda()
         place = torch.arange(sum(news), device="cuda") - starts[seq] + state.lens[seq]

@@ -56,3 +56,9 @@ def test_slots_past_the_capacity_are_none():
     seq = torch.tensor([0, 0, 0, 1, 1, 1, 1])
     place = torch.tensor([0, 9, 10, 4, 11, 12, 1000])
     assert state.slots(seq, place).tolist() == [20, 13, -1, 8, -1, -1, -1]
+
+
+def test_prompts_of_no_tokens():
+    dec, state = made([3, 10], 10)
+    out = dec.prompt(state, [tokens(0), tokens(0)])
+    assert [tuple(x.shape) for x in out] == [(0, 8), (0, 8)] and state.held == [3, 10]
