@@ -6,7 +6,7 @@
 // channels of one token.  The sums are exact 32-bit integers, so no tile and no
 // order of the reduction changes a result.
 //
-// One kernel, tiles of ten sizes.  A few tokens are bound by the weights'
+// One kernel, tiles of eight sizes.  A few tokens are bound by the weights'
 // bytes, many by the matrix cores; in between by what a compute unit can fetch,
 // which grows with the wavefronts that wait side by side: there several groups
 // of wavefronts share a tile and divide its reduction.
@@ -301,15 +301,15 @@ int go_tile(MatArgs a, hipStream_t st)
 // work-group on each of 256 compute units, or, where two fit one, with one and
 // with two on each (measured, random operands; the launch's own 2 us apart).
 // Of two tiles that hold the same number of outputs the wider one suits few
-// tokens.
+// tokens.  (Two 16 x 32 tiles to a compute unit leave none for one of 32 x 32.)
 struct Tile {
     int bm, bn, per_cu;
     float one, two;
 };
 constexpr Tile kTiles[] = {
-    {16, 16, 2, 3.4f, 3.8f}, {16, 32, 2, 3.8f, 5.0f}, {32, 32, 1, 5.0f, 0.0f}, {32, 64, 1, 6.6f, 0.0f},
-    {64, 32, 1, 6.6f, 0.0f}, {64, 64, 1, 9.3f, 0.0f}, {128, 64, 1, 13.8f, 0.0f}, {128, 128, 1, 22.3f, 0.0f},
-    {128, 128, 2, 28.0f, 38.0f}, {256, 256, 1, 66.0f, 0.0f},
+    {16, 16, 2, 3.4f, 3.8f}, {16, 32, 2, 3.8f, 5.0f}, {32, 64, 1, 6.6f, 0.0f}, {64, 32, 1, 6.6f, 0.0f},
+    {64, 64, 1, 9.3f, 0.0f}, {128, 64, 1, 13.8f, 0.0f}, {128, 128, 1, 22.3f, 0.0f}, {128, 128, 2, 28.0f, 38.0f},
+    {256, 256, 1, 66.0f, 0.0f},
 };
 
 int pick_tile(const MatArgs &a)
@@ -333,13 +333,12 @@ int launch_matmul(const MatArgs &a, hipStream_t st)
     switch (pick_tile(a)) {
     case 0: return go_tile<T, 16, 16, 1, 1, 4, 4>(a, st);
     case 1: return go_tile<T, 16, 32, 1, 2, 4, 3>(a, st);
-    case 2: return go_tile<T, 32, 32, 1, 2, 4, 4>(a, st);
-    case 3: return go_tile<T, 32, 64, 1, 4, 4, 3>(a, st);
-    case 4: return go_tile<T, 64, 32, 2, 2, 4, 3>(a, st);
-    case 5: return go_tile<T, 64, 64, 2, 2, 2, 4>(a, st);
-    case 6: return go_tile<T, 128, 64, 4, 2, 2, 3>(a, st);
-    case 7: return go_tile<T, 128, 128, 2, 4, 1, 3>(a, st);
-    case 8: return go_tile<T, 128, 128, 2, 2, 1, 2>(a, st);
+    case 2: return go_tile<T, 32, 64, 1, 4, 4, 3>(a, st);
+    case 3: return go_tile<T, 64, 32, 2, 2, 4, 3>(a, st);
+    case 4: return go_tile<T, 64, 64, 2, 2, 2, 4>(a, st);
+    case 5: return go_tile<T, 128, 64, 4, 2, 2, 3>(a, st);
+    case 6: return go_tile<T, 128, 128, 2, 4, 1, 3>(a, st);
+    case 7: return go_tile<T, 128, 128, 2, 2, 1, 2>(a, st);
     default: return go_tile<T, 256, 256, 4, 2, 1, 2>(a, st);
     }
 }
