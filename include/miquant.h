@@ -73,8 +73,8 @@ int quant_rows_i8(long rows, long cols, int dtype, const void *x, long x_stride,
  * Errors: MICONV_ERR_NULL, MICONV_ERR_SHAPE (M < 0, N or K < 1, a stride below
  * its row), MICONV_ERR_UNSUPPORTED (out_dtype), MICONV_ERR_ALIGN,
  * MICONV_ERR_TOO_LARGE (K > 131071, where the sum could pass 32 bits; M or
- * N >= 2^31, or so many outputs that a grid does not hold them),
- * MICONV_ERR_WORKSPACE. */
+ * N > 2^31 - 256; so many outputs that a grid does not hold them, or 2^35 bytes
+ * of rows to copy), MICONV_ERR_WORKSPACE. */
 long quant_matmul_workspace_bytes(long M, long N, long K, const int8_t *a, long a_stride, const int8_t *w,
                                   long w_stride);
 int quant_matmul_i8(long M, long N, long K, const int8_t *a, long a_stride, const float *a_scale, const int8_t *w,

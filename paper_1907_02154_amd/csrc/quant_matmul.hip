@@ -367,7 +367,8 @@ namespace {
 int check_matmul(long M, long N, long K, long a_stride, long w_stride)
 {
     if (M < 0 || N < 1 || K < 1 || a_stride < K || w_stride < K) return MICONV_ERR_SHAPE;
-    if (M >= 1L << 31 || N >= 1L << 31 || K > 131071) return MICONV_ERR_TOO_LARGE;
+    // rows and channels are numbered in 32 bits, those of the last tile that are not there too
+    if (M > (1L << 31) - 256 || N > (1L << 31) - 256 || K > 131071) return MICONV_ERR_TOO_LARGE;
     return MICONV_OK;
 }
 

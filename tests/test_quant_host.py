@@ -137,6 +137,17 @@ def test_attention_refusals(L):
     assert w(c, 1, 3, 1, 16, 1, 0) == miconv.ERR_SHAPE
 
 
+def test_matmul_refuses_rows_that_a_tile_numbers_past_32_bits(L):
+    """The last tile's rows that are not there have numbers too: 255 of them at most."""
+    w = L.quant_matmul_workspace_bytes
+    most = (1 << 31) - 256
+    assert w(most, 1, 16, FAKE, 16, FAKE, 16) == w(1, most, 16, FAKE, 16, FAKE, 16) == 0
+    for M, N in ((most + 1, 1), (1, most + 1), ((1 << 31) - 1, 8)):
+        assert w(M, N, 16, FAKE, 16, FAKE, 16) == miconv.ERR_TOO_LARGE
+        assert L.quant_matmul_i8(M, N, 16, FAKE, 16, FAKE, FAKE, 16, FAKE, None, None, 0, 1, FAKE, N, 0, None, 0,
+                                 None) == miconv.ERR_TOO_LARGE
+
+
 def test_matmul_workspace_of_rows_far_apart(L, monkeypatch):
     """Aligned rows 2^23 bytes apart are copied: the query says so, and the binding brings the workspace."""
     w = L.quant_matmul_workspace_bytes
