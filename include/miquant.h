@@ -82,6 +82,13 @@ int quant_matmul_i8(long M, long N, long K, const int8_t *a, long a_stride, cons
                     long residual_stride, int out_dtype, void *y, long y_stride, int relu, void *ws,
                     size_t ws_bytes, void *stream);
 
+/* The kernels (as a profiler prints them, "a + b" for two launches) and the
+ * number of launches of a call; buf is cut at buflen.  Nothing is launched, and
+ * of the operands only the addresses matter.
+ * Errors: those of the call, and MICONV_ERR_NULL for buf or launches. */
+int quant_matmul_describe(long M, long N, long K, const int8_t *a, long a_stride, const int8_t *w, long w_stride,
+                          int out_dtype, char *buf, int buflen, int *launches);
+
 /* A paged cache of keys and values in 4 bits.  Along a head's channels every
  * 32 values share a power of two, 2^(byte - 127); a value is four bits, sign
  * then the index of 0, .5, 1, 1.5, 2, 3, 4, 6, two to a byte, the lower
@@ -147,6 +154,9 @@ int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, long tokens
                         const int32_t *starts, const int32_t *lens, const int32_t *table, int table_stride,
                         int max_new, int max_len, float scale, int causal, int window, void *out, long out_stride,
                         void *ws, size_t ws_bytes, void *stream);
+/* The kernels of a call, as quant_matmul_describe names them. */
+int quant_attention_describe(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len, int causal,
+                             int window, char *buf, int buflen, int *launches);
 
 #ifdef __cplusplus
 }

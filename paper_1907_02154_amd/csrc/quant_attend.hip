@@ -14,6 +14,7 @@
 #include "quant.h"
 
 #include <algorithm>
+#include <stdio.h>
 
 namespace miconv {
 namespace quant {
@@ -891,6 +892,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttArgs a)
     store1(a.out + (sq.row0 + t) * a.os + (long)h * D + threadIdx.x, l == 0.0f ? 0.0f : x / l);
 }
 
+// Many rows: the heads that take them in steps.
+constexpr bool in_steps(int D) { return D == 96 || D == 128; }
+
 struct AttPlan {
     bool wide;
     int nb, row_blocks, splits, per_split;
@@ -946,6 +950,12 @@ int check_attend(const quant_kv4 *cache, int seqs, int heads, int max_new, int m
     return MICONV_OK;
 }
 
+// Whether a grid, of fewer than 2^32 threads, holds the plan's.
+bool grid_holds(const AttPlan &p, const Kv4 &c, int seqs)
+{
+    return (double)p.row_blocks * p.splits * (p.wide ? 512.0 * c.heads * seqs : 256.0) < 0x1p32;
+}
+
 template <int D>
 int launch_attend(const AttArgs &a, const AttPlan &p, hipStream_t st)
 {
@@ -953,7 +963,7 @@ int launch_attend(const AttArgs &a, const AttPlan &p, hipStream_t st)
     if (p.wide) {
         const dim3 all(grid.x * grid.y * grid.z);
         void (*k)(AttArgs);
-        if constexpr (D == 96 || D == 128) k = attend_kv4_steps_kernel<D>;
+        if constexpr (in_steps(D)) k = attend_kv4_steps_kernel<D>;
         else k = attend_kv4_wide_kernel<D>;
         launch_kernel(k, all, dim3(512), 0, st, a);
     } else {
@@ -983,6 +993,27 @@ extern "C" long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs
     return seqs ? (long)miconv::quant::plan_attend(c, seqs, heads, max_new, max_len, causal, window).bytes : 0;
 }
 
+extern "C" int quant_attention_describe(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len, int causal,
+                                        int window, char *buf, int buflen, int *launches)
+{
+    using namespace miconv::quant;
+    if (!buf || buflen <= 0 || !launches) return MICONV_ERR_NULL;
+    buf[0] = 0, *launches = 0;
+    Kv4 c;
+    const int rc = check_attend(cache, seqs, heads, max_new, max_len, &c);
+    if (rc != MICONV_OK) return rc;
+    if (seqs == 0) return MICONV_OK;
+    const AttPlan p = plan_attend(c, seqs, heads, max_new, max_len, causal, window);
+    if (!grid_holds(p, c, seqs)) return MICONV_ERR_TOO_LARGE;
+    char first[64], join[64] = "";
+    if (p.wide) snprintf(first, sizeof first, "attend_kv4_%s_kernel<%d>", in_steps(c.dim) ? "steps" : "wide", c.dim);
+    else snprintf(first, sizeof first, "attend_kv4_kernel<%d, %d>", c.dim, p.nb);
+    if (p.splits > 1) snprintf(join, sizeof join, " + attend_join_kernel<%d>", c.dim);
+    *launches = p.splits > 1 ? 2 : 1;
+    snprintf(buf, buflen, "%s%s", first, join);
+    return MICONV_OK;
+}
+
 extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, long tokens, const void *q,
                                    long q_stride, const int32_t *starts, const int32_t *lens, const int32_t *table,
                                    int table_stride, int max_new, int max_len, float scale, int causal, int window,
@@ -1003,8 +1034,7 @@ extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, 
         quant::misaligned(lens, 4) || quant::misaligned(table, 4))
         return MICONV_ERR_ALIGN;
     const quant::AttPlan p = quant::plan_attend(a.c, seqs, heads, max_new, max_len, causal, window);
-    // a grid holds fewer than 2^32 threads
-    if ((double)p.row_blocks * p.splits * (p.wide ? 512.0 * a.c.heads * seqs : 256.0) >= 0x1p32) return MICONV_ERR_TOO_LARGE;
+    if (!quant::grid_holds(p, a.c, seqs)) return MICONV_ERR_TOO_LARGE;
     if (p.bytes && (!ws || ws_bytes < p.bytes || quant::misaligned(ws, 256))) return MICONV_ERR_WORKSPACE;
     a.q = (const uint16_t *)q, a.out = (uint16_t *)out;
     a.starts = starts, a.lens = lens, a.table = table;

@@ -12,6 +12,8 @@
 // of wavefronts share a tile and divide its reduction.
 #include "quant.h"
 
+#include <stdio.h>
+
 namespace miconv {
 namespace quant {
 namespace {
@@ -285,41 +287,30 @@ __global__ __launch_bounds__(256) void matmul_i8_align_kernel(AlignArgs a)
         load16(a.src[o] + r * a.stride[o] + 16 * c, min(a.K - 16 * c, 16));
 }
 
-template <typename T, int BM, int BN, int WM, int WN, int KG, int NST>
-int go_tile(MatArgs a, hipStream_t st)
-{
-    a.mt = ceil_div(a.M, BM), a.nt = ceil_div(a.N, BN);
-    // a grid holds fewer than 2^32 threads
-    if ((long)a.mt * a.nt * (64 * WM * WN * KG) >= 1L << 32 || (long)kGroup * a.nt >= 1L << 31) return MICONV_ERR_TOO_LARGE;
-    a.tiles = a.mt * a.nt;
-    a.dv_group = make_fastdiv((unsigned)(kGroup * a.nt));
-    launch_kernel(matmul_i8_tile_kernel<T, BM, BN, WM, WN, KG, NST>, dim3((unsigned)a.tiles), dim3(64 * WM * WN * KG), 0, st, a);
-    return launched();
-}
-
 // The tiles, and what a round of them takes: microseconds at K = 4096 with a
 // work-group on each of 256 compute units, or, where two fit one, with one and
 // with two on each (measured, random operands; the launch's own 2 us apart).
 // Of two tiles that hold the same number of outputs the wider one suits few
 // tokens.  (Two 16 x 32 tiles to a compute unit leave none for one of 32 x 32.)
 struct Tile {
-    int bm, bn, per_cu;
+    int bm, bn, wm, wn, kg, nst;   // the kernel's parameters
+    int per_cu;
     float one, two;
 };
 constexpr Tile kTiles[] = {
-    {16, 16, 2, 3.4f, 3.8f}, {16, 32, 2, 3.8f, 5.0f}, {32, 64, 1, 6.6f, 0.0f}, {64, 32, 1, 6.6f, 0.0f},
-    {64, 64, 1, 9.3f, 0.0f}, {128, 64, 1, 13.8f, 0.0f}, {128, 128, 1, 22.3f, 0.0f}, {128, 128, 2, 28.0f, 38.0f},
-    {256, 256, 1, 66.0f, 0.0f},
+    {16, 16, 1, 1, 4, 4, 2, 3.4f, 3.8f},    {16, 32, 1, 2, 4, 3, 2, 3.8f, 5.0f},    {32, 64, 1, 4, 4, 3, 1, 6.6f, 0.0f},
+    {64, 32, 2, 2, 4, 3, 1, 6.6f, 0.0f},    {64, 64, 2, 2, 2, 4, 1, 9.3f, 0.0f},    {128, 64, 4, 2, 2, 3, 1, 13.8f, 0.0f},
+    {128, 128, 2, 4, 1, 3, 1, 22.3f, 0.0f}, {128, 128, 2, 2, 1, 2, 2, 28.0f, 38.0f}, {256, 256, 4, 2, 1, 2, 1, 66.0f, 0.0f},
 };
 
-int pick_tile(const MatArgs &a)
+int pick_tile(int M, int N)
 {
     const long cus = cu_count();
     int best = 0;
     double least = 1e300;
     for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
         const Tile &t = kTiles[i];
-        const long tiles = (long)ceil_div(a.M, t.bm) * ceil_div(a.N, t.bn), round = cus * t.per_cu, rest = tiles % round;
+        const long tiles = (long)ceil_div(M, t.bm) * ceil_div(N, t.bn), round = cus * t.per_cu, rest = tiles % round;
         const double full = t.per_cu == 2 ? t.two : t.one;
         const double cost = (double)(tiles / round) * full + (rest == 0 ? 0.0 : rest > cus ? full : t.one);
         if (cost < least) least = cost, best = i;
@@ -327,19 +318,33 @@ int pick_tile(const MatArgs &a)
     return best;
 }
 
+template <typename T, int I>
+int go_tile(MatArgs a, hipStream_t st)
+{
+    constexpr Tile t = kTiles[I];
+    constexpr int threads = 64 * t.wm * t.wn * t.kg;
+    a.mt = ceil_div(a.M, t.bm), a.nt = ceil_div(a.N, t.bn);
+    // a grid holds fewer than 2^32 threads
+    if ((long)a.mt * a.nt * threads >= 1L << 32 || (long)kGroup * a.nt >= 1L << 31) return MICONV_ERR_TOO_LARGE;
+    a.tiles = a.mt * a.nt;
+    a.dv_group = make_fastdiv((unsigned)(kGroup * a.nt));
+    launch_kernel(matmul_i8_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kg, t.nst>, dim3((unsigned)a.tiles), dim3(threads), 0, st, a);
+    return launched();
+}
+
 template <typename T>
 int launch_matmul(const MatArgs &a, hipStream_t st)
 {
-    switch (pick_tile(a)) {
-    case 0: return go_tile<T, 16, 16, 1, 1, 4, 4>(a, st);
-    case 1: return go_tile<T, 16, 32, 1, 2, 4, 3>(a, st);
-    case 2: return go_tile<T, 32, 64, 1, 4, 4, 3>(a, st);
-    case 3: return go_tile<T, 64, 32, 2, 2, 4, 3>(a, st);
-    case 4: return go_tile<T, 64, 64, 2, 2, 2, 4>(a, st);
-    case 5: return go_tile<T, 128, 64, 4, 2, 2, 3>(a, st);
-    case 6: return go_tile<T, 128, 128, 2, 4, 1, 3>(a, st);
-    case 7: return go_tile<T, 128, 128, 2, 2, 1, 2>(a, st);
-    default: return go_tile<T, 256, 256, 4, 2, 1, 2>(a, st);
+    switch (pick_tile(a.M, a.N)) {
+    case 0: return go_tile<T, 0>(a, st);
+    case 1: return go_tile<T, 1>(a, st);
+    case 2: return go_tile<T, 2>(a, st);
+    case 3: return go_tile<T, 3>(a, st);
+    case 4: return go_tile<T, 4>(a, st);
+    case 5: return go_tile<T, 5>(a, st);
+    case 6: return go_tile<T, 6>(a, st);
+    case 7: return go_tile<T, 7>(a, st);
+    default: return go_tile<T, 8>(a, st);
     }
 }
 
@@ -381,6 +386,24 @@ extern "C" long quant_matmul_workspace_bytes(long M, long N, long K, const int8_
     const int rc = check_matmul(M, N, K, a_stride, w_stride);
     if (rc != MICONV_OK) return rc;
     return M ? copy_bytes(M, a, a_stride, K) + copy_bytes(N, w, w_stride, K) : 0;
+}
+
+extern "C" int quant_matmul_describe(long M, long N, long K, const int8_t *a, long a_stride, const int8_t *w, long w_stride,
+                                     int out_dtype, char *buf, int buflen, int *launches)
+{
+    using namespace miconv::quant;
+    if (!buf || buflen <= 0 || !launches) return MICONV_ERR_NULL;
+    buf[0] = 0, *launches = 0;
+    const int rc = check_matmul(M, N, K, a_stride, w_stride);
+    if (rc != MICONV_OK) return rc;
+    if (!dtype_bytes(out_dtype)) return MICONV_ERR_UNSUPPORTED;
+    if (M == 0) return MICONV_OK;
+    const bool copy = copy_bytes(M, a, a_stride, K) + copy_bytes(N, w, w_stride, K) > 0;
+    const Tile t = kTiles[pick_tile((int)M, (int)N)];
+    *launches = 1 + copy;
+    snprintf(buf, buflen, "%smatmul_i8_tile_kernel<%s, %d, %d, %d, %d, %d, %d>", copy ? "matmul_i8_align_kernel + " : "",
+             out_dtype == kF32 ? "float" : "unsigned short", t.bm, t.bn, t.wm, t.wn, t.kg, t.nst);
+    return MICONV_OK;
 }
 
 extern "C" int quant_matmul_i8(long M, long N, long K, const int8_t *a, long a_stride, const float *a_scale,

@@ -47,8 +47,11 @@ def lib() -> ctypes.CDLL:
         L.quant_kv4_read.argtypes = [c, l, p, i, p, l, p, l, p]
         L.quant_attention_workspace_bytes.argtypes = [c, i, i, i, i, i, i]
         L.quant_attention_kv4.argtypes = [c, i, i, l, p, l, p, p, p, i, i, i, f, i, i, p, l, p, sz, p]
+        L.quant_matmul_describe.argtypes = [l, l, l, p, l, p, l, i, ctypes.c_char_p, i, ctypes.POINTER(i)]
+        L.quant_attention_describe.argtypes = [c, i, i, i, i, i, i, ctypes.c_char_p, i, ctypes.POINTER(i)]
         L.quant_matmul_workspace_bytes.restype = L.quant_attention_workspace_bytes.restype = l
-        for name in ("rmsnorm_i8", "rows_i8", "matmul_i8", "kv4_write", "kv4_read", "attention_kv4"):
+        for name in ("rmsnorm_i8", "rows_i8", "matmul_i8", "kv4_write", "kv4_read", "attention_kv4", "matmul_describe",
+                     "attention_describe"):
             getattr(L, "quant_" + name).restype = i
         _bound = L
     return _bound
@@ -211,6 +214,19 @@ def matmul_workspace_bytes(a, w) -> int:
     return int(n)
 
 
+def _describe(f, what: str, *args):
+    buf, n = ctypes.create_string_buffer(256), ctypes.c_int()
+    _check(f(*args, buf, 256, ctypes.byref(n)), what)
+    return buf.value.decode(), n.value
+
+
+def matmul_describe(M: int, N: int, K: int, out_dtype=torch.bfloat16, a_stride: Optional[int] = None,
+                    w_stride: Optional[int] = None):
+    """(kernel names, launch count) of matmul_i8 for operands at 16-byte aligned addresses (strides: dense rows)."""
+    return _describe(lib().quant_matmul_describe, "quant_matmul_describe", M, N, K, None, K if a_stride is None else a_stride,
+                     None, K if w_stride is None else w_stride, _CODE[out_dtype])
+
+
 def matmul_i8(a, a_scale, w, w_scale, bias=None, residual=None, relu: bool = False, out=None,
               out_dtype=torch.bfloat16, ws=None, stream=None):
     """act(a_scale[m] * w_scale[n] * (a w^T)[m][n] + bias[n] + residual[m][n]) of a int8 [M][K] and w int8 [N][K];
@@ -353,6 +369,14 @@ def attention_workspace_bytes(cache: KV4Cache, seqs: int, heads: int, max_new: i
     if n < 0:
         _check(int(n), "quant_attention_workspace_bytes")
     return int(n)
+
+
+def attention_describe(cache: KV4Cache, seqs: int, heads: int, max_new: int, max_len: int, causal: bool = True,
+                       window: int = 0):
+    """(kernel names, launch count) of attention_kv4 with these bounds."""
+    _int32(seqs=seqs, heads=heads, max_new=max_new, max_len=max_len, window=window)
+    return _describe(lib().quant_attention_describe, "quant_attention_describe", _cache(cache)._desc, seqs, heads, max_new,
+                     max_len, causal, window)
 
 
 def attention_kv4(q, cache: KV4Cache, table, lens, starts=None, max_new: Optional[int] = None,

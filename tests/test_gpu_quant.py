@@ -254,6 +254,64 @@ def test_matmul_scales_that_are_not_finite_stay_in_their_row_or_column():
         assert torch.equal(y[rest], (a.float() @ w.float().t()).clamp_min(0)[rest])
 
 
+# A tile of the product's kernel, and shapes that the rule sends to it: one row and channel past a whole number of tiles, or one
+# short of it (or one of each).
+TILES = [("16, 16, 1, 1, 4, 4", (17, 33), (31, 47)), ("16, 32, 1, 2, 4, 3", (1, 8193), (911, 129)),
+         ("32, 64, 1, 4, 4, 3", (33, 5441), (927, 257)), ("64, 32, 2, 2, 4, 3", (897, 513), (831, 577)),
+         ("64, 64, 2, 2, 2, 4", (65, 5441), (383, 1345)), ("128, 64, 4, 2, 2, 3", (129, 6529), (767, 1345)),
+         ("128, 128, 2, 4, 1, 3", (129, 10881), (767, 2689)), ("128, 128, 2, 2, 1, 2", (257, 13057), (383, 10881)),
+         ("256, 256, 4, 2, 1, 2", (769, 14081), (1279, 9983))]
+TILE_IDS = [t[0].replace(", ", "x") for t in TILES]
+
+
+def runs_on(tile, M, N, K, dtype):
+    name = quant.matmul_describe(M, N, K, dtype)[0].split(" + ")[-1]
+    return name == f"matmul_i8_tile_kernel<{'float' if dtype == F32 else 'unsigned short'}, {tile}>"
+
+
+@pytest.mark.parametrize("K", [16, 333, 2064])
+@pytest.mark.parametrize("tile,over,under", TILES, ids=TILE_IDS)
+def test_matmul_of_every_tile(tile, over, under, K):
+    """K: shorter than a step of any group, copied to aligned rows, and several rounds of the stages with a rest."""
+    for (M, N), dtype in ((over, BF16), (under, F32), (over, F32), (under, BF16)):
+        assert runs_on(tile, M, N, K, dtype)
+        check_matmul(M, N, K, dtype, bias=dtype == F32, res=dtype == BF16, relu=K == 333)
+
+
+@pytest.mark.parametrize("tile,over,under", TILES, ids=TILE_IDS)
+def test_matmul_of_every_tile_strided_and_in_place(tile, over, under):
+    for (M, N), dtype in ((over, F32), (under, BF16)):
+        g = gen(M + N)
+        K = 272
+        assert runs_on(tile, M, N, K, dtype)
+        a, w = i8(g, M, K + 48), i8(g, N, K + 16)
+        r = torch.randn(M, N + 5, generator=g).to(dtype)
+        sa, sw = torch.rand(M, generator=g), torch.rand(N, generator=g)
+        out = r.cuda()
+        y = quant.matmul_i8(a.cuda()[:, 32:32 + K], sa.cuda(), w.cuda()[:, :K], sw.cuda(), residual=out[:, 2:2 + N],
+                            out=out[:, 2:2 + N])
+        want, tol = ref.matmul_i8(a[:, 32:32 + K], sa, w[:, :K], sw, None, r[:, 2:2 + N], False, dtype == BF16)
+        assert ((y.cpu().double() - want).abs() <= tol).all()
+        assert torch.equal(out[:, :2].cpu(), r[:, :2]) and torch.equal(out[:, 2 + N:].cpu(), r[:, 2 + N:])
+
+
+@pytest.mark.parametrize("K", [131071, 131056])
+@pytest.mark.parametrize("tile,over,under", TILES, ids=TILE_IDS)
+def test_matmul_of_every_tile_largest_sums(tile, over, under, K):
+    """Sums up to 128 * 128 * K, exact: a row of a is one number, of w two, so that each sum is known."""
+    M, N = over
+    assert runs_on(tile, M, N, K, F32)
+    am = torch.where(torch.arange(M) % 2 == 0, -128, 127)
+    wn = (torch.arange(N) % 256) - 128
+    third = torch.arange(K, device="cuda") % 3 == 0
+    a = am.to(torch.int8).cuda()[:, None].expand(M, K).contiguous()
+    w = torch.where(third, torch.ones((), dtype=torch.int8, device="cuda"), wn.to(torch.int8).cuda()[:, None])
+    y = quant.matmul_i8(a, torch.ones(M, device="cuda"), w, torch.ones(N, device="cuda"), out_dtype=F32)
+    ones = int(third.sum())
+    want = am[:, None] * (ones + (K - ones) * wn)
+    assert torch.equal(y.cpu(), want.double().float())     # rounded once, as the kernel's conversion does
+
+
 def test_matmul_no_rows():
     y = quant.matmul_i8(torch.empty(0, 16, dtype=torch.int8, device="cuda"), torch.empty(0, device="cuda"),
                         torch.zeros(8, 16, dtype=torch.int8, device="cuda"), torch.ones(8, device="cuda"))
@@ -523,6 +581,35 @@ def test_attention_strided_rows(news):
     out = hold[:, 33:33 + 512].unflatten(1, (4, 128))
     s.check(s.run(q=q, out=out))
     assert (hold[:, :33] == 7).all() and (hold[:, 33 + 512:] == 7).all()
+
+
+# Rows of a key head as tokens x heads of its group, and the kernel that they reach.
+FEW = [(32, 1, 1, 1), (32, 17, 1, 2), (32, 8, 4, 2), (32, 33, 1, 4), (32, 16, 4, 4), (64, 5, 3, 1), (64, 17, 1, 2), (64, 10, 3, 2),
+       (64, 11, 3, 4), (64, 64, 1, 4), (96, 4, 4, 1), (96, 17, 1, 2), (96, 8, 4, 2), (128, 2, 8, 1), (128, 6, 3, 2), (128, 32, 1, 2),
+       (192, 16, 1, 1), (256, 4, 4, 1)]
+MANY = [(32, 65, 1, "wide"), (64, 13, 5, "wide"), (96, 33, 1, "steps"), (128, 11, 3, "steps"), (192, 17, 1, "wide"), (256, 3, 6, "wide")]
+
+
+@pytest.mark.parametrize("d,new,group,nb", FEW + MANY)
+def test_attention_of_every_kernel(d, new, group, nb):
+    """Lengths past one split, ragged, with a window that leaves one split and one that leaves several."""
+    kv = 2
+    s = Setup([900, 437, 391], [new, new - new // 3, new], kv * group, kv, d, 40)
+    kernel = f"attend_kv4_{nb}_kernel<{d}>" if isinstance(nb, str) else f"attend_kv4_kernel<{d}, {nb}>"
+
+    def runs_on(max_len, joined, **k):
+        name, n = quant.attention_describe(s.cache, 3, kv * group, new, max_len, **k)
+        joined = n == 2 if joined is None else joined
+        assert name == kernel + (f" + attend_join_kernel<{d}>" if joined else "") and n == 1 + joined
+    few = not isinstance(nb, str)
+    for k in (dict(), dict(causal=False), dict(window=700)):
+        runs_on(900, True if few else None, **k)            # few rows: several splits
+        s.check(s.run(**k), **k)
+        loose = dict(k, window=3500) if "window" in k else k
+        runs_on(4000, True, **loose)                        # a loose bound: splits for many rows as well, most of them empty
+        s.check(s.run(max_len=4000, **loose), **loose)
+    runs_on(900, False if few else None, window=29)
+    s.check(s.run(window=29), window=29)
 
 
 def test_attention_is_the_same_bits_again_and_on_another_stream():

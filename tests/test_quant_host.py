@@ -174,6 +174,41 @@ def test_matmul_workspace_of_rows_far_apart(L, monkeypatch):
         assert (given[-1] >= w(4, 8, 16, a.data_ptr(), sa, b.data_ptr(), sw)) and (given[-1] > 0) == (max(sa, sw) >= far)
 
 
+def test_described_kernels(L):
+    """Every kernel of the product and of attention is reached by some shape, under the name of its source."""
+    from paper_1907_02154_amd import traffic
+    seen = set()
+    for M, N in ((1, 16), (1, 8193), (33, 5441), (897, 513), (65, 5441), (129, 6529), (129, 10881), (257, 13057), (769, 14081)):
+        for dtype in (torch.float32, torch.bfloat16):
+            name, n = quant.matmul_describe(M, N, 64, dtype)
+            assert n == 1 and " + " not in name
+            assert quant.matmul_describe(M, N, 63, dtype) == ("matmul_i8_align_kernel + " + name, 2)
+            assert quant.matmul_describe(M, N, 64, dtype, w_stride=72) == ("matmul_i8_align_kernel + " + name, 2)
+            seen.add(name)
+    assert len(seen) == 18
+    buf, n = ctypes.create_string_buffer(256), ctypes.c_int()
+    for d in quant.HEAD_DIMS:
+        for rows in (1, 16, 17, 32, 33, 64, 65, 5000):
+            for max_len in (100, 100000):
+                rc = L.quant_attention_describe(cache(pages=9999, head_dim=d), 1, 2, rows, max_len, 1, 0, buf, 256, ctypes.byref(n))
+                names = buf.value.decode().split(" + ")
+                assert rc == miconv.OK and n.value == len(names) == 1 + (
+                    L.quant_attention_workspace_bytes(cache(pages=9999, head_dim=d), 1, 2, rows, max_len, 1, 0) > 0)
+                seen |= set(names)
+    assert len(seen) == 18 + 6 + 4 + 2 + 6 + 6          # few rows by 1, 2 and 4 blocks; many; the joins
+    assert all(k.split("<")[0] in traffic.SOURCES for k in seen)
+    assert quant.matmul_describe(0, 8, 16) == ("", 0)
+    d = lambda *a, dt=0, b=buf, k=256, p=ctypes.byref(n): L.quant_matmul_describe(*a, None, a[2], None, a[2], dt, b, k, p)  # noqa: E731
+    assert d(4, 8, 0) == miconv.ERR_SHAPE and d(4, 8, 16, dt=2) == miconv.ERR_UNSUPPORTED and d(4, 8, 131072) == miconv.ERR_TOO_LARGE
+    assert d(4, 8, 16, b=None) == d(4, 8, 16, k=0) == d(4, 8, 16, p=None) == miconv.ERR_NULL
+    short = ctypes.create_string_buffer(b"x" * 12, 12)
+    assert d(4, 8, 16, b=short, k=8) == miconv.OK and short.raw == b"matmul_\0xxxx"
+    f = lambda c, *a, b=buf, k=256, p=ctypes.byref(n): L.quant_attention_describe(c, *a, b, k, p)  # noqa: E731
+    assert f(None, 1, 2, 1, 8, 1, 0) == f(cache(), 1, 2, 1, 8, 1, 0, b=None) == f(cache(), 1, 2, 1, 8, 1, 0, p=None) == miconv.ERR_NULL
+    assert f(cache(), 1, 3, 1, 8, 1, 0) == miconv.ERR_SHAPE and f(cache(head_dim=48), 1, 2, 1, 8, 1, 0) == miconv.ERR_UNSUPPORTED
+    assert f(cache(), 0, 2, 1, 8, 1, 0) == miconv.OK and buf.value == b"" and n.value == 0
+
+
 @pytest.mark.parametrize("scale", [NAN, float("inf"), -float("inf"), 3e38, -3e38])
 def test_attention_refuses_scales_that_are_not_finite(L, scale):
     assert L.quant_attention_kv4(cache(), 2, 4, 2, FAKE, 256, None, FAKE, FAKE, 3, 1, 48, scale, 1, 0, FAKE, 256, None, 0,
