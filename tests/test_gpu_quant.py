@@ -697,6 +697,22 @@ def test_attention_lengths_past_the_bound(lens, news, heads, d, page, k):
         assert ((out.cpu().double() - want).abs() <= tol).all()
 
 
+def test_streams_given_by_their_handles():
+    """A stream as torch's object, as its handle, and the default stream as 0: outputs and workspaces made for it."""
+    g = gen(12)
+    x = torch.randn(40, 333, generator=g).to(BF16).cuda()
+    s = Setup([2500, 900], [1, 1], 16, 4, 128, 64)
+    q, scale = quant.rows_i8(x)
+    y, a = quant.matmul_i8(q, scale, q, scale), s.run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream, 0, torch.cuda.default_stream()):
+        got = quant.rows_i8(x, stream=stream)
+        again = [got[0], quant.matmul_i8(*got, *got, stream=stream), s.run(stream=stream)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(m, n) for m, n in zip(again, (q, y, a)))
+
+
 # ------------------------------------------------------------------ refusals through the binding
 
 def test_binding_refusals():
