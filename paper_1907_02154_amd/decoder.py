@@ -45,7 +45,8 @@ class State:
             raise ValueError("a state holds one sequence of one token at least, in pages of one at least")
         pages = -(-max_len // page_size)
         g = torch.Generator().manual_seed(seed)      # pages in no order, as a server that reuses them has them
-        self.table = torch.randperm(seqs * pages, generator=g).reshape(seqs, pages).to(torch.int32).cuda()
+        table = torch.randperm(seqs * pages, generator=g).reshape(seqs, pages).to(torch.int32)
+        self.table, self.slot = table.cuda(), self.slots_of(table, max_len, page_size).cuda()
         self.caches = [quant.KV4Cache.allocate(seqs * pages, dec.kv_heads, page_size, dec.head_dim) for _ in dec.blocks]
         self.lens = torch.zeros(seqs, dtype=torch.int32, device="cuda")
         self.held = [0] * seqs
@@ -61,11 +62,16 @@ class State:
             raise ValueError(f"sequence {s} holds {self.held[s]} tokens of {self.max_len} at most: no room for {news[s]} more")
         self.held = after
 
+    @staticmethod
+    def slots_of(table: torch.Tensor, max_len: int, page_size: int) -> torch.Tensor:
+        """The slot of every place of each sequence, and -1, which is not written, behind the last one."""
+        place = torch.arange(max_len)
+        slot = table.long()[:, place // page_size] * page_size + place % page_size
+        return torch.nn.functional.pad(slot, (0, 1), value=-1).to(torch.int32)
+
     def slots(self, seq: torch.Tensor, place: torch.Tensor) -> torch.Tensor:
-        """Cache slots of the tokens at `place` of sequences `seq`; -1, which is not written, past max_len."""
-        page = self.table[seq, torch.div(place.clamp(max=self.max_len - 1), self.page_size, rounding_mode="floor")]
-        slot = page * self.page_size + place % self.page_size
-        return torch.where(place < self.max_len, slot, -1).to(torch.int32)
+        """Cache slots of the tokens at `place` of sequences `seq`; -1 past max_len."""
+        return self.slot[seq, place.clamp(max=self.max_len)]
 
 
 class Block:

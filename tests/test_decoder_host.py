@@ -52,7 +52,8 @@ def test_states_that_hold_nothing(seqs, max_len, page):
 
 def test_slots_past_the_capacity_are_none():
     _, state = made([0, 0], 10)
-    state.table = torch.tensor([[5, 0, 3], [1, 2, 4]], dtype=torch.int32)
+    state.slot = state.slots_of(torch.tensor([[5, 0, 3], [1, 2, 4]], dtype=torch.int32), state.max_len, state.page_size)
+    assert state.slot.dtype == torch.int32
     seq = torch.tensor([0, 0, 0, 1, 1, 1, 1])
     place = torch.tensor([0, 9, 10, 4, 11, 12, 1000])
     assert state.slots(seq, place).tolist() == [20, 13, -1, 8, -1, -1, -1]
