@@ -128,26 +128,27 @@ int quant_kv4_read(const quant_kv4 *cache, long tokens, const int32_t *slots, in
  * queries at rows starts[s] .. starts[s + 1] of q (starts NULL: row s alone);
  * query i of n stands at place p = lens[s] - n + i.  It sees the places
  * 0 .. p (0 .. lens[s] - 1 unless causal), of these with window > 0 only those
- * above p - window.  lens[s] may pass what can be seen (max_len and the table's
- * end, below): the queries keep their places.  For each of the `heads` query heads, head j reading key
- * head j / (heads / cache->heads):
+ * above p - window.  max_new and max_len bound the queries and the places of any
+ * sequence: rows past max_new are not computed, and places past max_len (or the
+ * table's end) are not seen; where lens[s] passes these, the queries keep their
+ * places.  For each of the `heads` query heads, head j reading key head
+ * j / (heads / cache->heads):
  *   out = softmax(scale * q k^T over the places seen) v
  * zeros where none is seen, NaN where a key or value that is seen is not
  * finite; what is not seen never reaches the result.
  * q, out: bf16 [tokens][heads][head_dim], rows q_stride / out_stride elements
- * apart.  max_new and max_len bound the queries and the length of any
- * sequence: rows past max_new are not computed, places past max_len (or the
- * table's end) are not seen.  Scores, softmax statistics and sums are fp32.
- * For the matrix cores the probabilities are rounded to bf16, and the sum they
- * are divided by is that of the rounded ones; where a key head has few query
- * rows (64, 32 or 16 of head_dim 64, 128 or more) they keep a second bf16
- * part, 16 bits in all.
+ * apart.  Scores, softmax statistics and sums are fp32: queries are finite and
+ * scores within fp32's range, values below 2^90 (the sums hold up to 2^8 times a
+ * value for each place).  For the matrix cores the probabilities are rounded to
+ * bf16, and the sum they are divided by is that of the rounded ones; where a key
+ * head has few query rows (64, 32 or 16 of head_dim 64, 128 or more) they keep a
+ * second bf16 part, 16 bits in all.
  * Errors: MICONV_ERR_NULL, MICONV_ERR_SHAPE (heads no multiple of the cache's,
  * a stride below its row, max_new or max_len < 1, table_stride < 1, a scale that
- * is not finite, also times log2(e)), MICONV_ERR_UNSUPPORTED (head_dim), MICONV_ERR_ALIGN, MICONV_ERR_TOO_LARGE
- * (2^31 slots, 2^31 rows of heads in a page, a max_len of 2^30, 2^16 sequences or
- * heads, 2^24 query rows of a key head, or so much work that a grid does not hold
- * it), MICONV_ERR_WORKSPACE. */
+ * is not finite, also times log2(e)), MICONV_ERR_UNSUPPORTED (head_dim),
+ * MICONV_ERR_ALIGN, MICONV_ERR_TOO_LARGE (2^31 slots, 2^31 rows of heads in a
+ * page, a max_len of 2^30, 2^16 sequences or heads, 2^24 query rows of a key
+ * head, or so much work that a grid does not hold it), MICONV_ERR_WORKSPACE. */
 long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len,
                                      int causal, int window);
 int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, long tokens, const void *q, long q_stride,

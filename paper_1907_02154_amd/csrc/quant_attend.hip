@@ -126,7 +126,13 @@ __device__ __forceinline__ bf16x8 query8(const AttArgs &a, const uint16_t *q)
     return __builtin_bit_cast(bf16x8, v);
 }
 
-// Two probabilities 2^(s c - base) as bf16, added to l as rounded.
+// Two probabilities 2^(s c - base) as bf16, the matrix cores' operand, added to l
+// as rounded: what a rounding adds above and below the line is the same, so that
+// only the difference of a value from the row's result counts.  Against 64 bits
+// the results of two prompts of 4096 tokens are off by 0.0021 of their size (root
+// mean square), where probabilities in fp32 and the result's own rounding to bf16
+// make 0.0016.  A second part, as few rows have it below, would add half as many
+// products again, and these are a good part of what binds.
 __device__ __forceinline__ uint32_t weights2(float s0, float s1, float c, float base, float &l)
 {
     const uint32_t w = pack_bf16x2(__builtin_amdgcn_exp2f(__builtin_fmaf(s0, c, -base)),
@@ -587,18 +593,23 @@ __device__ __forceinline__ bool wide_place(const AttArgs &a, Seq *sq, int *s, in
 // The wavefronts' barrier; loads of later tiles stay in flight across it.
 __device__ __forceinline__ void wide_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// Many rows, for heads that leave the registers of a SIMD to four wavefronts (up
-// to 64 channels), where these overlap one another, and for heads whose sums
-// fill those of two (192 and more).  The first four wavefronts move the keys and
-// the others the values: the next tile is widened first, over the tile before,
-// then this one worked on, and one barrier a tile keeps the wavefronts together.
+// Many rows, for heads of up to 64 channels, whose registers leave a SIMD four
+// wavefronts, and of 192 and more, whose sums fill those of two (at 256 channels
+// 256 registers, and 19 more in scratch).  The first four wavefronts move the
+// keys and the others the values: the next tile is widened first, over the tile
+// before, then this one worked on, and one barrier a tile keeps the wavefronts
+// together.
 //
-// Bound by the probabilities' exponentials at few channels, at many by LDS
-// reads and products, which a barrier keeps in phase.  Two prompts of 4096
-// tokens, causal, 32 heads on 8 key heads: of 32 channels 133 us, of 64 173 (755
-// TFLOP/s); 20 heads of 192 on 5, 283 us (870), 16 of 256 on 4, 294 (890).  With
-// four wavefronts in place of eight, and registers for all they hold, the last
-// two took 460 and 482: one wavefront a SIMD has nothing to overlap.
+// Two prompts of 4096 tokens, causal, 32 heads on 8 key heads: of 32 channels 133
+// us, of 64 173 (755 TFLOP/s); 20 heads of 192 on 5, 283 us (870), 16 of 256 on
+// 4, 294 (890).  Bound at few channels by vector instructions and products that
+// take turns, for the barrier keeps a SIMD's wavefronts in much the same phase: of
+// a SIMD's cycles the ones take 56% at 64 channels and the others 34%, 68 and 21%
+// at 32.  Of the vector work the exponentials are less than a third.  At 256
+// channels they take 24 and 37%; LDS is busy for 46% of the cycles, half of them
+// bank conflicts, and the wavefronts wait for it and for one another.  With
+// four wavefronts in place of eight, and registers for all they hold, the wide
+// heads took 460 and 482 us: one wavefront a SIMD has nothing to overlap.
 template <int D>
 __global__ __launch_bounds__(512, 2) void attend_kv4_wide_kernel(AttArgs a)
 {
@@ -916,7 +927,10 @@ AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len,
     if (causal && window > 0) len = std::min(len, (long)window + block / group + 1 + 64);
     // The places are split, at most until work-groups fill the card once, three on
     // a compute unit (one, with many rows): 16 sequences of up to 32768 places, 8 key
-    // heads of 128, take 94 us so, 109 with four and 101 with six or eight.
+    // heads of 128, take 94 us so, 109 with four and 101 with six or eight.  Three is
+    // what the registers allow there (<128, 1>), and at <64, 2> and <32, 4>; <64, 4>,
+    // <96, 2>, <128, 2>, <192, 1> and <256, 1> allow two, the others four and more:
+    // the fill was not measured on these.
     const long groups = (long)seqs * c.heads * p.row_blocks, fill = ((p.wide ? 1L : 3L) * cu_count() + groups - 1) / groups;
     long want = 1;
     if (p.wide) {

@@ -9,7 +9,7 @@
 //
 // Bound by memory: a row is read once, kept in registers across the one
 // reduction (sum and maximum together), and written once: 16384 rows of 4096 in
-// bf16 with the residual, 470 MB, take 96 us, 4.9 TB/s (a large copy: 5.2).  A
+// bf16 with the residual, 470 MB, take 97 us, 4.8 TB/s (a large copy: 5.2).  A
 // wavefront takes a row of up to 1024, so that short rows need no barrier; a
 // work-group a longer one.
 #include "quant.h"
