@@ -9,7 +9,7 @@ tokens, as e4m3 values in blocks that share a power of two (a byte, exponent plu
   attend   attention of queries over that cache: single tokens, chunks of a prompt, whole prompts
   sample   a token drawn from each row of logits: temperature, top-k, top-p, min-p, a given random number
 
-A block's exponent is the smallest e with max|x| <= 448 * 2^e, held to -117 .. 120.  A cache is
+A block's exponent is the smallest e with max|x| <= 448 * 2^e, held to -117 .. 119.  A cache is
 values [pages][heads][page size][head size] and exponents [pages][heads][page size / block], for
 keys and for values: a block is `block` places of a page and a head.  Tokens that are added to a
 block raise its exponent where they need it, and the values it holds are rounded again.
@@ -133,15 +133,15 @@ def draw(rng):
 # ------------------------------------------------------------------ the inputs
 
 def _exponent(top):
-    """The smallest e in -117 .. 120 with top <= 448 * 2^e."""
+    """The smallest e in -117 .. 119 with top <= 448 * 2^e."""
     m, x = torch.frexp(top)
-    e = torch.where(m > 0.875, x - 8, x - 9).clamp(-117, 120)
+    e = torch.where(m > 0.875, x - 8, x - 9).clamp(-117, 119)
     return torch.where(top == 0, torch.full_like(e, -117), e)
 
 
 def _encode(x, e):
     """x fp32 as e4m3 values of the power e (int32, broadcast): the nearest, ties to even."""
-    return torch.ldexp(x, -e).to(F8)
+    return torch.ldexp(x, -e).clamp(-448, 448).to(F8)
 
 
 def _decode(codes, byte):
@@ -441,7 +441,7 @@ def work(case):
 
 def _power64(top):
     """2^e of a block by its largest magnitude, in 64 bits."""
-    return torch.exp2(torch.ceil(torch.log2(top.double().clamp_min(2.0 ** -130) / 448.0)).clamp(-117, 120))
+    return torch.exp2(torch.ceil(torch.log2(top.double().clamp_min(2.0 ** -130) / 448.0)).clamp(-117, 119))
 
 
 def _near64(x, power):
