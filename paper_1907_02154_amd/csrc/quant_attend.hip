@@ -1,4 +1,5 @@
-// Attention over the paged 4-bit cache (quant_attention_kv4).
+// Attention over the paged caches of 4 and of 8 bits (quant_attention_kv4,
+// quant_attention_kv8).
 //
 // Scores are computed transposed, S^T = K Q^T: the cached tokens are the rows
 // of the matrix instruction and the queries its columns, so each lane holds
@@ -33,7 +34,7 @@ constexpr float kNegInf = -__builtin_inff();
 constexpr float kGrow = 8.0f;   // log2 of how far scores may pass the running maximum before it moves
 
 struct AttArgs {
-    Kv4 c;
+    KvView c;
     const uint16_t *q;
     uint16_t *out;
     const int32_t *starts, *lens, *table;
@@ -83,19 +84,67 @@ __device__ __forceinline__ void seen(const AttArgs &a, const Seq &q, int i, int 
     *hi = h < 0 ? 0 : h;
 }
 
-// Scale bits of an exponent byte; above 252 an infinite scale, which converts to NaN.
-__device__ __forceinline__ float exp_scale(uint32_t e)
-{
-    return __builtin_bit_cast(float, (e > kMaxExp ? 255u : e) << 23);
-}
+// What the kernels know of a cache's format: 32-bit words that hold 8 channels,
+// whether a token's 32 channels have an exponent of their own, and the way to
+// bf16, which holds every value of either format.
 
-__device__ __forceinline__ bf16x8 widen8(uint32_t code, float s)
+// Four bits a value, an exponent for each 32 channels of a token.
+struct Fp4 {
+    static constexpr int WORDS = 1;
+    static constexpr bool GROUPS = true;
+    // Scale bits of an exponent byte; above 252 an infinite scale, which converts to NaN.
+    static __device__ __forceinline__ float scale(uint32_t e)
+    {
+        return __builtin_bit_cast(float, (e > kMaxExp ? 255u : e) << 23);
+    }
+    // Of keys and of values, by the exponents of both.  A value that is not finite makes the token's score NaN, which
+    // reaches the queries that see it; its own NaN times a probability of 0 would reach the others too.
+    static __device__ __forceinline__ float keys(uint32_t ke, uint32_t ve) { return scale(ve > kMaxExp ? 255u : ke); }
+    static __device__ __forceinline__ float values(uint32_t ve) { return scale(ve > kMaxExp ? 127u : ve); }
+    static __device__ __forceinline__ bf16x8 widen8(const uint32_t *w, float s)
+    {
+        const uint32_t code = *w;
+        u32x4 r = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3))};
+        return __builtin_bit_cast(bf16x8, r);
+    }
+    static __device__ __forceinline__ void clean(uint32_t &) {}
+};
+
+// Eight bits a value, an exponent for a block of tokens.  Keys that are not
+// numbers make the token's score NaN, which reaches the queries that see it.
+// Values are written as numbers alone; a place that no one sees may hold
+// anything, and its values must not bring a NaN to a product with a probability
+// of 0: where a tile holds such places codes that are no numbers become 448, and
+// exponents stay where the format has them.
+struct Fp8 {
+    static constexpr int WORDS = 2;
+    static constexpr bool GROUPS = false;
+    static __device__ __forceinline__ float keys(uint32_t ke, uint32_t) { return __builtin_bit_cast(float, ke << 23); }
+    static __device__ __forceinline__ float values(uint32_t ve)
+    {
+        return __builtin_bit_cast(float, (ve > (uint32_t)kF8Hi ? (uint32_t)kF8Hi : ve) << 23);
+    }
+    static __device__ __forceinline__ bf16x8 widen8(const uint32_t *w, float s)
+    {
+        u32x4 r = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], s, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], s, true)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], s, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], s, true))};
+        return __builtin_bit_cast(bf16x8, r);
+    }
+    static __device__ __forceinline__ void clean(uint32_t &w)   // 0x7F and 0xFF become 0x7E and 0xFE
+    {
+        w ^= (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;
+    }
+};
+
+// The exponent of a token's keys or values among those of its page and head.
+__device__ __forceinline__ uint64_t exponent_of(const KvView &c, unsigned page, int head, int place)
 {
-    u32x4 r = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 0)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 1)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 2)),
-               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, s, 3))};
-    return __builtin_bit_cast(bf16x8, r);
+    return ((uint64_t)page * (unsigned)c.heads + (unsigned)head) * (unsigned)c.blocks + fdiv((unsigned)place, c.dv_block);
 }
 
 // N words from p on, which is aligned to the widest access that divides them.
@@ -150,8 +199,8 @@ __device__ __forceinline__ uint32_t weights2(float s0, float s1, float c, float 
 // and the last tiles take the rest.  Short calls are latencies in a row: one
 // token over 100 places 4.3 us, 17 tokens each with a window of 1000, 12 us with
 // the join.
-template <int D, int NB>
-__global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
+template <class F, int D, int NB>
+__device__ __forceinline__ void attend_few(const AttArgs &a)
 {
     constexpr int NU = D / 32;           // units of 8 channels a lane holds of a cached row
     constexpr int CB = D / 16;           // blocks of 16 channels
@@ -206,11 +255,12 @@ __global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
     const int last_page = (int)(a.c.slots / a.c.page_size) - 1;
     const int page_rows = a.c.heads * a.c.page_size, head_row = kvh * a.c.page_size;
     unsigned char *vt = lds + wave * VBYTES;
-    // What a lane holds of a tile: of token 16 k + col the units quad * NU .. + NU - 1 and the exponents of their groups.
-    constexpr int NE = D == 96 || D > 128 ? 2 : 1;
+    // What a lane holds of a tile: of token 16 k + col the units quad * NU .. + NU - 1 and the exponents of their groups,
+    // or the token's.
+    constexpr int W = F::WORDS, NE = F::GROUPS && (D == 96 || D > 128) ? 2 : 1;
     const int g0 = quad * NU / 4, g1 = min(g0 + 1, D / 32 - 1);
     struct Held {
-        uint32_t kc[2][NU], vc[2][NU], ke[2][NE], ve[2][NE];
+        uint32_t kc[2][NU * W], vc[2][NU * W], ke[2][NE], ve[2][NE];
     };
     int page[2], place[2];
     const auto look = [&](int t0) {   // the pages of a tile's tokens
@@ -228,49 +278,50 @@ __global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
         for (int k = 0; k < 2; ++k) {
             const unsigned pg = (unsigned)min(max(page[k], 0), last_page);
             const uint64_t row = (uint64_t)pg * (unsigned)page_rows + (unsigned)(head_row + place[k]);
-            load_words<NU>(a.c.kc + row * (D / 2) + quad * (D / 8), to.kc[k]);
-            load_words<NU>(a.c.vc + row * (D / 2) + quad * (D / 8), to.vc[k]);
-            to.ke[k][0] = a.c.ke[row * (D / 32) + g0];
-            to.ve[k][0] = a.c.ve[row * (D / 32) + g0];
+            load_words<NU * W>(a.c.kc + row * (D / 2 * W) + quad * (D / 8 * W), to.kc[k]);
+            load_words<NU * W>(a.c.vc + row * (D / 2 * W) + quad * (D / 8 * W), to.vc[k]);
+            const uint64_t e = F::GROUPS ? row * (D / 32) + g0 : exponent_of(a.c, pg, kvh, place[k]);
+            to.ke[k][0] = a.c.ke[e];
+            to.ve[k][0] = a.c.ve[e];
             if constexpr (NE == 2) {
                 to.ke[k][1] = a.c.ke[row * (D / 32) + g1];
                 to.ve[k][1] = a.c.ve[row * (D / 32) + g1];
             }
         }
     };
-    const auto tile = [&](const Held &cur, Held &next, int t0) {
+    const auto tile = [&](Held &cur, Held &next, int t0) {
         if (t0 + 128 < hi) {
             fetch(next);
             if (t0 + 256 < hi) look(t0 + 256);
         }
         f32x4 sc[2][NB];
+        const bool edge = t0 < from || t0 + 32 > all;   // holds places that not every row sees
+        if constexpr (!F::GROUPS)
+            if (edge)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int u = 0; u < NU * W; ++u) F::clean(cur.vc[k][u]);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             float ks[NE], vs[NE];
 #pragma unroll
-            for (int e = 0; e < NE; ++e) {
-                // A value that is not finite makes the token's score NaN, which reaches
-                // the queries that see it; its own NaN times a probability of 0 would
-                // reach the others too.
-                const bool bad = cur.ve[k][e] > kMaxExp;
-                ks[e] = exp_scale(bad ? 255u : cur.ke[k][e]);
-                vs[e] = exp_scale(bad ? 127u : cur.ve[k][e]);
-            }
+            for (int e = 0; e < NE; ++e) ks[e] = F::keys(cur.ke[k][e], cur.ve[k][e]), vs[e] = F::values(cur.ve[k][e]);
 #pragma unroll
             for (int b = 0; b < NB; ++b) sc[k][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
                 const int e = NE == 1 ? 0 : (quad * NU + u) / 4 - g0;
-                const bf16x8 kf = widen8(cur.kc[k][u], e == 0 ? ks[0] : ks[NE - 1]);
+                const bf16x8 kf = F::widen8(cur.kc[k] + W * u, e == 0 ? ks[0] : ks[NE - 1]);
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
                     sc[k][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[b][u], sc[k][b], 0, 0, 0);
                 *(bf16x8 *)(vt + (16 * k + col) * PITCH + quad * (D / 2) + 16 * u) =
-                    widen8(cur.vc[k][u], e == 0 ? vs[0] : vs[NE - 1]);
+                    F::widen8(cur.vc[k] + W * u, e == 0 ? vs[0] : vs[NE - 1]);
             }
         }
-        if (t0 < from || t0 + 32 > all) {
+        if (edge) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -391,6 +442,18 @@ __global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
             if (u == 0) part[D] = mm, part[D + 1] = ll;
         }
     }
+}
+
+template <int D, int NB>
+__global__ __launch_bounds__(256, 2) void attend_kv4_kernel(AttArgs a)
+{
+    attend_few<Fp4, D, NB>(a);
+}
+
+template <int D, int NB>
+__global__ __launch_bounds__(256, 2) void attend_kv8_kernel(AttArgs a)
+{
+    attend_few<Fp8, D, NB>(a);
 }
 
 // What the kernels for many rows share: eight wavefronts of 32 rows, tiles of 64
@@ -514,10 +577,11 @@ struct Wide {
 // Keys or values of a tile on their way from the cache to LDS, by NT threads:
 // groups of 32 channels by tokens.  Loads run a tile ahead of the conversion,
 // the page table's two.
-template <int D, int NT>
+template <class F, int D, int NT>
 struct Mover {
     static constexpr int PARTS = Wide<D>::PARTS, UNITS = Wide<D>::UNITS, PER = (UNITS + NT - 1) / NT;
-    u32x4 code[PER];
+    static constexpr int W = F::WORDS;
+    uint32_t code[PER][4 * W];
     uint32_t exp[PER], vexp[PER];
     int page[PER], place[PER];
 
@@ -540,16 +604,24 @@ struct Mover {
             const unsigned pg = (unsigned)min(max(page[i], 0), last_page);
             const uint64_t row = (uint64_t)pg * (unsigned)(a.c.heads * a.c.page_size) + (unsigned)(kvh * a.c.page_size + place[i]);
             const uint64_t at = row * PARTS + (unsigned)((i * NT + tid) % PARTS);
-            code[i] = *(const u32x4 *)((keys ? a.c.kc : a.c.vc) + at * 16);
-            exp[i] = (keys ? a.c.ke : a.c.ve)[at];
-            vexp[i] = a.c.ve[at];
+            load_words<4 * W>((keys ? a.c.kc : a.c.vc) + at * (16 * W), code[i]);
+            const uint64_t e = F::GROUPS ? at : exponent_of(a.c, pg, kvh, place[i]);
+            exp[i] = (keys ? a.c.ke : a.c.ve)[e];
+            if constexpr (F::GROUPS) vexp[i] = a.c.ve[e];
         }
     }
-    // A value that is not finite makes the token's score NaN, which reaches the queries that see it; its own NaN times
-    // a probability of 0 would reach the others too.
     __device__ __forceinline__ float scale(int i, bool keys) const
     {
-        return exp_scale(vexp[i] <= kMaxExp ? exp[i] : keys ? 255u : 127u);
+        if constexpr (F::GROUPS) return keys ? F::keys(exp[i], vexp[i]) : F::values(exp[i]);
+        else return keys ? F::keys(exp[i], 0) : F::values(exp[i]);
+    }
+    // For a tile with places that not every row of the block sees.
+    __device__ __forceinline__ void clean()
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int j = 0; j < 4 * W; ++j) F::clean(code[i][j]);
     }
     __device__ __forceinline__ void widen(unsigned char *to, int pitch, bool keys, int tid)
     {
@@ -560,18 +632,18 @@ struct Mover {
                 unsigned char *at = to + idx / PARTS * pitch + idx % PARTS * 64;
                 const float f = scale(i, keys);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) *(bf16x8 *)(at + 16 * j) = widen8(code[i][j], f);
+                for (int j = 0; j < 4; ++j) *(bf16x8 *)(at + 16 * j) = F::widen8(code[i] + W * j, f);
             }
         }
     }
 };
 
-// The places that any row of a block sees within a split.
-__device__ __forceinline__ void block_range(const AttArgs &a, const Seq &sq, int r0, int r_last, int split, int *lo, int *hi)
+// The places that any row of a block sees within a split, and those that every row does (from, all).
+__device__ __forceinline__ void block_range(const AttArgs &a, const Seq &sq, int r0, int r_last, int split, int *lo, int *hi,
+                                            int *from, int *all)
 {
-    int x;
-    seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), lo, &x);
-    seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), &x, hi);
+    seen(a, sq, (int)fdiv((unsigned)r0, a.dv_group), lo, all);
+    seen(a, sq, (int)fdiv((unsigned)r_last, a.dv_group), from, hi);
     *lo = (*lo & ~63) + split * a.per_split;   // per_split is a multiple of the tile
     *hi = *lo + min(*hi - *lo, a.per_split);
 }
@@ -610,8 +682,8 @@ __device__ __forceinline__ void wide_barrier() { asm volatile("s_waitcnt lgkmcnt
 // bank conflicts, and the wavefronts wait for it and for one another.  With
 // four wavefronts in place of eight, and registers for all they hold, the wide
 // heads took 460 and 482 us: one wavefront a SIMD has nothing to overlap.
-template <int D>
-__global__ __launch_bounds__(512, 2) void attend_kv4_wide_kernel(AttArgs a)
+template <class F, int D>
+__device__ __forceinline__ void attend_wide(const AttArgs &a)
 {
     typedef Wide<D> W;
     constexpr int TILE = W::TILE;
@@ -619,18 +691,20 @@ __global__ __launch_bounds__(512, 2) void attend_kv4_wide_kernel(AttArgs a)
     unsigned char *const keys = lds, *const vals = lds + 2 * W::KBYTES;
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
-    int s, kvh, split, r0, rows, lo, hi;
+    int s, kvh, split, r0, rows, lo, hi, from, all;
     Seq sq;
     if (!wide_place(a, &sq, &s, &kvh, &split, &r0, &rows)) return;
-    block_range(a, sq, r0, min(r0 + kWideRows, rows) - 1, split, &lo, &hi);
+    block_range(a, sq, r0, min(r0 + kWideRows, rows) - 1, split, &lo, &hi, &from, &all);
     const int tiles = hi > lo ? (hi - lo + TILE - 1) / TILE : 0;
 
     const int tid = threadIdx.x % 256;
     const bool mk = wave < 4;   // moves keys
     const int32_t *pages = a.table + (long)s * a.table_stride;
-    Mover<D, 256> mv;
+    Mover<F, D, 256> mv;
     const auto look = [&](int t) { mv.look(a, pages, tid, lo + t * TILE, lo, hi); };
     const auto widen = [&](int t) {
+        if constexpr (!F::GROUPS)
+            if (!mk && (lo + t * TILE < from || lo + (t + 1) * TILE > all)) mv.clean();
         if (mk) mv.widen(keys + (t & 1) * W::KBYTES, W::KP, true, tid);
         else mv.widen(vals + (t & 1) * W::VBYTES, W::VP, false, tid);
     };
@@ -694,6 +768,18 @@ __global__ __launch_bounds__(512, 2) void attend_kv4_wide_kernel(AttArgs a)
     w.finish(a, sq, s, split, half);
 }
 
+template <int D>
+__global__ __launch_bounds__(512, 2) void attend_kv4_wide_kernel(AttArgs a)
+{
+    attend_wide<Fp4, D>(a);
+}
+
+template <int D>
+__global__ __launch_bounds__(512, 2) void attend_kv8_wide_kernel(AttArgs a)
+{
+    attend_wide<Fp8, D>(a);
+}
+
 // Many rows, heads of 96 and 128 channels: two wavefronts on a SIMD, each of which
 // gives the matrix cores and the vector unit work side by side.  A step takes 32
 // cached tokens in two phases: the products of the NEXT step's scores beside
@@ -714,8 +800,8 @@ __global__ __launch_bounds__(512, 2) void attend_kv4_wide_kernel(AttArgs a)
 // phase that needs them; 64 rows a wavefront, one on a SIMD, half the LDS reads,
 // 286 (a lone wavefront's product takes 51 cycles in that loop); two groups of
 // wavefronts half a tile apart 313.  Heads of 64 take 191 so, 173 in the kernel above.
-template <int D>
-__global__ __launch_bounds__(512, 2) void attend_kv4_steps_kernel(AttArgs a)
+template <class F, int D>
+__device__ __forceinline__ void attend_steps(const AttArgs &a)
 {
     typedef Wide<D> W;
     constexpr int TILE = W::TILE;
@@ -724,16 +810,20 @@ __global__ __launch_bounds__(512, 2) void attend_kv4_steps_kernel(AttArgs a)
     unsigned char *const keys = lds, *const vals = lds + 2 * W::KBYTES;
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
-    int s, kvh, split, r0, rows, lo, hi;
+    int s, kvh, split, r0, rows, lo, hi, from, all;
     Seq sq;
     if (!wide_place(a, &sq, &s, &kvh, &split, &r0, &rows)) return;
-    block_range(a, sq, r0, min(r0 + kWideRows, rows) - 1, split, &lo, &hi);
+    block_range(a, sq, r0, min(r0 + kWideRows, rows) - 1, split, &lo, &hi, &from, &all);
     const int tiles = hi > lo ? (hi - lo + TILE - 1) / TILE : 0;
 
     const int tid = threadIdx.x % 256;
     const bool mk = wave < 4;   // moves keys
     const int32_t *pages = a.table + (long)s * a.table_stride;
-    Mover<D, 256> mv, first;
+    Mover<F, D, 256> mv, first;
+    const auto clean = [&](int t) {   // of values on their way to tile t
+        if constexpr (!F::GROUPS)
+            if (!mk && (lo + t * TILE < from || lo + (t + 1) * TILE > all)) mv.clean();
+    };
     const auto look = [&](int t) { mv.look(a, pages, tid, lo + t * TILE + (mk ? 32 : 0), lo, hi); };
     if (tiles > 0) {
         first.look(a, pages, tid, lo - 32, lo, hi);
@@ -754,6 +844,7 @@ __global__ __launch_bounds__(512, 2) void attend_kv4_steps_kernel(AttArgs a)
             first.widen(keys + W::KBYTES, W::KP, true, tid);
             mv.widen(keys, W::KP, true, tid);
         } else {
+            clean(0);
             mv.widen(vals, W::VP, false, tid);
         }
         if (tiles > 1) mv.fetch(a, mk, tid, kvh);
@@ -837,11 +928,12 @@ __global__ __launch_bounds__(512, 2) void attend_kv4_steps_kernel(AttArgs a)
         // The next tile goes where nothing is read since the barrier before; the last one's turn writes what no one reads.
         unsigned char *const to = put + (b ^ 1) * put_step;
         const float scale = mv.scale(0, mk);
+        clean(t + 1);
         step(even, odd, vt, 0, t0, [] {}, [&](int i) {
             kf[i] = W::key(kt, lane, 1, i);
             if (W::UNITS == 256 || tid < W::UNITS)
 #pragma unroll
-                for (int j = i * 4 / NQ; j < (i + 1) * 4 / NQ; ++j) *(bf16x8 *)(to + 16 * j) = widen8(mv.code[0][j], scale);
+                for (int j = i * 4 / NQ; j < (i + 1) * 4 / NQ; ++j) *(bf16x8 *)(to + 16 * j) = F::widen8(mv.code[0] + F::WORDS * j, scale);
         });
         if (t + 2 < tiles) mv.fetch(a, mk, tid, kvh);
         if (t + 3 < tiles) look(t + 3);
@@ -849,6 +941,18 @@ __global__ __launch_bounds__(512, 2) void attend_kv4_steps_kernel(AttArgs a)
         step(odd, even, vt, 1, t0 + 32, [] { wide_barrier(); }, [&](int i) { kf[i] = W::key(kn, lane, 0, i); });
     }
     w.finish(a, sq, s, split, half);
+}
+
+template <int D>
+__global__ __launch_bounds__(512, 2) void attend_kv4_steps_kernel(AttArgs a)
+{
+    attend_steps<Fp4, D>(a);
+}
+
+template <int D>
+__global__ __launch_bounds__(512, 2) void attend_kv8_steps_kernel(AttArgs a)
+{
+    attend_steps<Fp8, D>(a);
 }
 
 // Joins the splits of a row of a head: four wavefronts take turns at them, four
@@ -912,7 +1016,7 @@ struct AttPlan {
     size_t bytes;
 };
 
-AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len, int causal, int window)
+AttPlan plan_attend(const KvView &c, int seqs, int heads, int max_new, int max_len, int causal, int window)
 {
     AttPlan p;
     const long group = heads / c.heads, rows = (long)max_new * group;
@@ -953,9 +1057,13 @@ AttPlan plan_attend(const Kv4 &c, int seqs, int heads, int max_new, int max_len,
     return p;
 }
 
-int check_attend(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len, Kv4 *c)
+int view(const quant_kv4 *cache, KvView *c) { return kv4_view(cache, c); }
+int view(const quant_kv8 *cache, KvView *c) { return kv8_view(cache, c); }
+
+template <class C>
+int check_attend(const C *cache, int seqs, int heads, int max_new, int max_len, KvView *c)
 {
-    const int rc = kv4_view(cache, c);
+    const int rc = view(cache, c);
     if (rc != MICONV_OK) return rc;
     if (seqs < 0 || heads < 1 || heads % c->heads || max_new < 1 || max_len < 1) return MICONV_ERR_SHAPE;
     if ((long)max_new * (heads / c->heads) >= 1L << 24 || max_len >= 1 << 30 || seqs > 65535 || heads > 65535)
@@ -965,27 +1073,43 @@ int check_attend(const quant_kv4 *cache, int seqs, int heads, int max_new, int m
 }
 
 // Whether a grid, of fewer than 2^32 threads, holds the plan's.
-bool grid_holds(const AttPlan &p, const Kv4 &c, int seqs)
+bool grid_holds(const AttPlan &p, const KvView &c, int seqs)
 {
     return (double)p.row_blocks * p.splits * (p.wide ? 512.0 * c.heads * seqs : 256.0) < 0x1p32;
 }
 
-template <int D>
+template <class F, int D, int NB>
+constexpr auto few_kernel()
+{
+    if constexpr (F::GROUPS) return attend_kv4_kernel<D, NB>;
+    else return attend_kv8_kernel<D, NB>;
+}
+
+template <class F, int D>
+constexpr auto many_kernel()
+{
+    if constexpr (F::GROUPS) {
+        if constexpr (in_steps(D)) return attend_kv4_steps_kernel<D>;
+        else return attend_kv4_wide_kernel<D>;
+    } else {
+        if constexpr (in_steps(D)) return attend_kv8_steps_kernel<D>;
+        else return attend_kv8_wide_kernel<D>;
+    }
+}
+
+template <class F, int D>
 int launch_attend(const AttArgs &a, const AttPlan &p, hipStream_t st)
 {
     const dim3 grid((unsigned)((long)p.row_blocks * p.splits), (unsigned)a.c.heads, (unsigned)a.seqs);
     if (p.wide) {
         const dim3 all(grid.x * grid.y * grid.z);
-        void (*k)(AttArgs);
-        if constexpr (in_steps(D)) k = attend_kv4_steps_kernel<D>;
-        else k = attend_kv4_wide_kernel<D>;
-        launch_kernel(k, all, dim3(512), 0, st, a);
+        launch_kernel(many_kernel<F, D>(), all, dim3(512), 0, st, a);
     } else {
-        void (*k)(AttArgs) = attend_kv4_kernel<D, 1>;
+        void (*k)(AttArgs) = few_kernel<F, D, 1>();
         if constexpr (D <= 128)
-            if (p.nb == 2) k = attend_kv4_kernel<D, 2>;
+            if (p.nb == 2) k = few_kernel<F, D, 2>();
         if constexpr (D <= 64)
-            if (p.nb == 4) k = attend_kv4_kernel<D, 4>;
+            if (p.nb == 4) k = few_kernel<F, D, 4>();
         launch_kernel(k, grid, dim3(256), 0, st, a);
     }
     int rc = launched();
@@ -994,48 +1118,43 @@ int launch_attend(const AttArgs &a, const AttPlan &p, hipStream_t st)
     return launched();
 }
 
-}  // namespace
-}  // namespace quant
-}  // namespace miconv
-
-extern "C" long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len,
-                                                int causal, int window)
+template <class C>
+long attend_workspace(const C *cache, int seqs, int heads, int max_new, int max_len, int causal, int window)
 {
-    miconv::quant::Kv4 c;
-    const int rc = miconv::quant::check_attend(cache, seqs, heads, max_new, max_len, &c);
+    KvView c;
+    const int rc = check_attend(cache, seqs, heads, max_new, max_len, &c);
     if (rc != MICONV_OK) return rc;
-    return seqs ? (long)miconv::quant::plan_attend(c, seqs, heads, max_new, max_len, causal, window).bytes : 0;
+    return seqs ? (long)plan_attend(c, seqs, heads, max_new, max_len, causal, window).bytes : 0;
 }
 
-extern "C" int quant_attention_describe(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len, int causal,
-                                        int window, char *buf, int buflen, int *launches)
+template <class C>
+int attend_describe(const C *cache, int bits, int seqs, int heads, int max_new, int max_len, int causal, int window, char *buf,
+                    int buflen, int *launches)
 {
-    using namespace miconv::quant;
     if (!buf || buflen <= 0 || !launches) return MICONV_ERR_NULL;
     buf[0] = 0, *launches = 0;
-    Kv4 c;
+    KvView c;
     const int rc = check_attend(cache, seqs, heads, max_new, max_len, &c);
     if (rc != MICONV_OK) return rc;
     if (seqs == 0) return MICONV_OK;
     const AttPlan p = plan_attend(c, seqs, heads, max_new, max_len, causal, window);
     if (!grid_holds(p, c, seqs)) return MICONV_ERR_TOO_LARGE;
     char first[64], join[64] = "";
-    if (p.wide) snprintf(first, sizeof first, "attend_kv4_%s_kernel<%d>", in_steps(c.dim) ? "steps" : "wide", c.dim);
-    else snprintf(first, sizeof first, "attend_kv4_kernel<%d, %d>", c.dim, p.nb);
+    if (p.wide) snprintf(first, sizeof first, "attend_kv%d_%s_kernel<%d>", bits, in_steps(c.dim) ? "steps" : "wide", c.dim);
+    else snprintf(first, sizeof first, "attend_kv%d_kernel<%d, %d>", bits, c.dim, p.nb);
     if (p.splits > 1) snprintf(join, sizeof join, " + attend_join_kernel<%d>", c.dim);
     *launches = p.splits > 1 ? 2 : 1;
     snprintf(buf, buflen, "%s%s", first, join);
     return MICONV_OK;
 }
 
-extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, long tokens, const void *q,
-                                   long q_stride, const int32_t *starts, const int32_t *lens, const int32_t *table,
-                                   int table_stride, int max_new, int max_len, float scale, int causal, int window,
-                                   void *out, long out_stride, void *ws, size_t ws_bytes, void *stream)
+template <class F, class C>
+int attend(const C *cache, int seqs, int heads, long tokens, const void *q, long q_stride, const int32_t *starts,
+           const int32_t *lens, const int32_t *table, int table_stride, int max_new, int max_len, float scale, int causal,
+           int window, void *out, long out_stride, void *ws, size_t ws_bytes, void *stream)
 {
-    using namespace miconv;
-    quant::AttArgs a = {};
-    const int rc = quant::check_attend(cache, seqs, heads, max_new, max_len, &a.c);
+    AttArgs a = {};
+    const int rc = check_attend(cache, seqs, heads, max_new, max_len, &a.c);
     if (rc != MICONV_OK) return rc;
     const long width = (long)heads * a.c.dim;
     a.scale = scale * 1.44269504088896340736f;
@@ -1044,12 +1163,11 @@ extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, 
     if (tokens >= 1L << 31) return MICONV_ERR_TOO_LARGE;
     if (seqs == 0 || tokens == 0) return MICONV_OK;
     if (!q || !out || !lens || !table) return MICONV_ERR_NULL;
-    if (quant::misaligned(q, 2) || quant::misaligned(out, 2) || quant::misaligned(starts, 4) ||
-        quant::misaligned(lens, 4) || quant::misaligned(table, 4))
+    if (misaligned(q, 2) || misaligned(out, 2) || misaligned(starts, 4) || misaligned(lens, 4) || misaligned(table, 4))
         return MICONV_ERR_ALIGN;
-    const quant::AttPlan p = quant::plan_attend(a.c, seqs, heads, max_new, max_len, causal, window);
-    if (!quant::grid_holds(p, a.c, seqs)) return MICONV_ERR_TOO_LARGE;
-    if (p.bytes && (!ws || ws_bytes < p.bytes || quant::misaligned(ws, 256))) return MICONV_ERR_WORKSPACE;
+    const AttPlan p = plan_attend(a.c, seqs, heads, max_new, max_len, causal, window);
+    if (!grid_holds(p, a.c, seqs)) return MICONV_ERR_TOO_LARGE;
+    if (p.bytes && (!ws || ws_bytes < p.bytes || misaligned(ws, 256))) return MICONV_ERR_WORKSPACE;
     a.q = (const uint16_t *)q, a.out = (uint16_t *)out;
     a.starts = starts, a.lens = lens, a.table = table;
     a.part = (float *)ws;
@@ -1061,11 +1179,57 @@ extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, 
     a.dv_group = make_fastdiv((unsigned)a.group);
     hipStream_t st = static_cast<hipStream_t>(stream);
     switch (a.c.dim) {
-    case 32: return quant::launch_attend<32>(a, p, st);
-    case 64: return quant::launch_attend<64>(a, p, st);
-    case 96: return quant::launch_attend<96>(a, p, st);
-    case 128: return quant::launch_attend<128>(a, p, st);
-    case 192: return quant::launch_attend<192>(a, p, st);
-    default: return quant::launch_attend<256>(a, p, st);
+    case 32: return launch_attend<F, 32>(a, p, st);
+    case 64: return launch_attend<F, 64>(a, p, st);
+    case 96: return launch_attend<F, 96>(a, p, st);
+    case 128: return launch_attend<F, 128>(a, p, st);
+    case 192: return launch_attend<F, 192>(a, p, st);
+    default: return launch_attend<F, 256>(a, p, st);
     }
+}
+
+}  // namespace
+}  // namespace quant
+}  // namespace miconv
+
+extern "C" long quant_attention_workspace_bytes(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len,
+                                                int causal, int window)
+{
+    return miconv::quant::attend_workspace(cache, seqs, heads, max_new, max_len, causal, window);
+}
+
+extern "C" int quant_attention_describe(const quant_kv4 *cache, int seqs, int heads, int max_new, int max_len, int causal,
+                                        int window, char *buf, int buflen, int *launches)
+{
+    return miconv::quant::attend_describe(cache, 4, seqs, heads, max_new, max_len, causal, window, buf, buflen, launches);
+}
+
+extern "C" int quant_attention_kv4(const quant_kv4 *cache, int seqs, int heads, long tokens, const void *q,
+                                   long q_stride, const int32_t *starts, const int32_t *lens, const int32_t *table,
+                                   int table_stride, int max_new, int max_len, float scale, int causal, int window,
+                                   void *out, long out_stride, void *ws, size_t ws_bytes, void *stream)
+{
+    return miconv::quant::attend<miconv::quant::Fp4>(cache, seqs, heads, tokens, q, q_stride, starts, lens, table, table_stride,
+                                               max_new, max_len, scale, causal, window, out, out_stride, ws, ws_bytes, stream);
+}
+
+extern "C" long quant_attention_kv8_workspace_bytes(const quant_kv8 *cache, int seqs, int heads, int max_new, int max_len,
+                                                int causal, int window)
+{
+    return miconv::quant::attend_workspace(cache, seqs, heads, max_new, max_len, causal, window);
+}
+
+extern "C" int quant_attention_kv8_describe(const quant_kv8 *cache, int seqs, int heads, int max_new, int max_len, int causal,
+                                        int window, char *buf, int buflen, int *launches)
+{
+    return miconv::quant::attend_describe(cache, 8, seqs, heads, max_new, max_len, causal, window, buf, buflen, launches);
+}
+
+extern "C" int quant_attention_kv8(const quant_kv8 *cache, int seqs, int heads, long tokens, const void *q,
+                                   long q_stride, const int32_t *starts, const int32_t *lens, const int32_t *table,
+                                   int table_stride, int max_new, int max_len, float scale, int causal, int window,
+                                   void *out, long out_stride, void *ws, size_t ws_bytes, void *stream)
+{
+    return miconv::quant::attend<miconv::quant::Fp8>(cache, seqs, heads, tokens, q, q_stride, starts, lens, table, table_stride,
+                                               max_new, max_len, scale, causal, window, out, out_stride, ws, ws_bytes, stream);
 }

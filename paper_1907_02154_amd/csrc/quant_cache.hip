@@ -12,7 +12,7 @@
 namespace miconv {
 namespace quant {
 
-int kv4_view(const quant_kv4 *c, Kv4 *out)
+int kv4_view(const quant_kv4 *c, KvView *out)
 {
     if (!c) return MICONV_ERR_NULL;
     if (c->pages < 1 || c->heads < 1 || c->page_size < 1) return MICONV_ERR_SHAPE;
@@ -26,6 +26,7 @@ int kv4_view(const quant_kv4 *c, Kv4 *out)
     out->slots = c->pages * c->page_size;
     out->heads = c->heads, out->page_size = c->page_size, out->dim = D;
     out->dv_page = make_fastdiv((unsigned)c->page_size);
+    out->block = out->blocks = 0, out->dv_block = FastDiv{0, 0};
     return MICONV_OK;
 }
 
@@ -34,7 +35,7 @@ namespace {
 constexpr int kWrite = 8, kRead = 4;   // tokens a work-group handles, keys or values
 
 struct CacheArgs {
-    Kv4 c;
+    KvView c;
     void *k, *v;           // the tokens' rows (read by the write, written by the read)
     long ks, vs;           // their strides in elements
     const int32_t *slots;
@@ -54,7 +55,7 @@ __device__ __forceinline__ long first_token(int tokens)
 }
 
 // Row of the cache (of head_dim / 2 bytes of codes) that holds (slot, head).
-__device__ __forceinline__ long cache_row(const Kv4 &c, int slot, int head)
+__device__ __forceinline__ long cache_row(const KvView &c, int slot, int head)
 {
     const unsigned page = fdiv((unsigned)slot, c.dv_page), place = (unsigned)slot - page * (unsigned)c.page_size;
     return ((long)page * c.heads + head) * c.page_size + place;
@@ -63,7 +64,7 @@ __device__ __forceinline__ long cache_row(const Kv4 &c, int slot, int head)
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_write_kernel(CacheArgs a)
 {
-    const Kv4 &c = a.c;
+    const KvView &c = a.c;
     const bool val = blockIdx.y;
     const T *src = (const T *)(val ? a.v : a.k);
     const long stride = val ? a.vs : a.ks;
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(CacheArgs a)
 template <typename T>
 __global__ __launch_bounds__(256) void kv4_read_kernel(CacheArgs a)
 {
-    const Kv4 &c = a.c;
+    const KvView &c = a.c;
     const bool val = blockIdx.y;
     T *dst = (T *)(val ? a.v : a.k);
     const long stride = val ? a.vs : a.ks;

@@ -10,85 +10,13 @@
 // bytes, many by the matrix cores; in between by what a compute unit can fetch,
 // which grows with the wavefronts that wait side by side: there several groups
 // of wavefronts share a tile and divide its reduction.
-#include "quant.h"
+#include "quant_tiles.h"
 
 #include <stdio.h>
 
 namespace miconv {
 namespace quant {
 namespace {
-
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-struct MatArgs {
-    const int8_t *a, *w;
-    const float *sa, *sw, *bias;
-    const void *res;
-    void *y;
-    long as, ws, rs, ys;   // row strides in elements
-    int M, N, K;
-    int relu;
-    // tile order: tiles along m and n, tiles in all
-    int mt, nt, tiles;
-    FastDiv dv_group;      // by kGroup * nt
-};
-
-constexpr int kXcds = 8;    // a work-group runs on the die of its number modulo 8
-constexpr int kGroup = 4;   // tiles along m that are taken together
-
-// The tile of a work-group: each die gets a run of tiles that follow one
-// another, down kGroup tiles and on to the next channels, so that what its
-// work-groups read at a time meets in its L2.
-__device__ __forceinline__ void tile_of(const MatArgs &a, int id, int *m, int *n)
-{
-    const int x = id % kXcds, q = a.tiles / kXcds, r = a.tiles % kXcds;
-    const int t = x * q + (x < r ? x : r) + id / kXcds;
-    const int g = (int)fdiv((unsigned)t, a.dv_group), in = t - g * kGroup * a.nt;
-    const int rows = min(a.mt - g * kGroup, kGroup);
-    *n = rows == kGroup ? in / kGroup : in / rows;
-    *m = g * kGroup + in - *n * rows;
-}
-
-// Four sums of token m, channels n .. n + 3, into y.
-template <typename T>
-__device__ __forceinline__ void finish4(const MatArgs &a, int m, int n, i32x4 sum, float sa)
-{
-    const int live = a.N - n;
-    if (live <= 0) return;
-    T *y = (T *)a.y + (long)m * a.ys + n;
-    const T *res = a.res ? (const T *)a.res + (long)m * a.rs + n : nullptr;
-    float v[4], f[4] = {}, b[4] = {};
-    if (live >= 4) {
-        memcpy(f, a.sw + n, 16);
-        if (a.bias) memcpy(b, a.bias + n, 16);
-    } else {
-        for (int i = 0; i < live; ++i) f[i] = a.sw[n + i], b[i] = a.bias ? a.bias[n + i] : 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (float)sum[i] * sa * f[i];
-    if (a.bias)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += b[i];
-    if (live >= 4) {
-        if (res) {
-            float r[4];
-            load4(res, r);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += r[i];
-        }
-        if (a.relu)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];   // a NaN stays
-        store4(y, v);
-    } else {
-        for (int i = 0; i < live; ++i) {
-            float x = v[i];
-            if (res) x += load1(res + i);
-            if (a.relu) x = x < 0.0f ? 0.0f : x;
-            store1(y + i, x);
-        }
-    }
-}
 
 // The first n of 16 bytes from p on, at any alignment, and zeros: the aligned
 // words that hold at least one of them, shifted.
@@ -108,14 +36,6 @@ __device__ __forceinline__ i32x4 load16(const int8_t *p, int n)
     }
     return v;
 }
-
-template <int N>
-__device__ __forceinline__ void wait_vmcnt()
-{
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-
-typedef __attribute__((address_space(3))) void lds_void_t;
 
 // BM tokens x BN channels a work-group of KG groups of WM x WN wavefronts; a
 // stage is 128 bytes of the reduction for each group, NST of them in LDS, and
@@ -258,7 +178,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul_i8_tile_kernel(MatAr
         if (m >= a.M) continue;
         const float sa = a.sa[m];
 #pragma unroll
-        for (int i = 0; i < TN; ++i) finish4<T>(a, m, n0 + wid / WM * (BN / WN) + 16 * i + 4 * quad, acc[i][j], sa);
+        for (int i = 0; i < TN; ++i) finish4<T, true>(a, m, n0 + wid / WM * (BN / WN) + 16 * i + 4 * quad, acc[i][j], sa);
     }
 }
 
@@ -299,31 +219,13 @@ __global__ __launch_bounds__(256) void matmul_i8_align_kernel(AlignArgs a)
 // 1024 channels, where 16 x 16 and 16 x 32 tie and the first is taken (K = 4096 5.6
 // us, and 4.8 the other; K = 16384 14.5 and 12.1), and 16 tokens, 11000 channels
 // at K = 16384 (39.8, and 34.0 in tiles of 16 x 16).
-struct Tile {
-    int bm, bn, wm, wn, kg, nst;   // the kernel's parameters
-    int per_cu;
-    float one, two;
-};
 constexpr Tile kTiles[] = {
     {16, 16, 1, 1, 4, 4, 2, 3.4f, 3.8f},    {16, 32, 1, 2, 4, 3, 2, 3.8f, 5.0f},    {32, 64, 1, 4, 4, 3, 1, 6.6f, 0.0f},
     {64, 32, 2, 2, 4, 3, 1, 6.6f, 0.0f},    {64, 64, 2, 2, 2, 4, 1, 9.3f, 0.0f},    {128, 64, 4, 2, 2, 3, 1, 13.8f, 0.0f},
     {128, 128, 2, 4, 1, 3, 1, 22.3f, 0.0f}, {128, 128, 2, 2, 1, 2, 2, 28.0f, 38.0f}, {256, 256, 4, 2, 1, 2, 1, 66.0f, 0.0f},
 };
 
-int pick_tile(int M, int N)
-{
-    const long cus = cu_count();
-    int best = 0;
-    double least = 1e300;
-    for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
-        const Tile &t = kTiles[i];
-        const long tiles = (long)ceil_div(M, t.bm) * ceil_div(N, t.bn), round = cus * t.per_cu, rest = tiles % round;
-        const double full = t.per_cu == 2 ? t.two : t.one;
-        const double cost = (double)(tiles / round) * full + (rest == 0 ? 0.0 : rest > cus ? full : t.one);
-        if (cost < least) least = cost, best = i;
-    }
-    return best;
-}
+int pick(int M, int N) { return pick_tile(kTiles, (int)(sizeof(kTiles) / sizeof(kTiles[0])), M, N); }
 
 template <typename T, int I>
 int go_tile(MatArgs a, hipStream_t st)
@@ -342,7 +244,7 @@ int go_tile(MatArgs a, hipStream_t st)
 template <typename T>
 int launch_matmul(const MatArgs &a, hipStream_t st)
 {
-    switch (pick_tile(a.M, a.N)) {
+    switch (pick(a.M, a.N)) {
     case 0: return go_tile<T, 0>(a, st);
     case 1: return go_tile<T, 1>(a, st);
     case 2: return go_tile<T, 2>(a, st);
@@ -355,22 +257,26 @@ int launch_matmul(const MatArgs &a, hipStream_t st)
     }
 }
 
-// Whether an operand's rows can be loaded as they are: 16-byte chunks, and the
-// 256 rows of the largest tile within the 31-bit offsets of a buffer.
-bool rows_aligned(const int8_t *p, long stride, long K)
-{
-    return K % 16 == 0 && stride % 16 == 0 && !misaligned(p, 16) && 256 * stride < 1L << 31;
-}
-
-long align_up(long v, long to) { return (v + to - 1) / to * to; }
-
-// Bytes of the aligned copy of an operand that needs one.
-long copy_bytes(long rows, const int8_t *p, long stride, long K)
-{
-    return rows_aligned(p, stride, K) ? 0 : align_up(rows * align_up(K, 16), 256);
-}
-
 }  // namespace
+
+int align_operands(MatArgs &a, long ca, long cw, void *ws, hipStream_t st)
+{
+    const long pitch = align_up(a.K, 16);
+    int8_t *to_a = (int8_t *)ws, *to_w = to_a + ca;
+    AlignArgs c = {{a.a, a.w}, {to_a, to_w}, {a.as, a.ws}, {ca ? a.M : 0, cw ? a.N : 0},
+                   a.K, (int)(pitch / 16), 0, make_fastdiv((unsigned)(pitch / 16))};
+    const long total = ((long)c.rows[0] + c.rows[1]) * c.chunks;
+    if (total >= 1L << 31) return MICONV_ERR_TOO_LARGE;
+    c.total = (unsigned)total;
+    launch_kernel(matmul_i8_align_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, c);
+    const int e = launched();
+    if (e != MICONV_OK) return e;
+    if (ca) a.a = to_a, a.as = pitch;
+    if (cw) a.w = to_w, a.ws = pitch;
+    a.K = (int)pitch;   // the copies are zero from K on; an operand read in place has K % 16 == 0
+    return MICONV_OK;
+}
+
 }  // namespace quant
 }  // namespace miconv
 
@@ -406,7 +312,7 @@ extern "C" int quant_matmul_describe(long M, long N, long K, const int8_t *a, lo
     if (!dtype_bytes(out_dtype)) return MICONV_ERR_UNSUPPORTED;
     if (M == 0) return MICONV_OK;
     const bool copy = copy_bytes(M, a, a_stride, K) + copy_bytes(N, w, w_stride, K) > 0;
-    const Tile t = kTiles[pick_tile((int)M, (int)N)];
+    const Tile t = kTiles[pick((int)M, (int)N)];
     *launches = 1 + copy;
     snprintf(buf, buflen, "%smatmul_i8_tile_kernel<%s, %d, %d, %d, %d, %d, %d>", copy ? "matmul_i8_align_kernel + " : "",
              out_dtype == kF32 ? "float" : "unsigned short", t.bm, t.bn, t.wm, t.wn, t.kg, t.nst);
@@ -435,19 +341,8 @@ extern "C" int quant_matmul_i8(long M, long N, long K, const int8_t *a, long a_s
                            y_stride, (int)M, (int)N, (int)K, relu, 0, 0, 0, {}};
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (ca + cw) {
-        const long pitch = quant::align_up(K, 16);
-        int8_t *to_a = (int8_t *)ws, *to_w = to_a + ca;
-        quant::AlignArgs c = {{a, w}, {to_a, to_w}, {a_stride, w_stride}, {ca ? (int)M : 0, cw ? (int)N : 0},
-                              (int)K, (int)(pitch / 16), 0, make_fastdiv((unsigned)(pitch / 16))};
-        const long total = ((long)c.rows[0] + c.rows[1]) * c.chunks;
-        if (total >= 1L << 31) return MICONV_ERR_TOO_LARGE;
-        c.total = (unsigned)total;
-        launch_kernel(quant::matmul_i8_align_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, c);
-        const int e = quant::launched();
+        const int e = quant::align_operands(args, ca, cw, ws, st);
         if (e != MICONV_OK) return e;
-        if (ca) args.a = to_a, args.as = pitch;
-        if (cw) args.w = to_w, args.ws = pitch;
-        args.K = (int)pitch;   // the copies are zero from K on; an operand read in place has K % 16 == 0
     }
     return out_dtype == quant::kF32 ? quant::launch_matmul<float>(args, st) : quant::launch_matmul<uint16_t>(args, st);
 }

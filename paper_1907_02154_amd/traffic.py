@@ -89,7 +89,14 @@ SOURCES = {
     "attend_kv4_kernel": "quant_attend.hip",
     "attend_kv4_wide_kernel": "quant_attend.hip",
     "attend_kv4_steps_kernel": "quant_attend.hip",
+    "attend_kv8_kernel": "quant_attend.hip",
+    "attend_kv8_wide_kernel": "quant_attend.hip",
+    "attend_kv8_steps_kernel": "quant_attend.hip",
     "attend_join_kernel": "quant_attend.hip",
+    "kv8_write_kernel": "quant_cache8.hip",
+    "kv8_read_kernel": "quant_cache8.hip",
+    "matmul_f8_tile_kernel": "quant_matmul_f8.hip",
+    "rows_f8_kernel": "quant_rows_f8.hip",
     "kv4_write_kernel": "quant_cache.hip",
     "kv4_read_kernel": "quant_cache.hip",
     "matmul_i8_tile_kernel": "quant_matmul.hip",

@@ -1,0 +1,766 @@
+"""GPU: the operators in 8-bit floats (include/miquant.h) against the oracle
+(oracle/quant.py), through the binding.
+
+Values, exponents and cache contents are unique and compared bit for bit.  The
+others are held to bounds that follow from the kernels' roundings: a row's scale
+to SCALE_TOL (below), a product and an attention row to the bound that the
+oracle computes with them.
+"""
+import math
+
+import pytest
+import torch
+
+from oracle import quant as ref
+from paper_1907_02154_amd import miconv, quant
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32, U8 = torch.bfloat16, torch.float32, torch.uint8
+
+
+def scale_tol(cols):
+    """A row's squares: in each of 64 lanes at least, then ten additions; halved by the root, five roundings follow."""
+    return ((cols / 64 + 8 + 12) / 2 + 5) * 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    quant.lib()
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def bits(t):
+    return t.view(U8).cpu()
+
+
+# ------------------------------------------------------------------ rows
+
+def check_rows(x, weight=None, residual=None, eps=1e-6, got=None):
+    codes, byte, scale, h = ref.rows_f8(x, weight, residual, eps)
+    if got is None:
+        got = quant.rmsnorm_f8(x.cuda(), None if weight is None else weight.cuda(), None if residual is None else residual.cuda(),
+                               eps=eps)
+    assert got[0].dtype == quant.F8 and torch.equal(got[1].cpu(), byte) and torch.equal(bits(got[0]), codes)
+    s = got[2].cpu().double()
+    fine = torch.isfinite(scale)
+    assert torch.equal(torch.isnan(s), ~fine)
+    assert ((s - scale).abs()[fine] <= scale_tol(x.shape[1]) * scale[fine]).all()
+    assert (got[3] is None) == (residual is None)
+    if residual is not None:
+        same = (got[3].cpu() == h) | (torch.isnan(got[3].cpu()) & torch.isnan(h))
+        assert same.all()
+    return got
+
+
+ROWS = [(1, 1), (3, 7), (5, 8), (2, 100), (2, 127), (4, 128), (3, 129), (9, 511), (6, 512), (4, 513), (7, 1000), (1, 1024),
+        (3, 1031), (2, 2048), (3, 2100), (5, 4096), (2, 4097), (1, 8192), (2, 8200), (1, 40003), (70, 256), (600, 64)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", ROWS)
+def test_rmsnorm(dtype, rows, cols):
+    g = gen(rows * 7919 + cols)
+    x = (torch.randn(rows, cols, generator=g) * 2).to(dtype)
+    r = torch.randn(rows, cols, generator=g).to(dtype)
+    w = torch.randn(cols, generator=g)
+    check_rows(x, w, r)
+    check_rows(x, w)
+    check_rows(x, None, r)
+    q, e = quant.rows_f8(x.cuda())
+    codes, byte, _, _ = ref.rows_f8(x)
+    assert torch.equal(bits(q), codes) and torch.equal(e.cpu(), byte)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_rmsnorm_strides_alignment_and_in_place(dtype):
+    g = gen(5)
+    rows, cols = 6, 203
+    wide = torch.randn(rows, cols + 30, generator=g).to(dtype)
+    r = torch.randn(rows, cols, generator=g).to(dtype)
+    wide_d = wide.cuda()
+    x = wide_d[:, 3:3 + cols]                              # rows start at odd elements, and are not contiguous
+    hold = r.cuda()
+    q = torch.full((rows, cols + 5), 99, dtype=U8, device="cuda")
+    e = torch.full((rows, 5), 98, dtype=U8, device="cuda")
+    got = quant.rmsnorm_f8(x, None, hold, h=hold, q=q.view(quant.F8)[:, 1:1 + cols], exps=e[:, 2:4])
+    assert got[3] is hold
+    check_rows(wide[:, 3:3 + cols], None, r, got=(got[0].contiguous(), got[1], got[2], got[3]))
+    assert (q[:, 0] == 99).all() and (q[:, 1 + cols:] == 99).all() and torch.equal(wide_d.cpu(), wide)
+    assert (e[:, :2] == 98).all() and (e[:, 4:] == 98).all()
+    got = quant.rmsnorm_f8(x, None, r.cuda(), h=x)         # the sum over x itself
+    check_rows(wide[:, 3:3 + cols], None, r, got=got)
+    assert torch.equal(wide_d.cpu()[:, :3], wide[:, :3]) and torch.equal(wide_d.cpu()[:, 3 + cols:], wide[:, 3 + cols:])
+
+
+def edge_values():
+    """Values at and beside every rounding boundary of the format and every change of the exponent, over fp32's range."""
+    grid = ref.E4M3
+    mids = (grid[1:] + grid[:-1]) / 2
+    m = torch.cat([grid, mids])
+    m = torch.cat([m, -m])
+    rows = []
+    for e in (-140, -127, -126, -125, -118, -117, -116, -60, -9, -1, 0, 1, 50, 100, 117, 118, 119):
+        for top in (448.0, 440.0, 256.0, 230.0, 449.0):
+            v = (m.clamp(-min(top, 448.0), min(top, 448.0)) * 2.0 ** e).float()
+            for part in v.split(126):
+                for nudge in (-1, 0, 1):
+                    f = torch.nextafter(part, part + nudge * math.inf) if nudge else part
+                    row = torch.zeros(128)
+                    row[:len(f)] = f
+                    row[127] = top * 2.0 ** e if top * 2.0 ** e < 3.4e38 else 3.4e38   # the block's largest
+                    rows.append(row)
+    return torch.nan_to_num(torch.stack(rows), nan=0.0, posinf=3.4028234e38, neginf=-3.4028234e38)
+
+
+def test_rows_every_boundary():
+    x = edge_values()
+    q, e = quant.rows_f8(x.cuda())
+    codes, byte, _, _ = ref.rows_f8(x)
+    assert torch.equal(e.cpu(), byte)
+    off = (bits(q) != codes).nonzero()
+    assert len(off) == 0, (off[:3].tolist(), x[off[0, 0], off[0, 1]], codes[off[0, 0], off[0, 1]], bits(q)[off[0, 0], off[0, 1]])
+
+
+def test_rmsnorm_extremes():
+    cols = 300
+    x = torch.zeros(9, cols)
+    x[1] = 1.0
+    x[2, 7] = math.nan
+    x[3, 299] = math.inf
+    x[4, 0] = -math.inf
+    x[5] = 2.0 ** -140
+    x[6] = 2.0 ** -99
+    x[7, 3] = 3e38                                         # its square overflows
+    x[8, 5] = -1e-3
+    q, e, scale, _ = check_rows(x, eps=0.0)
+    assert e.cpu()[2].tolist() == [255, 10, 10] and e.cpu()[3].tolist() == [10, 10, 255] and bits(q)[2:5].max() == 0
+    assert float(scale[0]) == torch.finfo(F32).max         # a row of zeros
+    big = torch.full((300,), 3e38)
+    check_rows(torch.where(torch.isfinite(x), x, torch.zeros_like(x)) * 4, big, eps=1e-6)   # the product with the weight passes fp32
+    for dtype in (BF16, F32):                              # no rows
+        z = torch.empty(0, 8, dtype=dtype, device="cuda")
+        o = quant.rmsnorm_f8(z, residual=z)
+        assert o[0].shape == (0, 8) and o[1].shape == (0, 1) and o[2].shape == (0,) and o[3].shape == (0, 8)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("cols", [1, 300, 1500, 5000])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-6, 1e6])
+def test_rmsnorm_scales_over_the_range_of_fp32(dtype, cols, eps):
+    """Rows whose squares pass fp32 at either end, of one magnitude and of all: the scale is the definition's."""
+    g = gen(cols)
+    e = torch.tensor([-126, -99, -90, -80, -75, -64, -63, -50, -41, -40, -39, -20, 0, 40, 56, 60, 62, 63, 64, 70, 100, 124])
+    n = len(e)
+    x = 0.5 + torch.rand(n + 4, cols, generator=g)
+    x[:n] *= torch.exp2(e.float())[:, None]
+    x[n:] *= torch.exp2(torch.randint(-120, 125, (4, cols), generator=g).float())
+    x = x.to(dtype)
+    check_rows(x, eps=eps)
+    r = (torch.randn(x.shape, generator=g) * x.abs().float()).to(dtype)
+    keep = ((x.double() + r.double()).abs().amax(1) < 2.0 ** 127)
+    hold = r[keep].cuda()
+    check_rows(x[keep], torch.ones(cols), r[keep], eps,
+               got=quant.rmsnorm_f8(x[keep].cuda(), torch.ones(cols, device="cuda"), hold, eps=eps, h=hold))
+
+
+# ------------------------------------------------------------------ product
+
+def operand(g, rows, K, spread=6):
+    """Codes of every kind but NaN and exponents over a range, on the host, and their values in 64 bits."""
+    c = torch.randint(0, 256, (rows, K), generator=g).to(U8)
+    c = torch.where(c % 128 == 127, c - 1, c)
+    e = torch.randint(127 - spread, 128 + spread, (rows, -(-K // 128)), generator=g).to(U8)
+    return c, e, ref.rows_f8_value(c, e)
+
+
+def check_matmul(M, N, K, dtype, scaled, bias, res, relu, seed=0, a=None, w=None):
+    g = gen(seed + M * 31 + N * 17 + K)
+    a, w = operand(g, M, K) if a is None else a, operand(g, N, K) if w is None else w
+    sa = torch.rand(M, generator=g) - 0.2 if scaled else None
+    b = 1000 * torch.randn(N, generator=g) if bias else None
+    r = (1000 * torch.randn(M, N, generator=g)).to(dtype) if res else None
+    dev = lambda t: None if t is None else t.cuda()  # noqa: E731
+    y = quant.matmul_f8(a[0].cuda().view(quant.F8), a[1].cuda(), w[0].cuda().view(quant.F8), w[1].cuda(), a_scale=dev(sa),
+                        bias=dev(b), residual=dev(r), relu=relu, out_dtype=dtype)
+    assert y.dtype == dtype and tuple(y.shape) == (M, N)
+    want, tol = ref.matmul_f8(a[2], w[2], sa, b, r, relu, dtype == BF16)
+    off = (y.cpu().double() - want).abs()
+    assert (off <= tol).all(), (float((off / tol).max()), (off > tol).nonzero()[:4].tolist())
+
+
+MATMUL = [(1, 1, 1), (1, 64, 64), (3, 5, 7), (1, 1000, 1024), (16, 16, 16), (17, 33, 65), (2, 130, 4096), (8, 256, 100),
+          (16, 512, 512), (31, 100, 48), (33, 1000, 1999), (48, 512, 4096), (64, 64, 128), (65, 129, 130), (100, 72, 272),
+          (128, 128, 128), (129, 384, 640), (200, 1000, 513), (255, 257, 80), (256, 256, 256), (257, 264, 1040),
+          (300, 520, 2048), (512, 1024, 192)]
+
+
+@pytest.mark.parametrize("M,N,K", MATMUL)
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_matmul(M, N, K, dtype):
+    check_matmul(M, N, K, dtype, scaled=M % 2 == 0, bias=(M + N) % 2 == 0, res=K % 2 == 0, relu=N % 3 == 0)
+    check_matmul(M, N, K, dtype, False, False, False, False, seed=1)
+
+
+@pytest.mark.parametrize("K", [16, 32, 112, 128, 144, 272, 400, 528])
+@pytest.mark.parametrize("M,N", [(1, 1), (1, 17), (17, 1), (16, 33), (33, 16)])
+def test_matmul_reductions_shorter_than_the_groups_parts(M, N, K):
+    """Groups of wavefronts whose blocks begin past the last, one row of an operand the shortest buffer."""
+    check_matmul(M, N, K, BF16, True, True, False, False)
+    check_matmul(M, N, K, F32, False, False, True, True)
+
+
+def test_matmul_sums_are_exact_where_fp32_holds_them():
+    """Whole numbers that fp32 holds at every step: each product in its place, with its own row's and block's exponents."""
+    g = gen(3)
+    M, N, K = 37, 70, 1000
+    c = lambda n: torch.randint(0, 9, (n, K), generator=g)  # noqa: E731
+    whole = torch.tensor([0x00, 0x38, 0x40, 0x44, 0x48, 0xB8, 0xC0, 0xC4, 0xC8], dtype=U8)     # 0, 1, 2, 3, 4 and negative ones
+    a, w = whole[c(M)], whole[c(N)]
+    ea, ew = (torch.randint(125, 130, (n, 8), generator=g).to(U8) for n in (M, N))
+    y = quant.matmul_f8(a.cuda().view(quant.F8), ea.cuda(), w.cuda().view(quant.F8), ew.cuda(), out_dtype=F32)
+    assert torch.equal(y.cpu().double(), ref.rows_f8_value(a, ea) @ ref.rows_f8_value(w, ew).t())
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 40, 300), (130, 300, 1000)])
+def test_matmul_exponents_over_their_range_and_blocks_that_are_not_finite(M, N, K):
+    g = gen(9)
+    a, w = operand(g, M, K), operand(g, N, K)
+    ea = torch.randint(10, 247, (M, 1), generator=g)
+    a = (a[0], (ea + torch.randint(-3, 4, a[1].shape, generator=g)).clamp(10, 246).to(U8), None)
+    ew = torch.randint(60, 130, (N, 1), generator=g)
+    w = (w[0], ew.expand(-1, w[1].shape[1]).to(U8), None)
+    a, w = (t[:2] + (ref.rows_f8_value(*t[:2]),) for t in (a, w))
+    y = quant.matmul_f8(a[0].cuda().view(quant.F8), a[1].cuda(), w[0].cuda().view(quant.F8), w[1].cuda(), out_dtype=F32).cpu()
+    want, tol = ref.matmul_f8(a[2], w[2], bf16=False)
+    size = a[2].abs() @ w[2].abs().t()
+    keep = (size > 2.0 ** -100) & (size < 2.0 ** 126)                  # products and sums that fp32 holds in full
+    assert keep.float().mean() > 0.5 and ((y.double() - want).abs() <= tol)[keep].all()
+    a[1][M // 2, 1], w[1][3, 0] = 255, 255
+    a[0][1, K - 1] = 0x7F                                               # a value that is NaN
+    y = quant.matmul_f8(a[0].cuda().view(quant.F8), a[1].cuda(), w[0].cuda().view(quant.F8), w[1].cuda(), out_dtype=F32).cpu()
+    nan = torch.zeros(M, N, dtype=torch.bool)
+    nan[M // 2], nan[1], nan[:, 3] = True, True, True
+    assert torch.isnan(y[nan]).all() and not torch.isnan(y[~nan & keep]).any()
+    z = quant.matmul_f8(a[0].cuda().view(quant.F8), a[1].cuda(), w[0].cuda().view(quant.F8), w[1].cuda(), relu=True).cpu()
+    assert torch.isnan(z[nan]).all() and (z[~nan & keep] >= 0).all()
+
+
+# A tile of the product's kernel, and shapes that the rule sends to it: one row and channel past a whole number of tiles, or one
+# short of it.
+TILES = {"16, 16, 1, 1, 4, 4": (17, 17), "16, 32, 1, 2, 4, 3": (1, 8193), "32, 64, 1, 4, 4, 3": (33, 5441),
+         "64, 32, 2, 2, 4, 3": (897, 513), "64, 64, 2, 2, 2, 4": (65, 5441), "128, 64, 4, 2, 2, 3": (129, 6529),
+         "128, 128, 2, 4, 1, 3": (129, 10881), "128, 128, 2, 2, 1, 2": (257, 13057), "256, 256, 4, 2, 1, 2": (769, 14081)}
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("tile", TILES)
+def test_matmul_of_every_tile(tile, dtype):
+    M, N = TILES[tile]
+    for K in (400, 129):
+        assert quant.matmul_f8_describe(M, N, 400, dtype) == (
+            f"matmul_f8_tile_kernel<{'float' if dtype == F32 else 'unsigned short'}, {tile}>", 1)
+        check_matmul(M, N, K, dtype, True, True, False, False)
+
+
+def test_matmul_strides_and_in_place_residual():
+    g = gen(4)
+    M, N, K = 70, 90, 256
+    a, w = operand(g, M, K), operand(g, N, K)
+    wide_a, wide_w = torch.full((M, K + 48), 0x7F, dtype=U8), torch.full((N, K + 7), 0x7F, dtype=U8)
+    wide_a[:, 32:32 + K], wide_w[:, 3:3 + K] = a[0], w[0]                 # one aligned, one copied
+    wide_ea, wide_ew = torch.full((M, 5), 255, dtype=U8), torch.full((N, 3), 255, dtype=U8)
+    wide_ea[:, 2:4], wide_ew[:, 1:] = a[1], w[1]
+    hold = torch.randn(M, N + 11, generator=g).cuda()
+    res = hold[:, 5:5 + N]
+    before = hold.cpu()
+    da, dw = wide_a.cuda().view(quant.F8)[:, 32:32 + K], wide_w.cuda().view(quant.F8)[:, 3:3 + K]
+    assert quant.matmul_f8_workspace_bytes(da, dw) > 0
+    y = quant.matmul_f8(da, wide_ea.cuda()[:, 2:4], dw, wide_ew.cuda()[:, 1:], residual=res, out=res)
+    want, tol = ref.matmul_f8(a[2], w[2], residual=before[:, 5:5 + N], bf16=False)
+    assert y is res and ((res.cpu().double() - want).abs() <= tol).all()
+    assert torch.equal(hold.cpu()[:, :5], before[:, :5]) and torch.equal(hold.cpu()[:, 5 + N:], before[:, 5 + N:])
+
+
+def test_matmul_no_rows():
+    y = quant.matmul_f8(torch.empty(0, 16, device="cuda").to(quant.F8), torch.empty(0, 1, dtype=U8, device="cuda"),
+                        torch.zeros(8, 16, device="cuda").to(quant.F8), torch.ones(8, 1, dtype=U8, device="cuda"))
+    assert y.shape == (0, 8)
+
+
+# ------------------------------------------------------------------ the 8-bit cache
+
+def state(cache):
+    return ref.KV8([bits(cache.k_codes), bits(cache.v_codes)], [cache.k_exps.cpu(), cache.v_exps.cpu()])
+
+
+def same(cache, want):
+    for c, w in ((cache.k_codes, want.codes[0]), (cache.v_codes, want.codes[1])):
+        off = (bits(c) != w).nonzero()
+        assert len(off) == 0, off[:4].tolist()
+    for e, w in ((cache.k_exps, want.byte[0]), (cache.v_exps, want.byte[1])):
+        assert torch.equal(e.cpu(), w), (e.cpu() != w).nonzero()[:4].tolist()
+
+
+def random_cache(g, pages, heads, page, d, block):
+    """A cache of anything, as a program that reuses its pages has it."""
+    c = quant.KV8Cache.allocate(pages, heads, page, d, block)
+    for t in (c.k_codes, c.v_codes):
+        t.view(U8).copy_(torch.randint(0, 256, t.shape, generator=g).to(U8))
+    for t in (c.k_exps, c.v_exps):
+        t.copy_(torch.randint(100, 150, t.shape, generator=g).to(U8))
+    return c
+
+
+def starts_of(news):
+    return torch.tensor([0, *torch.tensor(news).cumsum(0).tolist()], dtype=torch.int32, device="cuda")
+
+
+WRITES = [   # page, block, head dim, heads, calls: new tokens of each sequence
+    (16, 16, 64, 2, [[1, 1], [1, 1], [14, 3], [1, 40]]), (64, 64, 128, 3, [[70, 1, 0], [1, 1, 1], [5, 64, 130]]),
+    (48, 16, 96, 1, [[17], [31], [1], [95]]), (24, 8, 32, 4, [[3, 9, 8], [8, 0, 25]]), (5, 5, 192, 2, [[4, 6], [1, 1], [12, 5]]),
+    (10, 1, 256, 1, [[3, 11], [1, 1]]), (256, 256, 64, 1, [[200], [1], [100]]), (30, 2, 64, 5, [[1], [1], [1], [1], [7]])]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("page,block,d,heads,calls", WRITES)
+def test_cache_writes(page, block, d, heads, calls, dtype):
+    """Call after call, each larger or smaller than what its blocks hold: the oracle's cache, bit for bit, and what is read."""
+    g = gen(page + d)
+    n = len(calls[0])
+    total = [sum(c[s] for c in calls) for s in range(n)]
+    per = max(-(-t // page) for t in total)
+    pages = n * per + 2
+    table = torch.randperm(pages, generator=g)[:n * per].reshape(n, per).to(torch.int32)
+    cache = random_cache(g, pages, heads, page, d, block)
+    want = state(cache)
+    lens = [0] * n
+    for i, news in enumerate(calls):
+        lens = [a + b for a, b in zip(lens, news)]
+        m = sum(news)
+        x = torch.randn(m, 2 * heads * d + 24, generator=g) * torch.exp2(torch.randint(-8, 4 + 6 * i, (m, 1), generator=g).float())
+        x = x.to(dtype)
+        k, v = (x[:, o:o + heads * d].unflatten(1, (heads, d)) for o in (0, heads * d + 24))
+        xd = x.cuda()
+        kd, vd = (xd[:, o:o + heads * d].unflatten(1, (heads, d)) for o in (0, heads * d + 24))
+        want.write(k.double(), v.double(), news, lens, table)
+        quant.kv8_write(kd, vd, cache, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), starts_of(news),
+                        max_new=max(news) if i % 2 else None)
+        same(cache, want)
+    slots = torch.cat([table[s, torch.arange(t) // page] * page + torch.arange(t) % page for s, t in enumerate(total)]).to(torch.int32)
+    for out in (BF16, F32):
+        k, v = quant.kv8_read(slots.cuda(), cache, dtype=out)
+        assert torch.equal(k.cpu().double(), want.values(0, slots)) and torch.equal(v.cpu().double(), want.values(1, slots))
+
+
+def test_cache_every_boundary():
+    x = edge_values()[:, :, None].transpose(1, 2)                       # a token a row, one head of 128
+    n = x.shape[0]
+    cache = random_cache(gen(1), 1, 1, n, 128, 1)
+    want = state(cache)
+    table = torch.zeros(1, 1, dtype=torch.int32)
+    want.write(x.double(), -x.double(), [n], [n], table)
+    quant.kv8_write(x.cuda(), -x.cuda(), cache, table.cuda(), torch.tensor([n], dtype=torch.int32, device="cuda"), starts_of([n]))
+    same(cache, want)
+    k, v = quant.kv8_read(torch.arange(n, dtype=torch.int32, device="cuda"), cache, dtype=F32)
+    assert torch.isfinite(k).all() and torch.equal(k.cpu().double(), want.values(0, torch.arange(n))) and torch.equal(k, -v)
+
+
+def test_cache_held_values_are_rounded_again_at_every_boundary():
+    """A block of every code, and a token that raises the exponent by 1 to 12, or far."""
+    for grow in (*range(0, 13), 40, 200):
+        cache = quant.KV8Cache.allocate(2, 1, 4, 128)
+        codes = torch.arange(256, dtype=torch.int32).to(U8).reshape(2, 128)
+        for t in (cache.k_codes, cache.v_codes):
+            t.view(U8)[0, 0, 1:3] = codes.cuda()
+        e = 30
+        cache.k_exps[0] = cache.v_exps[0] = e
+        want = state(cache)
+        x = torch.full((1, 1, 128), 448.0 * 2.0 ** (e - 127 + grow))
+        table = torch.zeros(1, 1, dtype=torch.int32)
+        want.write(x.double(), x.double(), [1], [4], table)
+        quant.kv8_write(x.cuda(), x.cuda(), cache, table.cuda(), torch.tensor([4], dtype=torch.int32, device="cuda"))
+        assert int(cache.k_exps[0, 0, 0]) == e + grow
+        same(cache, want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_cache_tokens_that_are_not_finite(dtype):
+    g = gen(6)
+    page, d, heads = 32, 64, 3
+    k, v = torch.randn(2, 70, heads, d, generator=g).to(dtype)
+    k[3, 1, 5], v[10, 0, 63], k[40, 2, 0], v[40, 2, 1], v[69, 1, 7] = math.nan, math.inf, -math.inf, 5e4, math.nan
+    cache = random_cache(g, 4, heads, page, d, 16)
+    want = state(cache)
+    table = torch.tensor([[2, 0, 3]], dtype=torch.int32)
+    at = 0
+    for n in (1, 4, 30, 35):                                             # alone in its block, first, and among others
+        want.write(k[at:at + n].double(), v[at:at + n].double(), [n], [at + n], table)
+        quant.kv8_write(k[at:at + n].cuda(), v[at:at + n].cuda(), cache, table.cuda(),
+                        torch.tensor([at + n], dtype=torch.int32, device="cuda"), starts_of([n]))
+        same(cache, want)
+        at += n
+    slots = (table[0, torch.arange(70) // page] * page + torch.arange(70) % page).to(torch.int32)
+    rk, rv = quant.kv8_read(slots.cuda(), cache)
+    bad = torch.zeros(70, heads, dtype=torch.bool)
+    for t, h in ((3, 1), (10, 0), (40, 2), (69, 1)):
+        bad[t, h] = True
+    assert torch.equal(torch.isnan(rk.cpu()).all(-1), bad) and torch.equal(torch.isnan(rk.cpu()).any(-1), bad)
+    assert (rv.cpu()[bad] == 0).all() and torch.isfinite(rv).all()
+
+
+def test_cache_places_outside():
+    """Tokens before place 0, past the table's end, past max_new, in pages outside the cache; sequences of nothing."""
+    g = gen(2)
+    page, block, d, heads = 8, 4, 64, 2
+    news, lens = [5, 6, 4, 3, 2, 0], [3, 20, 9, -4, 2 ** 31 - 1, 16]
+    x = torch.randn(2, sum(news), heads, d, generator=g)
+    table = torch.tensor([[0, 1], [2, 3], [-1, 4], [5, 5], [6, 6], [7, 7]], dtype=torch.int32)
+    for max_new in (None, 6, 3):
+        for bad_page in (9, -2 ** 31, 2 ** 31 - 1):
+            table[2, 1] = bad_page if max_new == 6 else 4
+            cache = random_cache(g, 9, heads, page, d, block)
+            want = state(cache)
+            want.write(x[0].double(), x[1].double(), news, [max(n, 0) for n in lens], table, max_new)
+            quant.kv8_write(x[0].cuda(), x[1].cuda(), cache, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                            starts_of(news), max_new=max_new)
+            same(cache, want)
+    slots = torch.tensor([-1, 72, 3, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda")
+    k, v = quant.kv8_read(slots, cache)
+    assert k[[0, 1, 3, 4]].abs().max() == 0 and v[[0, 1, 3, 4]].abs().max() == 0
+    quant.kv8_write(x[0, :0].cuda(), x[0, :0].cuda(), cache, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                    starts_of([0] * 6))
+    same(cache, want)
+    assert quant.kv8_read(slots[:0], cache)[0].shape == (0, heads, d)
+    wild = torch.tensor([-3, 2, 99, 5, -7, 2 ** 31 - 1, 20], dtype=torch.int32, device="cuda")   # clamped; nothing outside is touched
+    quant.kv8_write(x[0].cuda(), x[1].cuda(), cache, table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), wild)
+    torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------ attention
+
+class Setup:
+    """Sequences in a shuffled paged cache; what no sequence holds is filled with codes of every kind, NaN among them, and
+    exponents that are never written."""
+
+    def __init__(self, lens, news, heads, kv_heads, d, page, block=None, seed=0, spread=1.0):
+        g = gen(seed + 1000 * d + sum(lens))
+        self.lens, self.news, self.d = lens, news, d
+        per = [-(-n // page) for n in lens]
+        pages = sum(per) + 2
+        cache = quant.KV8Cache.allocate(pages, kv_heads, page, d, block)
+        for t in (cache.k_exps, cache.v_exps):
+            t.fill_(255)
+        for t in (cache.k_codes, cache.v_codes):
+            t.view(U8).copy_(torch.randint(0, 256, t.shape, generator=g).to(U8))
+            t.view(U8)[:, :, ::3] = 127
+        order = torch.randperm(pages, generator=g).to(torch.int32)
+        width = max(1, max(per))
+        table = torch.full((len(lens), width), -7, dtype=torch.int32)      # past a sequence's pages: never read
+        at = 0
+        for s in range(len(lens)):
+            table[s, :per[s]] = order[at:at + per[s]]
+            at += per[s]
+        self.cache, self.table = cache, table.cuda()
+        self.lens_d = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        x = torch.randn(2, sum(lens), kv_heads, d, generator=g) * spread
+        quant.kv8_write(x[0].cuda(), x[1].cuda(), cache, self.table, self.lens_d, starts_of(lens), max_new=max(1, max(lens)))
+        now = state(cache)
+        self.k, self.v = ([], [])
+        for s, n in enumerate(lens):
+            slots = table[s, torch.arange(n) // page] * page + torch.arange(n) % page
+            self.k.append(now.values(0, slots)), self.v.append(now.values(1, slots))
+        self.starts = starts_of(news)
+        self.q = (torch.randn(sum(news), heads, d, generator=g) * 1.5).to(BF16)
+        self.scale = d ** -0.5
+
+    def run(self, **k):
+        k.setdefault("max_new", max(1, max(self.news)))
+        k.setdefault("max_len", max(1, max(self.lens)))
+        return quant.attention_kv8(k.pop("q", None) if "q" in k else self.q.cuda(), self.cache, self.table, self.lens_d,
+                                   starts=k.pop("starts", self.starts), **k)
+
+    def check(self, got, **k):
+        want, tol = ref.attention(self.q, self.k, self.v, self.news, self.lens, self.scale, **k)
+        off = (got.cpu().double() - want).abs()
+        assert not torch.isnan(off).any()
+        assert (off <= tol).all(), (float((off / tol).max()), (off > tol).nonzero()[:4].tolist())
+
+
+TOKENS = [   # lens, heads, kv heads, head dim, page, block
+    ([1], 1, 1, 32, 1, 1), ([17], 4, 1, 64, 16, 16), ([5, 0, 40], 8, 8, 96, 7, 7), ([100, 33, 64, 31], 32, 8, 128, 16, 16),
+    ([260, 1], 12, 4, 64, 48, 16), ([70, 129], 6, 2, 192, 100, 50), ([90, 257], 16, 2, 256, 64, 64), ([63, 500], 40, 1, 128, 32, 8),
+    ([1500, 700, 2], 16, 1, 64, 64, 64), ([40, 128], 71, 1, 64, 64, 1), ([3000], 8, 2, 128, 64, 32), ([5000, 4100], 2, 1, 32, 128, 128)]
+
+
+@pytest.mark.parametrize("lens,heads,kv,d,page,block", TOKENS)
+def test_attention_of_single_tokens(lens, heads, kv, d, page, block):
+    s = Setup(lens, [1] * len(lens), heads, kv, d, page, block)
+    s.check(s.run())
+    s.check(s.run(starts=None))                            # one query each is what no starts means
+    s.check(s.run(window=20), window=20)
+    s.check(s.run(max_len=None))                           # the table's width as the bound: other splits
+
+
+CHUNKS = [   # lens, news, heads, kv heads, head dim, page, block
+    ([3], [3], 1, 1, 32, 16, 8), ([40, 9, 77], [7, 9, 0], 4, 2, 64, 16, 16), ([130, 20], [17, 20], 8, 1, 128, 48, 16),
+    ([200, 64, 65], [64, 64, 65], 2, 2, 96, 32, 32), ([300], [129], 6, 2, 128, 64, 64), ([150, 90], [150, 33], 4, 1, 256, 64, 16),
+    ([97], [97], 3, 1, 192, 10, 5), ([700, 3], [5, 3], 3, 3, 64, 64, 64), ([900, 333], [300, 333], 8, 2, 64, 64, 32),
+    ([520], [260], 10, 2, 128, 16, 4)]
+
+
+@pytest.mark.parametrize("lens,news,heads,kv,d,page,block", CHUNKS)
+def test_attention_of_chunks_and_prompts(lens, news, heads, kv, d, page, block):
+    s = Setup(lens, news, heads, kv, d, page, block)
+    s.check(s.run())
+    s.check(s.run(window=13), window=13)
+    s.check(s.run(causal=False), causal=False)
+    s.check(s.run(max_new=None, max_len=None))
+
+
+@pytest.mark.parametrize("d", [32, 64, 96, 128, 192, 256])
+def test_attention_of_many_rows_at_the_edges_of_tiles(d):
+    """Prompts that end at, before and after the 32 and 64 cached tokens that are worked on together, one split in two."""
+    lens = [1, 31, 32, 33, 63, 64, 65, 95, 96, 97, 127, 128, 129]
+    s = Setup(lens, lens, 8, 2, d, 24, 8)
+    s.check(s.run())
+    s.check(s.run(window=33), window=33)
+    s.check(s.run(causal=False), causal=False)
+    s = Setup([1100], [70], 4, 1, d, 24)
+    s.check(s.run())
+    s.check(s.run(window=600), window=600)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_rows_that_see_nothing(d):
+    """Empty sequences, and more queries than cached places: the first ones stand before the start."""
+    s = Setup([0, 2, 5], [3, 6, 5], 4, 2, d, 16)
+    out = s.run()
+    s.check(out)
+    assert out[:7].abs().max() == 0 and out[7].abs().max() > 0
+    s.check(s.run(window=2), window=2)
+    s.check(s.run(causal=False, window=1), causal=False, window=1)
+
+
+@pytest.mark.parametrize("news", [[1, 1], [9, 30], [60, 200]])
+def test_attention_extreme_scores(news):
+    """Scores of several hundred, both signs: one weight takes all, or the running maximum moves often."""
+    s = Setup([250, 400], news, 4, 2, 64, 32, 16, spread=60.0)
+    s.check(s.run())
+    s = Setup([250, 400], news, 4, 2, 64, 32, 16, spread=1e-3)
+    s.check(s.run())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("news", [1, 4, 40, 200])
+def test_attention_keys_and_values_that_are_not_finite(news, d):
+    """A token with a NaN makes NaN of the rows that see it, in its key head, and of no other."""
+    for which in (0, 1):
+        s = Setup([300], [news], 4, 2, d, 16)
+        bad = 300 - max(1, news // 2)                       # half of the queries stand before it
+        page, place = int(s.table[0, bad // 16]), bad % 16
+        x = torch.zeros(2, 1, 2, d)                         # one block of one place in that page's stead: written alone
+        x[which, 0, 1, 40] = math.nan
+        one = quant.KV8Cache.allocate(1, 2, 1, d)
+        quant.kv8_write(x[0].cuda(), x[1].cuda(), one, torch.zeros(1, 1, dtype=torch.int32, device="cuda"),
+                        torch.ones(1, dtype=torch.int32, device="cuda"))
+        s.cache.k_codes.view(U8)[page, :, place] = one.k_codes.view(U8)[0, :, 0]
+        s.cache.v_codes.view(U8)[page, :, place] = one.v_codes.view(U8)[0, :, 0]
+        s.k[0][bad], s.v[0][bad] = 0.0, 0.0
+        out = s.run().cpu()
+        sees = torch.arange(300 - news, 300) >= bad
+        assert torch.isnan(out[sees][:, 2:]).all() and not torch.isnan(out[:, :2]).any() and not torch.isnan(out[~sees]).any()
+        want, tol = ref.attention(s.q, s.k, s.v, [news], [300], s.scale)
+        keep = torch.ones(news, 4, dtype=torch.bool)
+        keep[sees, 2:] = False
+        assert ((out.double() - want).abs() <= tol)[keep].all()
+
+
+@pytest.mark.parametrize("news", [[1, 1, 1], [5, 21, 70]])
+def test_attention_strided_rows(news):
+    s = Setup([200, 64, 90], news, 4, 2, 128, 16)
+    n = sum(news)
+    wide = torch.zeros(n, 4 * 128 + 57, dtype=BF16, device="cuda")
+    q = wide[:, 9:9 + 512].unflatten(1, (4, 128))           # rows at odd elements
+    q.copy_(s.q)
+    hold = torch.full((n, 600), 7.0, dtype=BF16, device="cuda")
+    out = hold[:, 33:33 + 512].unflatten(1, (4, 128))
+    s.check(s.run(q=q, out=out))
+    assert (hold[:, :33] == 7).all() and (hold[:, 33 + 512:] == 7).all()
+
+
+# Rows of a key head as tokens x heads of its group, and the kernel that they reach.
+FEW = [(32, 1, 1, 1), (32, 17, 1, 2), (32, 33, 1, 4), (64, 5, 3, 1), (64, 10, 3, 2), (64, 64, 1, 4), (96, 4, 4, 1), (96, 8, 4, 2),
+       (128, 2, 8, 1), (128, 6, 3, 2), (128, 32, 1, 2), (192, 16, 1, 1), (256, 4, 4, 1)]
+MANY = [(32, 65, 1, "wide"), (64, 13, 5, "wide"), (96, 33, 1, "steps"), (128, 11, 3, "steps"), (192, 17, 1, "wide"), (256, 3, 6, "wide")]
+
+
+@pytest.mark.parametrize("d,new,group,nb", FEW + MANY)
+def test_attention_of_every_kernel(d, new, group, nb):
+    """Lengths past one split, ragged, with a window that leaves one split and one that leaves several."""
+    kv = 2
+    s = Setup([900, 437, 391], [new, new - new // 3, new], kv * group, kv, d, 40, 8)
+    kernel = f"attend_kv8_{nb}_kernel<{d}>" if isinstance(nb, str) else f"attend_kv8_kernel<{d}, {nb}>"
+    for k in (dict(), dict(causal=False), dict(window=700), dict(window=29)):
+        name, n = quant.attention_kv8_describe(s.cache, 3, kv * group, new, 900, **k)
+        assert name.split(" + ")[0] == kernel and n == name.count(" + ") + 1
+        s.check(s.run(**k), **k)
+    name, n = quant.attention_kv8_describe(s.cache, 3, kv * group, new, 4000)
+    assert name == kernel + f" + attend_join_kernel<{d}>"
+    s.check(s.run(max_len=4000))
+
+
+def test_attention_is_the_same_bits_again_and_on_another_stream():
+    s = Setup([2500, 900], [1, 1], 16, 4, 128, 64)
+    first = s.run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    again = [s.run(stream=side) for _ in range(3)]
+    side.synchronize()
+    assert all(torch.equal(first, x) for x in again)
+
+
+def test_bounds_in_device_data_are_clamped():
+    """Lengths past the bound, starts past the queries, pages outside the cache: nothing outside the buffers is touched."""
+    s = Setup([100, 50], [1, 3], 4, 2, 64, 16)
+    lens = torch.tensor([10 ** 9, -5], dtype=torch.int32, device="cuda")
+    table = torch.randint(-2 ** 31, 2 ** 31 - 1, (2, 7), dtype=torch.int32, device="cuda")
+    starts = torch.tensor([-3, 2, 99], dtype=torch.int32, device="cuda")
+    out = quant.attention_kv8(s.q.cuda(), s.cache, table, lens, starts=starts, max_new=4, max_len=112)
+    torch.cuda.synchronize()
+    assert out.shape == s.q.shape
+
+
+def test_cache_beyond_32_bit_offsets():
+    """Codes of more than 2^32 bytes: tokens in the last page, written, read back and attended."""
+    heads, page, d = 8, 64, 128
+    pages = (1 << 32) // (heads * page * d) + 100
+    cache = quant.KV8Cache.allocate(pages, heads, page, d, 16)
+    assert cache.k_codes.numel() > 1 << 32
+    g = gen(8)
+    n = 40
+    x = torch.randn(2, n, heads, d, generator=g)
+    table = torch.tensor([[pages - 1]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    quant.kv8_write(x[0].cuda(), x[1].cuda(), cache, table, lens, starts_of([n]))
+    want = ref.KV8([torch.zeros(1, heads, page, d, dtype=U8)] * 2, [torch.full((1, heads, 4), 127, dtype=U8)] * 2)
+    want.write(x[0].double(), x[1].double(), [n], [n], torch.zeros(1, 1, dtype=torch.int32))
+    k, v = (want.values(i, torch.arange(n)) for i in (0, 1))
+    slots = torch.arange((pages - 1) * page, (pages - 1) * page + n, dtype=torch.int64).to(torch.int32).cuda()
+    rk, rv = quant.kv8_read(slots, cache)
+    assert torch.equal(rk.cpu().double(), k) and torch.equal(rv.cpu().double(), v)
+    for news in (1, 40):
+        q = torch.randn(news, 16, d, generator=g).to(BF16)
+        out = quant.attention_kv8(q.cuda(), cache, table, lens, starts=starts_of([news]), max_new=news)
+        want_o, tol = ref.attention(q, [k], [v], [news], [n], d ** -0.5)
+        assert ((out.cpu().double() - want_o).abs() <= tol).all()
+
+
+# ------------------------------------------------------------------ streams and graphs
+
+def test_streams_given_by_their_handles():
+    """A stream as torch's object, as its handle, and the default stream as 0: outputs and workspaces made for it."""
+    g = gen(12)
+    x = torch.randn(40, 333, generator=g).to(BF16).cuda()
+    s = Setup([2500, 900], [1, 1], 16, 4, 128, 64)
+    q, e = quant.rows_f8(x)
+    y, a = quant.matmul_f8(q, e, q, e), s.run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream, 0, torch.cuda.default_stream()):
+        got = quant.rows_f8(x, stream=stream)
+        again = [got[0].view(U8), quant.matmul_f8(*got, *got, stream=stream), s.run(stream=stream)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(m, n) for m, n in zip(again, (q.view(U8), y, a)))
+
+
+def test_a_run_of_them_as_a_graph():
+    """Norm, product, cache and attention captured together and replayed, eager work between the replays."""
+    g = gen(13)
+    heads, kv, d, n, page = 8, 2, 64, 3, 16
+    width = (heads + 2 * kv) * d
+    x = torch.randn(n, 500, generator=g).to(BF16).cuda()
+    w, we = quant.rows_f8((torch.randn(width, 500, generator=g) * 0.06).cuda())
+    table = torch.randperm(3 * n, generator=g).reshape(n, 3).to(torch.int32).cuda()
+    cache = quant.KV8Cache.allocate(3 * n, kv, page, d)
+    lens = torch.tensor([5, 16, 32], dtype=torch.int32, device="cuda")
+    before = [t.clone() for t in (cache.k_codes.view(U8), cache.k_exps, cache.v_codes.view(U8), cache.v_exps)]
+
+    def run():
+        q, e, scale, _ = quant.rmsnorm_f8(x)
+        y = quant.matmul_f8(q, e, w, we, a_scale=scale).unflatten(1, (-1, d))
+        quant.kv8_write(y[:, heads:heads + kv], y[:, heads + kv:], cache, table, lens)
+        return quant.attention_kv8(y[:, :heads], cache, table, lens, max_len=48)
+
+    def reset():
+        for t, b in zip((cache.k_codes.view(U8), cache.k_exps, cache.v_codes.view(U8), cache.v_exps), before):
+            t.copy_(b)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    reset()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for i in range(4):
+        x.copy_(torch.randn(n, 500, generator=g).to(BF16))
+        reset()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, held = out.clone(), cache.k_codes.view(U8).clone()
+        reset()
+        assert torch.equal(run(), got) and torch.equal(cache.k_codes.view(U8), held)
+
+
+# ------------------------------------------------------------------ refusals through the binding
+
+def test_binding_refusals():
+    x = torch.zeros(4, 64, dtype=BF16, device="cuda")
+    a = torch.zeros(4, 64, device="cuda").to(quant.F8)
+    e = torch.full((4, 1), 127, dtype=U8, device="cuda")
+    one = torch.ones(4, device="cuda")
+    cache = quant.KV8Cache.allocate(2, 2, 16, 64)
+    q = torch.zeros(2, 4, 64, dtype=BF16, device="cuda")
+    table = torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    lens = torch.ones(2, dtype=torch.int32, device="cuda")
+    kv = torch.zeros(2, 2, 64, dtype=BF16, device="cuda")
+    bad = [
+        lambda: quant.rmsnorm_f8(x.half()), lambda: quant.rmsnorm_f8(x.t()), lambda: quant.rmsnorm_f8(x, weight=one),
+        lambda: quant.rmsnorm_f8(x, residual=x.float()), lambda: quant.rmsnorm_f8(x, h=x), lambda: quant.rmsnorm_f8(x, eps=-1.0),
+        lambda: quant.rmsnorm_f8(x[:1].expand(4, 64)), lambda: quant.rows_f8(x[0]), lambda: quant.rows_f8(x, q=a[:2]),
+        lambda: quant.rows_f8(x, q=a.view(U8)), lambda: quant.rows_f8(x, exps=e[:3]), lambda: quant.rmsnorm_f8(x, scale=one[:3]),
+        lambda: quant.matmul_f8(a, e, a[:, :32], e), lambda: quant.matmul_f8(a, e[:2], a, e), lambda: quant.matmul_f8(a, e, a, e.float()),
+        lambda: quant.matmul_f8(x, e, a, e), lambda: quant.matmul_f8(a, e, a, e, bias=one[:3]),
+        lambda: quant.matmul_f8(a, e, a, e, a_scale=one[:3]), lambda: quant.matmul_f8(a, e, a, e, a_scale=one.double()),
+        lambda: quant.matmul_f8(a, e, a, e, residual=torch.zeros(4, 4, device="cuda")),
+        lambda: quant.matmul_f8(a, e, a, e, out_dtype=torch.float16),
+        lambda: quant.KV8Cache(cache.k_codes, cache.k_exps, cache.v_codes[:1], cache.v_exps),
+        lambda: quant.KV8Cache(cache.k_codes, cache.k_codes, cache.v_codes, cache.v_exps),
+        lambda: quant.KV8Cache(cache.k_codes.view(U8), cache.k_exps, cache.v_codes, cache.v_exps),
+        lambda: quant.KV8Cache.allocate(2, 2, 16, 64, 5), lambda: quant.KV8Cache.allocate(2, 2, 512, 64),
+        lambda: quant.KV8Cache.allocate(2, 2, 16, 48),
+        lambda: quant.kv8_write(kv, kv.float(), cache, table, lens), lambda: quant.kv8_write(kv, kv, cache, table, lens.long()),
+        lambda: quant.kv8_write(q, q, cache, table, lens), lambda: quant.kv8_write(kv[:1], kv[:1], cache, table, lens),
+        lambda: quant.kv8_write(kv, kv, cache, table[0], lens), lambda: quant.kv8_write(kv, kv, cache, table, lens, max_new=0),
+        lambda: quant.kv8_write(kv, kv, cache, table, lens, starts=lens), lambda: quant.kv8_write(kv, kv, None, table, lens),
+        lambda: quant.kv8_read(lens, cache, dtype=torch.float16),
+        lambda: quant.attention_kv8(q.float(), cache, table, lens), lambda: quant.attention_kv8(q[:1], cache, table, lens),
+        lambda: quant.attention_kv8(q[..., :32], cache, table, lens), lambda: quant.attention_kv8(q, cache, table.long(), lens),
+        lambda: quant.attention_kv8(q, cache, table, lens[:1]), lambda: quant.attention_kv8(q, cache, table, lens, starts=lens),
+        lambda: quant.attention_kv8(q, quant.KV4Cache.allocate(2, 2, 16, 64), table, lens),
+        lambda: quant.attention_kv8(q[:, :3], cache, table, lens), lambda: quant.attention_kv8(q, cache, table, lens, max_len=0),
+        lambda: quant.attention_kv8(q, cache, table, lens, scale=math.inf), lambda: quant.attention_kv8(q, cache, table, lens, window=1 << 31),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises((ValueError, TypeError, miconv.MiconvError)):
+            f()
+            print("case", i)
