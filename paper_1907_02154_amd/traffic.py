@@ -102,6 +102,7 @@ SOURCES = {
     "matmul_i8_tile_kernel": "quant_matmul.hip",
     "matmul_i8_align_kernel": "quant_matmul.hip",
     "rows_i8_kernel": "quant_rows.hip",
+    "sample_rows_kernel": "sample.hip",
     "rows_i8_long_kernel": "quant_rows.hip",
 }
 
