@@ -10,19 +10,23 @@
 #include "../../include/misample.h"
 #include "quant.h"
 
+#include <type_traits>
+
 namespace miconv {
 namespace {
 
 using quant::kBF16;
 using quant::kF32;
 using quant::load1;
-using quant::load8;
 using quant::misaligned;
 
 typedef unsigned long long u64;
 
 constexpr float kNegInf = -__builtin_inff();
-constexpr int kBins = 2048, kList = 4096;   // bins of a histogram; candidates that LDS holds
+constexpr int kList = 4096;                 // candidates that LDS holds, and partial sums of a row
+constexpr int kDigit = 2048;                // values of a digit of the radix search
+constexpr int kValueThreads = 1024;          // of a work-group, for bf16 rows of more than 4096
+constexpr int kThreads = 512;                // for other rows of more than 4096
 constexpr int kUnit = 512;                  // tokens that a wavefront takes together, 8 a lane
 
 struct SampleArgs {
@@ -50,228 +54,370 @@ __device__ __forceinline__ float logit_of(uint32_t k)
 // A token's place in the order of logit, then index: all are distinct.
 __device__ __forceinline__ u64 place_of(float x, int i) { return (u64)key_of(x) << 32 | (uint32_t)~i; }
 
-// 2^t for t <= 0, by the series of exp: |f ln 2| <= .35, the first term left out 6e-15.
-__device__ __forceinline__ double power_of(double t, int shift)
+// Of a row: how a logit's weight follows from it.
+//
+// 2^t with t = (x - top) log2(e) / T is the power of two of t's whole part, the
+// entry of a table (in LDS) for the next six bits, and the series of exp for the
+// rest f: |f ln 2| <= .0055, the first term left out 4e-17.  Weights are this times
+// 2^shift, and smaller than half a grain where t passes -(shift + 3).
+constexpr int kTable = 64;
+struct Row {
+    double top, factor, least;   // the largest logit; log2(e) / temperature; the x - top from which on weights are 0
+    const double *table;
+    int shift;
+    __device__ __forceinline__ double share(float x) const
+    {
+        constexpr double kRound = 0x1.8p52 / kTable;   // added, leaves multiples of 1 / kTable
+        const double d = fmax((double)x - top, least);
+        const double up = fma(d, factor, kRound);
+        const double f = fma(d, factor, kRound - up);
+        const int n = (int)(uint32_t)__builtin_bit_cast(u64, up);   // 64 t, rounded
+        double p = 1.33335581464284434234e-3;
+        p = fma(p, f, 9.61812910762847716198e-3);
+        p = fma(p, f, 5.55041086648215799532e-2);
+        p = fma(p, f, 2.40226506959100712334e-1);
+        p = fma(p, f, 6.93147180559945309417e-1);
+        p = fma(p, f, 1.0);
+        const u64 w = __builtin_bit_cast(u64, p * table[n & (kTable - 1)]);
+        return __builtin_bit_cast(double, w + ((u64)(uint32_t)((n >> 6) + shift) << 52));
+    }
+    static __device__ __forceinline__ u64 whole(double w)
+    {
+        return __builtin_bit_cast(u64, w + 0x1p52) & ((1ull << 52) - 1);   // at most 2^51: the sum's low bits
+    }
+    __device__ __forceinline__ u64 weight(float x) const { return whole(share(x)); }
+};
+
+// Sums over a wavefront's lanes up to each, by the data paths between lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v, uint32_t none = 0)
 {
-    t = fmax(t, -1100.0);
-    const double n = rint(t), f = t - n;
-    double p = 4.44553827187081149760e-10;
-    p = fma(p, f, 7.05491162080112332987e-9);
-    p = fma(p, f, 1.01780860092396997275e-7);
-    p = fma(p, f, 1.32154867901443094885e-6);
-    p = fma(p, f, 1.52527338040598402800e-5);
-    p = fma(p, f, 1.54035303933816099544e-4);
-    p = fma(p, f, 1.33335581464284434234e-3);
-    p = fma(p, f, 9.61812910762847716198e-3);
-    p = fma(p, f, 5.55041086648215799532e-2);
-    p = fma(p, f, 2.40226506959100712334e-1);
-    p = fma(p, f, 6.93147180559945309417e-1);
-    p = fma(p, f, 1.0);
-    return ldexp(p, (int)n + shift);
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 plus_lane(u64 v)
+{
+    return v + ((u64)from_lane<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | from_lane<CTRL, ROWS>((uint32_t)v));
+}
+__device__ __forceinline__ u64 wave_scan(u64 v)
+{
+    v = plus_lane<0x111, 0xF>(v);   // from 1, 2, 4 and 8 lanes before, within 16
+    v = plus_lane<0x112, 0xF>(v);
+    v = plus_lane<0x114, 0xF>(v);
+    v = plus_lane<0x118, 0xF>(v);
+    v = plus_lane<0x142, 0xA>(v);   // the last of 16 to the next 16, of 32 to the next 32
+    return plus_lane<0x143, 0xC>(v);
+}
+__device__ __forceinline__ u64 last_lane(u64 v)
+{
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ u64 wave_sum(u64 v) { return last_lane(wave_scan(v)); }
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+    v = max(v, from_lane<0x111, 0xF>(v));
+    v = max(v, from_lane<0x112, 0xF>(v));
+    v = max(v, from_lane<0x114, 0xF>(v));
+    v = max(v, from_lane<0x118, 0xF>(v));
+    v = max(v, from_lane<0x142, 0xA>(v));
+    v = max(v, from_lane<0x143, 0xC>(v));
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
-struct Row {
-    double top, factor;   // the largest logit; log2(e) / temperature
-    int shift;
-    // The weight over the largest, and as a whole number.
-    __device__ __forceinline__ double share(float x) const { return power_of(((double)x - top) * factor, 0); }
-    __device__ __forceinline__ u64 weight(float x) const
+// A lane's 8 logits of a unit as they are held.  At a row's end a lane reads the
+// last 8, of which those before its own count as minus infinity: no load depends
+// on a branch, or each would be waited for.  (Rows of fewer than 8 are read one
+// by one.)
+typedef uint32_t words_at_2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t words_at_4 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T, bool SHORT>
+struct Held {
+    typedef typename std::conditional<sizeof(T) == 2, words_at_2, words_at_4>::type words;
+    words w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T *x, int vocab, int unit, int lane)
     {
-        const double w = power_of(((double)x - top) * factor, shift) + 0x1p52;   // at most 2^51: the sum's low bits
-        return __builtin_bit_cast(u64, w) & ((1ull << 52) - 1);
+        const int at = unit * kUnit + lane * 8;
+        if constexpr (SHORT) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t b = __builtin_bit_cast(uint32_t, at + i < vocab ? load1(x + at + i) : kNegInf);
+                if constexpr (sizeof(T) == 4) w[i / 4][i % 4] = b;
+                else w[0][i / 2] = i % 2 ? (w[0][i / 2] & 0xFFFFu) | (b & 0xFFFF0000u) : b >> 16;
+            }
+        } else {
+            const words *p = (const words *)(x + min(at, vocab - 8));
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = p[i];
+        }
+    }
+    // The logits, and the index of the first.
+    __device__ __forceinline__ int widen(float (&v)[8], int vocab, int unit, int units, int lane) const
+    {
+        const int at = unit * kUnit + lane * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t b = sizeof(T) == 4 ? w[i / 4 % (sizeof(T) / 2)][i % 4] : i % 2 ? w[0][i / 2] & 0xFFFF0000u : w[0][i / 2] << 16;
+            v[i] = __builtin_bit_cast(float, b);
+        }
+        if (SHORT || unit < units - 1) return at;
+        const int from = min(at, vocab - 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = from + i < at ? kNegInf : v[i];
+        return from;
     }
 };
 
-// A lane's 8 logits of a unit; minus infinity past the row's end.
-template <typename T>
-__device__ __forceinline__ void unit_of(const T *x, int vocab, int unit, int lane, float (&v)[8])
+// The first n of the list in order, the largest first.  (Up to a few wavefronts each thread counts what comes before its
+// own: one round of reads against a barrier for each of log^2 steps.)
+template <int NT>
+__device__ __forceinline__ void sort_list(u64 *list, int n, int tid)
 {
-    const int at = unit * kUnit + lane * 8;
-    if (at + 8 <= vocab) {
-        load8(x + at, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = at + i < vocab ? load1(x + at + i) : kNegInf;
+    if (n <= 256) {
+        const u64 mine = tid < n ? list[tid] : 0;
+        int rank = 0;
+        if (tid / 64 * 64 < n)
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) rank += list[i] > mine;
+        __syncthreads();
+        if (tid < n) list[rank] = mine;
+        __syncthreads();
+        return;
     }
+    int size = 512;
+    while (size < n) size *= 2;
+    for (int i = n + tid; i < size; i += NT) list[i] = 0;
+    __syncthreads();
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            for (int t = tid; t < size / 2; t += NT) {
+                const int i = 2 * t - (t & (j - 1)), o = i + j;   // the t-th pair j apart
+                const u64 p = list[i], q = list[o];
+                if ((p < q) == ((i & k) == 0)) list[i] = q, list[o] = p;
+            }
+            __syncthreads();
+        }
 }
 
-template <typename V, typename F>
-__device__ __forceinline__ V wave_reduce(V v, F f)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v = f(v, (V)__shfl_xor(v, d));
-    return v;
-}
-
-template <typename T, int NT>
+template <typename T, int NT, bool SHORT>
 struct Picker {
-    static constexpr int WAVES = NT / 64;
+    static constexpr int WAVES = NT / 64, BINS = NT > 256 ? 8192 : kDigit;   // BINS: of logits, 32 bits each
     struct Shared {
-        u64 list[kList];
-        u64 bins[kBins];
-        u64 part[WAVES], found;
-        int count;
+        u64 list[kList], sums[NT > 256 ? kList : 8];
+        union {
+            uint32_t counts[BINS];
+            u64 digits[kDigit];
+        };
+        double table[kTable];
+        u64 part[2][WAVES], ahead, with;
+        float guess[WAVES];
+        int found, count;
     };
     const SampleArgs &a;
     Shared &s;
     const T *x;
-    int tid, lane, wave;
+    const int tid, lane, wave;
     Row row;
-    float top, inv;   // bins: (top - x) * inv
-    int last;
+    float anchor, inv;   // bins: (anchor - x) * inv
+    int turn = 0;        // the half of s.part that is free
 
-    __device__ Picker(const SampleArgs &args, Shared &sh, long r)
+    __device__ __forceinline__ Picker(const SampleArgs &args, Shared &sh, long r)
         : a(args), s(sh), x((const T *)args.x + r * args.stride), tid(threadIdx.x), lane(threadIdx.x % 64),
           wave(__builtin_amdgcn_readfirstlane(threadIdx.x / 64))
     {
     }
 
-    // f(logit, index) of every token, and of some past the row's end as minus infinity.
+    // f(logits, first index, unit) of every lane's 8 tokens of a unit, those past the row's end as minus infinity.
+    template <typename F>
+    __device__ __forceinline__ void units(F f)
+    {
+        constexpr int U = 3;   // units of a wavefront in flight
+        Held<T, SHORT> h[U];
+#pragma unroll
+        for (int n = 0; n < U; ++n) h[n].load(x, a.vocab, min(wave + n * WAVES, a.units - 1), lane);
+#pragma unroll 1
+        for (int unit = wave; unit < a.units; unit += WAVES) {
+            float v[8];
+            const int at = h[0].widen(v, a.vocab, unit, a.units, lane);
+#pragma unroll
+            for (int n = 0; n < U - 1; ++n) h[n] = h[n + 1];
+            h[U - 1].load(x, a.vocab, min(unit + U * WAVES, a.units - 1), lane);
+            f(v, at, unit);
+        }
+    }
+    // f(logit, index) of every token.
     template <typename F>
     __device__ __forceinline__ void scan(F f)
     {
-        constexpr int U = 2;
-        for (int u0 = wave; u0 < a.units; u0 += U * WAVES) {
-            float v[U][8];
+        units([&](const float (&v)[8], int at, int) {
 #pragma unroll
-            for (int n = 0; n < U; ++n) unit_of(x, a.vocab, u0 + n * WAVES, lane, v[n]);
-#pragma unroll
-            for (int n = 0; n < U; ++n)
-                if (u0 + n * WAVES < a.units)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f(v[n][i], (u0 + n * WAVES) * kUnit + lane * 8 + i);
-        }
+            for (int i = 0; i < 8; ++i) f(v[i], at + i);
+        });
     }
-    template <typename F>
-    __device__ __forceinline__ u64 reduce(u64 v, F f)   // over the work-group, for every thread
+    // The work-group's values of a wavefront each, for every thread; one barrier, since the halves take turns.
+    __device__ __forceinline__ const u64 *share_out(u64 v)
     {
-        v = wave_reduce(v, f);
+        u64 *p = s.part[turn];
+        turn ^= 1;
+        if (lane == 0) p[wave] = v;
         __syncthreads();
-        if (lane == 0) s.part[wave] = v;
-        __syncthreads();
-        v = s.part[0];
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i) v = f(v, s.part[i]);
-        return v;
+        return p;
     }
     __device__ __forceinline__ u64 sum(u64 v)
     {
-        return reduce(v, [](u64 p, u64 q) { return p + q; });
+        const u64 *p = share_out(wave_sum(v));
+        u64 all = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) all += p[i];
+        return all;
+    }
+    __device__ __forceinline__ uint32_t largest(uint32_t v)
+    {
+        const u64 *p = share_out(wave_max(v));
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) m = max(m, (uint32_t)p[i]);
+        return m;
     }
     // The sum of v over the threads before this one; *all: over every thread.
     __device__ __forceinline__ u64 before(u64 v, u64 *all)
     {
-        u64 in = v;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const u64 o = __shfl_up(in, d);
-            if (lane >= d) in += o;
-        }
-        __syncthreads();
-        if (lane == 63) s.part[wave] = in;
-        __syncthreads();
+        const u64 in = wave_scan(v);
+        const u64 *p = share_out(last_lane(in));
         u64 base = 0, total = 0;
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) {
-            if (i < wave) base += s.part[i];
-            total += s.part[i];
+            if (i < wave) base += p[i];
+            total += p[i];
         }
         *all = total;
         return base + in - v;
     }
-    __device__ __forceinline__ int bin_of(float v) const { return (int)fminf((top - v) * inv, (float)(kBins - 1)); }
+    __device__ __forceinline__ int bin_of(float v) const { return (int)fminf(fmaxf((anchor - v) * inv, 0.0f), (float)(BINS - 1)); }
 
-    __device__ __forceinline__ void clear_bins()
+    template <typename V, int N>
+    __device__ __forceinline__ void clear(V (&bins)[N])
     {
-        __syncthreads();
-        for (int i = tid; i < kBins; i += NT) s.bins[i] = 0;
+        for (int i = tid; i < N; i += NT) bins[i] = 0;
         __syncthreads();
     }
-    // The bin in whose sums, added up from the first, `end(sum before, sum with it)` holds; *ahead: the sum before it.
-    template <typename F>
-    __device__ __forceinline__ int crossing(F end, u64 *ahead, u64 *with)
+    // The bin in whose sums, added up from the first, `end(sum before, sum with it)` holds; these sums.
+    template <typename V, int N, typename F>
+    __device__ __forceinline__ int crossing(const V (&bins)[N], F end, u64 *ahead, u64 *with)
     {
-        constexpr int PER = kBins / NT;
-        __syncthreads();
-        u64 own[PER], total = 0, all;
+        constexpr int PER = N / NT;
+        u64 total = 0, all;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) own[i] = s.bins[tid * PER + i], total += own[i];
+        for (int i = 0; i < PER; ++i) total += bins[tid * PER + i];
         u64 b = before(total, &all);
-        __syncthreads();
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            if (end(b, b + own[i])) s.found = (u64)(tid * PER + i), s.part[0] = b, s.part[WAVES - 1] = b + own[i];
-            b += own[i];
+            const u64 w = b + bins[tid * PER + i];
+            if (end(b, w)) s.found = tid * PER + i, s.ahead = b, s.with = w;
+            b = w;
         }
         __syncthreads();
-        *ahead = s.part[0], *with = s.part[WAVES - 1];
-        return (int)s.found;
+        *ahead = s.ahead, *with = s.with;
+        return s.found;
+    }
+    // Bins between which the weights of the counted tokens, each taken to lie in the middle of its bin, pass a share p of
+    // theirs and `over` more, which come first: where they reach a 512th less, -1 if `over` does, and a 512th more.  (That
+    // covers what the middles are off by, also where few logits are possible and lie many bins apart.)
+    __device__ __forceinline__ void guess(float p, float over, int *from, int *to)
+    {
+        constexpr int PER = BINS / NT;
+        const float step = -(float)row.factor / inv, first = (anchor - (float)row.top) * (float)row.factor;
+        float in = 0.0f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            in += (float)s.counts[tid * PER + i] * __builtin_amdgcn_exp2f(first + step * ((float)(tid * PER + i) + 0.5f));
+        const float mine = in;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const float o = __shfl_up(in, d);
+            if (lane >= d) in += o;
+        }
+        if (lane == 63) s.guess[wave] = in;
+        if (tid == 0) s.found = -1, s.count = BINS - 1;
+        __syncthreads();
+        float b = in - mine + over, total = over;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            if (i < wave) b += s.guess[i];
+            total += s.guess[i];
+        }
+        const float less = p * total * (511.0f / 512.0f), more = fminf(p * total * (513.0f / 512.0f), total * 0.99999f);
+        if ((b < less && less <= b + mine) || (b < more && more <= b + mine))   // a thread's bins again
+#pragma unroll 1
+            for (int i = 0; i < PER; ++i) {
+                const int n = tid * PER + i;
+                const float w = (float)s.counts[n] * __builtin_amdgcn_exp2f(first + step * ((float)n + 0.5f));
+                if (b < less && less <= b + w) s.found = n;
+                if (b < more && more <= b + w) s.count = n;
+                b += w;
+            }
+        __syncthreads();
+        *from = s.found, *to = more <= over ? -1 : s.count;
     }
     // The places of the tokens for which f holds into the list; how many there are, also where that is more than it holds.
     template <typename F>
     __device__ __forceinline__ int gather(F f)
     {
-        __syncthreads();
         if (tid == 0) s.count = 0;
         __syncthreads();
         scan([&](float v, int i) {
-            if (f(v, i)) {
-                const int at = atomicAdd(&s.count, 1);
-                if (at < kList) s.list[at] = place_of(v, i);
-            }
+            if (f(v, i)) put(v, i);
         });
         __syncthreads();
         return s.count;
     }
-    // The first n of the list in order, the largest first.
-    __device__ __forceinline__ void sort(int n)
+    __device__ __forceinline__ void put(float v, int i)
     {
-        int size = 2;
-        while (size < n) size *= 2;
-        for (int i = n + tid; i < size; i += NT) s.list[i] = 0;
-        __syncthreads();
-        for (int k = 2; k <= size; k *= 2)
-            for (int j = k / 2; j > 0; j /= 2) {
-                for (int t = tid; t < size / 2; t += NT) {
-                    const int i = 2 * t - (t & (j - 1)), o = i + j;   // the t-th pair j apart
-                    const u64 p = s.list[i], q = s.list[o];
-                    if ((p < q) == ((i & k) == 0)) s.list[i] = q, s.list[o] = p;
-                }
-                __syncthreads();
-            }
+        const int at = atomicAdd(&s.count, 1);
+        if (at < kList) s.list[at] = place_of(v, i);
     }
+    __device__ __forceinline__ void sort(int n) { sort_list<NT>(s.list, n, tid); }
+    __device__ __forceinline__ float listed(int i) const { return logit_of((uint32_t)(s.list[i] >> 32)); }
     // Of the first n of the sorted list, how many have less than `most` before them, whose weights follow `ahead`; one at least.
     __device__ __forceinline__ int fit(int n, u64 ahead, double most)
     {
-        int kept = 0;
+        u64 kept = 0;
         for (int i0 = 0; i0 < n; i0 += NT) {
             const int i = i0 + tid;
             u64 all;
-            const u64 b = ahead + before(i < n ? row.weight(logit_of((uint32_t)(s.list[i] >> 32))) : 0, &all);
+            const u64 b = ahead + before(i < n ? row.weight(listed(i)) : 0, &all);
             kept += i < n && (double)b < most;
             ahead += all;
         }
-        const int c = (int)sum((u64)kept);
+        const int c = (int)sum(kept);
         return c < 1 ? 1 : c;
     }
-    // The place at which the order's tokens from `floor` up end that `end(before, with)` is given for: digits of 11 bits of
-    // the places, the highest first, until what is left fits the list.  By(logit): what is added up.
-    template <typename By, typename F>
-    __device__ __forceinline__ u64 radix(u64 floor, By by, F end, bool count, u64 k, double most)
+    __device__ __forceinline__ u64 listed_sum(int n)
+    {
+        u64 w = 0;
+        for (int i = tid; i < n; i += NT) w += row.weight(listed(i));
+        return sum(w);
+    }
+    // The place at which the order's tokens from `floor` up end: digits of 11 bits of the places, the highest first, until
+    // what is left fits the list.  By number (k of them) or by weight (less than `most` before the last).
+    __device__ __forceinline__ u64 radix(u64 floor, bool count, u64 k, double most)
     {
         u64 prefix = 0, ahead = 0;
         for (int low = 53;; low -= 11) {   // places with the prefix's bits above low + 11
             const int at = low < 0 ? 0 : low;
             const u64 mask = low + 11 >= 64 ? 0 : ~0ull << (low + 11);
-            clear_bins();
+            __syncthreads();
+            clear(s.digits);
             scan([&](float v, int i) {
                 const u64 p = place_of(v, i);
                 if (p >= floor && (p & mask) == prefix)
-                    atomicAdd(&s.bins[kBins - 1 - ((p >> at) & ((1ull << (low + 11 - at)) - 1))], by(v));
+                    atomicAdd(&s.digits[kDigit - 1 - ((p >> at) & ((1ull << (low + 11 - at)) - 1))], count ? 1ull : row.weight(v));
             });
+            __syncthreads();
             u64 b, w;
-            const int bin = crossing([&](u64 p, u64 q) { return end(ahead + p, ahead + q); }, &b, &w);
-            prefix |= (u64)(kBins - 1 - bin) << at, ahead += b;
+            const int bin = crossing(s.digits, [&](u64 p, u64 q) {
+                return count ? ahead + p < k && k <= ahead + q : (double)(ahead + p) < most && most <= (double)(ahead + q);
+            }, &b, &w);
+            prefix |= (u64)(kDigit - 1 - bin) << at, ahead += b;
             const u64 m2 = ~0ull << at;
             const int n = gather([&](float v, int i) {
                 const u64 p = place_of(v, i);
@@ -285,8 +431,9 @@ struct Picker {
         }
     }
 
-    __device__ void run(long r);
-    __device__ void done(long r, int token, float logprob)
+    __device__ __forceinline__ u64 search(long r, u64 floor, bool count, u64 k, double most);
+    __device__ __forceinline__ void run(long r);
+    __device__ __forceinline__ void done(long r, int token, float logprob)
     {
         if (tid == 0) {
             a.token[r] = token;
@@ -299,101 +446,225 @@ struct Picker {
     }
 };
 
-template <typename T, int NT>
-__device__ void Picker<T, NT>::run(long r)
+// Apart, so that the rare search takes no registers from the rest.
+template <typename T, int NT, bool SHORT>
+__device__ __noinline__ u64 radix_search(SampleArgs a, typename Picker<T, NT, SHORT>::Shared *s, Row row, long r, u64 floor, bool count,
+                                         u64 k, double most)
 {
-    // the first token of the order, the smallest finite logit, and whether a logit is none
-    u64 best = 0;
-    float low = __builtin_inff();
-    bool bad = false;
-    scan([&](float v, int i) {
-        const u64 p = place_of(v, i);
-        best = p > best ? p : best;
-        low = v > kNegInf && v < low ? v : low;
-        bad |= !(v < __builtin_inff());
-    });
-    const auto larger = [](u64 p, u64 q) { return p > q ? p : q; };
-    best = reduce(best, larger);
-    // (largest bad, largest -low) together
-    const u64 both = reduce((u64)bad << 32 | key_of(-low), larger);
-    low = -logit_of((uint32_t)both);
-    top = logit_of((uint32_t)(best >> 32));
-    const int first = (int)~(uint32_t)best;
-    if (both >> 32 || top == kNegInf) return done(r, -1, __builtin_nanf(""));
-    const float t = a.temperature ? a.temperature[r] : 1.0f;
-    if (!(t > 0.0f)) return done(r, first, 0.0f);
-    row.top = top;
-    row.factor = fmax(1.44269504088896340736 / (double)t, 1e-300);   // above 0, so that minus infinity stays below everything
-    row.shift = a.shift;
-    // Bins over what the row spans, or over what counts of it.
-    const float span = fminf(top - low, 64.0f * fmaxf(t, 1.0f));
-    inv = span > 0.0f ? fminf((float)kBins / span, 0x1p100f) : 0.0f;
+    Picker<T, NT, SHORT> p(a, *s, r);
+    p.row = row;
+    return p.radix(floor, count, k, most);
+}
 
+template <typename T, int NT, bool SHORT>
+__device__ __forceinline__ u64 Picker<T, NT, SHORT>::search(long r, u64 floor, bool count, u64 k, double most)
+{
+    __syncthreads();
+    const u64 cut = radix_search<T, NT, SHORT>(a, &s, row, r, floor, count, k, most);
+    __syncthreads();
+    return cut;
+}
+
+template <typename T, int NT, bool SHORT>
+__device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
+{
+    const float t = a.temperature ? a.temperature[r] : 1.0f;
     const int k = a.top_k ? a.top_k[r] : 0;
     const float p = a.top_p ? a.top_p[r] : 1.0f, m = a.min_p ? a.min_p[r] : 0.0f;
-    const bool by_k = k > 0 && k < a.vocab, by_p = p < 1.0f, by_m = m > 0.0f;
-    u64 cut = 0;        // places from here on are kept
-    int n = 0;          // of the list, if it holds all that are kept
+    const bool by_k = k > 0 && k < a.vocab, by_p = p < 1.0f && p > 0.0f;
+    if (tid < kTable) s.table[tid] = exp2((double)tid / kTable);
+    if (tid == 0) s.count = 0;
+
+    // The first token of the order, and whether a logit is none.  For top_p alone the tokens are counted at once, in bins
+    // below the largest logit of a first look; what lies above that, a few, goes to the list.
+    const bool at_once = by_p && !by_k && t > 0.0f;
+    inv = fminf((float)BINS / (32.0f * t), 0x1p100f);
+    if (at_once) {
+        Held<T, SHORT> h;
+        float v[8], top = kNegInf;
+        h.load(x, a.vocab, min(wave, a.units - 1), lane);
+        h.widen(v, a.vocab, 0, 1 << 30, lane);   // of the row's last unit some twice
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i]);
+        clear(s.counts);
+        anchor = logit_of(largest(key_of(top)));
+    }
+    float most_v = kNegInf;
+    int most_i = 0;
+    bool bad = false;
+    units([&](const float (&v)[8], int at, int) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (v[i] > most_v) most_v = v[i], most_i = at + i;
+            bad |= !(v[i] < __builtin_inff());
+        }
+        if (at_once) {
+            int bin[8];
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) bin[i] = bin_of(v[i]), any |= v[i] > anchor;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (v[i] > kNegInf && v[i] <= anchor) atomicAdd(&s.counts[bin[i]], 1u);
+            if (any)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (v[i] > anchor) put(v[i], at + i);
+        }
+    });
+    const uint32_t mine = key_of(most_v), top_key = largest(mine);
+    const float top = logit_of(top_key);
+    const int first = (int)~largest(mine == top_key ? ~(uint32_t)most_i : 0u);
+    const u64 best = (u64)top_key << 32 | (uint32_t)~first;
+    if (__syncthreads_or(bad) || top == kNegInf) return done(r, -1, __builtin_nanf(""));
+    if (!(t > 0.0f)) return done(r, first, 0.0f);
+    row.top = top;
+    row.factor = fmax(1.44269504088896340736 / (double)t, 1e-300);
+    row.least = -(a.shift + 3) / row.factor;
+    row.table = s.table;
+    row.shift = a.shift;
+
+    // min_p as a logit: the smallest whose weight passes it, near where the logarithm has it.
+    float floor_v = kNegInf;
+    if (m > 0.0f) {
+        const double want = ldexp((double)fminf(m, 1.0f), row.shift);
+        const uint32_t near = key_of((float)fmax(row.top + log2((double)fminf(m, 1.0f)) / row.factor, -3.4e38));
+        const uint32_t key = near - 32u + (uint32_t)lane;
+        const u64 pass = __ballot(key >= top_key || row.share(logit_of(key)) >= want);
+        floor_v = pass ? fminf(logit_of(near - 32u + (uint32_t)__builtin_ctzll(pass)), top) : top;
+    }
+    u64 cut = p > 0.0f || !(p < 1.0f) ? 0 : best;   // places from here on are kept
+    int n = 0;                                      // of the list, if it holds all that are kept
+    bool summed = false;                            // whether the sums of the kept are there
     if (by_k) {
-        clear_bins();
-        scan([&](float v, int) { atomicAdd((unsigned int *)&s.bins[bin_of(v)], 1u); });
-        const auto end = [&](u64 b, u64 w) { return b < (u64)k && (u64)k <= w; };
+        // For few: k threads' largest logits are k tokens, so that nothing below the last of these counts.
+        const bool few = k <= NT / 4;
+        float low = few ? -logit_of(largest(most_v > kNegInf ? key_of(-most_v) : 0u)) : top - 64.0f * fmaxf(t, 1.0f);
+        anchor = top;
+        inv = top > low ? fminf((float)BINS / (top - low), 0x1p100f) : 0.0f;
+        clear(s.counts);
+        if (few) atomicAdd(&s.counts[bin_of(most_v)], 1u);
+        else scan([&](float v, int) { atomicAdd(&s.counts[bin_of(v)], 1u); });
+        __syncthreads();
         u64 ahead, with;
-        const int bin = crossing(end, &ahead, &with);
-        if (with <= (u64)kList) {
-            n = gather([&](float v, int) { return bin_of(v) <= bin; });
+        const int bin = crossing(s.counts, [&](u64 b, u64 w) { return b < (u64)k && (u64)k <= w; }, &ahead, &with);
+        n = gather([&](float v, int) { return bin_of(v) <= bin; });
+        if (n <= kList) {
             sort(n);
             n = k;
         } else {
-            cut = radix(0, [](float) { return 1ull; }, end, true, (u64)k, 0.0);
+            n = 0;
+            cut = max(cut, search(r, 0, true, (u64)k, 0.0));
         }
     }
-    if (by_p && p > 0.0f && !n) {
-        clear_bins();
-        scan([&](float v, int i) {
-            if (v > kNegInf && place_of(v, i) >= cut) atomicAdd(&s.bins[bin_of(v)], row.weight(v));
-        });
-        u64 total = 0;
-        __syncthreads();
-        for (int i = tid; i < kBins; i += NT) total += s.bins[i];
-        total = sum(total);
-        const double most = (double)p * (double)total;
-        const auto end = [&](u64 b, u64 w) { return (double)b < most && most <= (double)w; };
-        u64 ahead, with;
-        const int bin = crossing(end, &ahead, &with);
-        const int c = gather([&](float v, int i) { return bin_of(v) == bin && place_of(v, i) >= cut; });
-        if (c <= kList) {
-            sort(c);
-            cut = s.list[fit(c, ahead, most) - 1];
-        } else {
-            cut = radix(cut, [&](float v) { return row.weight(v); }, end, false, 0, most);
-        }
-    } else if (by_p && n) {
-        u64 total = 0;
-        for (int i = tid; i < n; i += NT) total += row.weight(logit_of((uint32_t)(s.list[i] >> 32)));
-        total = sum(total);
-        n = p > 0.0f ? fit(n, 0, (double)p * (double)total) : 1;
+    if (by_p && n) {
+        n = fit(n, 0, (double)p * (double)listed_sum(n));
+    } else if (n && cut) {
+        n = 1;
     } else if (by_p) {
-        cut = best;
+        // The neighbourhood of the end, from the number of tokens in each bin alone; then the weights, once: the sums of
+        // what lies above it, by units, and its tokens into the list.  Where the end turns out to lie elsewhere, or the
+        // list does not hold them, it is searched for digit by digit.
+        bool sure = true;
+        if (!at_once) {
+            anchor = top;
+            inv = fminf((float)BINS / (32.0f * t), 0x1p100f);
+            __syncthreads();
+            clear(s.counts);
+            scan([&](float v, int i) {
+                if (v > kNegInf && place_of(v, i) >= cut) atomicAdd(&s.counts[bin_of(v)], 1u);
+            });
+            if (tid == 0) s.count = 0;
+            __syncthreads();
+        }
+        const int above = s.count;
+        sure = above <= kList;
+        float over = 0.0f;   // of every thread the same: the list is short
+        if (sure)
+            for (int i0 = 0; i0 < above; i0 += 64)
+                over += i0 + lane < above ? __builtin_amdgcn_exp2f((listed(i0 + lane) - top) * (float)row.factor) : 0.0f;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) over += __shfl_xor(over, d);
+        int from, to;
+        guess(p, over, &from, &to);
+        // above hi: certainly kept; down to lo: the neighbourhood
+        float hi = from < 2 ? __builtin_inff() : anchor - (float)(from - 1) / inv;
+        float lo = anchor - (float)(to + 2) / inv;
+        if (floor_v > lo) {   // min_p ends what is kept before: everything from there on
+            if (floor_v > kNegInf && floor_v <= hi) lo = floor_v;
+            else lo = hi = floor_v;
+        }
+        // what counts in full lies above `over_v`
+        const bool no_list = lo == hi;
+        const uint32_t below = key_of(hi) - 1u;   // -0 and 0 have one key
+        const float over_v = no_list ? logit_of(below == 0x7FFFFFFFu ? below - 1u : below) : hi;
+        __syncthreads();
+        if (tid == 0) s.count = 0;
+        clear(s.sums);
+        u64 total = 0;
+        const auto add_up = [&](auto partly) {   // partly: of the tokens from `cut` on
+            units([&](const float (&v)[8], int at, int unit) {
+                u64 kept = 0;
+                bool any = false;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {   // no branch: the chains of eight weights run side by side
+                    u64 w = row.weight(v[i]);
+                    if (partly) w = place_of(v[i], at + i) < cut ? 0 : w;
+                    total += w;
+                    kept += v[i] > over_v ? w : 0;
+                    any |= v[i] <= over_v && v[i] >= lo;
+                }
+                if (any)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (v[i] <= over_v && v[i] >= lo && (!partly || place_of(v[i], at + i) >= cut)) put(v[i], at + i);
+                kept = wave_sum(kept);
+                if (lane == 0 && kept) atomicAdd(&s.sums[unit / a.runs], kept);
+            });
+        };
+        if (cut) add_up(std::true_type());
+        else add_up(std::false_type());
+        total = sum(total);
+        u64 ahead = 0;
+        const int parts = (a.units + a.runs - 1) / a.runs;
+        for (int i = tid; i < parts; i += NT) ahead += s.sums[i];
+        ahead = sum(ahead);
+        const double most = (double)p * (double)total;
+        const int c = s.count;
+        const u64 near = listed_sum(min(c, kList));
+        // behind a floor that the neighbourhood ends at, the end may also lie below
+        const bool ends = most <= (double)(ahead + near) || (floor_v > kNegInf && lo == floor_v);
+        if (sure && c <= kList && (double)ahead < most && ends) {
+            sort(c);
+            const int fits = c ? fit(c, ahead, most) : 0;
+            const u64 last = fits ? s.list[fits - 1] : 0;
+            for (int i = tid; i < fits; i += NT) atomicAdd(&s.sums[(int)(~(uint32_t)s.list[i]) / kUnit / a.runs], row.weight(listed(i)));
+            if (fits) cut = last;
+            else cut = max(cut, (u64)key_of(hi) << 32);
+            summed = true;
+        } else {
+            cut = search(r, cut, false, 0, most);
+        }
     }
+    // The weight of a kept token, 0 of another.
     const auto kept = [&](float v, int i) {
         const u64 q = place_of(v, i);
-        return v > kNegInf && q >= cut && (!by_m || q == best || row.share(v) >= (double)m);
+        return v > kNegInf && q >= cut && v >= floor_v ? row.weight(v) : 0;
     };
     float u = a.u[r];
     u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
+    __syncthreads();
     if (n) {   // everything is in the list: by index
-        __syncthreads();
         const int held = n;
-        int live = 0;
+        u64 live = 0;
         for (int i = tid; i < held; i += NT) {
             const u64 q = s.list[i];
-            const uint32_t key = (uint32_t)(q >> 32);
-            const bool is = kept(logit_of(key), (int)~(uint32_t)q);
+            const float v = logit_of((uint32_t)(q >> 32));
+            const bool is = v > kNegInf && v >= floor_v;
             live += is;
-            s.list[i] = is ? (q & 0xFFFFFFFFull) << 32 | key : 0;   // the lowest index sorts first: places hold its complement
+            s.list[i] = is ? (q & 0xFFFFFFFFull) << 32 | (q >> 32) : 0;   // the lowest index sorts first: places hold its complement
         }
-        n = (int)sum((u64)live);
+        n = (int)sum(live);
         sort(held);
         u64 total = 0;
         for (int i = tid; i < n; i += NT) total += row.weight(logit_of((uint32_t)s.list[i]));
@@ -415,70 +686,424 @@ __device__ void Picker<T, NT>::run(long r)
         return;
     }
     // Sums of runs of units, in the vocabulary's order.
-    __syncthreads();
     const int parts = (a.units + a.runs - 1) / a.runs;
-    for (int g = wave; g < parts; g += WAVES) {
-        u64 w = 0;
-        for (int un = g * a.runs; un < min((g + 1) * a.runs, a.units); ++un) {
-            float v[8];
-            unit_of(x, a.vocab, un, lane, v);
+    if (!summed) {
+        clear(s.sums);
+        units([&](const float (&v)[8], int at, int unit) {
+            u64 w = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (kept(v[i], un * kUnit + lane * 8 + i)) w += row.weight(v[i]);
-        }
-        w = wave_reduce(w, [](u64 p, u64 q) { return p + q; });
-        if (lane == 0) s.list[g] = w;
+            for (int i = 0; i < 8; ++i) w += kept(v[i], at + i);
+            w = wave_sum(w);
+            if (lane == 0 && w) atomicAdd(&s.sums[unit / a.runs], w);
+        });
+        __syncthreads();
     }
-    __syncthreads();
     u64 total = 0;
-    for (int i = tid; i < parts; i += NT) total += s.list[i];
+    for (int i = tid; i < parts; i += NT) total += s.sums[i];
     total = sum(total);
     const double target = (double)u * (double)total;
     u64 ahead = 0;
     for (int i0 = 0; i0 < parts; i0 += NT) {
         const int i = i0 + tid;
         u64 all;
-        const u64 w = i < parts ? s.list[i] : 0, b = ahead + before(w, &all);
-        if (w && (double)b <= target && target < (double)(b + w)) s.found = (u64)i, s.bins[0] = b;
+        const u64 w = i < parts ? s.sums[i] : 0, b = ahead + before(w, &all);
+        if (w && (double)b <= target && target < (double)(b + w)) s.found = i, s.ahead = b;
         ahead += all;
     }
     __syncthreads();
     if (wave != 0) return;
-    const int g = (int)s.found;
-    u64 b0 = s.bins[0];
+    const int g = s.found;
+    u64 b0 = s.ahead;
     for (int un = g * a.runs; un < min((g + 1) * a.runs, a.units); ++un) {
+        Held<T, SHORT> h;
         float v[8];
-        u64 w[8], own = 0;
-        unit_of(x, a.vocab, un, lane, v);
+        u64 own = 0;
+        h.load(x, a.vocab, un, lane);
+        const int at = h.widen(v, a.vocab, un, a.units, lane);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) own += kept(v[i], at + i);
+        const u64 in = wave_scan(own);
+        u64 b = b0 + in - own;
+        if ((double)b <= target && target < (double)(b + own)) {   // one lane: its tokens again
+            int in_lane = 0;
+            float hit = 0.0f;
+#pragma unroll
+            for (int i = 7; i >= 0; --i) {
+                const u64 w = kept(v[i], at + i);
+                own -= w;
+                if (w && (double)(b + own) <= target && target < (double)(b + own + w)) in_lane = i, hit = v[i];
+            }
+            a.token[r] = at + in_lane;
+            if (a.logprob) a.logprob[r] = logprob(hit, total);
+        }
+        b0 += last_lane(in);
+    }
+}
+
+template <typename T, int NT, bool SHORT>
+__global__ __launch_bounds__(NT) void sample_rows_kernel(SampleArgs a)
+{
+    __shared__ typename Picker<T, NT, SHORT>::Shared s;
+    Picker<T, NT, SHORT>(a, s, blockIdx.x).run(blockIdx.x);
+}
+
+// bf16 rows hold few different values, so tokens are counted by value, with a
+// counter for each of 2^-8 <= |x| < 2^7, and everything about the filters
+// follows from counters and the values' weights: the value that they end at, and
+// how many tokens of it, the lowest indexes, stay.  Each value's weight is
+// computed once and looked up.  What lies outside that range, a few tokens as a
+// rule, goes to a list; a row of which the list does not hold that is taken as
+// rows of fp32 are.
+//
+// Slots, in the order of the logits: the list's x >= 2^7; the positive values;
+// the list's |x| < 2^-8; the negative values; the list's x <= -2^7.
+constexpr int kValues = 15 * 128, kMiddle = kValues + 1, kSlots = 2 * kValues + 3;
+constexpr int kFirst = (127 - 8) << 7;   // bits of 2^-8
+constexpr uint32_t kForbidden = 0xFF80;  // bits of minus infinity
+
+struct Values {
+    uint32_t counts[kSlots];
+    u64 weights[kSlots + 1];   // of a token; of the list's slots the sum; the last one 0, for what has no counter
+    u64 list[kList / 2], sums[kList];
+    uint32_t ties[kList];
+    double table[kTable];
+    u64 part[2][16], ahead;
+    int found, count;
+};
+
+template <int NT>
+struct ByValue {
+    typedef uint16_t T;
+    static constexpr int WAVES = NT / 64, PER = (kSlots + NT - 1) / NT;
+    const SampleArgs &a;
+    Values &s;
+    const T *x;
+    const int tid, lane, wave;
+    Row row;
+    double want = 0.0;   // the weight that min_p asks for
+    int turn = 0;
+
+    __device__ __forceinline__ ByValue(const SampleArgs &args, Values &sh, long r)
+        : a(args), s(sh), x((const T *)args.x + r * args.stride), tid(threadIdx.x), lane(threadIdx.x % 64),
+          wave(__builtin_amdgcn_readfirstlane(threadIdx.x / 64))
+    {
+    }
+    // The slot of a value's 16 bits; kSlots for those without a counter.
+    static __device__ __forceinline__ int slot_of(uint32_t b)
+    {
+        const int i = (int)(b & 0x7FFFu) - kFirst, j = b & 0x8000u ? i + 1 : -1 - i;
+        return (unsigned)i < (unsigned)kValues ? kMiddle + j : kSlots;
+    }
+    static __device__ __forceinline__ float value_of(int slot)
+    {
+        return bf16_to_f32((uint16_t)(slot < kMiddle ? kMiddle - 1 - slot + kFirst : slot - kMiddle - 1 + kFirst + 0x8000));
+    }
+    static __device__ __forceinline__ bool of_list(int slot) { return slot == 0 || slot == kMiddle || slot == kSlots - 1; }
+    static __device__ __forceinline__ int slot_of_listed(float v) { return v >= 1.0f ? 0 : v <= -1.0f ? kSlots - 1 : kMiddle; }
+    __device__ __forceinline__ float listed(int i) const { return logit_of((uint32_t)(s.list[i] >> 32)); }
+
+    template <typename F>
+    __device__ __forceinline__ void units(F f)   // f(bits of 8 logits, first index, unit)
+    {
+        constexpr int U = 3;   // units of a wavefront in flight
+        Held<T, false> h[U];
+#pragma unroll
+        for (int n = 0; n < U; ++n) h[n].load(x, a.vocab, min(wave + n * WAVES, a.units - 1), lane);
+#pragma unroll 1
+        for (int unit = wave; unit < a.units; unit += WAVES) {
+            float v[8];
+            uint32_t b[8];
+            const int at = h[0].widen(v, a.vocab, unit, a.units, lane);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = __builtin_bit_cast(uint32_t, v[i]) >> 16;
+#pragma unroll
+            for (int n = 0; n < U - 1; ++n) h[n] = h[n + 1];
+            h[U - 1].load(x, a.vocab, min(unit + U * WAVES, a.units - 1), lane);
+            f(b, at, unit);
+        }
+    }
+    __device__ __forceinline__ const u64 *share_out(u64 v)
+    {
+        u64 *p = s.part[turn];
+        turn ^= 1;
+        if (lane == 0) p[wave] = v;
+        __syncthreads();
+        return p;
+    }
+    __device__ __forceinline__ u64 before(u64 v, u64 *all)   // as Picker's
+    {
+        const u64 in = wave_scan(v);
+        const u64 *p = share_out(last_lane(in));
+        u64 base = 0, total = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            if (i < wave) base += p[i];
+            total += p[i];
+        }
+        *all = total;
+        return base + in - v;
+    }
+    __device__ __forceinline__ u64 sum(u64 v)
+    {
+        const u64 *p = share_out(wave_sum(v));
+        u64 all = 0;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) all += p[i];
+        return all;
+    }
+    // Where the order's tokens end: those of the slots before `slot` stay, and the first `tokens` of its own.
+    struct End {
+        int slot, tokens;
+    };
+    // The sum of a slot's weights as far as `end` goes; its list's tokens are sorted.
+    __device__ __forceinline__ u64 sum_of(int slot, const End &end) const
+    {
+        if (slot > end.slot) return 0;
+        if (!of_list(slot)) return (slot == end.slot ? (u64)end.tokens : (u64)s.counts[slot]) * s.weights[slot];
+        if (slot < end.slot) return s.weights[slot];
+        u64 w = 0;
+        for (int i = 0, at = first_of(slot); i < end.tokens; ++i) w += row.weight(listed(at + i));
+        return w;
+    }
+    // The first of a slot's tokens in the sorted list.
+    __device__ __forceinline__ int first_of(int slot) const
+    {
+        return (slot > 0 ? (int)s.counts[0] : 0) + (slot > kMiddle ? (int)s.counts[kMiddle] : 0);
+    }
+    // The slot in whose sums of by(slot), added up from the first, end(before, with) holds, or kSlots; *ahead: the sum before.
+    template <typename By, typename F>
+    __device__ __forceinline__ int crossing(By by, F end, u64 *ahead)
+    {
+        u64 own[PER], total = 0, all;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) own[i] = tid * PER + i < kSlots ? by(tid * PER + i) : 0, total += own[i];
+        u64 b = before(total, &all);
+        if (tid == 0) s.found = kSlots;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (own[i] && end(b, b + own[i])) s.found = tid * PER + i, s.ahead = b;
+            b += own[i];
+        }
+        __syncthreads();
+        *ahead = s.ahead;
+        return s.found;
+    }
+    // Whether the row could be taken so.
+    __device__ __forceinline__ bool run(long r);
+};
+
+template <int NT>
+__device__ __forceinline__ bool ByValue<NT>::run(long r)
+{
+    float t = a.temperature ? a.temperature[r] : 1.0f;
+    int k = a.top_k ? a.top_k[r] : 0;
+    float p = a.top_p ? a.top_p[r] : 1.0f, m = a.min_p ? a.min_p[r] : 0.0f;
+    if (!(t > 0.0f)) t = 1.0f, k = 1, p = 1.0f, m = 0.0f;   // the first token
+    if (k < 1 || k > a.vocab) k = a.vocab;
+    if (tid < kTable) s.table[tid] = exp2((double)tid / kTable);
+    if (tid == 0) s.count = 0;
+    for (int i = tid; i < kSlots; i += NT) s.counts[i] = 0;
+    for (int i = tid; i < kList; i += NT) s.sums[i] = 0, s.ties[i] = 0;
+    __syncthreads();
+    bool bad = false;
+    units([&](const uint32_t (&b)[8], int at, int) {
+        int slot[8];
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) slot[i] = slot_of(b[i]), any |= slot[i] == kSlots && b[i] != kForbidden;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (slot[i] < kSlots) atomicAdd(&s.counts[slot[i]], 1u);
+        if (any)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (slot[i] == kSlots && b[i] != kForbidden) {
+                    const int c = atomicAdd(&s.count, 1);
+                    if (c < kList / 2) s.list[c] = place_of(bf16_to_f32((uint16_t)b[i]), at + i);
+                    bad |= (b[i] & 0x7FFFu) >= 0x7F80u;
+                }
+    });
+    bad = __syncthreads_or(bad);
+    const int outside = s.count;
+    if (!bad && outside > kList / 2) return false;
+    sort_list<NT>(s.list, bad ? 0 : outside, tid);
+    for (int i = tid; i < outside && !bad; i += NT) atomicAdd(&s.counts[slot_of_listed(listed(i))], 1u);
+    __syncthreads();
+    const auto number = [&](int slot) { return (u64)s.counts[slot]; };
+    u64 ahead;
+    const int best = bad ? kSlots : crossing(number, [](u64 b, u64 w) { return b == 0 && w > 0; }, &ahead);
+    if (best == kSlots) {
+        if (tid == 0) {
+            a.token[r] = -1;
+            if (a.logprob) a.logprob[r] = __builtin_nanf("");
+        }
+        return true;
+    }
+    const float top = of_list(best) ? listed(first_of(best)) : value_of(best);
+    row.top = top;
+    row.factor = fmax(1.44269504088896340736 / (double)t, 1e-300);
+    row.least = -(a.shift + 3) / row.factor;
+    row.table = s.table;
+    row.shift = a.shift;
+    want = m > 0.0f ? ldexp((double)m, a.shift) : 0.0;
+    for (int i = tid; i <= kSlots; i += NT) s.weights[i] = i < kSlots && !of_list(i) ? row.weight(value_of(i)) : 0;
+    __syncthreads();
+    for (int i = tid; i < outside; i += NT) atomicAdd(&s.weights[slot_of_listed(listed(i))], row.weight(listed(i)));
+    __syncthreads();
+
+    End end = {kSlots, 0};
+    if (k < a.vocab) {
+        const int slot = crossing(number, [&](u64 b, u64 w) { return b < (u64)k && (u64)k <= w; }, &ahead);
+        if (slot < kSlots) end = {slot, k - (int)ahead};   // else there are fewer
+    }
+    if (p < 1.0f) {
+        const auto weight = [&](int slot) { return sum_of(slot, end); };
+        u64 own = 0;
+        for (int i = tid; i < kSlots; i += NT) own += weight(i);
+        const double most = (double)p * (double)sum(own);
+        const auto within = [&](u64 b) { return (double)b < most; };
+        const int slot = p > 0.0f ? crossing(weight, [&](u64 b, u64 w) { return within(b) && most <= (double)w; }, &ahead) : kSlots;
+        if (slot == kSlots) {
+            end = {best, 1};
+        } else {
+            // how many have less than `most` before them
+            int tokens = slot == end.slot ? end.tokens : (int)s.counts[slot];
+            if (of_list(slot)) {
+                u64 b = ahead;
+                int c = 0;
+                for (int at = first_of(slot); c < tokens && within(b); ++c) b += row.weight(listed(at + c));
+                tokens = c;
+            } else {
+                int lo = 1, hi = tokens;   // the last has less than `most` before it, or is the first
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) / 2;
+                    if (within(ahead + (u64)(mid - 1) * s.weights[slot])) lo = mid;
+                    else hi = mid - 1;
+                }
+                tokens = lo;
+            }
+            end = {slot, tokens};
+        }
+    }
+    // What is kept: of the list's tokens and of the values' slots.  Of the last slot's tokens the first may be.
+    const u64 cut = end.slot < kSlots && of_list(end.slot) ? s.list[first_of(end.slot) + end.tokens - 1] : 0;
+    const auto kept = [&](float v, u64 place) {   // of the list's
+        const int slot = slot_of_listed(v);
+        return (slot < end.slot || (slot == end.slot && place >= cut)) && (row.share(v) >= want || (slot == best && v == top));
+    };
+    const bool some = end.slot < kSlots && !of_list(end.slot) && end.tokens < (int)s.counts[end.slot];
+    u64 tie = 0;   // the weight of a token of the last slot, where not all of them stay
+    if (some && (end.slot == best || row.share(value_of(end.slot)) >= want)) tie = s.weights[end.slot];
+    __syncthreads();
+    for (int i = tid; i < kSlots; i += NT)
+        if (i > end.slot || (some && i == end.slot) || (i != best && !of_list(i) && row.share(value_of(i)) < want)) s.weights[i] = 0;
+    for (int i = tid; i < outside; i += NT) {
+        const u64 q = s.list[i];
+        if (kept(listed(i), q)) atomicAdd(&s.sums[(int)(~(uint32_t)q) / kUnit / a.runs], row.weight(listed(i)));
+    }
+    __syncthreads();
+
+    // Sums of runs of units, in the vocabulary's order, and how many tokens of the last slot each holds.
+    units([&](const uint32_t (&b)[8], int, int unit) {
+        u64 w = 0;
+        uint32_t ties = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            w[i] = kept(v[i], un * kUnit + lane * 8 + i) ? row.weight(v[i]) : 0;
+            const int slot = slot_of(b[i]);
+            w += s.weights[slot];
+            ties += slot == end.slot;
+        }
+        w = wave_sum(w);
+        if (lane == 0 && w) atomicAdd(&s.sums[unit / a.runs], w);
+        if (tie) {
+            ties = (uint32_t)wave_sum(ties);
+            if (lane == 0 && ties) atomicAdd(&s.ties[unit / a.runs], ties);
+        }
+    });
+    __syncthreads();
+    const int parts = (a.units + a.runs - 1) / a.runs;
+    u64 total = 0, all, seen = 0;
+    if (tie)
+        for (int i0 = 0; i0 < parts; i0 += NT) {
+            const int i = i0 + tid;
+            const u64 c = i < parts ? s.ties[i] : 0, b = seen + before(c, &all);
+            if (i < parts) {
+                s.sums[i] += (b >= (u64)end.tokens ? 0 : min(c, (u64)end.tokens - b)) * tie;
+                s.ties[i] = (uint32_t)b;   // those before
+            }
+            seen += all;
+        }
+    __syncthreads();
+    for (int i = tid; i < parts; i += NT) total += s.sums[i];
+    total = sum(total);
+    float u = a.u[r];
+    u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
+    const double target = (double)u * (double)total;
+    ahead = 0;
+    for (int i0 = 0; i0 < parts; i0 += NT) {
+        const int i = i0 + tid;
+        const u64 w = i < parts ? s.sums[i] : 0, b = ahead + before(w, &all);
+        if (w && (double)b <= target && target < (double)(b + w)) s.found = i, s.ahead = b;
+        ahead += all;
+    }
+    __syncthreads();
+    if (wave != 0) return true;
+    const int g = s.found;
+    u64 b0 = s.ahead, t0 = s.ties[g];
+    for (int un = g * a.runs; un < min((g + 1) * a.runs, a.units); ++un) {
+        Held<T, false> h;
+        float v[8];
+        u64 w[8], own = 0, ties = 0;
+        h.load(x, a.vocab, un, lane);
+        const int at = h.widen(v, a.vocab, un, a.units, lane);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ties += tie && slot_of(__builtin_bit_cast(uint32_t, v[i]) >> 16) == end.slot;
+        const u64 in_ties = wave_scan(ties);
+        u64 rank = t0 + in_ties - ties;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int slot = slot_of(__builtin_bit_cast(uint32_t, v[i]) >> 16);
+            w[i] = s.weights[slot];
+            if (slot == kSlots && v[i] > kNegInf && kept(v[i], place_of(v[i], at + i))) w[i] = row.weight(v[i]);
+            if (tie && slot == end.slot) w[i] = rank++ < (u64)end.tokens ? tie : 0;
             own += w[i];
         }
-        u64 in = own;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const u64 o = __shfl_up(in, d);
-            if (lane >= d) in += o;
-        }
+        const u64 in = wave_scan(own);
         u64 b = b0 + in - own;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (w[i] && (double)b <= target && target < (double)(b + w[i])) {
-                a.token[r] = un * kUnit + lane * 8 + i;
-                if (a.logprob) a.logprob[r] = logprob(v[i], total);
+                a.token[r] = at + i;
+                if (a.logprob)
+                    a.logprob[r] = (float)(((double)v[i] - row.top) * row.factor * 0.693147180559945309417 -
+                                           log(ldexp((double)total, -row.shift)));
             }
             b += w[i];
         }
-        b0 += __shfl(in, 63);
+        b0 += last_lane(in), t0 += last_lane(in_ties);
     }
+    return true;
 }
 
-template <typename T, int NT>
-__global__ __launch_bounds__(NT) void sample_rows_kernel(SampleArgs a)
+// Apart, as the rare search is.
+template <int NT>
+__device__ __noinline__ void row_by_bins(SampleArgs a, typename Picker<uint16_t, NT, false>::Shared *s, long r)
 {
-    __shared__ typename Picker<T, NT>::Shared s;
-    Picker<T, NT>(a, s, blockIdx.x).run(blockIdx.x);
+    Picker<uint16_t, NT, false>(a, *s, r).run(r);
+}
+
+template <int NT>
+__global__ __launch_bounds__(NT) void sample_values_kernel(SampleArgs a)
+{
+    __shared__ union {
+        Values values;
+        typename Picker<uint16_t, NT, false>::Shared bins;
+    } s;
+    if (!ByValue<NT>(a, s.values, blockIdx.x).run(blockIdx.x)) {
+        __syncthreads();
+        row_by_bins<NT>(a, &s.bins, blockIdx.x);
+    }
 }
 
 int check_sample(long rows, long vocab, int dtype)
@@ -518,9 +1143,14 @@ extern "C" int sample_tokens(long rows, long vocab, int dtype, const void *x, lo
     a.runs = (a.units + kList - 1) / kList;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)rows);
-    if (vocab <= 4096)
-        launch_kernel(dtype == kF32 ? sample_rows_kernel<float, 256> : sample_rows_kernel<uint16_t, 256>, grid, dim3(256), 0, st, a);
-    else
-        launch_kernel(dtype == kF32 ? sample_rows_kernel<float, 1024> : sample_rows_kernel<uint16_t, 1024>, grid, dim3(1024), 0, st, a);
+    const auto go = [&](auto of) {
+        typedef decltype(of) T;
+        if (vocab < 8) launch_kernel(sample_rows_kernel<T, 256, true>, grid, dim3(256), 0, st, a);
+        else if (vocab <= 4096) launch_kernel(sample_rows_kernel<T, 256, false>, grid, dim3(256), 0, st, a);
+        else if (sizeof(T) == 2) launch_kernel(sample_values_kernel<kValueThreads>, grid, dim3(kValueThreads), 0, st, a);
+        else launch_kernel(sample_rows_kernel<float, kThreads, false>, grid, dim3(kThreads), 0, st, a);
+    };
+    if (dtype == kF32) go(float());
+    else go(uint16_t());
     return quant::launched();
 }

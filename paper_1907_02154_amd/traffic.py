@@ -103,6 +103,7 @@ SOURCES = {
     "matmul_i8_align_kernel": "quant_matmul.hip",
     "rows_i8_kernel": "quant_rows.hip",
     "sample_rows_kernel": "sample.hip",
+    "sample_values_kernel": "sample.hip",
     "rows_i8_long_kernel": "quant_rows.hip",
 }
 

@@ -184,6 +184,28 @@ def test_more_candidates_than_a_list_holds(vocab):
             check(x, u, top_k=kk, top_p=[.5, .9, .3, .999], temperature=[1.0, 20.0, 5.0, 40.0])
 
 
+@pytest.mark.parametrize("vocab", [5000, 30011])
+@pytest.mark.parametrize("share", [0.01, 0.05, 0.5])
+def test_bf16_logits_outside_the_range_of_the_counters(vocab, share):
+    """Large and tiny magnitudes of either sign among the others, a few and more than a list holds, at every filter's end."""
+    g = gen(vocab + int(100 * share))
+    x = 2 * torch.randn(8, vocab, generator=g)
+    kind = torch.rand(8, vocab, generator=g)
+    tiny = torch.randn(8, vocab, generator=g) * 2.0 ** -12
+    huge = (130 + 5 * torch.rand(8, vocab, generator=g)) * torch.sign(torch.randn(8, vocab, generator=g))
+    x = torch.where(kind < share, tiny, x)
+    for part in (x, torch.where((kind > 1 - share) & (torch.arange(8)[:, None] % 2 == 0), huge, x), x * 1e-4,
+                 x.clamp(max=0), torch.where(kind > share, torch.full_like(x, -math.inf), x), 100 * x):
+        part = part.to(BF16)
+        u = torch.rand(8, generator=g).tolist()
+        t = [0.3, 1.0, 2.0, 5.0, 0.0, 1.0, 30.0, 0.05]
+        for k in (dict(), dict(top_k=[1, 2, 40, vocab // 3, 5, vocab // 2, vocab - 1, 4000]),
+                  dict(top_p=[.1, .5, .9, .99, .5, .3, .7, .95]), dict(min_p=[.5, .1, .01, .9, .5, 1.0, .99, 1e-6]),
+                  dict(top_k=[1, 2, 40, vocab // 3, 5, vocab // 2, vocab - 1, 4000], top_p=[.1, .5, .9, .99, .5, .3, .7, .95],
+                       min_p=[.5, .1, .01, .9, .5, .2, .99, 1e-6])):
+            check(part, u, temperature=t, **k)
+
+
 def test_every_token_is_reached():
     """u over a fine grid: each token as often as its weight says, in the vocabulary's order."""
     x = torch.tensor([[0.0, math.log(3.0), -math.inf, math.log(2.0), 0.0, math.log(0.5)]])
