@@ -38,7 +38,7 @@ struct SampleArgs {
     int32_t *token;
     float *logprob;
     int shift;        // weights are multiples of 2^-shift
-    int units, runs;  // units of a row, and how many of them make one of the partial sums
+    int units, runs;  // units of a row, and how many of them, a power of two, make one of the partial sums
 };
 
 // A logit's place in the order, larger for larger logits; -0 counts as 0.
@@ -198,6 +198,30 @@ __device__ __forceinline__ void sort_list(u64 *list, int n, int tid)
         }
 }
 
+// A row's units, f(held, unit, last): a wavefront takes runs of them, every NT / 64-th, three units in flight; `last`
+// of a run.
+template <typename T, bool SHORT, int NT, typename F>
+__device__ __forceinline__ void each_unit(const SampleArgs &a, const T *x, int lane, int wave, F f)
+{
+    constexpr int U = 3, WAVES = NT / 64;
+    const int step = (WAVES - 1) * a.runs;
+    const auto next = [&](int u) { return (u + 1) & (a.runs - 1) ? u + 1 : u + 1 + step; };
+    Held<T, SHORT> h[U];
+    int u = wave * a.runs, ahead = u;
+#pragma unroll
+    for (int n = 0; n < U; ++n) h[n].load(x, a.vocab, min(ahead, a.units - 1), lane), ahead = next(ahead);
+#pragma unroll 1
+    while (u < a.units) {
+        const Held<T, SHORT> now = h[0];
+#pragma unroll
+        for (int n = 0; n < U - 1; ++n) h[n] = h[n + 1];
+        h[U - 1].load(x, a.vocab, min(ahead, a.units - 1), lane);
+        ahead = next(ahead);
+        f(now, u, ((u + 1) & (a.runs - 1)) == 0 || u == a.units - 1);
+        u = next(u);
+    }
+}
+
 template <typename T, int NT, bool SHORT>
 struct Picker {
     static constexpr int WAVES = NT / 64, BINS = NT > 256 ? 8192 : kDigit;   // BINS: of logits, 32 bits each
@@ -210,7 +234,7 @@ struct Picker {
         double table[kTable];
         u64 part[2][WAVES], ahead, with;
         float guess[WAVES];
-        int found, count;
+        int found, until, count;
     };
     const SampleArgs &a;
     Shared &s;
@@ -226,29 +250,22 @@ struct Picker {
     {
     }
 
-    // f(logits, first index, unit) of every lane's 8 tokens of a unit, those past the row's end as minus infinity.
+    // f(logits, first index, unit, last of a run) of every lane's 8 tokens of a unit, those past the row's end as minus
+    // infinity.
     template <typename F>
     __device__ __forceinline__ void units(F f)
     {
-        constexpr int U = 3;   // units of a wavefront in flight
-        Held<T, SHORT> h[U];
-#pragma unroll
-        for (int n = 0; n < U; ++n) h[n].load(x, a.vocab, min(wave + n * WAVES, a.units - 1), lane);
-#pragma unroll 1
-        for (int unit = wave; unit < a.units; unit += WAVES) {
+        each_unit<T, SHORT, NT>(a, x, lane, wave, [&](const Held<T, SHORT> &h, int unit, bool last) {
             float v[8];
-            const int at = h[0].widen(v, a.vocab, unit, a.units, lane);
-#pragma unroll
-            for (int n = 0; n < U - 1; ++n) h[n] = h[n + 1];
-            h[U - 1].load(x, a.vocab, min(unit + U * WAVES, a.units - 1), lane);
-            f(v, at, unit);
-        }
+            const int at = h.widen(v, a.vocab, unit, a.units, lane);
+            f(v, at, unit, last);
+        });
     }
     // f(logit, index) of every token.
     template <typename F>
     __device__ __forceinline__ void scan(F f)
     {
-        units([&](const float (&v)[8], int at, int) {
+        units([&](const float (&v)[8], int at, int, bool) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) f(v[i], at + i);
         });
@@ -337,7 +354,7 @@ struct Picker {
             if (lane >= d) in += o;
         }
         if (lane == 63) s.guess[wave] = in;
-        if (tid == 0) s.found = -1, s.count = BINS - 1;
+        if (tid == 0) s.found = -1, s.until = BINS - 1;
         __syncthreads();
         float b = in - mine + over, total = over;
 #pragma unroll
@@ -352,11 +369,11 @@ struct Picker {
                 const int n = tid * PER + i;
                 const float w = (float)s.counts[n] * __builtin_amdgcn_exp2f(first + step * ((float)n + 0.5f));
                 if (b < less && less <= b + w) s.found = n;
-                if (b < more && more <= b + w) s.count = n;
+                if (b < more && more <= b + w) s.until = n;
                 b += w;
             }
         __syncthreads();
-        *from = s.found, *to = more <= over ? -1 : s.count;
+        *from = s.found, *to = more <= over ? -1 : s.until;
     }
     // The places of the tokens for which f holds into the list; how many there are, also where that is more than it holds.
     template <typename F>
@@ -492,7 +509,7 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
     float most_v = kNegInf;
     int most_i = 0;
     bool bad = false;
-    units([&](const float (&v)[8], int at, int) {
+    units([&](const float (&v)[8], int at, int, bool) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (v[i] > most_v) most_v = v[i], most_i = at + i;
@@ -603,8 +620,8 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
         clear(s.sums);
         u64 total = 0;
         const auto add_up = [&](auto partly) {   // partly: of the tokens from `cut` on
-            units([&](const float (&v)[8], int at, int unit) {
-                u64 kept = 0;
+            u64 kept = 0;
+            units([&](const float (&v)[8], int at, int unit, bool last) {
                 bool any = false;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {   // no branch: the chains of eight weights run side by side
@@ -618,8 +635,10 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
                         if (v[i] <= over_v && v[i] >= lo && (!partly || place_of(v[i], at + i) >= cut)) put(v[i], at + i);
+                if (!last) return;
                 kept = wave_sum(kept);
-                if (lane == 0 && kept) atomicAdd(&s.sums[unit / a.runs], kept);
+                if (lane == 0) s.sums[unit / a.runs] = kept;
+                kept = 0;
             });
         };
         if (cut) add_up(std::true_type());
@@ -689,12 +708,14 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
     const int parts = (a.units + a.runs - 1) / a.runs;
     if (!summed) {
         clear(s.sums);
-        units([&](const float (&v)[8], int at, int unit) {
-            u64 w = 0;
+        u64 w = 0;
+        units([&](const float (&v)[8], int at, int unit, bool last) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) w += kept(v[i], at + i);
+            if (!last) return;
             w = wave_sum(w);
-            if (lane == 0 && w) atomicAdd(&s.sums[unit / a.runs], w);
+            if (lane == 0) s.sums[unit / a.runs] = w;
+            w = 0;
         });
         __syncthreads();
     }
@@ -761,9 +782,13 @@ constexpr int kValues = 15 * 128, kMiddle = kValues + 1, kSlots = 2 * kValues + 
 constexpr int kFirst = (127 - 8) << 7;   // bits of 2^-8
 constexpr uint32_t kForbidden = 0xFF80;  // bits of minus infinity
 
+// In LDS: positive values by magnitude with a place for what lies below and one for what lies above, the negative ones
+// the same, the list's three slots.  The places of what has no counter stay 0.
+constexpr int kSide = kValues + 2, kPlaces = 2 * kSide + 3;
+
 struct Values {
-    uint32_t counts[kSlots];
-    u64 weights[kSlots + 1];   // of a token; of the list's slots the sum; the last one 0, for what has no counter
+    uint32_t counts[kPlaces];
+    u64 weights[kPlaces];      // of a token; of the list's slots the sum
     u64 list[kList / 2], sums[kList];
     uint32_t ties[kList];
     double table[kTable];
@@ -794,6 +819,20 @@ struct ByValue {
         const int i = (int)(b & 0x7FFFu) - kFirst, j = b & 0x8000u ? i + 1 : -1 - i;
         return (unsigned)i < (unsigned)kValues ? kMiddle + j : kSlots;
     }
+    // A slot's place in LDS.
+    static __device__ __forceinline__ int place_in(int slot)
+    {
+        const int j = slot - kMiddle;
+        return of_list(slot) ? 2 * kSide + (j > 0) - (j < 0) + 1 : j < 0 ? -j : kSide + j;
+    }
+    // Of two values' bits their places.
+    typedef uint16_t two __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ two places_of(uint32_t b)
+    {
+        const two v = __builtin_bit_cast(two, b);
+        const two m = __builtin_elementwise_min(__builtin_elementwise_max((two)(v & (two)0x7FFF), (two)(kFirst - 1)), (two)(kFirst + kValues));
+        return (v >> (two)15) * (two)kSide + (m - (two)(kFirst - 1));
+    }
     static __device__ __forceinline__ float value_of(int slot)
     {
         return bf16_to_f32((uint16_t)(slot < kMiddle ? kMiddle - 1 - slot + kFirst : slot - kMiddle - 1 + kFirst + 0x8000));
@@ -802,25 +841,24 @@ struct ByValue {
     static __device__ __forceinline__ int slot_of_listed(float v) { return v >= 1.0f ? 0 : v <= -1.0f ? kSlots - 1 : kMiddle; }
     __device__ __forceinline__ float listed(int i) const { return logit_of((uint32_t)(s.list[i] >> 32)); }
 
+    // f(bits of 8 logits by twos, first index, unit, last of a run)
     template <typename F>
-    __device__ __forceinline__ void units(F f)   // f(bits of 8 logits, first index, unit)
+    __device__ __forceinline__ void units(F f)
     {
-        constexpr int U = 3;   // units of a wavefront in flight
-        Held<T, false> h[U];
+        each_unit<T, false, NT>(a, x, lane, wave, [&](const Held<T, false> &h, int unit, bool last) {
+            uint32_t b[4] = {h.w[0][0], h.w[0][1], h.w[0][2], h.w[0][3]};
+            int at = unit * kUnit + lane * 8;
+            if (unit == a.units - 1) {   // those that the lane before has
+                const int from = min(at, a.vocab - 8);
 #pragma unroll
-        for (int n = 0; n < U; ++n) h[n].load(x, a.vocab, min(wave + n * WAVES, a.units - 1), lane);
-#pragma unroll 1
-        for (int unit = wave; unit < a.units; unit += WAVES) {
-            float v[8];
-            uint32_t b[8];
-            const int at = h[0].widen(v, a.vocab, unit, a.units, lane);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) b[i] = __builtin_bit_cast(uint32_t, v[i]) >> 16;
-#pragma unroll
-            for (int n = 0; n < U - 1; ++n) h[n] = h[n + 1];
-            h[U - 1].load(x, a.vocab, min(unit + U * WAVES, a.units - 1), lane);
-            f(b, at, unit);
-        }
+                for (int i = 0; i < 4; ++i) {
+                    if (from + 2 * i < at) b[i] = (b[i] & 0xFFFF0000u) | kForbidden;
+                    if (from + 2 * i + 1 < at) b[i] = (b[i] & 0xFFFFu) | kForbidden << 16;
+                }
+                at = from;
+            }
+            f(b, at, unit, last);
+        });
     }
     __device__ __forceinline__ const u64 *share_out(u64 v)
     {
@@ -859,8 +897,8 @@ struct ByValue {
     __device__ __forceinline__ u64 sum_of(int slot, const End &end) const
     {
         if (slot > end.slot) return 0;
-        if (!of_list(slot)) return (slot == end.slot ? (u64)end.tokens : (u64)s.counts[slot]) * s.weights[slot];
-        if (slot < end.slot) return s.weights[slot];
+        if (!of_list(slot)) return (slot == end.slot ? (u64)end.tokens : (u64)s.counts[place_in(slot)]) * s.weights[place_in(slot)];
+        if (slot < end.slot) return s.weights[place_in(slot)];
         u64 w = 0;
         for (int i = 0, at = first_of(slot); i < end.tokens; ++i) w += row.weight(listed(at + i));
         return w;
@@ -868,18 +906,19 @@ struct ByValue {
     // The first of a slot's tokens in the sorted list.
     __device__ __forceinline__ int first_of(int slot) const
     {
-        return (slot > 0 ? (int)s.counts[0] : 0) + (slot > kMiddle ? (int)s.counts[kMiddle] : 0);
+        return (slot > 0 ? (int)s.counts[2 * kSide] : 0) + (slot > kMiddle ? (int)s.counts[2 * kSide + 1] : 0);
     }
     // The slot in whose sums of by(slot), added up from the first, end(before, with) holds, or kSlots; *ahead: the sum before.
-    template <typename By, typename F>
-    __device__ __forceinline__ int crossing(By by, F end, u64 *ahead)
+    // known(sum of all) is called first.
+    template <typename By, typename F, typename G>
+    __device__ __forceinline__ int crossing(By by, F end, u64 *ahead, G known)
     {
         u64 own[PER], total = 0, all;
 #pragma unroll
         for (int i = 0; i < PER; ++i) own[i] = tid * PER + i < kSlots ? by(tid * PER + i) : 0, total += own[i];
-        u64 b = before(total, &all);
         if (tid == 0) s.found = kSlots;
-        __syncthreads();
+        u64 b = before(total, &all);
+        known(all);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             if (own[i] && end(b, b + own[i])) s.found = tid * PER + i, s.ahead = b;
@@ -903,36 +942,41 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     if (k < 1 || k > a.vocab) k = a.vocab;
     if (tid < kTable) s.table[tid] = exp2((double)tid / kTable);
     if (tid == 0) s.count = 0;
-    for (int i = tid; i < kSlots; i += NT) s.counts[i] = 0;
+    for (int i = tid; i < kPlaces; i += NT) s.counts[i] = 0, s.weights[i] = 0;
     for (int i = tid; i < kList; i += NT) s.sums[i] = 0, s.ties[i] = 0;
     __syncthreads();
     bool bad = false;
-    units([&](const uint32_t (&b)[8], int at, int) {
-        int slot[8];
+    units([&](const uint32_t (&b)[4], int at, int, bool) {
+        uint32_t place[4];
         bool any = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) slot[i] = slot_of(b[i]), any |= slot[i] == kSlots && b[i] != kForbidden;
+        for (int i = 0; i < 4; ++i) place[i] = __builtin_bit_cast(uint32_t, places_of(b[i]));
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (slot[i] < kSlots) atomicAdd(&s.counts[slot[i]], 1u);
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t v = i % 2 ? b[i / 2] >> 16 : b[i / 2] & 0xFFFFu, to = i % 2 ? place[i / 2] >> 16 : place[i / 2] & 0xFFFFu;
+            const bool in = (v & 0x7FFFu) - kFirst < (unsigned)kValues;
+            if (in) atomicAdd(&s.counts[to], 1u);
+            any |= !in && v != kForbidden;
+        }
         if (any)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (slot[i] == kSlots && b[i] != kForbidden) {
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t v = i % 2 ? b[i / 2] >> 16 : b[i / 2] & 0xFFFFu;
+                if ((v & 0x7FFFu) - kFirst >= (unsigned)kValues && v != kForbidden) {
                     const int c = atomicAdd(&s.count, 1);
-                    if (c < kList / 2) s.list[c] = place_of(bf16_to_f32((uint16_t)b[i]), at + i);
-                    bad |= (b[i] & 0x7FFFu) >= 0x7F80u;
+                    if (c < kList / 2) s.list[c] = place_of(bf16_to_f32((uint16_t)v), at + i);
+                    bad |= (v & 0x7FFFu) >= 0x7F80u;
                 }
+            }
     });
     bad = __syncthreads_or(bad);
     const int outside = s.count;
     if (!bad && outside > kList / 2) return false;
-    sort_list<NT>(s.list, bad ? 0 : outside, tid);
-    for (int i = tid; i < outside && !bad; i += NT) atomicAdd(&s.counts[slot_of_listed(listed(i))], 1u);
+    for (int i = tid; i < outside && !bad; i += NT) atomicAdd(&s.counts[place_in(slot_of_listed(listed(i)))], 1u);
     __syncthreads();
-    const auto number = [&](int slot) { return (u64)s.counts[slot]; };
+    const auto number = [&](int slot) { return (u64)s.counts[place_in(slot)]; };
     u64 ahead;
-    const int best = bad ? kSlots : crossing(number, [](u64 b, u64 w) { return b == 0 && w > 0; }, &ahead);
+    const int best = bad ? kSlots : crossing(number, [](u64 b, u64 w) { return b == 0 && w > 0; }, &ahead, [](u64) {});
     if (best == kSlots) {
         if (tid == 0) {
             a.token[r] = -1;
@@ -940,36 +984,45 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
         }
         return true;
     }
-    const float top = of_list(best) ? listed(first_of(best)) : value_of(best);
+    bool sorted = false;   // the list, where a slot of its own matters
+    const auto of_sorted_list = [&](int slot) {
+        if (of_list(slot) && !sorted) {
+            __syncthreads();
+            sort_list<NT>(s.list, outside, tid);
+            sorted = true;
+        }
+        return of_list(slot);
+    };
+    const float top = of_sorted_list(best) ? listed(first_of(best)) : value_of(best);
     row.top = top;
     row.factor = fmax(1.44269504088896340736 / (double)t, 1e-300);
     row.least = -(a.shift + 3) / row.factor;
     row.table = s.table;
     row.shift = a.shift;
     want = m > 0.0f ? ldexp((double)m, a.shift) : 0.0;
-    for (int i = tid; i <= kSlots; i += NT) s.weights[i] = i < kSlots && !of_list(i) ? row.weight(value_of(i)) : 0;
-    __syncthreads();
-    for (int i = tid; i < outside; i += NT) atomicAdd(&s.weights[slot_of_listed(listed(i))], row.weight(listed(i)));
+    for (int i = tid; i < kSlots; i += NT)
+        if (!of_list(i)) s.weights[place_in(i)] = row.weight(value_of(i));
+    for (int i = tid; i < outside; i += NT) atomicAdd(&s.weights[place_in(slot_of_listed(listed(i)))], row.weight(listed(i)));
     __syncthreads();
 
     End end = {kSlots, 0};
     if (k < a.vocab) {
-        const int slot = crossing(number, [&](u64 b, u64 w) { return b < (u64)k && (u64)k <= w; }, &ahead);
+        const int slot = crossing(number, [&](u64 b, u64 w) { return b < (u64)k && (u64)k <= w; }, &ahead, [](u64) {});
         if (slot < kSlots) end = {slot, k - (int)ahead};   // else there are fewer
+        of_sorted_list(slot);
     }
     if (p < 1.0f) {
-        const auto weight = [&](int slot) { return sum_of(slot, end); };
-        u64 own = 0;
-        for (int i = tid; i < kSlots; i += NT) own += weight(i);
-        const double most = (double)p * (double)sum(own);
+        double most = 0.0;   // known once the sums are
         const auto within = [&](u64 b) { return (double)b < most; };
-        const int slot = p > 0.0f ? crossing(weight, [&](u64 b, u64 w) { return within(b) && most <= (double)w; }, &ahead) : kSlots;
-        if (slot == kSlots) {
+        const int slot = crossing([&](int slot) { return sum_of(slot, end); },
+                                  [&](u64 b, u64 w) { return within(b) && most <= (double)w; }, &ahead,
+                                  [&](u64 total) { most = (double)p * (double)total; });
+        if (slot == kSlots) {   // p is not above 0
             end = {best, 1};
         } else {
             // how many have less than `most` before them
-            int tokens = slot == end.slot ? end.tokens : (int)s.counts[slot];
-            if (of_list(slot)) {
+            int tokens = slot == end.slot ? end.tokens : (int)s.counts[place_in(slot)];
+            if (of_sorted_list(slot)) {
                 u64 b = ahead;
                 int c = 0;
                 for (int at = first_of(slot); c < tokens && within(b); ++c) b += row.weight(listed(at + c));
@@ -978,7 +1031,7 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
                 int lo = 1, hi = tokens;   // the last has less than `most` before it, or is the first
                 while (lo < hi) {
                     const int mid = (lo + hi + 1) / 2;
-                    if (within(ahead + (u64)(mid - 1) * s.weights[slot])) lo = mid;
+                    if (within(ahead + (u64)(mid - 1) * s.weights[place_in(slot)])) lo = mid;
                     else hi = mid - 1;
                 }
                 tokens = lo;
@@ -992,34 +1045,40 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
         const int slot = slot_of_listed(v);
         return (slot < end.slot || (slot == end.slot && place >= cut)) && (row.share(v) >= want || (slot == best && v == top));
     };
-    const bool some = end.slot < kSlots && !of_list(end.slot) && end.tokens < (int)s.counts[end.slot];
+    const bool some = end.slot < kSlots && !of_list(end.slot) && end.tokens < (int)s.counts[place_in(end.slot)];
     u64 tie = 0;   // the weight of a token of the last slot, where not all of them stay
-    if (some && (end.slot == best || row.share(value_of(end.slot)) >= want)) tie = s.weights[end.slot];
+    if (some && (end.slot == best || row.share(value_of(end.slot)) >= want)) tie = s.weights[place_in(end.slot)];
     __syncthreads();
     for (int i = tid; i < kSlots; i += NT)
-        if (i > end.slot || (some && i == end.slot) || (i != best && !of_list(i) && row.share(value_of(i)) < want)) s.weights[i] = 0;
+        if (i > end.slot || (some && i == end.slot) || (i != best && !of_list(i) && row.share(value_of(i)) < want)) s.weights[place_in(i)] = 0;
     for (int i = tid; i < outside; i += NT) {
         const u64 q = s.list[i];
         if (kept(listed(i), q)) atomicAdd(&s.sums[(int)(~(uint32_t)q) / kUnit / a.runs], row.weight(listed(i)));
     }
     __syncthreads();
 
-    // Sums of runs of units, in the vocabulary's order, and how many tokens of the last slot each holds.
-    units([&](const uint32_t (&b)[8], int, int unit) {
-        u64 w = 0;
-        uint32_t ties = 0;
+    // Sums of runs of units, in the vocabulary's order, and how many tokens of the last slot each holds.  Values that are
+    // not kept weigh 0; they are looked up in one place, where lanes do not wait for one another.
+    const float from = end.slot == kSlots ? kNegInf : !of_list(end.slot) ? value_of(end.slot)
+                       : end.slot == 0 ? __builtin_inff() : end.slot == kMiddle ? 0.0f : kNegInf;
+    const uint32_t tie_bits = tie ? __builtin_bit_cast(uint32_t, value_of(end.slot)) >> 16 : 0x10000u;
+    u64 w = 0;
+    uint32_t ties = 0;
+    units([&](const uint32_t (&b)[4], int, int unit, bool last) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int slot = slot_of(b[i]);
-            w += s.weights[slot];
-            ties += slot == end.slot;
+            const uint32_t place = __builtin_bit_cast(uint32_t, places_of(b[i / 2])), v = i % 2 ? b[i / 2] >> 16 : b[i / 2] & 0xFFFFu;
+            const bool is = __builtin_bit_cast(float, i % 2 ? b[i / 2] & 0xFFFF0000u : b[i / 2] << 16) >= from;
+            w += s.weights[is ? i % 2 ? place >> 16 : place & 0xFFFFu : 0];
+            ties += (uint32_t)__builtin_popcountll(__ballot(v == tie_bits));
         }
+        if (!last) return;
         w = wave_sum(w);
-        if (lane == 0 && w) atomicAdd(&s.sums[unit / a.runs], w);
-        if (tie) {
-            ties = (uint32_t)wave_sum(ties);
-            if (lane == 0 && ties) atomicAdd(&s.ties[unit / a.runs], ties);
+        if (lane == 0) {
+            if (w) atomicAdd(&s.sums[unit / a.runs], w);   // beside the list's tokens
+            s.ties[unit / a.runs] = ties;
         }
+        w = 0, ties = 0;
     });
     __syncthreads();
     const int parts = (a.units + a.runs - 1) / a.runs;
@@ -1054,17 +1113,17 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     for (int un = g * a.runs; un < min((g + 1) * a.runs, a.units); ++un) {
         Held<T, false> h;
         float v[8];
-        u64 w[8], own = 0, ties = 0;
+        u64 w[8], own = 0, tied = 0;
         h.load(x, a.vocab, un, lane);
         const int at = h.widen(v, a.vocab, un, a.units, lane);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ties += tie && slot_of(__builtin_bit_cast(uint32_t, v[i]) >> 16) == end.slot;
-        const u64 in_ties = wave_scan(ties);
-        u64 rank = t0 + in_ties - ties;
+        for (int i = 0; i < 8; ++i) tied += tie && slot_of(__builtin_bit_cast(uint32_t, v[i]) >> 16) == end.slot;
+        const u64 in_ties = wave_scan(tied);
+        u64 rank = t0 + in_ties - tied;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int slot = slot_of(__builtin_bit_cast(uint32_t, v[i]) >> 16);
-            w[i] = s.weights[slot];
+            w[i] = slot < kSlots ? s.weights[place_in(slot)] : 0;
             if (slot == kSlots && v[i] > kNegInf && kept(v[i], place_of(v[i], at + i))) w[i] = row.weight(v[i]);
             if (tie && slot == end.slot) w[i] = rank++ < (u64)end.tokens ? tie : 0;
             own += w[i];
@@ -1140,7 +1199,9 @@ extern "C" int sample_tokens(long rows, long vocab, int dtype, const void *x, lo
     while (1L << bits < vocab) ++bits;
     SampleArgs a = {x, stride, (int)vocab, u, temperature, top_p, min_p, top_k, token, logprob,
                     62 - bits < 51 ? 62 - bits : 51, (int)((vocab + kUnit - 1) / kUnit), 0};
-    a.runs = (a.units + kList - 1) / kList;
+    // Runs of up to 8 units, so that their sums are few, and 48 or more runs for the wavefronts.
+    a.runs = 1;
+    while ((a.units / (2 * a.runs) >= 48 && a.runs < 8) || (a.units + a.runs - 1) / a.runs > kList) a.runs *= 2;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const dim3 grid((unsigned)rows);
     const auto go = [&](auto of) {
