@@ -78,7 +78,7 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul_f8_tile_kernel(F8Arg
     const int wid = __builtin_amdgcn_readfirstlane(tid / 64);
     int m0, n0;
     tile_of(a, blockIdx.x, &m0, &n0);
-    m0 *= BM, n0 *= BN;
+    m0 = __builtin_amdgcn_readfirstlane(m0) * BM, n0 = __builtin_amdgcn_readfirstlane(n0) * BN;
     const int nm = min(a.M - m0, BM), nn = min(a.N - n0, BN);
     const int8_t *pa = a.a + (long)m0 * a.as, *pw = a.w + (long)n0 * a.ws;
     const int steps = ceil_div(f.blocks, KG);   // group kg has blocks t * KG + kg
@@ -96,7 +96,9 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul_f8_tile_kernel(F8Arg
     }
     // Its row's exponents: channels first, then tokens.  Where there is no such row, or block, those of the last stand in:
     // the values are 0 there, or belong to no output.
-    const uint8_t *ep = tid < BN ? f.ew + (n0 + min(tid, nn - 1)) * f.ews : f.ea + (m0 + min(max(tid - BN, 0), nm - 1)) * f.eas;
+    const bool of_w = tid < BN;
+    const int last = (of_w ? nn : nm) - 1, erow = min(max(of_w ? tid : tid - BN, 0), last);
+    const uint8_t *ep = (of_w ? f.ew : f.ea) + ((of_w ? n0 : m0) + erow) * (of_w ? f.ews : f.eas);
     f32x4 acc[TN][TM] = {};
     int waddr[TN], aaddr[TM];
 #pragma unroll
@@ -136,26 +138,29 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul_f8_tile_kernel(F8Arg
                 __builtin_amdgcn_s_setprio(0);
             }
         } else {
-            i32x8 fa[TM];
+            i32x8 fa[TM], fw[2];   // the next channels' weights come while these are multiplied
+            fw[0] = operand(st, waddr[0]);
 #pragma unroll
             for (int j = 0; j < TM; ++j) fa[j] = operand(st, aaddr[j]);
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int i = 0; i < TN; ++i) {
-                const i32x8 fw = operand(st, waddr[i]);
+                if (i + 1 < TN) fw[(i + 1) % 2] = operand(st, waddr[i + 1]);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int j = 0; j < TM; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw, fa[j], acc[i][j], 0, 0, 0, ew[i], 0, ea[j]);
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i % 2], fa[j], acc[i][j], 0, 0, 0, ew[i], 0, ea[j]);
+                __builtin_amdgcn_sched_barrier(0);
             }
             __builtin_amdgcn_s_setprio(0);
         }
     };
 
     i32x4 *mine = smem + kg * STAGE;   // this group's part of the first stage
-    const auto buffer = [](const void *p, long bytes) {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)0, (int)bytes, 0x00020000);
-    };
-    const __amdgpu_buffer_rsrc_t wres = buffer(pw, (nn - 1) * a.ws + a.K), ares = buffer(pa, (nm - 1) * a.as + a.K);
+    const __amdgpu_buffer_rsrc_t wres = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<int8_t *>(pw), (short)0, __builtin_amdgcn_readfirstlane((int)((nn - 1) * a.ws + a.K)), 0x00020000);
+    const __amdgpu_buffer_rsrc_t ares = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<int8_t *>(pa), (short)0, __builtin_amdgcn_readfirstlane((int)((nm - 1) * a.as + a.K)), 0x00020000);
     constexpr int PER = LOADS + 1;   // loads of a stage
     const auto issue = [&](int t, int stage) {
         i32x4 *st = mine + stage * (KG * STAGE) + wid * 64;
