@@ -774,8 +774,8 @@ __global__ __launch_bounds__(512, 2) void attend_kv4_wide_kernel(AttArgs a)
     attend_wide<Fp4, D>(a);
 }
 
-template <int D>
-__global__ __launch_bounds__(512, 2) void attend_kv8_wide_kernel(AttArgs a)
+template <int D>   // up to 64 channels four wavefronts a SIMD, which 128 registers allow (left alone it takes 134)
+__global__ __launch_bounds__(512, D <= 64 ? 4 : 2) void attend_kv8_wide_kernel(AttArgs a)
 {
     attend_wide<Fp8, D>(a);
 }

@@ -40,18 +40,21 @@ struct WriteArgs {
     const int32_t *starts, *lens, *table;
     int table_stride, max_new;
     int units;                     // of 8 channels in a head's row
-    FastDiv dv_units;
+    FastDiv dv_units, dv_heads;
 };
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu; }
 
-template <typename T, int NT>
+// PER > 0: the new tokens of a block are PER units of 8 channels a thread at most, read once and kept; 0: read twice.
+template <typename T, int NT, int PER>
 __global__ __launch_bounds__(NT) void kv8_write_kernel(WriteArgs a)
 {
     constexpr int WAVES = NT / 64;
     __shared__ uint32_t tops[2][WAVES > 1 ? WAVES : 1], bad[256];
     const KvView &c = a.c;
-    const int s = blockIdx.z, head = blockIdx.y, tid = threadIdx.x;
+    // heads first: work-groups that run together read a token's row together
+    const int s = blockIdx.y, at_block = (int)fdiv(blockIdx.x, a.dv_heads), head = (int)blockIdx.x - at_block * c.heads;
+    const int tid = threadIdx.x;
     long r0 = a.starts ? a.starts[s] : s, r1 = a.starts ? a.starts[s + 1] : s + 1;
     r0 = r0 < 0 ? 0 : r0 > a.tokens ? a.tokens : r0;
     r1 = r1 < r0 ? r0 : r1 > a.tokens ? a.tokens : r1;
@@ -61,7 +64,7 @@ __global__ __launch_bounds__(NT) void kv8_write_kernel(WriteArgs a)
     const long begin = (long)len - news;
     const long end = min(min((long)len, begin + a.max_new), room);
     const long first = begin < 0 ? 0 : begin;
-    const long p0 = ((long)fdiv((unsigned)first, c.dv_block) + blockIdx.x) * c.block;   // the block's first place
+    const long p0 = ((long)fdiv((unsigned)first, c.dv_block) + at_block) * c.block;   // the block's first place
     if (p0 >= end) return;
     const int lo = (int)(max(first, p0) - p0), hi = (int)(min(end, p0 + c.block) - p0);   // its new tokens
     if (lo >= hi) return;
@@ -79,6 +82,32 @@ __global__ __launch_bounds__(NT) void kv8_write_kernel(WriteArgs a)
         const T *p = (const T *)(val ? a.v : a.k) + (src0 + tok) * (val ? a.vs : a.ks) + (long)head * c.dim + 8 * u;
         load8(p, x);
     };
+    float kept[PER > 0 ? PER : 1][8];
+    if constexpr (PER > 0) {
+#pragma unroll
+        for (int n = 0; n < PER; ++n) {
+            int tok, u;
+            const int i = min(n * NT + tid, 2 * count - 1);
+            load(i >= count ? i - count : i, i >= count, kept[n], tok, u);
+        }
+    }
+    // f(values, token, unit, whether they are values) of this thread's units
+    const auto each = [&](auto f) {
+        if constexpr (PER > 0) {
+#pragma unroll
+            for (int n = 0; n < PER; ++n) {
+                const int i = n * NT + tid, in = i >= count ? i - count : i, tok = (int)fdiv((unsigned)in, a.dv_units);
+                if (i < 2 * count) f(kept[n], tok + lo, in - tok * a.units, i >= count);
+            }
+        } else {
+            for (int i = tid; i < 2 * count; i += NT) {
+                float x[8];
+                int tok, u;
+                load(i >= count ? i - count : i, i >= count, x, tok, u);
+                f(x, tok, u, i >= count);
+            }
+        }
+    };
     const auto reduce = [&](uint32_t &tk, uint32_t &tv) {   // the work-group's largest
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -94,17 +123,13 @@ __global__ __launch_bounds__(NT) void kv8_write_kernel(WriteArgs a)
         }
     };
     uint32_t top[2] = {0, 0};
-    for (int i = tid; i < 2 * count; i += NT) {
-        const bool val = i >= count;
-        float x[8];
-        int tok, u;
-        load(val ? i - count : i, val, x, tok, u);
+    each([&](const float (&x)[8], int, int, bool val) {
         uint32_t t = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) t = max(t, magnitude(x[j]));
         if (val) top[1] = max(top[1], t);
         else top[0] = max(top[0], t);
-    }
+    });
     reduce(top[0], top[1]);
     const bool any_bad = max(top[0], top[1]) >= 0x7F800000u;   // the same for all threads
     if (any_bad) {   // which tokens, and the largest of the others
@@ -112,11 +137,7 @@ __global__ __launch_bounds__(NT) void kv8_write_kernel(WriteArgs a)
         __syncthreads();
         for (int pass = 0; pass < 2; ++pass) {
             top[0] = top[1] = 0;
-            for (int i = tid; i < 2 * count; i += NT) {
-                const bool val = i >= count;
-                float x[8];
-                int tok, u;
-                load(val ? i - count : i, val, x, tok, u);
+            each([&](const float (&x)[8], int tok, int, bool val) {
                 uint32_t t = 0;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) t = max(t, magnitude(x[j]));
@@ -126,7 +147,7 @@ __global__ __launch_bounds__(NT) void kv8_write_kernel(WriteArgs a)
                     if (val) top[1] = max(top[1], t);
                     else top[0] = max(top[0], t);
                 }
-            }
+            });
             __syncthreads();
         }
         reduce(top[0], top[1]);
@@ -136,15 +157,12 @@ __global__ __launch_bounds__(NT) void kv8_write_kernel(WriteArgs a)
 #pragma unroll
     for (int n = 0; n < 2; ++n) was[n] = min(was[n], kF8Hi), byte[n] = max(byte[n], was[n]);
     const float power[2] = {f8_power(byte[0]), f8_power(byte[1])};
-    for (int i = tid; i < 2 * count; i += NT) {
-        const bool val = i >= count;
-        float x[8];
-        int tok, u;
-        load(val ? i - count : i, val, x, tok, u);
-        uint32_t v[2] = {f8_encode4(x, power[val]), f8_encode4(x + 4, power[val])};
+    each([&](const float (&x)[8], int tok, int u, bool val) {
+        const float p = val ? power[1] : power[0];
+        uint32_t v[2] = {f8_encode4(x, p), f8_encode4(x + 4, p)};
         if (any_bad && bad[tok]) v[0] = v[1] = val ? 0u : 0x7F7F7F7Fu;
         memcpy((val ? c.vc : c.kc) + at_code + (long)tok * c.dim + 8 * u, v, 8);
-    }
+    });
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
         if (lo == 0 || byte[n] == was[n]) continue;   // nothing held, or its exponent stays
@@ -228,8 +246,9 @@ extern "C" int quant_kv8_write(const quant_kv8 *cache, int seqs, long tokens, in
     if (seqs > 65535 || tokens >= 1L << 31) return MICONV_ERR_TOO_LARGE;
     // Blocks that new tokens can reach, wherever they begin.
     const long blocks = ((long)max_new + a.c.block - 2) / a.c.block + 1;
-    const int nt = (std::min((long)max_new, (long)a.c.block) * a.c.dim / 8 * 2) > 64 ? 256 : 64;
-    if (blocks * nt >= 1L << 32) return MICONV_ERR_TOO_LARGE;   // a grid holds fewer than 2^32 threads
+    const long most = std::min((long)max_new, (long)a.c.block) * (a.c.dim / 8) * 2;   // units of a block's new tokens
+    const int nt = most > 64 ? 256 : 64;
+    if (blocks * a.c.heads * nt >= 1L << 32 || blocks * a.c.heads >= 1L << 31) return MICONV_ERR_TOO_LARGE;   // threads of a grid
     if (seqs == 0 || tokens == 0) return MICONV_OK;
     if (!k || !v || !lens || !table) return MICONV_ERR_NULL;
     if (misaligned(k, b) || misaligned(v, b) || misaligned(starts, 4) || misaligned(lens, 4) || misaligned(table, 4))
@@ -239,13 +258,21 @@ extern "C" int quant_kv8_write(const quant_kv8 *cache, int seqs, long tokens, in
     a.table_stride = table_stride, a.max_new = max_new;
     a.units = a.c.dim / 8;
     a.dv_units = make_fastdiv((unsigned)a.units);
-    const dim3 grid((unsigned)blocks, (unsigned)a.c.heads, (unsigned)seqs);
+    a.dv_heads = make_fastdiv((unsigned)a.c.heads);
+    const dim3 grid((unsigned)(blocks * a.c.heads), (unsigned)seqs);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (nt == 64)
-        launch_kernel(dtype == kF32 ? kv8_write_kernel<float, 64> : kv8_write_kernel<uint16_t, 64>, grid, dim3(64), 0, st, a);
-    else
-        launch_kernel(dtype == kF32 ? kv8_write_kernel<float, 256> : kv8_write_kernel<uint16_t, 256>, grid, dim3(256), 0, st, a);
-    return launched();
+    const auto go = [&](auto of) {
+        typedef decltype(of) T;
+        void (*kernel)(WriteArgs) = kv8_write_kernel<T, 256, 0>;
+        if (nt == 64) kernel = kv8_write_kernel<T, 64, 1>;
+        else if (most <= 256) kernel = kv8_write_kernel<T, 256, 1>;
+        else if (most <= 512) kernel = kv8_write_kernel<T, 256, 2>;
+        else if (most <= 1024) kernel = kv8_write_kernel<T, 256, 4>;
+        else if (most <= 2048) kernel = kv8_write_kernel<T, 256, 8>;
+        launch_kernel(kernel, grid, dim3((unsigned)nt), 0, st, a);
+        return launched();
+    };
+    return dtype == kF32 ? go(float()) : go(uint16_t());
 }
 
 extern "C" int quant_kv8_read(const quant_kv8 *cache, long tokens, const int32_t *slots, int dtype, void *k,
