@@ -222,6 +222,39 @@ __device__ __forceinline__ void each_unit(const SampleArgs &a, const T *x, int l
     }
 }
 
+// For one wavefront: of up to 128 sums, two neighbours a lane, the one that a share u of all falls into, what comes
+// before it, and the total.  (For more of them the work-group looks.)
+constexpr int kPairs = 128;
+struct Fall {
+    int part;
+    u64 before, total;
+    double target;
+};
+__device__ __forceinline__ Fall fall_into(u64 w0, u64 w1, float u, int lane)
+{
+    const u64 in = wave_scan(w0 + w1), b0 = in - w0 - w1, b1 = in - w1;
+    Fall f;
+    f.total = last_lane(in);
+    f.target = (double)u * (double)f.total;
+    const bool hit0 = w0 && (double)b0 <= f.target && f.target < (double)b1;
+    const bool hit1 = w1 && (double)b1 <= f.target && f.target < (double)in;
+    const u64 hits = __ballot(hit0 || hit1);
+    const int at = hits ? __builtin_ctzll(hits) : 0;
+    f.part = 2 * at + __builtin_amdgcn_readlane((int)hit1, at);
+    const u64 b = hit1 ? b1 : b0;
+    f.before = (u64)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), at) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, at);
+    return f;
+}
+__device__ __forceinline__ u64 from_any(u64 v, int lane)   // of one lane, the same for all
+{
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+__device__ __forceinline__ float drawn(const SampleArgs &a, long r)   // u as it counts
+{
+    const float u = a.u[r];
+    return u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
+}
+
 template <typename T, int NT, bool SHORT>
 struct Picker {
     static constexpr int WAVES = NT / 64, BINS = NT > 256 ? 8192 : kDigit;   // BINS: of logits, 32 bits each
@@ -309,7 +342,8 @@ struct Picker {
         *all = total;
         return base + in - v;
     }
-    __device__ __forceinline__ int bin_of(float v) const { return (int)fminf(fmaxf((anchor - v) * inv, 0.0f), (float)(BINS - 1)); }
+    template <int N = BINS>
+    __device__ __forceinline__ int bin_of(float v) const { return (int)fminf(fmaxf((anchor - v) * inv, 0.0f), (float)(N - 1)); }
 
     template <typename V, int N>
     __device__ __forceinline__ void clear(V (&bins)[N])
@@ -318,8 +352,8 @@ struct Picker {
         __syncthreads();
     }
     // The bin in whose sums, added up from the first, `end(sum before, sum with it)` holds; these sums.
-    template <typename V, int N, typename F>
-    __device__ __forceinline__ int crossing(const V (&bins)[N], F end, u64 *ahead, u64 *with)
+    template <int N, typename V, typename F>
+    __device__ __forceinline__ int crossing(const V *bins, F end, u64 *ahead, u64 *with)
     {
         constexpr int PER = N / NT;
         u64 total = 0, all;
@@ -431,7 +465,7 @@ struct Picker {
             });
             __syncthreads();
             u64 b, w;
-            const int bin = crossing(s.digits, [&](u64 p, u64 q) {
+            const int bin = crossing<kDigit>(s.digits, [&](u64 p, u64 q) {
                 return count ? ahead + p < k && k <= ahead + q : (double)(ahead + p) < most && most <= (double)(ahead + q);
             }, &b, &w);
             prefix |= (u64)(kDigit - 1 - bin) << at, ahead += b;
@@ -450,6 +484,39 @@ struct Picker {
 
     __device__ __forceinline__ u64 search(long r, u64 floor, bool count, u64 k, double most);
     __device__ __forceinline__ void run(long r);
+    // The n <= 64 first tokens of the list, by one wavefront: ordered, cut off after k, at p (`one`: after the first) and
+    // below floor_v, and drawn from.
+    __device__ __forceinline__ void finish_few(long r, int n, int k, float p, bool one, float floor_v)
+    {
+        u64 q = lane < n ? s.list[lane] : 0;
+        int rank = 0;
+        for (int i = 0; i < n; ++i) rank += from_any(q, i) > q;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (lane < n) s.list[rank] = q;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        q = lane < n ? s.list[lane] : 0;
+        const float v = logit_of((uint32_t)(q >> 32));
+        n = min(n, k);
+        u64 w = lane < n ? row.weight(v) : 0, in = wave_scan(w);
+        if (p < 1.0f) {
+            const double most = (double)p * (double)last_lane(in);
+            if (lane > 0 && (one || (double)(in - w) >= most)) w = 0;
+        }
+        if (v < floor_v) w = 0;
+        // the sum of what is kept with a lower index
+        const uint32_t index = ~(uint32_t)q;
+        u64 b = 0, total = 0;
+        for (int i = 0; i < n; ++i) {
+            const u64 o = from_any(w, i);
+            b += (uint32_t)__builtin_amdgcn_readlane((int)index, i) < index ? o : 0;
+            total += o;
+        }
+        const double target = (double)drawn(a, r) * (double)total;
+        if (w && (double)b <= target && target < (double)(b + w)) {
+            a.token[r] = (int)index;
+            if (a.logprob) a.logprob[r] = logprob(v, total);
+        }
+    }
     __device__ __forceinline__ void done(long r, int token, float logprob)
     {
         if (tid == 0) {
@@ -509,7 +576,29 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
     float most_v = kNegInf;
     int most_i = 0;
     bool bad = false;
-    units([&](const float (&v)[8], int at, int, bool) {
+    // Rows of few units stay in registers for the search of the first few.
+    constexpr int HELD = SHORT || NT == 256 ? 1 : 8;
+    Held<T, SHORT> h[HELD];
+    const bool held = by_k && k <= NT / 4 && a.units <= HELD * WAVES && a.runs == 1;
+    const auto each_held = [&](auto f) {
+#pragma unroll
+        for (int n = 0; n < HELD; ++n) {
+            const int unit = wave + n * WAVES;
+            float v[8];
+            const int at = h[n].widen(v, a.vocab, min(unit, a.units - 1), a.units, lane);
+            if (unit < a.units)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f(v[i], at + i);
+        }
+    };
+    if (held) {
+#pragma unroll
+        for (int n = 0; n < HELD; ++n) h[n].load(x, a.vocab, min(wave + n * WAVES, a.units - 1), lane);
+        each_held([&](float v, int i) {
+            if (v > most_v) most_v = v, most_i = i;
+            bad |= !(v < __builtin_inff());
+        });
+    } else units([&](const float (&v)[8], int at, int, bool) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (v[i] > most_v) most_v = v[i], most_i = at + i;
@@ -556,16 +645,43 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
     if (by_k) {
         // For few: k threads' largest logits are k tokens, so that nothing below the last of these counts.
         const bool few = k <= NT / 4;
-        float low = few ? -logit_of(largest(most_v > kNegInf ? key_of(-most_v) : 0u)) : top - 64.0f * fmaxf(t, 1.0f);
-        anchor = top;
-        inv = top > low ? fminf((float)BINS / (top - low), 0x1p100f) : 0.0f;
-        clear(s.counts);
-        if (few) atomicAdd(&s.counts[bin_of(most_v)], 1u);
-        else scan([&](float v, int) { atomicAdd(&s.counts[bin_of(v)], 1u); });
-        __syncthreads();
+        const auto end = [&](u64 b, u64 w) { return b < (u64)k && (u64)k <= w; };
         u64 ahead, with;
-        const int bin = crossing(s.counts, [&](u64 b, u64 w) { return b < (u64)k && (u64)k <= w; }, &ahead, &with);
-        n = gather([&](float v, int) { return bin_of(v) <= bin; });
+        anchor = top;
+        if (few) {
+            const float low = -logit_of(largest(most_v > kNegInf ? key_of(-most_v) : 0u));
+            inv = top > low ? fminf((float)NT / (top - low), 0x1p100f) : 0.0f;
+            s.counts[tid] = 0;
+            __syncthreads();
+            atomicAdd(&s.counts[bin_of<NT>(most_v)], 1u);
+            __syncthreads();
+            const int bin = crossing<NT>(s.counts, end, &ahead, &with);
+            if (tid == 0) s.count = 0;
+            __syncthreads();
+            if (held) {
+                if (bin_of<NT>(most_v) <= bin)
+                    each_held([&](float v, int i) {
+                        if (bin_of<NT>(v) <= bin) put(v, i);
+                    });
+            } else {
+                scan([&](float v, int i) {
+                    if (bin_of<NT>(v) <= bin) put(v, i);
+                });
+            }
+            __syncthreads();
+            n = s.count;
+        } else {
+            inv = fminf((float)BINS / (64.0f * fmaxf(t, 1.0f)), 0x1p100f);
+            clear(s.counts);
+            scan([&](float v, int) { atomicAdd(&s.counts[bin_of(v)], 1u); });
+            __syncthreads();
+            const int bin = crossing<BINS>(s.counts, end, &ahead, &with);
+            n = gather([&](float v, int) { return bin_of(v) <= bin; });
+        }
+        if (n <= 64) {
+            if (wave == 0) finish_few(r, n, k, p, cut != 0, floor_v);
+            return;
+        }
         if (n <= kList) {
             sort(n);
             n = k;
@@ -670,8 +786,7 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
         const u64 q = place_of(v, i);
         return v > kNegInf && q >= cut && v >= floor_v ? row.weight(v) : 0;
     };
-    float u = a.u[r];
-    u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
+    const float u = drawn(a, r);
     __syncthreads();
     if (n) {   // everything is in the list: by index
         const int held = n;
@@ -719,22 +834,29 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
         });
         __syncthreads();
     }
-    u64 total = 0;
-    for (int i = tid; i < parts; i += NT) total += s.sums[i];
-    total = sum(total);
-    const double target = (double)u * (double)total;
-    u64 ahead = 0;
-    for (int i0 = 0; i0 < parts; i0 += NT) {
-        const int i = i0 + tid;
-        u64 all;
-        const u64 w = i < parts ? s.sums[i] : 0, b = ahead + before(w, &all);
-        if (w && (double)b <= target && target < (double)(b + w)) s.found = i, s.ahead = b;
-        ahead += all;
+    int g;
+    u64 b0, total = 0;
+    double target;
+    if (parts <= kPairs) {
+        if (wave != 0) return;
+        const Fall f = fall_into(2 * lane < parts ? s.sums[2 * lane] : 0, 2 * lane + 1 < parts ? s.sums[2 * lane + 1] : 0, u, lane);
+        g = f.part, b0 = f.before, total = f.total, target = f.target;
+    } else {
+        for (int i = tid; i < parts; i += NT) total += s.sums[i];
+        total = sum(total);
+        target = (double)u * (double)total;
+        u64 ahead = 0;
+        for (int i0 = 0; i0 < parts; i0 += NT) {
+            const int i = i0 + tid;
+            u64 all;
+            const u64 w = i < parts ? s.sums[i] : 0, b = ahead + before(w, &all);
+            if (w && (double)b <= target && target < (double)(b + w)) s.found = i, s.ahead = b;
+            ahead += all;
+        }
+        __syncthreads();
+        if (wave != 0) return;
+        g = s.found, b0 = s.ahead;
     }
-    __syncthreads();
-    if (wave != 0) return;
-    const int g = s.found;
-    u64 b0 = s.ahead;
     for (int un = g * a.runs; un < min((g + 1) * a.runs, a.units); ++un) {
         Held<T, SHORT> h;
         float v[8];
@@ -792,8 +914,8 @@ struct Values {
     u64 list[kList / 2], sums[kList];
     uint32_t ties[kList];
     double table[kTable];
-    u64 part[2][16], ahead;
-    int found, count;
+    u64 part[2][16], ahead[2];
+    int found[2], count;
 };
 
 template <int NT>
@@ -806,7 +928,7 @@ struct ByValue {
     const int tid, lane, wave;
     Row row;
     double want = 0.0;   // the weight that min_p asks for
-    int turn = 0;
+    int turn = 0, found_turn = 0;
 
     __device__ __forceinline__ ByValue(const SampleArgs &args, Values &sh, long r)
         : a(args), s(sh), x((const T *)args.x + r * args.stride), tid(threadIdx.x), lane(threadIdx.x % 64),
@@ -913,20 +1035,23 @@ struct ByValue {
     template <typename By, typename F, typename G>
     __device__ __forceinline__ int crossing(By by, F end, u64 *ahead, G known)
     {
+        // Calls take turns at two results: of the one before, some thread may still be reading.
+        const int at = found_turn;
+        found_turn ^= 1;
         u64 own[PER], total = 0, all;
 #pragma unroll
         for (int i = 0; i < PER; ++i) own[i] = tid * PER + i < kSlots ? by(tid * PER + i) : 0, total += own[i];
-        if (tid == 0) s.found = kSlots;
+        if (tid == 0) s.found[at] = kSlots;
         u64 b = before(total, &all);
         known(all);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            if (own[i] && end(b, b + own[i])) s.found = tid * PER + i, s.ahead = b;
+            if (own[i] && end(b, b + own[i])) s.found[at] = tid * PER + i, s.ahead[at] = b;
             b += own[i];
         }
         __syncthreads();
-        *ahead = s.ahead;
-        return s.found;
+        *ahead = s.ahead[at];
+        return s.found[at];
     }
     // Whether the row could be taken so.
     __device__ __forceinline__ bool run(long r);
@@ -976,7 +1101,14 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     __syncthreads();
     const auto number = [&](int slot) { return (u64)s.counts[place_in(slot)]; };
     u64 ahead;
-    const int best = bad ? kSlots : crossing(number, [](u64 b, u64 w) { return b == 0 && w > 0; }, &ahead, [](u64) {});
+    uint32_t left = 0;   // slots from the first one that is taken on
+#pragma unroll
+    for (int i = PER - 1; i >= 0; --i)
+        if (tid * PER + i < kSlots && !bad && number(tid * PER + i)) left = kSlots - (tid * PER + i);
+    const u64 *lefts = share_out(wave_max(left));
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) left = max(left, (uint32_t)lefts[i]);
+    const int best = kSlots - (int)left;
     if (best == kSlots) {
         if (tid == 0) {
             a.token[r] = -1;
@@ -1028,13 +1160,12 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
                 for (int at = first_of(slot); c < tokens && within(b); ++c) b += row.weight(listed(at + c));
                 tokens = c;
             } else {
-                int lo = 1, hi = tokens;   // the last has less than `most` before it, or is the first
-                while (lo < hi) {
-                    const int mid = (lo + hi + 1) / 2;
-                    if (within(ahead + (u64)(mid - 1) * s.weights[place_in(slot)])) lo = mid;
-                    else hi = mid - 1;
-                }
-                tokens = lo;
+                // the last has less than `most` before it, or is the first: about so many, and then exactly
+                const u64 each = s.weights[place_in(slot)];
+                int c = (int)fmin(fmax((most - (double)ahead) / (double)each, 1.0), (double)tokens);
+                while (c < tokens && within(ahead + (u64)c * each)) ++c;
+                while (c > 1 && !within(ahead + (u64)(c - 1) * each)) --c;
+                tokens = c;
             }
             end = {slot, tokens};
         }
@@ -1049,7 +1180,7 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     u64 tie = 0;   // the weight of a token of the last slot, where not all of them stay
     if (some && (end.slot == best || row.share(value_of(end.slot)) >= want)) tie = s.weights[place_in(end.slot)];
     __syncthreads();
-    for (int i = tid; i < kSlots; i += NT)
+    for (int i = m > 0.0f ? tid : min(end.slot, kSlots) / NT * NT + tid; i < kSlots; i += NT)
         if (i > end.slot || (some && i == end.slot) || (i != best && !of_list(i) && row.share(value_of(i)) < want)) s.weights[place_in(i)] = 0;
     for (int i = tid; i < outside; i += NT) {
         const u64 q = s.list[i];
@@ -1082,34 +1213,48 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     });
     __syncthreads();
     const int parts = (a.units + a.runs - 1) / a.runs;
-    u64 total = 0, all, seen = 0;
-    if (tie)
+    const float u = drawn(a, r);
+    // of a part's tokens of the last slot, b of which come before them, those that stay
+    const auto of_ties = [&](u64 c, u64 b) { return (b >= (u64)end.tokens ? 0 : min(c, (u64)end.tokens - b)) * tie; };
+    int g;
+    u64 b0, t0, total = 0;
+    double target;
+    if (parts <= kPairs) {
+        if (wave != 0) return true;
+        const int i = 2 * lane;
+        u64 w0 = i < parts ? s.sums[i] : 0, w1 = i + 1 < parts ? s.sums[i + 1] : 0, c0 = 0, c1 = 0, before_c = 0;
+        if (tie) {
+            c0 = i < parts ? s.ties[i] : 0, c1 = i + 1 < parts ? s.ties[i + 1] : 0;
+            before_c = wave_scan(c0 + c1) - c0 - c1;
+            w0 += of_ties(c0, before_c), w1 += of_ties(c1, before_c + c0);
+        }
+        const Fall f = fall_into(w0, w1, u, lane);
+        g = f.part, b0 = f.before, total = f.total, target = f.target;
+        t0 = from_any(g % 2 ? before_c + c0 : before_c, g / 2);
+    } else {
+        u64 all, seen = 0;
+        if (tie)
+            for (int i0 = 0; i0 < parts; i0 += NT) {
+                const int i = i0 + tid;
+                const u64 c = i < parts ? s.ties[i] : 0, b = seen + before(c, &all);
+                if (i < parts) s.sums[i] += of_ties(c, b), s.ties[i] = (uint32_t)b;   // those before
+                seen += all;
+            }
+        __syncthreads();
+        for (int i = tid; i < parts; i += NT) total += s.sums[i];
+        total = sum(total);
+        target = (double)u * (double)total;
+        ahead = 0;
         for (int i0 = 0; i0 < parts; i0 += NT) {
             const int i = i0 + tid;
-            const u64 c = i < parts ? s.ties[i] : 0, b = seen + before(c, &all);
-            if (i < parts) {
-                s.sums[i] += (b >= (u64)end.tokens ? 0 : min(c, (u64)end.tokens - b)) * tie;
-                s.ties[i] = (uint32_t)b;   // those before
-            }
-            seen += all;
+            const u64 w = i < parts ? s.sums[i] : 0, b = ahead + before(w, &all);
+            if (w && (double)b <= target && target < (double)(b + w)) s.found[0] = i, s.ahead[0] = b;
+            ahead += all;
         }
-    __syncthreads();
-    for (int i = tid; i < parts; i += NT) total += s.sums[i];
-    total = sum(total);
-    float u = a.u[r];
-    u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
-    const double target = (double)u * (double)total;
-    ahead = 0;
-    for (int i0 = 0; i0 < parts; i0 += NT) {
-        const int i = i0 + tid;
-        const u64 w = i < parts ? s.sums[i] : 0, b = ahead + before(w, &all);
-        if (w && (double)b <= target && target < (double)(b + w)) s.found = i, s.ahead = b;
-        ahead += all;
+        __syncthreads();
+        if (wave != 0) return true;
+        g = s.found[0], b0 = s.ahead[0], t0 = s.ties[g];
     }
-    __syncthreads();
-    if (wave != 0) return true;
-    const int g = s.found;
-    u64 b0 = s.ahead, t0 = s.ties[g];
     for (int un = g * a.runs; un < min((g + 1) * a.runs, a.units); ++un) {
         Held<T, false> h;
         float v[8];
