@@ -245,6 +245,26 @@ __device__ __forceinline__ Fall fall_into(u64 w0, u64 w1, float u, int lane)
     f.before = (u64)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), at) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, at);
     return f;
 }
+// The units of run g, for one wavefront: f(held, unit); the loads of up to 8 of them are in flight together.
+template <typename T, bool SHORT, typename F>
+__device__ __forceinline__ void each_of_run(const SampleArgs &a, const T *x, int lane, int g, F f)
+{
+    constexpr int U = 8;
+    const int end = min((g + 1) * a.runs, a.units);
+#pragma unroll 1
+    for (int u0 = g * a.runs; u0 < end; u0 += U) {
+        Held<T, SHORT> h[U];
+#pragma unroll
+        for (int n = 0; n < U; ++n)
+            if (u0 + n < end) h[n].load(x, a.vocab, u0 + n, lane);
+#pragma unroll 1
+        for (int u = u0; u < min(u0 + U, end); ++u) {
+            f(h[0], u);
+#pragma unroll
+            for (int n = 0; n < U - 1; ++n) h[n] = h[n + 1];
+        }
+    }
+}
 __device__ __forceinline__ u64 from_any(u64 v, int lane)   // of one lane, the same for all
 {
     return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
@@ -857,11 +877,9 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
         if (wave != 0) return;
         g = s.found, b0 = s.ahead;
     }
-    for (int un = g * a.runs; un < min((g + 1) * a.runs, a.units); ++un) {
-        Held<T, SHORT> h;
+    each_of_run<T, SHORT>(a, x, lane, g, [&](const Held<T, SHORT> &h, int un) {
         float v[8];
         u64 own = 0;
-        h.load(x, a.vocab, un, lane);
         const int at = h.widen(v, a.vocab, un, a.units, lane);
 #pragma unroll
         for (int i = 0; i < 8; ++i) own += kept(v[i], at + i);
@@ -880,7 +898,7 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
             if (a.logprob) a.logprob[r] = logprob(hit, total);
         }
         b0 += last_lane(in);
-    }
+    });
 }
 
 template <typename T, int NT, bool SHORT>
@@ -1255,11 +1273,9 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
         if (wave != 0) return true;
         g = s.found[0], b0 = s.ahead[0], t0 = s.ties[g];
     }
-    for (int un = g * a.runs; un < min((g + 1) * a.runs, a.units); ++un) {
-        Held<T, false> h;
+    each_of_run<T, false>(a, x, lane, g, [&](const Held<T, false> &h, int un) {
         float v[8];
         u64 w[8], own = 0, tied = 0;
-        h.load(x, a.vocab, un, lane);
         const int at = h.widen(v, a.vocab, un, a.units, lane);
 #pragma unroll
         for (int i = 0; i < 8; ++i) tied += tie && slot_of(__builtin_bit_cast(uint32_t, v[i]) >> 16) == end.slot;
@@ -1286,7 +1302,7 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
             b += w[i];
         }
         b0 += last_lane(in), t0 += last_lane(in_ties);
-    }
+    });
     return true;
 }
 
