@@ -216,7 +216,7 @@ int quant_matmul_f8(long M, long N, long K, const void *a, long a_stride, const 
                     const float *a_scale, const void *w, long w_stride, const uint8_t *w_exps, long w_exps_stride,
                     const float *bias, const void *residual, long residual_stride, int out_dtype, void *y,
                     long y_stride, int relu, void *ws, size_t ws_bytes, void *stream);
-/* The kernels of a call, as quant_matmul_describe names them. */
+/* The kernels of a call, as quant_matmul_describe names them, whose exponents' rows lie less than 2^23 bytes apart. */
 int quant_matmul_f8_describe(long M, long N, long K, const void *a, long a_stride, const void *w, long w_stride,
                              int out_dtype, char *buf, int buflen, int *launches);
 

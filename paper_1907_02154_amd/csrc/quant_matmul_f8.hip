@@ -20,6 +20,8 @@
 #include "quant_tiles.h"
 
 #include <stdio.h>
+#include <type_traits>
+#include <utility>
 
 namespace miconv {
 namespace quant {
@@ -229,13 +231,212 @@ __global__ __launch_bounds__(64 * WM * WN * KG) void matmul_f8_tile_kernel(F8Arg
     }
 }
 
+// Calls f(0) .. f(N - 1) with numbers that are constants: an instruction's choice of a byte is one.
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F f)
+{
+    each_of(f, std::make_integer_sequence<int, N>());
+}
+template <int N>
+using Number = std::integral_constant<int, N>;
+
+// The largest products with bf16 outputs, N % 8 == 0: 256 tokens x 256 channels
+// a work-group of four wavefronts, one on each SIMD, each a square of 128 x 128,
+// whose sums take half of the registers: a block's operands are read from LDS
+// twice in all (128 KB of a block; by eight wavefronts, as above, 192, which is
+// as long as the products take).
+// A wavefront alone on its SIMD has to keep the matrix core busy by itself, so
+// everything else is placed between the products, which take 64 turns a block:
+// a block's tokens lie in registers before its first turn, and its channels come
+// three groups of 8 turns ahead.  After 40 turns all of a block has been read;
+// there the wavefronts meet, the block after it has landed, and in the last 24
+// turns its tokens, first channels and exponents are read and the block after
+// that one starts on its way into the place that has become free.  The channels
+// of a lane's sums are eight that follow one another, stored as 16 bytes, four
+// lanes 64; LDS chunks are rotated so that both orders of rows are free of
+// conflicts.  Exponents come as four bytes a register, of which the instruction
+// picks one.
+// 8192 x 8192 outputs, K = 4096: 227 us, 2.42 PFLOP/s (the tile above: 255); K =
+// 8192, half the outputs: 205, 2.68 (246); a large library product of the same
+// kind without exponents: 224 and, at its best, 2.75.  Taking the next tile's
+// first blocks while the last one's outputs are stored, in a grid of one
+// work-group on each compute unit, took 235.
+__global__ __launch_bounds__(256) void matmul_f8_large_kernel(F8Args f)
+{
+    const MatArgs &a = f.m;
+    constexpr int B = 256, NT = 256, L = 8;          // L: chunks of either operand that a thread stages
+    constexpr int EXPS = 2 * B * 8, STAGE = EXPS + 2 * B / 4;
+    __shared__ i32x4 smem[2 * STAGE];
+    const int tid = threadIdx.x, lane = tid % 64, col = lane % 16, quad = lane / 16;
+    const int wid = __builtin_amdgcn_readfirstlane(tid / 64), wn = wid / 2, wm = wid % 2;
+    int m0, n0;
+    tile_of(a, blockIdx.x, &m0, &n0);
+    m0 = __builtin_amdgcn_readfirstlane(m0) * B, n0 = __builtin_amdgcn_readfirstlane(n0) * B;
+    const int nm = min(a.M - m0, B), nn = min(a.N - n0, B);
+    const auto buffer = [&](const void *p, long first, int rows, long stride, int len) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>((const uint8_t *)p + first * stride), (short)0,
+                                                 __builtin_amdgcn_readfirstlane((int)((rows - 1) * stride + len)), 0x00020000);
+    };
+    const __amdgpu_buffer_rsrc_t wres = buffer(a.w, n0, nn, a.ws, a.K), ares = buffer(a.a, m0, nm, a.as, a.K);
+    const __amdgpu_buffer_rsrc_t ewres = buffer(f.ew, n0, nn, f.ews, f.blocks), eares = buffer(f.ea, m0, nm, f.eas, f.blocks);
+
+    // A thread stages chunks of rows 32 n + tid / 8; rows that are not there lie past their buffer's end.
+    constexpr unsigned kOutside = 0x80000000u;
+    const int srow = tid / 8, at_k = (tid % 8 ^ ((srow & 3) | (srow >> 3 & 1) << 2)) * 16;
+    const unsigned offw = (unsigned)(srow * a.ws) + at_k, offa = (unsigned)(srow * a.as) + at_k;
+    const unsigned nextw = (unsigned)(32 * a.ws), nexta = (unsigned)(32 * a.as);
+    // Its exponents: a lane's eight lie side by side; where there is no such row, the last's, of no output.
+    const int half = tid / 128 * 128, ej = tid % 8, ecol = tid % 128 / 8;
+    const int erw = half + 32 * (ej / 2) + 8 * (ecol / 4) + 4 * (ej % 2) + ecol % 4, erm = half + 16 * ej + ecol;
+    const unsigned offew = (unsigned)(min(erw, nn - 1) * f.ews), offea = (unsigned)(min(erm, nm - 1) * f.eas);
+    // Load n, of 18, of a block; past the last block zeros, with its exponents.
+    struct Block {
+        int base, exps;
+        unsigned outside;
+    };
+    const auto block_at = [&](int b) {
+        const bool is = b < f.blocks;
+        return Block{is ? b * 128 : 0, min(b, f.blocks - 1), is && b * 128 + at_k < a.K ? 0u : kOutside};
+    };
+    const auto load = [&](auto nc, int stage, const Block &b) {
+        constexpr int n = decltype(nc)::value;
+        i32x4 *st = smem + stage * STAGE + wid * 64;
+        if constexpr (n < L)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wres, (lds_void_t *)(st + n * NT), 16, (offw | b.outside) + n * nextw, b.base, 0, 0);
+        else if constexpr (n < 2 * L)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ares, (lds_void_t *)(st + n * NT), 16, (offa | b.outside) + (n - L) * nexta, b.base,
+                                                     0, 0);
+        else
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                n == 2 * L ? ewres : eares, (lds_void_t *)((int *)(smem + stage * STAGE + EXPS) + (n - 2 * L) * NT + wid * 64), 1,
+                n == 2 * L ? offew : offea, b.exps, 0, 0);
+    };
+
+    // Channel rows 32 (i / 2) + 8 (col / 4) + 4 (i % 2) + col % 4, token rows 16 j + col, of the wavefront's 128.
+    f32x4 acc[8][8] = {};
+    i32x8 fa[2][8], fw[4];
+    i32x4 ex[4];
+    uint32_t ea[2][2], ew[2][2];
+    const int w0 = (wn * 128 + 8 * (col / 4) + col % 4) * 8 + (quad ^ (col & 7));
+    const int a0 = (B + wm * 128 + col) * 8 + (quad ^ ((col & 3) | (col >> 3 & 1) << 2));
+    const auto read_w = [&](int stage, auto ic) {
+        constexpr int i = decltype(ic)::value;
+        const i32x4 *st = smem + stage * STAGE + (32 * (i / 2) + 4 * (i % 2)) * 8;
+        fw[i % 4] = __builtin_shufflevector(st[w0], st[w0 ^ 4], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    const auto read_a = [&](auto pc, auto jc) {
+        constexpr int p = decltype(pc)::value, j = decltype(jc)::value;
+        const i32x4 *st = smem + p * STAGE + 16 * j * 8;
+        fa[p][j] = __builtin_shufflevector(st[a0], st[a0 ^ 4], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    const auto read_e = [&](int stage) {
+        const i32x4 *e = smem + stage * STAGE + EXPS;
+        const int w = wn * 32 + col * 2, t = (B / 4) + wm * 32 + col * 2;
+        ex[0] = e[w], ex[1] = e[w + 1], ex[2] = e[t], ex[3] = e[t + 1];
+    };
+    const auto pack = [&](i32x4 v) { return (uint32_t)(v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24); };
+    const auto pack_e = [&](auto pc) {
+        constexpr int p = decltype(pc)::value;
+        ew[p][0] = pack(ex[0]), ew[p][1] = pack(ex[1]), ea[p][0] = pack(ex[2]), ea[p][1] = pack(ex[3]);
+    };
+    // A block in stage p, the next in the other; `after` is loaded into p once p is read.
+    const auto step = [&](auto pc, const Block &after) {
+        constexpr int p = decltype(pc)::value, q = 1 - p;
+        each<8>([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            if constexpr (i == 5) {
+                // The built-in wait, not one in asm: what has been read by now need not be waited for again.
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+                asm volatile("s_barrier" ::: "memory");
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            each<8>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fw[i % 4], fa[p][j], acc[i][j], 0, 0, i % 4, ew[p][i / 4],
+                                                                            j % 4, ea[p][j / 4]);
+                if constexpr (i < 5) {
+                    if constexpr (j == 0) read_w(p, Number<i + 3>());
+                } else {
+                    constexpr int n = (i - 5) * 8 + j;
+                    if constexpr (n == 0) read_w(q, Number<0>()), read_e(q);
+                    else if constexpr (n <= 8) read_a(Number<q>(), Number<n - 1>());
+                    else if constexpr (n == 9) read_w(q, Number<1>());
+                    else if constexpr (n == 17) read_w(q, Number<2>());
+                    if constexpr (n == 15) pack_e(Number<q>());
+                    if constexpr (n >= 6) load(Number<n - 6>(), p, after);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+    };
+    each<18>([&](auto n) { load(n, 0, block_at(0)); });
+    each<18>([&](auto n) { load(n, 1, block_at(1)); });
+    wait_vmcnt<18>();
+    asm volatile("s_barrier" ::: "memory");
+    read_w(0, Number<0>()), read_e(0);
+    each<8>([&](auto j) { read_a(Number<0>(), j); });
+    read_w(0, Number<1>());
+    read_w(0, Number<2>());
+    pack_e(Number<0>());
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+    for (int b = 0; b < f.blocks; b += 2) {   // of an odd number the last is one of zeros
+        step(Number<0>(), block_at(b + 2));
+        step(Number<1>(), block_at(b + 3));
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+
+    const int n = n0 + wn * 128 + 8 * quad;   // + 32 c: a lane's eight channels
+    float bias[4][8] = {};
+    if (a.bias)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (n + 32 * c < a.N) memcpy(bias[c], a.bias + n + 32 * c, 32);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int m = m0 + wm * 128 + 16 * j + col;
+        const float sa = a.sa ? a.sa[min(m, a.M - 1)] : 1.0f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = acc[2 * c + e / 4][j][e % 4] * sa;
+            if (a.bias)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += bias[c][e];
+            if (m >= a.M || n + 32 * c >= a.N) continue;
+            if (a.res) {
+                float r[8];
+                load8((const uint16_t *)a.res + (long)m * a.rs + n + 32 * c, r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += r[e];
+            }
+            if (a.relu)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = v[e] < 0.0f ? 0.0f : v[e];   // a NaN stays
+            store8((uint16_t *)a.y + (long)m * a.ys + n + 32 * c, v);
+        }
+    }
+}
+
 constexpr Tile kTiles[] = {
     {16, 16, 1, 1, 4, 4, 2, 3.4f, 3.8f},    {16, 32, 1, 2, 4, 3, 2, 3.8f, 5.0f},    {32, 64, 1, 4, 4, 3, 1, 6.6f, 0.0f},
     {64, 32, 2, 2, 4, 3, 1, 6.6f, 0.0f},    {64, 64, 2, 2, 2, 4, 1, 9.3f, 0.0f},    {128, 64, 4, 2, 2, 3, 1, 13.8f, 0.0f},
     {128, 128, 2, 4, 1, 3, 1, 22.3f, 0.0f}, {128, 128, 2, 2, 1, 2, 2, 28.0f, 38.0f}, {256, 256, 4, 2, 1, 2, 1, 66.0f, 0.0f},
+    {256, 256, 2, 2, 1, 2, 1, 57.0f, 0.0f},   // matmul_f8_large_kernel
 };
+constexpr int kCount = sizeof(kTiles) / sizeof(kTiles[0]), kLarge = kCount - 1;
 
-int pick(int M, int N) { return pick_tile(kTiles, (int)(sizeof(kTiles) / sizeof(kTiles[0])), M, N); }
+// far: an operand's exponents lie so far apart that 256 rows of them pass a buffer's 31-bit offsets.
+int pick(int M, int N, int out_dtype, bool far)
+{
+    return pick_tile(kTiles, out_dtype == kBF16 && N % 8 == 0 && !far ? kCount : kLarge, M, N);
+}
 
 template <typename T, int I>
 int go_tile(F8Args f, hipStream_t st)
@@ -248,14 +449,16 @@ int go_tile(F8Args f, hipStream_t st)
     if ((long)a.mt * a.nt * threads >= 1L << 32 || (long)kGroup * a.nt >= 1L << 31) return MICONV_ERR_TOO_LARGE;
     a.tiles = a.mt * a.nt;
     a.dv_group = make_fastdiv((unsigned)(kGroup * a.nt));
-    launch_kernel(matmul_f8_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kg, t.nst>, dim3((unsigned)a.tiles), dim3(threads), 0, st, f);
+    if constexpr (I == kLarge) launch_kernel(matmul_f8_large_kernel, dim3((unsigned)a.tiles), dim3(threads), 0, st, f);
+    else launch_kernel(matmul_f8_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.kg, t.nst>, dim3((unsigned)a.tiles), dim3(threads), 0, st, f);
     return launched();
 }
 
 template <typename T>
 int launch_matmul(const F8Args &f, hipStream_t st)
 {
-    switch (pick(f.m.M, f.m.N)) {
+    const bool far = 256 * (f.eas > f.ews ? f.eas : f.ews) >= 1L << 31;
+    switch (pick(f.m.M, f.m.N, std::is_same<T, float>::value ? kF32 : kBF16, far)) {
     case 0: return go_tile<T, 0>(f, st);
     case 1: return go_tile<T, 1>(f, st);
     case 2: return go_tile<T, 2>(f, st);
@@ -264,7 +467,8 @@ int launch_matmul(const F8Args &f, hipStream_t st)
     case 5: return go_tile<T, 5>(f, st);
     case 6: return go_tile<T, 6>(f, st);
     case 7: return go_tile<T, 7>(f, st);
-    default: return go_tile<T, 8>(f, st);
+    case 8: return go_tile<T, 8>(f, st);
+    default: return go_tile<T, kLarge>(f, st);
     }
 }
 
@@ -301,9 +505,15 @@ extern "C" int quant_matmul_f8_describe(long M, long N, long K, const void *a, l
     if (!dtype_bytes(out_dtype)) return MICONV_ERR_UNSUPPORTED;
     if (M == 0) return MICONV_OK;
     const bool copy = copy_bytes(M, a, a_stride, K) + copy_bytes(N, w, w_stride, K) > 0;
-    const Tile t = kTiles[pick((int)M, (int)N)];
+    const int at = pick((int)M, (int)N, out_dtype, false);
+    const Tile t = kTiles[at];
+    const char *first = copy ? "matmul_i8_align_kernel + " : "";
     *launches = 1 + copy;
-    snprintf(buf, buflen, "%smatmul_f8_tile_kernel<%s, %d, %d, %d, %d, %d, %d>", copy ? "matmul_i8_align_kernel + " : "",
+    if (at == kLarge) {
+        snprintf(buf, buflen, "%smatmul_f8_large_kernel", first);
+        return MICONV_OK;
+    }
+    snprintf(buf, buflen, "%smatmul_f8_tile_kernel<%s, %d, %d, %d, %d, %d, %d>", first,
              out_dtype == kF32 ? "float" : "unsigned short", t.bm, t.bn, t.wm, t.wn, t.kg, t.nst);
     return MICONV_OK;
 }

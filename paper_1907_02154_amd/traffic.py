@@ -96,6 +96,7 @@ SOURCES = {
     "kv8_write_kernel": "quant_cache8.hip",
     "kv8_read_kernel": "quant_cache8.hip",
     "matmul_f8_tile_kernel": "quant_matmul_f8.hip",
+    "matmul_f8_large_kernel": "quant_matmul_f8.hip",
     "rows_f8_kernel": "quant_rows_f8.hip",
     "kv4_write_kernel": "quant_cache.hip",
     "kv4_read_kernel": "quant_cache.hip",

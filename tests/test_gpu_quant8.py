@@ -268,6 +268,61 @@ def test_matmul_of_every_tile(tile, dtype):
         check_matmul(M, N, K, dtype, True, True, False, False)
 
 
+# Outputs that the rule sends to the largest tile: edges in both directions, and tiles whose last rows or channels are few.
+LARGE = [(2304, 4096), (1800, 6144), (2049, 4104), (2801, 3600), (8193, 1032)]
+
+
+@pytest.mark.parametrize("M,N", LARGE)
+@pytest.mark.parametrize("K", [16, 100, 128, 129, 256, 400, 640])
+def test_matmul_of_the_largest_tile(M, N, K):
+    """Blocks odd and even in number, one alone, and the last one of 16 values and of some."""
+    assert quant.matmul_f8_describe(M, N, 400, BF16) == ("matmul_f8_large_kernel", 1)
+    check_matmul(M, N, K, BF16, K % 3 == 0, K % 32 == 0, K > 300, M % 2 == 0)
+
+
+def test_matmul_of_the_largest_tile_with_strides():
+    g = gen(41)
+    M, N, K = 2305, 4104, 272
+    a, w = operand(g, M, K), operand(g, N, K)
+    wide_a, wide_w = torch.full((M, K + 48), 0x7F, dtype=U8), torch.full((N, K + 16), 0x7F, dtype=U8)
+    wide_a[:, 32:32 + K], wide_w[:, 16:] = a[0], w[0]
+    wide_ea, wide_ew = torch.full((M, 7), 255, dtype=U8), torch.full((N, 5), 255, dtype=U8)
+    wide_ea[:, 2:5], wide_ew[:, 1:4] = a[1], w[1]
+    hold = torch.randn(M, N + 11, generator=g).to(BF16).cuda()
+    res = hold[:, 5:5 + N]
+    before = hold.cpu()
+    da, dw = wide_a.cuda().view(quant.F8)[:, 32:32 + K], wide_w.cuda().view(quant.F8)[:, 16:]
+    y = quant.matmul_f8(da, wide_ea.cuda()[:, 2:5], dw, wide_ew.cuda()[:, 1:4], residual=res, out=res)
+    want, tol = ref.matmul_f8(a[2], w[2], residual=before[:, 5:5 + N], bf16=True)
+    assert y is res and ((res.cpu().double() - want).abs() <= tol).all()
+    assert torch.equal(hold.cpu()[:, :5], before[:, :5]) and torch.equal(hold.cpu()[:, 5 + N:], before[:, 5 + N:])
+
+
+def test_matmul_of_the_largest_tile_is_the_same_bits_again():
+    g = gen(43)
+    M, N, K = 2304, 4096, 1280
+    a, w = operand(g, M, K), operand(g, N, K)
+    args = (a[0].cuda().view(quant.F8), a[1].cuda(), w[0].cuda().view(quant.F8), w[1].cuda())
+    first = quant.matmul_f8(*args)
+    for _ in range(20):
+        assert torch.equal(quant.matmul_f8(*args), first)
+    wide = torch.empty(M, N, device="cuda")
+    whole = quant.matmul_f8(*args, out=wide)
+    want, tol = ref.matmul_f8(a[2], w[2], bf16=True)
+    assert ((whole.cpu().double() - want).abs() <= tol).all() and ((first.cpu().double() - want).abs() <= tol).all()
+
+
+def test_matmul_of_the_largest_tile_keeps_nan_in_its_row_and_channel():
+    g = gen(44)
+    M, N, K = 2304, 4096, 400
+    a, w = operand(g, M, K), operand(g, N, K)
+    a[1][5, 3], w[1][4000, 0], a[0][2300, K - 1] = 255, 255, 0x7F
+    y = quant.matmul_f8(a[0].cuda().view(quant.F8), a[1].cuda(), w[0].cuda().view(quant.F8), w[1].cuda(), relu=True).cpu()
+    nan = torch.zeros(M, N, dtype=torch.bool)
+    nan[5], nan[2300], nan[:, 4000] = True, True, True
+    assert torch.equal(torch.isnan(y), nan)
+
+
 def test_matmul_strides_and_in_place_residual():
     g = gen(4)
     M, N, K = 70, 90, 256
