@@ -113,6 +113,16 @@ __device__ __forceinline__ u64 last_lane(u64 v)
     return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 __device__ __forceinline__ u64 wave_sum(u64 v) { return last_lane(wave_scan(v)); }
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v)
+{
+    v += from_lane<0x111, 0xF>(v);
+    v += from_lane<0x112, 0xF>(v);
+    v += from_lane<0x114, 0xF>(v);
+    v += from_lane<0x118, 0xF>(v);
+    v += from_lane<0x142, 0xA>(v);
+    v += from_lane<0x143, 0xC>(v);
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
     v = max(v, from_lane<0x111, 0xF>(v));
@@ -198,29 +208,40 @@ __device__ __forceinline__ void sort_list(u64 *list, int n, int tid)
         }
 }
 
-// A row's units, f(held, unit, last): a wavefront takes runs of them, every NT / 64-th, three units in flight; `last`
-// of a run.
-template <typename T, bool SHORT, int NT, typename F>
-__device__ __forceinline__ void each_unit(const SampleArgs &a, const T *x, int lane, int wave, F f)
-{
-    constexpr int U = 3, WAVES = NT / 64;
-    const int step = (WAVES - 1) * a.runs;
-    const auto next = [&](int u) { return (u + 1) & (a.runs - 1) ? u + 1 : u + 1 + step; };
+// A row's units: a wavefront takes runs of them, every NT / 64-th, three units in flight, the first of which may be
+// on their way before they are worked on.
+template <typename T, bool SHORT, int NT>
+struct Units {
+    static constexpr int U = 3, WAVES = NT / 64;
     Held<T, SHORT> h[U];
-    int u = wave * a.runs, ahead = u;
-#pragma unroll
-    for (int n = 0; n < U; ++n) h[n].load(x, a.vocab, min(ahead, a.units - 1), lane), ahead = next(ahead);
-#pragma unroll 1
-    while (u < a.units) {
-        const Held<T, SHORT> now = h[0];
-#pragma unroll
-        for (int n = 0; n < U - 1; ++n) h[n] = h[n + 1];
-        h[U - 1].load(x, a.vocab, min(ahead, a.units - 1), lane);
-        ahead = next(ahead);
-        f(now, u, ((u + 1) & (a.runs - 1)) == 0 || u == a.units - 1);
-        u = next(u);
+    int u, ahead;
+
+    __device__ __forceinline__ int next(const SampleArgs &a, int unit) const
+    {
+        return (unit + 1) & (a.runs - 1) ? unit + 1 : unit + 1 + (WAVES - 1) * a.runs;
     }
-}
+    __device__ __forceinline__ void start(const SampleArgs &a, const T *x, int lane, int wave)
+    {
+        u = ahead = wave * a.runs;
+#pragma unroll
+        for (int n = 0; n < U; ++n) h[n].load(x, a.vocab, min(ahead, a.units - 1), lane), ahead = next(a, ahead);
+    }
+    // f(held, unit, last of a run)
+    template <typename F>
+    __device__ __forceinline__ void each(const SampleArgs &a, const T *x, int lane, F f)
+    {
+#pragma unroll 1
+        while (u < a.units) {
+            const Held<T, SHORT> now = h[0];
+#pragma unroll
+            for (int n = 0; n < U - 1; ++n) h[n] = h[n + 1];
+            h[U - 1].load(x, a.vocab, min(ahead, a.units - 1), lane);
+            ahead = next(a, ahead);
+            f(now, u, ((u + 1) & (a.runs - 1)) == 0 || u == a.units - 1);
+            u = next(a, u);
+        }
+    }
+};
 
 // For one wavefront: of up to 128 sums, two neighbours a lane, the one that a share u of all falls into, what comes
 // before it, and the total.  (For more of them the work-group looks.)
@@ -245,7 +266,7 @@ __device__ __forceinline__ Fall fall_into(u64 w0, u64 w1, float u, int lane)
     f.before = (u64)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), at) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, at);
     return f;
 }
-// The units of run g, for one wavefront: f(held, unit); the loads of up to 8 of them are in flight together.
+// The units of run g, for one wavefront, until f(held, unit) is true; the loads of up to 8 of them are in flight together.
 template <typename T, bool SHORT, typename F>
 __device__ __forceinline__ void each_of_run(const SampleArgs &a, const T *x, int lane, int g, F f)
 {
@@ -259,7 +280,7 @@ __device__ __forceinline__ void each_of_run(const SampleArgs &a, const T *x, int
             if (u0 + n < end) h[n].load(x, a.vocab, u0 + n, lane);
 #pragma unroll 1
         for (int u = u0; u < min(u0 + U, end); ++u) {
-            f(h[0], u);
+            if (f(h[0], u)) return;
 #pragma unroll
             for (int n = 0; n < U - 1; ++n) h[n] = h[n + 1];
         }
@@ -308,7 +329,9 @@ struct Picker {
     template <typename F>
     __device__ __forceinline__ void units(F f)
     {
-        each_unit<T, SHORT, NT>(a, x, lane, wave, [&](const Held<T, SHORT> &h, int unit, bool last) {
+        Units<T, SHORT, NT> all;
+        all.start(a, x, lane, wave);
+        all.each(a, x, lane, [&](const Held<T, SHORT> &h, int unit, bool last) {
             float v[8];
             const int at = h.widen(v, a.vocab, unit, a.units, lane);
             f(v, at, unit, last);
@@ -883,8 +906,10 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
         const int at = h.widen(v, a.vocab, un, a.units, lane);
 #pragma unroll
         for (int i = 0; i < 8; ++i) own += kept(v[i], at + i);
-        const u64 in = wave_scan(own);
+        const u64 in = wave_scan(own), with = b0 + last_lane(in);
         u64 b = b0 + in - own;
+        b0 = with;
+        if (!(target < (double)with)) return false;
         if ((double)b <= target && target < (double)(b + own)) {   // one lane: its tokens again
             int in_lane = 0;
             float hit = 0.0f;
@@ -897,7 +922,7 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
             a.token[r] = at + in_lane;
             if (a.logprob) a.logprob[r] = logprob(hit, total);
         }
-        b0 += last_lane(in);
+        return true;
     });
 }
 
@@ -925,6 +950,7 @@ constexpr uint32_t kForbidden = 0xFF80;  // bits of minus infinity
 // In LDS: positive values by magnitude with a place for what lies below and one for what lies above, the negative ones
 // the same, the list's three slots.  The places of what has no counter stay 0.
 constexpr int kSide = kValues + 2, kPlaces = 2 * kSide + 3;
+constexpr int kTieBit = 56;
 
 struct Values {
     uint32_t counts[kPlaces];
@@ -981,11 +1007,11 @@ struct ByValue {
     static __device__ __forceinline__ int slot_of_listed(float v) { return v >= 1.0f ? 0 : v <= -1.0f ? kSlots - 1 : kMiddle; }
     __device__ __forceinline__ float listed(int i) const { return logit_of((uint32_t)(s.list[i] >> 32)); }
 
-    // f(bits of 8 logits by twos, first index, unit, last of a run)
+    // f(bits of 8 logits by twos, first index, unit, last of a run); `all` has been started.
     template <typename F>
-    __device__ __forceinline__ void units(F f)
+    __device__ __forceinline__ void units(Units<T, false, NT> &all, F f)
     {
-        each_unit<T, false, NT>(a, x, lane, wave, [&](const Held<T, false> &h, int unit, bool last) {
+        all.each(a, x, lane, [&](const Held<T, false> &h, int unit, bool last) {
             uint32_t b[4] = {h.w[0][0], h.w[0][1], h.w[0][2], h.w[0][3]};
             int at = unit * kUnit + lane * 8;
             if (unit == a.units - 1) {   // those that the lane before has
@@ -1062,11 +1088,12 @@ struct ByValue {
         if (tid == 0) s.found[at] = kSlots;
         u64 b = before(total, &all);
         known(all);
+        if (total && end(b, b + total))   // one thread, if any
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if (own[i] && end(b, b + own[i])) s.found[at] = tid * PER + i, s.ahead[at] = b;
-            b += own[i];
-        }
+            for (int i = 0; i < PER; ++i) {
+                if (own[i] && end(b, b + own[i])) s.found[at] = tid * PER + i, s.ahead[at] = b;
+                b += own[i];
+            }
         __syncthreads();
         *ahead = s.ahead[at];
         return s.found[at];
@@ -1083,13 +1110,18 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     float p = a.top_p ? a.top_p[r] : 1.0f, m = a.min_p ? a.min_p[r] : 0.0f;
     if (!(t > 0.0f)) t = 1.0f, k = 1, p = 1.0f, m = 0.0f;   // the first token
     if (k < 1 || k > a.vocab) k = a.vocab;
+    const int parts = (a.units + a.runs - 1) / a.runs;
+    Units<T, false, NT> all;
+    all.start(a, x, lane, wave);
     if (tid < kTable) s.table[tid] = exp2((double)tid / kTable);
     if (tid == 0) s.count = 0;
-    for (int i = tid; i < kPlaces; i += NT) s.counts[i] = 0, s.weights[i] = 0;
-    for (int i = tid; i < kList; i += NT) s.sums[i] = 0, s.ties[i] = 0;
+    for (int i = tid; i < kPlaces; i += NT) s.counts[i] = 0;
+    // the values' weights are all written later
+    if (tid < 7) s.weights[tid < 3 ? 2 * kSide + tid : tid == 3 ? 0 : tid == 4 ? kSide - 1 : tid == 5 ? kSide : 2 * kSide - 1] = 0;
+    for (int i = tid; i < parts; i += NT) s.sums[i] = 0;
     __syncthreads();
     bool bad = false;
-    units([&](const uint32_t (&b)[4], int at, int, bool) {
+    units(all, [&](const uint32_t (&b)[4], int at, int, bool) {
         uint32_t place[4];
         bool any = false;
 #pragma unroll
@@ -1112,6 +1144,7 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
                 }
             }
     });
+    all.start(a, x, lane, wave);   // the second pass
     bad = __syncthreads_or(bad);
     const int outside = s.count;
     if (!bad && outside > kList / 2) return false;
@@ -1151,7 +1184,7 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     row.shift = a.shift;
     want = m > 0.0f ? ldexp((double)m, a.shift) : 0.0;
     for (int i = tid; i < kSlots; i += NT)
-        if (!of_list(i)) s.weights[place_in(i)] = row.weight(value_of(i));
+        if (!of_list(i) && s.counts[place_in(i)]) s.weights[place_in(i)] = row.weight(value_of(i));   // of others none is read
     for (int i = tid; i < outside; i += NT) atomicAdd(&s.weights[place_in(slot_of_listed(listed(i)))], row.weight(listed(i)));
     __syncthreads();
 
@@ -1198,57 +1231,61 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     u64 tie = 0;   // the weight of a token of the last slot, where not all of them stay
     if (some && (end.slot == best || row.share(value_of(end.slot)) >= want)) tie = s.weights[place_in(end.slot)];
     __syncthreads();
-    for (int i = m > 0.0f ? tid : min(end.slot, kSlots) / NT * NT + tid; i < kSlots; i += NT)
-        if (i > end.slot || (some && i == end.slot) || (i != best && !of_list(i) && row.share(value_of(i)) < want)) s.weights[place_in(i)] = 0;
+    if (m > 0.0f)
+        for (int i = tid; i < kSlots; i += NT)
+            if (i <= end.slot && i != best && !of_list(i) && row.share(value_of(i)) < want) s.weights[place_in(i)] = 0;
+    if (some && tid == end.slot % NT) s.weights[place_in(end.slot)] = tie ? 1ull << kTieBit : 0;
     for (int i = tid; i < outside; i += NT) {
         const u64 q = s.list[i];
         if (kept(listed(i), q)) atomicAdd(&s.sums[(int)(~(uint32_t)q) / kUnit / a.runs], row.weight(listed(i)));
     }
     __syncthreads();
 
-    // Sums of runs of units, in the vocabulary's order, and how many tokens of the last slot each holds.  Values that are
-    // not kept weigh 0; they are looked up in one place, where lanes do not wait for one another.
+    // Sums of runs of units, in the vocabulary's order, and how many tokens of the last slot each holds: a lane's weights of a
+    // run, at most 128, stay below 2^56, above which it counts these.  Values past the last slot are looked up in one place,
+    // where lanes do not wait for one another, and which holds 0.
     const float from = end.slot == kSlots ? kNegInf : !of_list(end.slot) ? value_of(end.slot)
                        : end.slot == 0 ? __builtin_inff() : end.slot == kMiddle ? 0.0f : kNegInf;
-    const uint32_t tie_bits = tie ? __builtin_bit_cast(uint32_t, value_of(end.slot)) >> 16 : 0x10000u;
+    const auto looked_up = [&](const uint32_t (&b)[4], int i) {
+        const uint32_t place = __builtin_bit_cast(uint32_t, places_of(b[i / 2]));
+        const bool is = __builtin_bit_cast(float, i % 2 ? b[i / 2] & 0xFFFF0000u : b[i / 2] << 16) >= from;
+        return s.weights[is ? i % 2 ? place >> 16 : place & 0xFFFFu : 0];
+    };
     u64 w = 0;
-    uint32_t ties = 0;
-    units([&](const uint32_t (&b)[4], int, int unit, bool last) {
+    units(all, [&](const uint32_t (&b)[4], int, int unit, bool last) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t place = __builtin_bit_cast(uint32_t, places_of(b[i / 2])), v = i % 2 ? b[i / 2] >> 16 : b[i / 2] & 0xFFFFu;
-            const bool is = __builtin_bit_cast(float, i % 2 ? b[i / 2] & 0xFFFF0000u : b[i / 2] << 16) >= from;
-            w += s.weights[is ? i % 2 ? place >> 16 : place & 0xFFFFu : 0];
-            ties += (uint32_t)__builtin_popcountll(__ballot(v == tie_bits));
-        }
+        for (int i = 0; i < 8; ++i) w += looked_up(b, i);
         if (!last) return;
-        w = wave_sum(w);
+        const uint32_t ties = tie ? wave_sum((uint32_t)(w >> kTieBit)) : 0;
+        w = wave_sum(w & ((1ull << kTieBit) - 1));
         if (lane == 0) {
             if (w) atomicAdd(&s.sums[unit / a.runs], w);   // beside the list's tokens
             s.ties[unit / a.runs] = ties;
         }
-        w = 0, ties = 0;
+        w = 0;
     });
     __syncthreads();
-    const int parts = (a.units + a.runs - 1) / a.runs;
     const float u = drawn(a, r);
     // of a part's tokens of the last slot, b of which come before them, those that stay
     const auto of_ties = [&](u64 c, u64 b) { return (b >= (u64)end.tokens ? 0 : min(c, (u64)end.tokens - b)) * tie; };
+    // The run that the draw falls into, what comes before it, and the total.
     int g;
     u64 b0, t0, total = 0;
-    double target;
     if (parts <= kPairs) {
-        if (wave != 0) return true;
-        const int i = 2 * lane;
-        u64 w0 = i < parts ? s.sums[i] : 0, w1 = i + 1 < parts ? s.sums[i + 1] : 0, c0 = 0, c1 = 0, before_c = 0;
-        if (tie) {
-            c0 = i < parts ? s.ties[i] : 0, c1 = i + 1 < parts ? s.ties[i + 1] : 0;
-            before_c = wave_scan(c0 + c1) - c0 - c1;
-            w0 += of_ties(c0, before_c), w1 += of_ties(c1, before_c + c0);
+        if (wave == 0) {
+            const int i = 2 * lane;
+            u64 w0 = i < parts ? s.sums[i] : 0, w1 = i + 1 < parts ? s.sums[i + 1] : 0, c0 = 0, c1 = 0, before_c = 0;
+            if (tie) {
+                c0 = i < parts ? s.ties[i] : 0, c1 = i + 1 < parts ? s.ties[i + 1] : 0;
+                before_c = wave_scan(c0 + c1) - c0 - c1;
+                w0 += of_ties(c0, before_c), w1 += of_ties(c1, before_c + c0);
+            }
+            const Fall f = fall_into(w0, w1, u, lane);
+            const u64 ties = from_any(f.part % 2 ? before_c + c0 : before_c, f.part / 2);
+            if (lane == 0) s.found[0] = f.part, s.ahead[0] = f.before, s.ahead[1] = f.total, s.found[1] = (int)ties;
         }
-        const Fall f = fall_into(w0, w1, u, lane);
-        g = f.part, b0 = f.before, total = f.total, target = f.target;
-        t0 = from_any(g % 2 ? before_c + c0 : before_c, g / 2);
+        __syncthreads();
+        g = s.found[0], b0 = s.ahead[0], total = s.ahead[1], t0 = (u64)s.found[1];
     } else {
         u64 all, seen = 0;
         if (tie)
@@ -1261,7 +1298,7 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
         __syncthreads();
         for (int i = tid; i < parts; i += NT) total += s.sums[i];
         total = sum(total);
-        target = (double)u * (double)total;
+        const double target = (double)u * (double)total;
         ahead = 0;
         for (int i0 = 0; i0 < parts; i0 += NT) {
             const int i = i0 + tid;
@@ -1270,39 +1307,57 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
             ahead += all;
         }
         __syncthreads();
-        if (wave != 0) return true;
         g = s.found[0], b0 = s.ahead[0], t0 = s.ties[g];
     }
-    each_of_run<T, false>(a, x, lane, g, [&](const Held<T, false> &h, int un) {
-        float v[8];
-        u64 w[8], own = 0, tied = 0;
-        const int at = h.widen(v, a.vocab, un, a.units, lane);
+    const double target = (double)u * (double)total;
+    // A unit of the run for each wavefront, its weights in registers.
+    static_assert(WAVES >= 16, "a run has 16 units at most");
+    const int un = g * a.runs + wave;
+    const bool mine = wave < a.runs && un < a.units;
+    Held<T, false> h;
+    h.load(x, a.vocab, min(un, a.units - 1), lane);
+    const uint32_t bits[4] = {h.w[0][0], h.w[0][1], h.w[0][2], h.w[0][3]};
+    float v[8];
+    u64 each[8], own = 0, tied = 0;
+    const int at = h.widen(v, a.vocab, min(un, a.units - 1), a.units, lane);
+    bool listed_one = false;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) tied += tie && slot_of(__builtin_bit_cast(uint32_t, v[i]) >> 16) == end.slot;
-        const u64 in_ties = wave_scan(tied);
-        u64 rank = t0 + in_ties - tied;
+    for (int i = 0; i < 8; ++i) {
+        each[i] = looked_up(bits, i);
+        listed_one |= slot_of(__builtin_bit_cast(uint32_t, v[i]) >> 16) == kSlots && v[i] > kNegInf;
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int slot = slot_of(__builtin_bit_cast(uint32_t, v[i]) >> 16);
-            w[i] = slot < kSlots ? s.weights[place_in(slot)] : 0;
-            if (slot == kSlots && v[i] > kNegInf && kept(v[i], place_of(v[i], at + i))) w[i] = row.weight(v[i]);
-            if (tie && slot == end.slot) w[i] = rank++ < (u64)end.tokens ? tie : 0;
-            own += w[i];
-        }
-        const u64 in = wave_scan(own);
-        u64 b = b0 + in - own;
+    for (int i = 0; i < 8; ++i) each[i] = mine && v[i] > kNegInf ? each[i] : 0;   // not what the lane before has
+    if (mine && listed_one)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (w[i] && (double)b <= target && target < (double)(b + w[i])) {
-                a.token[r] = at + i;
-                if (a.logprob)
-                    a.logprob[r] = (float)(((double)v[i] - row.top) * row.factor * 0.693147180559945309417 -
-                                           log(ldexp((double)total, -row.shift)));
-            }
-            b += w[i];
-        }
-        b0 += last_lane(in), t0 += last_lane(in_ties);
-    });
+        for (int i = 0; i < 8; ++i)
+            if (slot_of(__builtin_bit_cast(uint32_t, v[i]) >> 16) == kSlots && v[i] > kNegInf && kept(v[i], place_of(v[i], at + i)))
+                each[i] = row.weight(v[i]);
+    if (tie) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tied += each[i] >> kTieBit;
+        u64 all;
+        u64 rank = t0 + before(tied, &all);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (each[i] >> kTieBit) each[i] = rank++ < (u64)end.tokens ? tie : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) own += each[i];
+    u64 all_of_run;
+    b0 += before(own, &all_of_run);
+    if (!((double)b0 <= target && target < (double)(b0 + own))) return true;
+    int in_lane = 0;   // one lane
+    float hit = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (each[i] && (double)b0 <= target && target < (double)(b0 + each[i])) in_lane = i, hit = v[i];
+        b0 += each[i];
+    }
+    a.token[r] = at + in_lane;
+    if (a.logprob)
+        a.logprob[r] = (float)(((double)hit - row.top) * row.factor * 0.693147180559945309417 -
+                               log(ldexp((double)total, -row.shift)));
     return true;
 }
 
