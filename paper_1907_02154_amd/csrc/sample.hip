@@ -527,6 +527,104 @@ struct Picker {
 
     __device__ __forceinline__ u64 search(long r, u64 floor, bool count, u64 k, double most);
     __device__ __forceinline__ void run(long r);
+    // The row's units in registers, where they are few.
+    static constexpr int HELD = SHORT || NT == 256 ? 1 : 8;
+    Held<T, SHORT> kept_units[HELD];
+    __device__ __forceinline__ bool fits() const { return a.units <= HELD * WAVES && a.runs == 1; }
+    __device__ __forceinline__ void hold()
+    {
+#pragma unroll
+        for (int n = 0; n < HELD; ++n) kept_units[n].load(x, a.vocab, min(wave + n * WAVES, a.units - 1), lane);
+    }
+    template <typename F>
+    __device__ __forceinline__ void each_held(F f)
+    {
+#pragma unroll
+        for (int n = 0; n < HELD; ++n) {
+            const int unit = wave + n * WAVES;
+            float v[8];
+            const int at = kept_units[n].widen(v, a.vocab, min(unit, a.units - 1), a.units, lane);
+            if (unit < a.units)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f(v[i], at + i);
+        }
+    }
+    // What the first of each thread's tokens say: the order's first place, and how weights follow.  0 where the row is done
+    // with: no token can be drawn, or the first is asked for.
+    __device__ __forceinline__ u64 top_of(long r, float t, float most_v, int most_i, bool bad)
+    {
+        const uint32_t mine = key_of(most_v), top_key = largest(mine);
+        const float top = logit_of(top_key);
+        const int first = (int)~largest(mine == top_key ? ~(uint32_t)most_i : 0u);
+        const bool none = __syncthreads_or(bad) || top == kNegInf;
+        if (none || !(t > 0.0f)) {
+            done(r, none ? -1 : first, none ? __builtin_nanf("") : 0.0f);
+            return 0;
+        }
+        row.top = top;
+        row.factor = fmax(1.44269504088896340736 / (double)t, 1e-300);
+        row.least = -(a.shift + 3) / row.factor;
+        row.table = s.table;
+        row.shift = a.shift;
+        return (u64)top_key << 32 | (uint32_t)~first;
+    }
+    // min_p as a logit: the smallest whose weight passes it, near where the logarithm has it.
+    __device__ __forceinline__ float floor_of(float m, uint32_t top_key) const
+    {
+        if (!(m > 0.0f)) return kNegInf;
+        const double want = ldexp((double)fminf(m, 1.0f), row.shift);
+        const uint32_t near = key_of((float)fmax(row.top + log2((double)fminf(m, 1.0f)) / row.factor, -3.4e38));
+        const uint32_t key = near - 32u + (uint32_t)lane;
+        const u64 pass = __ballot(key >= top_key || row.share(logit_of(key)) >= want);
+        const float top = logit_of(top_key);
+        return pass ? fminf(logit_of(near - 32u + (uint32_t)__builtin_ctzll(pass)), top) : top;
+    }
+    // For few: k threads' largest logits are k tokens, so that nothing below the last of these counts.  The others into the
+    // list; how many there are.
+    __device__ __forceinline__ int candidates(int k, float most_v, bool held)
+    {
+        u64 ahead, with;
+        anchor = (float)row.top;
+        const float low = -logit_of(largest(most_v > kNegInf ? key_of(-most_v) : 0u));
+        inv = anchor > low ? fminf((float)NT / (anchor - low), 0x1p100f) : 0.0f;
+        s.counts[tid] = 0;
+        __syncthreads();
+        atomicAdd(&s.counts[bin_of<NT>(most_v)], 1u);
+        __syncthreads();
+        const int bin = crossing<NT>(s.counts, [&](u64 b, u64 w) { return b < (u64)k && (u64)k <= w; }, &ahead, &with);
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        const auto take = [&](float v, int i) {
+            if (bin_of<NT>(v) <= bin) put(v, i);
+        };
+        if (!held) scan(take);
+        else if (bin_of<NT>(most_v) <= bin) each_held(take);
+        __syncthreads();
+        return s.count;
+    }
+    // The pick of row r among its first k tokens, if the candidates for them are 64 at most; else nothing is done.
+    __device__ __forceinline__ bool few(long r, int k)
+    {
+        const float t = a.temperature ? a.temperature[r] : 1.0f, p = a.top_p ? a.top_p[r] : 1.0f, m = a.min_p ? a.min_p[r] : 0.0f;
+        if (tid < kTable) s.table[tid] = exp2((double)tid / kTable);
+        float most_v = kNegInf;
+        int most_i = 0;
+        bool bad = false;
+        const auto look = [&](float v, int i) {
+            if (v > most_v) most_v = v, most_i = i;
+            bad |= !(v < __builtin_inff());
+        };
+        const bool held = fits();
+        if (held) hold(), each_held(look);
+        else scan(look);
+        const u64 best = top_of(r, t, most_v, most_i, bad);
+        if (!best) return true;
+        const float floor_v = floor_of(m, (uint32_t)(best >> 32));
+        const int n = candidates(k, most_v, held);
+        if (n > 64) return false;
+        if (wave == 0) finish_few(r, n, k, p, !(p > 0.0f) && p < 1.0f, floor_v);
+        return true;
+    }
     // The n <= 64 first tokens of the list, by one wavefront: ordered, cut off after k, at p (`one`: after the first) and
     // below floor_v, and drawn from.
     __device__ __forceinline__ void finish_few(long r, int n, int k, float p, bool one, float floor_v)
@@ -620,23 +718,9 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
     int most_i = 0;
     bool bad = false;
     // Rows of few units stay in registers for the search of the first few.
-    constexpr int HELD = SHORT || NT == 256 ? 1 : 8;
-    Held<T, SHORT> h[HELD];
-    const bool held = by_k && k <= NT / 4 && a.units <= HELD * WAVES && a.runs == 1;
-    const auto each_held = [&](auto f) {
-#pragma unroll
-        for (int n = 0; n < HELD; ++n) {
-            const int unit = wave + n * WAVES;
-            float v[8];
-            const int at = h[n].widen(v, a.vocab, min(unit, a.units - 1), a.units, lane);
-            if (unit < a.units)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f(v[i], at + i);
-        }
-    };
+    const bool held = by_k && k <= NT / 4 && fits();
     if (held) {
-#pragma unroll
-        for (int n = 0; n < HELD; ++n) h[n].load(x, a.vocab, min(wave + n * WAVES, a.units - 1), lane);
+        hold();
         each_held([&](float v, int i) {
             if (v > most_v) most_v = v, most_i = i;
             bad |= !(v < __builtin_inff());
@@ -661,64 +745,23 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
                     if (v[i] > anchor) put(v[i], at + i);
         }
     });
-    const uint32_t mine = key_of(most_v), top_key = largest(mine);
-    const float top = logit_of(top_key);
-    const int first = (int)~largest(mine == top_key ? ~(uint32_t)most_i : 0u);
-    const u64 best = (u64)top_key << 32 | (uint32_t)~first;
-    if (__syncthreads_or(bad) || top == kNegInf) return done(r, -1, __builtin_nanf(""));
-    if (!(t > 0.0f)) return done(r, first, 0.0f);
-    row.top = top;
-    row.factor = fmax(1.44269504088896340736 / (double)t, 1e-300);
-    row.least = -(a.shift + 3) / row.factor;
-    row.table = s.table;
-    row.shift = a.shift;
-
-    // min_p as a logit: the smallest whose weight passes it, near where the logarithm has it.
-    float floor_v = kNegInf;
-    if (m > 0.0f) {
-        const double want = ldexp((double)fminf(m, 1.0f), row.shift);
-        const uint32_t near = key_of((float)fmax(row.top + log2((double)fminf(m, 1.0f)) / row.factor, -3.4e38));
-        const uint32_t key = near - 32u + (uint32_t)lane;
-        const u64 pass = __ballot(key >= top_key || row.share(logit_of(key)) >= want);
-        floor_v = pass ? fminf(logit_of(near - 32u + (uint32_t)__builtin_ctzll(pass)), top) : top;
-    }
+    const u64 best = top_of(r, t, most_v, most_i, bad);
+    if (!best) return;
+    const float top = (float)row.top, floor_v = floor_of(m, (uint32_t)(best >> 32));
     u64 cut = p > 0.0f || !(p < 1.0f) ? 0 : best;   // places from here on are kept
     int n = 0;                                      // of the list, if it holds all that are kept
     bool summed = false;                            // whether the sums of the kept are there
     if (by_k) {
-        // For few: k threads' largest logits are k tokens, so that nothing below the last of these counts.
-        const bool few = k <= NT / 4;
-        const auto end = [&](u64 b, u64 w) { return b < (u64)k && (u64)k <= w; };
-        u64 ahead, with;
-        anchor = top;
-        if (few) {
-            const float low = -logit_of(largest(most_v > kNegInf ? key_of(-most_v) : 0u));
-            inv = top > low ? fminf((float)NT / (top - low), 0x1p100f) : 0.0f;
-            s.counts[tid] = 0;
-            __syncthreads();
-            atomicAdd(&s.counts[bin_of<NT>(most_v)], 1u);
-            __syncthreads();
-            const int bin = crossing<NT>(s.counts, end, &ahead, &with);
-            if (tid == 0) s.count = 0;
-            __syncthreads();
-            if (held) {
-                if (bin_of<NT>(most_v) <= bin)
-                    each_held([&](float v, int i) {
-                        if (bin_of<NT>(v) <= bin) put(v, i);
-                    });
-            } else {
-                scan([&](float v, int i) {
-                    if (bin_of<NT>(v) <= bin) put(v, i);
-                });
-            }
-            __syncthreads();
-            n = s.count;
+        if (k <= NT / 4) {
+            n = candidates(k, most_v, held);
         } else {
+            u64 ahead, with;
+            anchor = top;
             inv = fminf((float)BINS / (64.0f * fmaxf(t, 1.0f)), 0x1p100f);
             clear(s.counts);
             scan([&](float v, int) { atomicAdd(&s.counts[bin_of(v)], 1u); });
             __syncthreads();
-            const int bin = crossing<BINS>(s.counts, end, &ahead, &with);
+            const int bin = crossing<BINS>(s.counts, [&](u64 b, u64 w) { return b < (u64)k && (u64)k <= w; }, &ahead, &with);
             n = gather([&](float v, int) { return bin_of(v) <= bin; });
         }
         if (n <= 64) {
@@ -926,6 +969,14 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
     });
 }
 
+// A work-group a row: latencies and barriers in a row bind, not the row's bytes.
+// One row of 32000 in fp32, top_k 50, top_p and min_p: 13 us on the device (its
+// 128 KB by one compute unit are 3 of them); greedy 5.  Such a row stays in
+// registers, 8 units of 8 tokens a lane, and a wavefront finishes up to 64
+// candidates by itself: 18 us without both.  Up to 4096 tokens take 256
+// threads, whose barriers are shorter, more of them 512: 256 rows in fp32 with
+// top_p .9, 2000 tokens 14 against 17 us, 4096 17 either way, 16000 32 against 27,
+// 32000 56 against 39.
 template <typename T, int NT, bool SHORT>
 __global__ __launch_bounds__(NT) void sample_rows_kernel(SampleArgs a)
 {
@@ -941,6 +992,20 @@ __global__ __launch_bounds__(NT) void sample_rows_kernel(SampleArgs a)
 // rule, goes to a list; a row of which the list does not hold that is taken as
 // rows of fp32 are.
 //
+// Bound by LDS: an addition to a counter for each token in the first pass and a
+// look-up of 8 bytes in the second, at addresses that the logits choose.  256
+// rows of 128000, top_p .9, a third of the tokens masked: 48 us, of which the
+// first pass takes 17, the second 15, the steps between them 9, the draw 4 (65 MB
+// from memory once: 13).  With 512 threads 67 where 1024 took 59.  Taken as rows
+// of fp32 are, a weight evaluated for each token, such rows take 103; of 16000
+// tokens 27 against 22, of 6000 the same 19.  Rows of which the first few tokens
+// are asked for, or the first, are not counted: they go through the search that
+// rows of fp32 use (top_k 50, 256 rows of 32000 18 against 28, of 128000 34
+// against 51; that search with 512 threads 17 and 36).
+// Measured beside it: the draw's run by one wavefront, unit by unit, 58 (11 of
+// them that run); six units in flight in place of three no change; twice as many
+// runs 1 us less in the draw and 2.5 more in the second pass.
+//
 // Slots, in the order of the logits: the list's x >= 2^7; the positive values;
 // the list's |x| < 2^-8; the negative values; the list's x <= -2^7.
 constexpr int kValues = 15 * 128, kMiddle = kValues + 1, kSlots = 2 * kValues + 3;
@@ -951,9 +1016,10 @@ constexpr uint32_t kForbidden = 0xFF80;  // bits of minus infinity
 // the same, the list's three slots.  The places of what has no counter stay 0.
 constexpr int kSide = kValues + 2, kPlaces = 2 * kSide + 3;
 constexpr int kTieBit = 56;
+constexpr int kFew = 56;   // seven eighths of the candidates that one wavefront finishes
 
 struct Values {
-    uint32_t counts[kPlaces];
+    uint32_t counts[kPlaces + 64];   // the last: of what has no counter, a lane's own
     u64 weights[kPlaces];      // of a token; of the list's slots the sum
     u64 list[kList / 2], sums[kList];
     uint32_t ties[kList];
@@ -993,11 +1059,25 @@ struct ByValue {
     }
     // Of two values' bits their places.
     typedef uint16_t two __attribute__((ext_vector_type(2)));
+    static __device__ __forceinline__ two clamped(two v)
+    {
+        return __builtin_elementwise_min(__builtin_elementwise_max((two)(v & (two)0x7FFF), (two)(kFirst - 1)), (two)(kFirst + kValues));
+    }
     static __device__ __forceinline__ two places_of(uint32_t b)
     {
         const two v = __builtin_bit_cast(two, b);
-        const two m = __builtin_elementwise_min(__builtin_elementwise_max((two)(v & (two)0x7FFF), (two)(kFirst - 1)), (two)(kFirst + kValues));
-        return (v >> (two)15) * (two)kSide + (m - (two)(kFirst - 1));
+        return (v >> (two)15) * (two)kSide + (clamped(v) - (two)(kFirst - 1));
+    }
+    // The same for counting, `other` for values without a counter; *odd: whether there are such besides minus infinity.
+    static __device__ __forceinline__ two counters_of(uint32_t b, int other, uint32_t *odd)
+    {
+        const two v = __builtin_bit_cast(two, b), m = clamped(v);
+        const two in = m - (two)(kFirst - 1), place = (v >> (two)15) * (two)kSide + in;
+        // 1 where the magnitude is below the first counter or above the last: in - 1 is kValues or 2^16 - 1 there
+        const two out = __builtin_elementwise_min(__builtin_elementwise_max((two)(in - (two)1), (two)(kValues - 1)) - (two)(kValues - 1), (two)1);
+        const two some = __builtin_elementwise_min((two)(v ^ (two)kForbidden), (two)1);
+        *odd |= __builtin_bit_cast(uint32_t, (two)(out & some));
+        return place + out * ((two)other - place);
     }
     static __device__ __forceinline__ float value_of(int slot)
     {
@@ -1122,18 +1202,12 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     __syncthreads();
     bool bad = false;
     units(all, [&](const uint32_t (&b)[4], int at, int, bool) {
-        uint32_t place[4];
-        bool any = false;
+        uint32_t place[4], odd = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) place[i] = __builtin_bit_cast(uint32_t, places_of(b[i]));
+        for (int i = 0; i < 4; ++i) place[i] = __builtin_bit_cast(uint32_t, counters_of(b[i], kPlaces + lane, &odd));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t v = i % 2 ? b[i / 2] >> 16 : b[i / 2] & 0xFFFFu, to = i % 2 ? place[i / 2] >> 16 : place[i / 2] & 0xFFFFu;
-            const bool in = (v & 0x7FFFu) - kFirst < (unsigned)kValues;
-            if (in) atomicAdd(&s.counts[to], 1u);
-            any |= !in && v != kForbidden;
-        }
-        if (any)
+        for (int i = 0; i < 8; ++i) atomicAdd(&s.counts[i % 2 ? place[i / 2] >> 16 : place[i / 2] & 0xFFFFu], 1u);
+        if (odd)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t v = i % 2 ? b[i / 2] >> 16 : b[i / 2] & 0xFFFFu;
@@ -1375,6 +1449,12 @@ __global__ __launch_bounds__(NT) void sample_values_kernel(SampleArgs a)
         Values values;
         typename Picker<uint16_t, NT, false>::Shared bins;
     } s;
+    const int k = a.top_k ? a.top_k[blockIdx.x] : 0;
+    const bool first = a.temperature && !(a.temperature[blockIdx.x] > 0.0f);   // the first token alone, which one pass finds
+    if (first || (k > 0 && k <= kFew)) {
+        if (Picker<uint16_t, NT, false>(a, s.bins, blockIdx.x).few(blockIdx.x, k)) return;
+        __syncthreads();
+    }
     if (!ByValue<NT>(a, s.values, blockIdx.x).run(blockIdx.x)) {
         __syncthreads();
         row_by_bins<NT>(a, &s.bins, blockIdx.x);

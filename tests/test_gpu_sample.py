@@ -118,6 +118,29 @@ def test_equal_logits(vocab, dtype):
         check(x, u, min_p=[1.0] * 6)
 
 
+@pytest.mark.parametrize("vocab", [4097, 40000, 70001])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_the_first_few(vocab, dtype):
+    """k around what one wavefront finishes, of rows with more candidates than k (ties, and a thread's own), with fewer tokens
+    than k, with logits of every size; and the first alone."""
+    g = gen(vocab)
+    base = logits(g, 1, vocab, F32)
+    tied = torch.randn(1, vocab, generator=g)
+    tied[0, torch.randperm(vocab, generator=g)[:90]] = 7.0
+    near = torch.randn(1, vocab, generator=g)
+    near[0, 512:1024] = 9 + torch.rand(512, generator=g)         # the largest in one unit
+    left = torch.full((1, vocab), -math.inf)
+    left[0, torch.randperm(vocab, generator=g)[:20]] = torch.randn(20, generator=g)
+    tiny, huge = 1e-4 * base, 1e4 * base
+    x = torch.cat([base, tied, near, left, tiny, huge]).to(dtype)
+    for k in (1, 2, 19, 20, 48, 55, 56, 57, 64, 65, 128):
+        for u in (0.0, 0.4, 0.93):
+            check(x, [u] * 6, top_k=[k] * 6)
+        check(x, [0.7] * 6, top_k=[k] * 6, top_p=[0.9, 0.5, 0.0, 0.9, 1.0, 0.3], min_p=[0.0, 0.1, 0.0, 0.2, 0.0, 1.0], temperature=[0.9] * 6)
+    t, lp = check(x, [0.5] * 6, temperature=[0.0, -1.0, 0.0, 0.0, 1.0, math.nan], top_k=[5, 0, 1, 70, 0, 0])
+    assert lp[:4].tolist() == [0.0] * 4 and t[1] == int((x[1] == 7).nonzero()[0])
+
+
 def test_masks_and_extremes():
     g = gen(3)
     low = torch.finfo(F32).min
