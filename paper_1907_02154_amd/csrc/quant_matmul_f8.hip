@@ -256,16 +256,23 @@ using Number = std::integral_constant<int, N>;
 // three groups of 8 turns ahead.  After 40 turns all of a block has been read;
 // there the wavefronts meet, the block after it has landed, and in the last 24
 // turns its tokens, first channels and exponents are read and the block after
-// that one starts on its way into the place that has become free.  The channels
+// that one starts on its way into the place that has become free: 12 of its 18
+// loads a thread, every other turn, and the rest in the next block's first 16,
+// for a compute unit takes a load of 1 KB in 16 cycles, four wavefronts' 18 in
+// 1152, and more at a time hold the products up (all in 18 turns: 228 us where
+// this takes 215; 8 and 10: 218).  The channels
 // of a lane's sums are eight that follow one another, stored as 16 bytes, four
 // lanes 64; LDS chunks are rotated so that both orders of rows are free of
 // conflicts.  Exponents come as four bytes a register, of which the instruction
 // picks one.
-// 8192 x 8192 outputs, K = 4096: 227 us, 2.42 PFLOP/s (the tile above: 255); K =
-// 8192, half the outputs: 205, 2.68 (246); a large library product of the same
-// kind without exponents: 224 and, at its best, 2.75.  Taking the next tile's
-// first blocks while the last one's outputs are stored, in a grid of one
-// work-group on each compute unit, took 235.
+// 8192 x 8192 outputs, K = 4096: 215 us, 2.55 PFLOP/s (the tile above: 255); K =
+// 8192, half the outputs: 206, 2.67 (246); the library's product of the first size
+// without exponents 224, its best, 8192 x 8192 x 8192, 2.75 PFLOP/s.  The
+// instruction alone, on such values in registers, reaches 3.7 to 4.5, as the
+// clock follows the power it takes; a product has a turn of 44 to 50 cycles
+// here, of which it takes 32.  Taking the next tile's first blocks while the last
+// one's outputs are stored, in a grid of one work-group on each compute unit,
+// took 235 where it took 227 without.
 __global__ __launch_bounds__(256) void matmul_f8_large_kernel(F8Args f)
 {
     const MatArgs &a = f.m;
@@ -344,8 +351,10 @@ __global__ __launch_bounds__(256) void matmul_f8_large_kernel(F8Args f)
         constexpr int p = decltype(pc)::value;
         ew[p][0] = pack(ex[0]), ew[p][1] = pack(ex[1]), ea[p][0] = pack(ex[2]), ea[p][1] = pack(ex[3]);
     };
-    // A block in stage p, the next in the other; `after` is loaded into p once p is read.
-    const auto step = [&](auto pc, const Block &after) {
+    // A block in stage p, the next in the other, of which the last loads are issued first; then, once p is read, the first
+    // kEarly of `after` into p.
+    constexpr int kEarly = 12;
+    const auto step = [&](auto pc, const Block &next, const Block &after) {
         constexpr int p = decltype(pc)::value, q = 1 - p;
         each<8>([&](auto ic) {
             constexpr int i = decltype(ic)::value;
@@ -362,6 +371,7 @@ __global__ __launch_bounds__(256) void matmul_f8_large_kernel(F8Args f)
                                                                             j % 4, ea[p][j / 4]);
                 if constexpr (i < 5) {
                     if constexpr (j == 0) read_w(p, Number<i + 3>());
+                    if constexpr (i < 2 && j % 3 == 1) load(Number<kEarly + 3 * i + j / 3>(), q, next);
                 } else {
                     constexpr int n = (i - 5) * 8 + j;
                     if constexpr (n == 0) read_w(q, Number<0>()), read_e(q);
@@ -369,15 +379,15 @@ __global__ __launch_bounds__(256) void matmul_f8_large_kernel(F8Args f)
                     else if constexpr (n == 9) read_w(q, Number<1>());
                     else if constexpr (n == 17) read_w(q, Number<2>());
                     if constexpr (n == 15) pack_e(Number<q>());
-                    if constexpr (n >= 6) load(Number<n - 6>(), p, after);
+                    if constexpr (n % 2 == 1) load(Number<n / 2>(), p, after);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
     };
     each<18>([&](auto n) { load(n, 0, block_at(0)); });
-    each<18>([&](auto n) { load(n, 1, block_at(1)); });
-    wait_vmcnt<18>();
+    each<kEarly>([&](auto n) { load(n, 1, block_at(1)); });
+    wait_vmcnt<kEarly>();
     asm volatile("s_barrier" ::: "memory");
     read_w(0, Number<0>()), read_e(0);
     each<8>([&](auto j) { read_a(Number<0>(), j); });
@@ -386,8 +396,8 @@ __global__ __launch_bounds__(256) void matmul_f8_large_kernel(F8Args f)
     pack_e(Number<0>());
     __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
     for (int b = 0; b < f.blocks; b += 2) {   // of an odd number the last is one of zeros
-        step(Number<0>(), block_at(b + 2));
-        step(Number<1>(), block_at(b + 3));
+        step(Number<0>(), block_at(b + 1), block_at(b + 2));
+        step(Number<1>(), block_at(b + 2), block_at(b + 3));
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
