@@ -434,6 +434,11 @@ __global__ __launch_bounds__(256) void matmul_f8_large_kernel(F8Args f)
     }
 }
 
+// Costs as measured for 8-bit integers, whose products take as long; the last
+// one's its own.  With every tile timed at K = 1024 and 4096, N = 1024, 4096 and
+// 11000, M from 1 to 2048 and both outputs, the cheapest by this rule is the
+// fastest or a few percent off; worst are 128 tokens, 1024 channels and K = 4096,
+// 6.0 us where tiles of 16 x 32 take 5.3.
 constexpr Tile kTiles[] = {
     {16, 16, 1, 1, 4, 4, 2, 3.4f, 3.8f},    {16, 32, 1, 2, 4, 3, 2, 3.8f, 5.0f},    {32, 64, 1, 4, 4, 3, 1, 6.6f, 0.0f},
     {64, 32, 2, 2, 4, 3, 1, 6.6f, 0.0f},    {64, 64, 2, 2, 2, 4, 1, 9.3f, 0.0f},    {128, 64, 4, 2, 2, 3, 1, 13.8f, 0.0f},
