@@ -178,7 +178,8 @@ struct Held {
 };
 
 // The first n of the list in order, the largest first.  (Up to a few wavefronts each thread counts what comes before its
-// own: one round of reads against a barrier for each of log^2 steps.)
+// own: one round of reads against a barrier for each of log^2 steps.  More are merged, steps within 64 in registers: 64
+// fp32 rows of 64000, top_p .9, some 600 of each in the list, 57 us where a barrier a step took 60.)
 template <int NT>
 __device__ __forceinline__ void sort_list(u64 *list, int n, int tid)
 {
@@ -987,7 +988,7 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
 }
 
 // A work-group a row: latencies and barriers in a row bind, not the row's bytes.
-// One row of 32000 in fp32, top_k 50, top_p and min_p: 13 us on the device (its
+// One row of 32000 in fp32, top_k 50, top_p and min_p: 13 to 15 us on the device (its
 // 128 KB by one compute unit are 3 of them); greedy 5.  Such a row stays in
 // registers, 8 units of 8 tokens a lane, and a wavefront finishes up to 64
 // candidates by itself: 18 us without both.  Up to 4096 tokens take 256
