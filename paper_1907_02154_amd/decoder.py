@@ -223,7 +223,6 @@ class Decoder:
             x = self._block(b, cache, x, slots, state.table, state.lens, None, 1, state.max_len, trace)
         return x
 
-
     def answer(self, state: State, tokens: torch.Tensor, u: torch.Tensor, **filters):
         """One step on a token of every sequence, tokens int32 [seqs]: the (tokens, logprob) drawn to follow them.  A
         ValueError, and nothing done, where a sequence has no room."""
@@ -235,10 +234,10 @@ class Decoder:
 
 
 class Steps:
-    """A captured step: each replay takes the sequences of its state one token further."""
+    """A captured step: each replay takes the sequences of its state one token further.  It keeps what a replay reads."""
 
-    def __init__(self, state: State, graph: "torch.cuda.CUDAGraph"):
-        self.state, self.graph = state, graph
+    def __init__(self, state: State, graph: "torch.cuda.CUDAGraph", reads):
+        self.state, self.graph, self.reads = state, graph, reads
 
     def replay(self) -> None:
         """A ValueError, and nothing done, where a sequence has no room for a token more."""
@@ -246,7 +245,7 @@ class Steps:
         self.graph.replay()
 
 
-def _capture(state: State, once, again):
+def _capture(state: State, reads, once, again):
     """`again` as a HIP graph, after `once` outside it, for kernels are loaded on their first launch; the state goes back."""
     lens, held = state.lens.clone(), state.held
     side = torch.cuda.Stream()
@@ -259,26 +258,22 @@ def _capture(state: State, once, again):
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         out = again()
-    return Steps(state, graph), out
+    return Steps(state, graph, reads), out
 
 
 def capture_step(dec: Decoder, state: State, x: torch.Tensor):
     """A step on the tensor x as a HIP graph: (``Steps`` to replay, its output)."""
-    return _capture(state, lambda: dec.step(state, x), lambda: dec._step(state, x))
+    return _capture(state, (dec, x), lambda: dec.step(state, x), lambda: dec._step(state, x))
 
 
 def capture_answer(dec: Decoder, state: State, tokens: torch.Tensor, u: torch.Tensor, **filters):
     """An answer to the tensor of tokens as a HIP graph: (``Steps`` to replay, logprob).  A replay puts the tokens drawn by
     u in the place of those that it read, for the next one, whose u the caller fills in before."""
-    kept = tokens.clone()
-
     def again():
         drawn, logprob = dec.pick(dec._step(state, dec.embed(tokens)), u, **filters)
         tokens.copy_(drawn)
         return logprob
-    steps = _capture(state, lambda: dec.answer(state, tokens, u, **filters), again)
-    tokens.copy_(kept)
-    return steps
+    return _capture(state, (dec, tokens, u, filters), lambda: dec.answer(state, tokens, u, **filters), again)
 
 
 def main(seqs: int = 16, prompt: int = 1000, steps: int = 64) -> None:

@@ -161,6 +161,24 @@ def test_captured_answers_are_the_eager_ones(float8):
     assert state.lens.tolist() == twin.lens.tolist() == [36, 15, 67] and float(want[2]) == 0
 
 
+def test_a_captured_answer_keeps_what_it_reads():
+    """Filters that nothing else refers to, whose memory would go to the tensors made after the capture."""
+    dec, state = small()
+    _, twin = small()
+    for st in (state, twin):
+        dec.prompt(st, streams(dec, [30, 9, 61], 23))
+    tokens = torch.tensor([1, 2, 3], dtype=torch.int32, device="cuda")
+    eager = tokens.clone()
+    u = torch.full((3,), 0.999, device="cuda")
+    graph, _ = decoder.capture_answer(dec, state, tokens, u, temperature=torch.zeros(3, device="cuda"))
+    other = [torch.full((3,), 50.0, device="cuda") for _ in range(200)]
+    for i in range(4):
+        eager, _ = dec.answer(twin, eager, u, temperature=torch.zeros(3, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(tokens, eager) and len(other) == 200, i
+
+
 def test_two_captured_answers_of_one_state_take_turns():
     """Two graphs with workspaces and outputs of their own, replayed in turn on one state, against eager answers."""
     dec, state = small()
