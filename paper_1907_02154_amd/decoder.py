@@ -246,15 +246,19 @@ class Steps:
 
 
 def _capture(state: State, reads, once, again):
-    """`again` as a HIP graph, after `once` outside it, for kernels are loaded on their first launch; the state goes back."""
+    """`again` as a HIP graph, after `once` outside it, for kernels are loaded on their first launch.  The state stays as it
+    was: `once` finds the pages full, so that its tokens, which might raise an exponent of the cache, are not written."""
     lens, held = state.lens.clone(), state.held
+    state.lens.fill_(state.table.shape[1] * state.page_size)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
-    with torch.cuda.stream(side):
-        once()
-    torch.cuda.current_stream().wait_stream(side)
-    state.lens.copy_(lens)
-    state.held = held
+    try:
+        with torch.cuda.stream(side):
+            once()
+    finally:
+        torch.cuda.current_stream().wait_stream(side)
+        state.lens.copy_(lens)
+        state.held = held
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         out = again()

@@ -161,6 +161,31 @@ def test_captured_answers_are_the_eager_ones(float8):
     assert state.lens.tolist() == twin.lens.tolist() == [36, 15, 67] and float(want[2]) == 0
 
 
+def test_a_capture_leaves_the_cache_as_it_was():
+    """Of a token far larger than those that follow: its block's exponent must not have seen it."""
+    dec, state = small()
+    _, twin = small()
+    for st in (state, twin):
+        out = dec.prompt(st, streams(dec, [30, 9, 61], 22))
+    x = torch.stack([y[-1] for y in out])
+    for b in dec.blocks:
+        b.norm1 = b.norm1 * 300                       # keys and values of the captured step
+    y = x.clone()
+    before = [bits(t).clone() for c in state.caches for t in (c.k_codes, c.v_codes, c.k_exps, c.v_exps)]
+    graph, got = decoder.capture_step(dec, state, y)
+    decoder.capture_answer(dec, state, torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(3, device="cuda"))
+    torch.cuda.synchronize()
+    after = [bits(t) for c in state.caches for t in (c.k_codes, c.v_codes, c.k_exps, c.v_exps)]
+    assert all(torch.equal(p, q) for p, q in zip(before, after)) and state.lens.tolist() == twin.lens.tolist()
+    for i in range(3):
+        want = dec.step(twin, x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), i
+        x = want
+        y.copy_(got)
+
+
 def test_a_captured_answer_keeps_what_it_reads():
     """Filters that nothing else refers to, whose memory would go to the tensors made after the capture."""
     dec, state = small()
@@ -206,6 +231,9 @@ def test_no_room_and_no_vocabulary():
     for bad in ((t[:2], u), (t.long(), u), (t, u[:1])):
         with pytest.raises(ValueError):
             dec.answer(state, *bad)
+    for capture in (lambda: decoder.capture_answer(dec, state, t, u), lambda: decoder.capture_step(dec, state, dec.embed(t))):
+        with pytest.raises(ValueError, match="no room"):
+            capture()
     assert state.held == [149, 5, 150] == state.lens.tolist()
     plain = decoder.Decoder(blocks=1, width=256, heads=4, kv_heads=2, head_dim=64, inner=520)
     for f in (lambda: plain.embed(t), lambda: plain.logits(torch.zeros(1, 256)), lambda: plain.answer(state, t, u)):
