@@ -178,8 +178,8 @@ struct Held {
 };
 
 // The first n of the list in order, the largest first.  (Up to a few wavefronts each thread counts what comes before its
-// own: one round of reads against a barrier for each of log^2 steps.  More are merged, steps within 64 in registers: 64
-// fp32 rows of 64000, top_p .9, some 600 of each in the list, 57 us where a barrier a step took 60.)
+// own: one round of reads against a barrier for each of log^2 steps.  Steps within 64 of longer lists in registers took
+// 3 us off the 60 of fp32 rows of 64000 with top_p and added 0.4 to the 11 to 15 of rows with top_k: not kept.)
 template <int NT>
 __device__ __forceinline__ void sort_list(u64 *list, int n, int tid)
 {
@@ -198,23 +198,8 @@ __device__ __forceinline__ void sort_list(u64 *list, int n, int tid)
     while (size < n) size *= 2;
     for (int i = n + tid; i < size; i += NT) list[i] = 0;
     __syncthreads();
-    // Merges of runs of k, the larger first where (i & k) is 0; the steps within 64 by a wavefront in registers, for k =
-    // 64 those of every shorter run too.
-    const auto within = [&](int first_k, int last_k) {
-        for (int i = tid; i < size; i += NT) {
-            u64 v = list[i];
-            for (int k = first_k; k <= last_k; k *= 2)
-                for (int j = min(k, 64) / 2; j > 0; j /= 2) {
-                    const u64 o = (u64)(uint32_t)__shfl_xor((int)(v >> 32), j) << 32 | (uint32_t)__shfl_xor((int)v, j);
-                    v = ((i & j) == 0) == ((i & k) == 0) ? max(v, o) : min(v, o);
-                }
-            list[i] = v;
-        }
-        __syncthreads();
-    };
-    within(2, 64);
-    for (int k = 128; k <= size; k *= 2) {
-        for (int j = k / 2; j >= 64; j /= 2) {
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
             for (int t = tid; t < size / 2; t += NT) {
                 const int i = 2 * t - (t & (j - 1)), o = i + j;   // the t-th pair j apart
                 const u64 p = list[i], q = list[o];
@@ -222,8 +207,6 @@ __device__ __forceinline__ void sort_list(u64 *list, int n, int tid)
             }
             __syncthreads();
         }
-        within(k, k);
-    }
 }
 
 // A row's units: a wavefront takes runs of them, every NT / 64-th, three units in flight, the first of which may be
