@@ -236,7 +236,7 @@ class Decoder:
 class Steps:
     """A captured step: each replay takes the sequences of its state one token further.  It keeps what a replay reads."""
 
-    def __init__(self, state: State, graph: "torch.cuda.CUDAGraph", reads):
+    def __init__(self, state: State, graph: "torch.cuda.CUDAGraph", reads=()):
         self.state, self.graph, self.reads = state, graph, reads
 
     def replay(self) -> None:
