@@ -569,16 +569,27 @@ struct Picker {
         row.shift = a.shift;
         return (u64)top_key << 32 | (uint32_t)~first;
     }
-    // min_p as a logit: the smallest whose weight passes it, near where the logarithm has it.
+    // min_p as a logit: the smallest whose weight passes it.  As a rule it is one of the 64 around where the logarithm has it.
+    // Near 0 logits lie closer than weights tell them apart, so that all of these may pass, or none: then it is looked for
+    // among the others, 64 of them at a time.
     __device__ __forceinline__ float floor_of(float m, uint32_t top_key) const
     {
         if (!(m > 0.0f)) return kNegInf;
         const double want = ldexp((double)fminf(m, 1.0f), row.shift);
-        const uint32_t near = key_of((float)fmax(row.top + log2((double)fminf(m, 1.0f)) / row.factor, -3.4e38));
-        const uint32_t key = near - 32u + (uint32_t)lane;
-        const u64 pass = __ballot(key >= top_key || row.share(logit_of(key)) >= want);
-        const float top = logit_of(top_key);
-        return pass ? fminf(logit_of(near - 32u + (uint32_t)__builtin_ctzll(pass)), top) : top;
+        const auto passing = [&](uint32_t key, uint32_t surely) {   // lanes whose key passes; one from `surely` on does
+            return __ballot(key >= surely || row.share(logit_of(key)) >= want);
+        };
+        const uint32_t near = key_of((float)fmax(row.top + log2((double)fminf(m, 1.0f)) / row.factor, -3.4e38)), from = near - 32u;
+        const u64 pass = passing(from + (uint32_t)lane, top_key);
+        uint32_t lo = from - 1u, hi = from + (uint32_t)__builtin_ctzll(pass | 1ull << 63);   // does not pass, passes
+        if (!pass) lo = from + 63u, hi = top_key;
+        else if (pass & 1) lo = key_of(kNegInf);
+        while (hi - lo > 1u && (!pass || pass & 1)) {
+            const uint32_t step = (hi - lo + 63u) / 64u;
+            const int at = __builtin_ctzll(passing(lo + ((uint32_t)lane + 1u) * step, hi));   // the last lane's passes
+            hi = min(lo + ((uint32_t)at + 1u) * step, hi), lo += (uint32_t)at * step;
+        }
+        return fminf(logit_of(hi), logit_of(top_key));
     }
     // For few: k threads' largest logits are k tokens, so that nothing below the last of these counts.  The others into the
     // list; how many there are.
