@@ -291,6 +291,8 @@ __device__ __forceinline__ u64 from_any(u64 v, int lane)   // of one lane, the s
 {
     return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
 }
+// Whether top_p or min_p leave nothing but the first token.
+__device__ __forceinline__ bool first_alone(float p, float m) { return (p < 1.0f && !(p > 0.0f)) || m > 1.0f; }
 __device__ __forceinline__ float drawn(const SampleArgs &a, long r)   // u as it counts
 {
     const float u = a.u[r];
@@ -634,7 +636,7 @@ struct Picker {
         const float floor_v = floor_of(m, (uint32_t)(best >> 32));
         const int n = candidates(k, most_v, held);
         if (n > 64) return false;
-        if (wave == 0) finish_few(r, n, k, p, !(p > 0.0f) && p < 1.0f, floor_v);
+        if (wave == 0) finish_few(r, n, k, p, first_alone(p, m), floor_v);
         return true;
     }
     // The n <= 64 first tokens of the list, by one wavefront: ordered, cut off after k, at p (`one`: after the first) and
@@ -651,7 +653,7 @@ struct Picker {
         const float v = logit_of((uint32_t)(q >> 32));
         n = min(n, k);
         u64 w = lane < n ? row.weight(v) : 0, in = wave_scan(w);
-        if (p < 1.0f) {
+        if (one || p < 1.0f) {
             const double most = (double)p * (double)last_lane(in);
             if (lane > 0 && (one || (double)(in - w) >= most)) w = 0;
         }
@@ -708,7 +710,7 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
     const float t = a.temperature ? a.temperature[r] : 1.0f;
     const int k = a.top_k ? a.top_k[r] : 0;
     const float p = a.top_p ? a.top_p[r] : 1.0f, m = a.min_p ? a.min_p[r] : 0.0f;
-    const bool by_k = k > 0 && k < a.vocab, by_p = p < 1.0f && p > 0.0f;
+    const bool one = first_alone(p, m), by_k = k > 0 && k < a.vocab, by_p = p < 1.0f && !one;
     if (tid < kTable) s.table[tid] = exp2((double)tid / kTable);
     if (tid == 0) s.count = 0;
 
@@ -760,9 +762,9 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
     const u64 best = top_of(r, t, most_v, most_i, bad);
     if (!best) return;
     const float top = (float)row.top, floor_v = floor_of(m, (uint32_t)(best >> 32));
-    u64 cut = p > 0.0f || !(p < 1.0f) ? 0 : best;   // places from here on are kept
-    int n = 0;                                      // of the list, if it holds all that are kept
-    bool summed = false;                            // whether the sums of the kept are there
+    u64 cut = one ? best : 0;   // places from here on are kept
+    int n = 0;                  // of the list, if it holds all that are kept
+    bool summed = false;        // whether the sums of the kept are there
     if (by_k) {
         if (k <= NT / 4) {
             n = candidates(k, most_v, held);
@@ -777,7 +779,7 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
             n = gather([&](float v, int) { return bin_of(v) <= bin; });
         }
         if (n <= 64) {
-            if (wave == 0) finish_few(r, n, k, p, cut != 0, floor_v);
+            if (wave == 0) finish_few(r, n, k, p, one, floor_v);
             return;
         }
         if (n <= kList) {
@@ -790,7 +792,7 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
     }
     if (by_p && n) {
         n = fit(n, 0, (double)p * (double)listed_sum(n));
-    } else if (n && cut) {
+    } else if (n && one) {
         n = 1;
     } else if (by_p) {
         // The neighbourhood of the end, from the number of tokens in each bin alone; then the weights, once: the sums of
@@ -1200,7 +1202,8 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     float t = a.temperature ? a.temperature[r] : 1.0f;
     int k = a.top_k ? a.top_k[r] : 0;
     float p = a.top_p ? a.top_p[r] : 1.0f, m = a.min_p ? a.min_p[r] : 0.0f;
-    if (!(t > 0.0f)) t = 1.0f, k = 1, p = 1.0f, m = 0.0f;   // the first token
+    if (!(t > 0.0f) || m > 1.0f) k = 1, p = 1.0f, m = 0.0f;   // the first token
+    if (!(t > 0.0f)) t = 1.0f;
     if (k < 1 || k > a.vocab) k = a.vocab;
     const int parts = (a.units + a.runs - 1) / a.runs;
     Units<T, false, NT> all;
@@ -1311,15 +1314,15 @@ __device__ __forceinline__ bool ByValue<NT>::run(long r)
     const u64 cut = end.slot < kSlots && of_list(end.slot) ? s.list[first_of(end.slot) + end.tokens - 1] : 0;
     const auto kept = [&](float v, u64 place) {   // of the list's
         const int slot = slot_of_listed(v);
-        return (slot < end.slot || (slot == end.slot && place >= cut)) && (row.share(v) >= want || (slot == best && v == top));
+        return (slot < end.slot || (slot == end.slot && place >= cut)) && row.share(v) >= want;   // the first token's is a power of two
     };
     const bool some = end.slot < kSlots && !of_list(end.slot) && end.tokens < (int)s.counts[place_in(end.slot)];
     u64 tie = 0;   // the weight of a token of the last slot, where not all of them stay
-    if (some && (end.slot == best || row.share(value_of(end.slot)) >= want)) tie = s.weights[place_in(end.slot)];
+    if (some && row.share(value_of(end.slot)) >= want) tie = s.weights[place_in(end.slot)];
     __syncthreads();
     if (m > 0.0f)
         for (int i = tid; i < kSlots; i += NT)
-            if (i <= end.slot && i != best && !of_list(i) && row.share(value_of(i)) < want) s.weights[place_in(i)] = 0;
+            if (i <= end.slot && !of_list(i) && row.share(value_of(i)) < want) s.weights[place_in(i)] = 0;
     if (some && tid == end.slot % NT) s.weights[place_in(end.slot)] = tie ? 1ull << kTieBit : 0;
     for (int i = tid; i < outside; i += NT) {
         const u64 q = s.list[i];

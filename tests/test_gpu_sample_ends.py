@@ -61,3 +61,25 @@ def test_a_min_p_whose_logit_is_zero_in_long_rows(filters, dtype):
     x[:, 1500] = torch.tensor(top).to(dtype)
     u = torch.rand(len(t), generator=g).tolist()
     check(x, u, temperature=t, min_p=m, **{n: [v] * len(t) for n, v in filters.items()})
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [5, 900, 4500, 40000])
+def test_a_min_p_above_one_keeps_one_of_equal_tokens(vocab, dtype):
+    """The largest logit many times, within and outside the range of the counters of bf16 rows; of min_p = 1 all of them stay."""
+    g = gen(vocab)
+    x = torch.rand(6, vocab, generator=g) - 1.5
+    tops = torch.tensor([3.0, 200.0, 2.0 ** -12, -2.0 ** -12, 0.25, 0.0])
+    equal = torch.rand(vocab, generator=g) < 0.3
+    equal[[1, 3]] = True
+    x[:, equal] = tops[:, None]
+    x[5, equal] *= torch.where(torch.arange(int(equal.sum())) % 2 == 0, -1.0, 1.0)      # -0 and 0
+    x = x.to(dtype)
+    first = int(equal.nonzero()[0])
+    above = [math.nextafter(1.0, 2.0) + 2.0 ** -23, 2.0, math.inf, 1e30, 1.5, 4.0]
+    for u in (0.0, 0.6, 0.999):
+        for k in (dict(), dict(top_k=[2, 3, 4, 50, 4000, 60]), dict(top_p=[0.9] * 6), dict(top_k=[4, 50, 200, 5000, 4, 300], top_p=[0.99] * 6)):
+            for t in ([1.0] * 6, [0.3, 2.0, 1e-3, 50.0, 1.0, 0.7]):
+                token, lp = check(x, [u] * 6, temperature=t, min_p=above, **k)
+                assert token.tolist() == [first] * 6 and (lp == 0).all()
+                check(x, [u] * 6, temperature=t, min_p=[1.0] * 6, **k)
