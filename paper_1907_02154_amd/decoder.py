@@ -184,9 +184,11 @@ class Decoder:
         q, s, _ = quant.rmsnorm_i8(x, self.norm)
         return self.head(q, s)
 
-    def pick(self, x: torch.Tensor, u: torch.Tensor, **filters):
-        """(tokens, logprob) drawn for the stream x after the last block by u, as ``sample.tokens`` has it."""
-        return sample.tokens(self.logits(x), u, **filters)
+    def pick(self, x: torch.Tensor, u: torch.Tensor, temperature=None, top_k=None, top_p=None, min_p=None, out=None,
+             logprob=None, ws=None):
+        """(tokens, logprob) drawn for the stream x after the last block by u, as ``sample.tokens`` has it; on the current
+        stream, as the logits are."""
+        return sample.tokens(self.logits(x), u, temperature, top_k, top_p, min_p, out=out, logprob=logprob, ws=ws)
 
     def prompt(self, state: State, xs: List[torch.Tensor], trace=None) -> List[torch.Tensor]:
         """New tokens of every sequence, xs[s] bf16 [tokens][width] behind what the sequence holds: the stream after the

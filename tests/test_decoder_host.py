@@ -63,3 +63,11 @@ def test_prompts_of_no_tokens():
     dec, state = made([3, 10], 10)
     out = dec.prompt(state, [tokens(0), tokens(0)])
     assert [tuple(x.shape) for x in out] == [(0, 8), (0, 8)] and state.held == [3, 10]
+
+
+def test_a_pick_stays_on_the_stream_of_its_logits():
+    dec, _ = made([], 10)
+    dec.vocab = 50
+    for k in (dict(stream=0), dict(top_q=None)):
+        with pytest.raises(TypeError):
+            dec.pick(tokens(2), torch.zeros(2), **k)
