@@ -74,15 +74,19 @@ class State:
         self.held = [0] * seqs
         self.max_len, self.page_size = max_len, page_size
 
-    def take(self, news: List[int]) -> None:
-        """Counts news[s] more tokens of each sequence s, if all have room for theirs."""
+    def room(self, news: List[int]) -> List[int]:
+        """How many tokens each sequence s holds with news[s] more, if all have room for theirs."""
         if len(news) != len(self.held):
             raise ValueError(f"the state has {len(self.held)} sequences, got tokens of {len(news)}")
         after = [h + n for h, n in zip(self.held, news)]
         if max(after) > self.max_len:
             s = after.index(max(after))
             raise ValueError(f"sequence {s} holds {self.held[s]} tokens of {self.max_len} at most: no room for {news[s]} more")
-        self.held = after
+        return after
+
+    def take(self, news: List[int]) -> None:
+        """Counts news[s] more tokens of each sequence s, if all have room for theirs."""
+        self.held = self.room(news)
 
     @staticmethod
     def slots_of(table: torch.Tensor, max_len: int, page_size: int) -> torch.Tensor:
@@ -170,6 +174,17 @@ class Decoder:
         if not self.vocab:
             raise ValueError("the decoder has no vocabulary")
 
+    def _device(self, state: State, t: torch.Tensor, name: str) -> int:
+        """The device of a pass over a state, where t has to be, with caches as the decoder's blocks have them."""
+        dev = quant._here(t, name)
+        if state.lens.get_device() != dev:
+            raise ValueError(f"the state is on device {state.lens.get_device()}, {name} is on device {dev}")
+        cache = quant.KV8Cache if self.float8 else quant.KV4Cache
+        if len(state.caches) != len(self.blocks) or any(
+                not isinstance(c, cache) or c.heads != self.kv_heads or c.head_dim != self.head_dim for c in state.caches):
+            raise ValueError("the state is of another decoder")
+        return dev
+
     def embed(self, tokens: torch.Tensor) -> torch.Tensor:
         """The stream of tokens int32 [tokens], bf16 [tokens][width]; of -1 (no token was drawn) token 0's."""
         self._tokens()
@@ -192,13 +207,18 @@ class Decoder:
 
     def prompt(self, state: State, xs: List[torch.Tensor], trace=None) -> List[torch.Tensor]:
         """New tokens of every sequence, xs[s] bf16 [tokens][width] behind what the sequence holds: the stream after the
-        last block, a tensor for each sequence.  A ValueError, and nothing done, where a sequence has no room for its own."""
+        last block, a tensor for each sequence.  What is refused for want of room, or for a shape, type or device, leaves
+        the state as it was."""
         if any(x.dim() != 2 or x.shape[1] != self.width or x.dtype != torch.bfloat16 for x in xs):
             raise ValueError(f"tokens must be bf16 [tokens][{self.width}]")
         news = [x.shape[0] for x in xs]
-        state.take(news)
+        after = state.room(news)
         if not any(news):
             return list(xs)
+        dev = self._device(state, xs[0], "a sequence's tokens")
+        for x in xs:
+            quant._tensor(x, "a sequence's tokens", dev, torch.bfloat16)
+        state.held = after
         starts = torch.tensor([0, *torch.tensor(news).cumsum(0).tolist()], dtype=torch.int32).cuda()
         seq = torch.repeat_interleave(torch.arange(len(xs)), torch.tensor(news)).cuda()
         place = torch.arange(sum(news), device="cuda") - starts[seq] + state.lens[seq]
@@ -210,11 +230,13 @@ class Decoder:
         return list(x.split(news))
 
     def step(self, state: State, x: torch.Tensor, trace=None) -> torch.Tensor:
-        """One new token of every sequence, x bf16 [seqs][width]: the stream after the last block.  A ValueError, and
-        nothing done, where a sequence has no room for it."""
+        """One new token of every sequence, x bf16 [seqs][width]: the stream after the last block.  What is refused leaves
+        the state as it was, as of ``prompt``."""
         if x.dim() != 2 or x.shape[1] != self.width or x.dtype != torch.bfloat16:
             raise ValueError(f"tokens must be bf16 [sequences][{self.width}]")
-        state.take([1] * x.shape[0])
+        after = state.room([1] * x.shape[0])
+        quant._matrix(x, "x", self._device(state, x, "x"), None, None, torch.bfloat16)
+        state.held = after
         return self._step(state, x, trace)
 
     def _step(self, state: State, x: torch.Tensor, trace=None) -> torch.Tensor:
@@ -226,13 +248,16 @@ class Decoder:
         return x
 
     def answer(self, state: State, tokens: torch.Tensor, u: torch.Tensor, **filters):
-        """One step on a token of every sequence, tokens int32 [seqs]: the (tokens, logprob) drawn to follow them.  A
-        ValueError, and nothing done, where a sequence has no room."""
+        """One step on a token of every sequence, tokens int32 [seqs]: the (tokens, logprob) drawn to follow them, as
+        ``pick`` has it.  What is refused leaves the state as it was, as of ``prompt``."""
         self._tokens()
         if tokens.shape != (len(state.held),) or tokens.dtype != torch.int32 or u.shape != tokens.shape:
             raise ValueError(f"there are {len(state.held)} sequences: one int32 token and one random number for each")
-        state.take([1] * len(state.held))
-        return self.pick(self._step(state, self.embed(tokens)), u, **filters)
+        after = state.room([1] * len(state.held))
+        sample._operands(self._device(state, u, "u"), len(state.held), u, **filters)
+        x = self.embed(tokens)
+        state.held = after
+        return self.pick(self._step(state, x), u, **filters)
 
 
 class Steps:

@@ -43,6 +43,23 @@ def tokens_workspace_bytes(rows: int, vocab: int, dtype=torch.float32) -> int:
     return int(n)
 
 
+def _operands(dev: int, rows: int, u, temperature=None, top_k=None, top_p=None, min_p=None, out=None, logprob=None, ws=None) -> None:
+    """Refuses what a draw for `rows` rows on device dev cannot read, or write."""
+    _vector(u, "u", dev, rows, torch.float32)
+    if temperature is not None:
+        _vector(temperature, "temperature", dev, rows, torch.float32)
+    if top_k is not None:
+        _vector(top_k, "top_k", dev, rows, torch.int32)
+    if top_p is not None:
+        _vector(top_p, "top_p", dev, rows, torch.float32)
+    if min_p is not None:
+        _vector(min_p, "min_p", dev, rows, torch.float32)
+    if out is not None:
+        _vector(out, "out", dev, rows, torch.int32)
+    if logprob is not None:
+        _vector(logprob, "logprob", dev, rows, torch.float32)
+
+
 def tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=None, logprob=None, ws=None, stream=None):
     """Draws a token of each row of logits [rows][vocab] (fp32 or bf16): (token int32 [rows], logprob fp32 [rows]), logprob
     the logarithm of the probability that the filters leave it.
@@ -55,23 +72,11 @@ def tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=
     dev = _here(logits, "logits")
     stride = _matrix(logits, "logits", dev, None, None, torch.bfloat16, torch.float32)
     rows, vocab = logits.shape
-    _vector(u, "u", dev, rows, torch.float32)
-    if temperature is not None:
-        _vector(temperature, "temperature", dev, rows, torch.float32)
-    if top_k is not None:
-        _vector(top_k, "top_k", dev, rows, torch.int32)
-    if top_p is not None:
-        _vector(top_p, "top_p", dev, rows, torch.float32)
-    if min_p is not None:
-        _vector(min_p, "min_p", dev, rows, torch.float32)
+    _operands(dev, rows, u, temperature, top_k, top_p, min_p, out, logprob)
     if out is None:
         out = _empty(logits, rows, torch.int32, stream)
-    else:
-        _vector(out, "out", dev, rows, torch.int32)
     if logprob is None:
         logprob = _empty(logits, rows, torch.float32, stream)
-    else:
-        _vector(logprob, "logprob", dev, rows, torch.float32)
     L, code = lib(), _CODE[logits.dtype]
     wp, wn = _workspace(L.sample_tokens_workspace_bytes(rows, vocab, code), "sample_tokens", ws, logits, dev, stream)
     rc = L.sample_tokens(rows, vocab, code, logits.data_ptr(), stride, u.data_ptr(), _ptr(temperature), _ptr(top_k), _ptr(top_p),

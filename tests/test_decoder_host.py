@@ -71,3 +71,14 @@ def test_a_pick_stays_on_the_stream_of_its_logits():
     for k in (dict(stream=0), dict(top_q=None)):
         with pytest.raises(TypeError):
             dec.pick(tokens(2), torch.zeros(2), **k)
+
+
+def test_operands_off_the_device_leave_the_state():
+    dec, state = made([3, 4], 10)
+    dec.vocab, dec.embedding = 50, torch.zeros(50, 8)
+    state.lens = torch.tensor([3, 4], dtype=torch.int32)
+    for f in (lambda: dec.step(state, tokens(2)), lambda: dec.prompt(state, [tokens(2), tokens(0)]),
+              lambda: dec.answer(state, torch.zeros(2, dtype=torch.int32), torch.zeros(2))):
+        with pytest.raises(ValueError, match="device"):
+            f()
+        assert state.held == state.lens.tolist() == [3, 4]

@@ -239,3 +239,41 @@ def test_no_room_and_no_vocabulary():
     for f in (lambda: plain.embed(t), lambda: plain.logits(torch.zeros(1, 256)), lambda: plain.answer(state, t, u)):
         with pytest.raises(ValueError, match="vocabulary"):
             f()
+
+
+@pytest.mark.parametrize("float8", [False, True], ids=["int8", "float8"])
+def test_a_refused_call_leaves_the_state(float8):
+    """Shapes, types, devices, filters and states that do not fit: lengths and every byte of the caches stay, and the call
+    that follows gives what it gives without them."""
+    def made():
+        dec = decoder.Decoder(blocks=2, width=256, heads=4, kv_heads=2, head_dim=64, inner=520, seed=3, float8=float8, vocab=5003)
+        return dec, decoder.State(dec, seqs=3, max_len=150, page_size=16, seed=4)
+    dec, state = made()
+    _, twin = made()
+    for st in (state, twin):
+        out = dec.prompt(st, streams(dec, [30, 9, 61], 24))
+    x = torch.stack([y[-1] for y in out])
+    t, u = torch.tensor([5, 4000, 17], dtype=torch.int32, device="cuda"), torch.full((3,), 0.4, device="cuda")
+    ones, k = torch.ones(3, device="cuda"), torch.ones(3, dtype=torch.int32, device="cuda")
+    other = decoder.Decoder(blocks=1, width=256, heads=4, kv_heads=2, head_dim=64, inner=520, float8=float8, vocab=50)
+    kind = decoder.Decoder(blocks=2, width=256, heads=4, kv_heads=2, head_dim=64, inner=520, float8=not float8, vocab=50)
+    bad = [lambda f=f: dec.answer(state, t, u, **f) for f in (
+        dict(top_p=0.9), dict(top_p=ones[:2]), dict(top_p=ones.double()), dict(temperature=ones.cpu()), dict(temperature=k),
+        dict(top_k=ones), dict(top_k=k.long()), dict(min_p=ones[:2]), dict(top_q=ones), dict(stream=0), dict(out=ones),
+        dict(out=k[:1]), dict(logprob=k), dict(logprob=ones.cpu()))]
+    bad += [lambda f=f: decoder.capture_answer(dec, state, t, u, **f) for f in (dict(top_p=0.9), dict(top_k=ones))]
+    bad += [lambda: dec.answer(state, t, u.double()), lambda: dec.answer(state, t, u.cpu()), lambda: dec.step(state, x.cpu()),
+            lambda: dec.step(state, x.t().contiguous().t()), lambda: dec.prompt(state, [x.cpu()] * 3),
+            lambda: dec.prompt(state, [x, x.cpu(), x]), lambda: other.step(state, x), lambda: kind.step(state, x),
+            lambda: kind.answer(state, t, u), lambda: kind.prompt(state, [x] * 3)]
+    held = lambda: [bits(c) for cache in state.caches for c in (cache.k_codes, cache.v_codes, cache.k_exps, cache.v_exps)]  # noqa: E731
+    before = held()
+    for i, f in enumerate(bad):
+        with pytest.raises((ValueError, TypeError)):
+            f()
+        assert state.held == state.lens.tolist() == [30, 9, 61], i
+        assert all(torch.equal(p, q) for p, q in zip(before, held())), i
+    got, want = (dec.answer(st, t, u, temperature=ones, top_k=k * 40, top_p=0.9 * ones, out=k.clone(), logprob=ones.clone())
+                 for st in (state, twin))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and state.lens.tolist() == [31, 10, 62]
+    assert torch.equal(dec.step(state, x), dec.step(twin, x))
