@@ -67,7 +67,8 @@ class State:
         pages = -(-max_len // page_size)
         g = torch.Generator().manual_seed(seed)      # pages in no order, as a server that reuses them has them
         table = torch.randperm(seqs * pages, generator=g).reshape(seqs, pages).to(torch.int32)
-        self.table, self.slot = table.cuda(), self.slots_of(table, max_len, page_size).cuda()
+        self.table = table.cuda()
+        self.slot = None if dec.float8 else self.slots_of(table, max_len, page_size).cuda()   # the 8-bit cache takes the table
         cache = quant.KV8Cache if dec.float8 else quant.KV4Cache
         self.caches = [cache.allocate(seqs * pages, dec.kv_heads, page_size, dec.head_dim) for _ in dec.blocks]
         self.lens = torch.zeros(seqs, dtype=torch.int32, device="cuda")
@@ -220,9 +221,10 @@ class Decoder:
             quant._tensor(x, "a sequence's tokens", dev, torch.bfloat16)
         state.held = after
         starts = torch.tensor([0, *torch.tensor(news).cumsum(0).tolist()], dtype=torch.int32).cuda()
-        seq = torch.repeat_interleave(torch.arange(len(xs)), torch.tensor(news)).cuda()
-        place = torch.arange(sum(news), device="cuda") - starts[seq] + state.lens[seq]
-        slots = state.slots(seq, place)
+        slots = None
+        if not self.float8:
+            seq = torch.repeat_interleave(torch.arange(len(xs)), torch.tensor(news)).cuda()
+            slots = state.slots(seq, torch.arange(sum(news), device="cuda") - starts[seq] + state.lens[seq])
         state.lens += (starts[1:] - starts[:-1])
         x = torch.cat(xs)
         for b, cache in zip(self.blocks, state.caches):
@@ -240,8 +242,7 @@ class Decoder:
         return self._step(state, x, trace)
 
     def _step(self, state: State, x: torch.Tensor, trace=None) -> torch.Tensor:
-        seq = torch.arange(x.shape[0], device="cuda")
-        slots = state.slots(seq, state.lens)
+        slots = None if self.float8 else state.slots(torch.arange(x.shape[0], device="cuda"), state.lens)
         state.lens += 1
         for b, cache in zip(self.blocks, state.caches):
             x = self._block(b, cache, x, slots, state.table, state.lens, None, 1, state.max_len, trace)

@@ -277,3 +277,12 @@ def test_a_refused_call_leaves_the_state(float8):
                  for st in (state, twin))
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and state.lens.tolist() == [31, 10, 62]
     assert torch.equal(dec.step(state, x), dec.step(twin, x))
+
+
+def test_the_8_bit_form_asks_for_no_slots(monkeypatch):
+    """Its cache takes the page table: what the 4-bit cache's slots take would be launches for nothing."""
+    dec, state = small()
+    monkeypatch.setattr(decoder.State, "slots", None)
+    out = dec.prompt(state, streams(dec, [30, 9, 61], 25))
+    dec.step(state, torch.stack([y[-1] for y in out]))
+    assert state.lens.tolist() == [31, 10, 62]
