@@ -281,9 +281,13 @@ __device__ __forceinline__ void attend_few(const AttArgs &a)
             const uint64_t row = (uint64_t)pg * (unsigned)page_rows + (unsigned)(head_row + place[k]);
             load_words<NU * W>(a.c.kc + row * (D / 2 * W) + quad * (D / 8 * W), to.kc[k]);
             load_words<NU * W>(a.c.vc + row * (D / 2 * W) + quad * (D / 8 * W), to.vc[k]);
-            const uint64_t e = F::GROUPS ? row * (D / 32) + g0 : exponent_of(a.c, pg, kvh, place[k]);
-            to.ke[k][0] = a.c.ke[e];
-            to.ve[k][0] = a.c.ve[e];
+            if constexpr (F::GROUPS) {   // apart: with one index for either format they take 3% longer
+                to.ke[k][0] = a.c.ke[row * (D / 32) + g0];
+                to.ve[k][0] = a.c.ve[row * (D / 32) + g0];
+            } else {
+                const uint64_t e = exponent_of(a.c, pg, kvh, place[k]);
+                to.ke[k][0] = a.c.ke[e], to.ve[k][0] = a.c.ve[e];
+            }
             if constexpr (NE == 2) {
                 to.ke[k][1] = a.c.ke[row * (D / 32) + g1];
                 to.ve[k][1] = a.c.ve[row * (D / 32) + g1];
@@ -296,9 +300,8 @@ __device__ __forceinline__ void attend_few(const AttArgs &a)
             if (t0 + 256 < hi) look(t0 + 256);
         }
         f32x4 sc[2][NB];
-        const bool edge = t0 < from || t0 + 32 > all;   // holds places that not every row sees
         if constexpr (!F::GROUPS)
-            if (edge)
+            if (t0 < from || t0 + 32 > all)   // places that not every row sees
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -308,7 +311,13 @@ __device__ __forceinline__ void attend_few(const AttArgs &a)
         for (int k = 0; k < 2; ++k) {
             float ks[NE], vs[NE];
 #pragma unroll
-            for (int e = 0; e < NE; ++e) ks[e] = F::keys(cur.ke[k][e], cur.ve[k][e]), vs[e] = F::values(cur.ve[k][e]);
+            for (int e = 0; e < NE; ++e) {
+                if constexpr (F::GROUPS) {   // F's, with one comparison: over heads of 64 single tokens take 1% less so
+                    const bool bad = cur.ve[k][e] > (uint32_t)kMaxExp;
+                    ks[e] = F::scale(bad ? 255u : cur.ke[k][e]);
+                    vs[e] = F::scale(bad ? 127u : cur.ve[k][e]);
+                } else ks[e] = F::keys(cur.ke[k][e], cur.ve[k][e]), vs[e] = F::values(cur.ve[k][e]);
+            }
 #pragma unroll
             for (int b = 0; b < NB; ++b) sc[k][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -322,7 +331,7 @@ __device__ __forceinline__ void attend_few(const AttArgs &a)
                     F::widen8(cur.vc[k] + W * u, e == 0 ? vs[0] : vs[NE - 1]);
             }
         }
-        if (edge) {
+        if (t0 < from || t0 + 32 > all) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
