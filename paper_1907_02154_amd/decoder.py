@@ -301,6 +301,8 @@ def capture_step(dec: Decoder, state: State, x: torch.Tensor):
 def capture_answer(dec: Decoder, state: State, tokens: torch.Tensor, u: torch.Tensor, **filters):
     """An answer to the tensor of tokens as a HIP graph: (``Steps`` to replay, logprob).  A replay puts the tokens drawn by
     u in the place of those that it read, for the next one, whose u the caller fills in before."""
+    quant._vector(tokens, "tokens", quant._here(tokens, "tokens"), len(state.held), torch.int32)   # replays write it
+
     def again():
         drawn, logprob = dec.pick(dec._step(state, dec.embed(tokens)), u, **filters)
         tokens.copy_(drawn)

@@ -82,3 +82,29 @@ def test_operands_off_the_device_leave_the_state():
         with pytest.raises(ValueError, match="device"):
             f()
         assert state.held == state.lens.tolist() == [3, 4]
+
+
+class OnDevice(torch.Tensor):
+    """A tensor that says it is on device 0."""
+    def get_device(self):
+        return 0
+
+    is_cuda = True
+
+
+def on_device(t):
+    return t.as_subclass(OnDevice)
+
+
+def test_tokens_that_a_replay_cannot_write_are_not_captured(monkeypatch):
+    """Off the device, or one element for all sequences: refused before the state or a capture is touched."""
+    dec, state = made([3, 4], 10)
+    dec.vocab = 50
+    u = torch.zeros(2)
+    with pytest.raises(ValueError, match="device"):
+        decoder.capture_answer(dec, state, torch.zeros(2, dtype=torch.int32), u)
+    monkeypatch.setattr(decoder.quant, "_getdevice", lambda: 0)
+    for t in (torch.zeros(1, dtype=torch.int32).expand(2), torch.zeros(2, dtype=torch.int64), torch.zeros(3, dtype=torch.int32)):
+        with pytest.raises((ValueError, TypeError), match="tokens must be"):
+            decoder.capture_answer(dec, state, on_device(t), u)
+    assert state.held == [3, 4]
