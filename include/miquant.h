@@ -226,7 +226,10 @@ int quant_matmul_f8_describe(long M, long N, long K, const void *a, long a_strid
  * two in each head.  block divides page_size and is 256 at most.
  * A token whose keys or values of a head hold a NaN or an infinity is held with
  * NaN for its keys there and 0 for its values, and counts nothing to the
- * exponents.  An exponent byte above 246 is never written.
+ * exponents.  An exponent byte above 246 is never written, nor a code of values
+ * that is no number.  A cache that is filled by other means has to keep to that:
+ * what attention makes of rows that see such a code is NaN in some tiles and
+ * finite in others.
  * head_dim: 32, 64, 96, 128, 192 or 256.  Codes are 16-byte aligned. */
 typedef struct quant_kv8 {
     void *k_codes, *k_exps, *v_codes, *v_exps;
@@ -262,7 +265,8 @@ int quant_kv8_read(const quant_kv8 *cache, long tokens, const int32_t *slots, in
 
 /* Attention of new tokens over the 8-bit cache, which holds them already: as
  * quant_attention_kv4 in every argument, place, mask, result, rounding and
- * error.  A row that sees a token whose keys or values are not finite is NaN. */
+ * error.  A row that sees a token that was written with keys or values that are
+ * not finite is NaN. */
 long quant_attention_kv8_workspace_bytes(const quant_kv8 *cache, int seqs, int heads, int max_new, int max_len,
                                          int causal, int window);
 int quant_attention_kv8(const quant_kv8 *cache, int seqs, int heads, long tokens, const void *q, long q_stride,

@@ -688,7 +688,8 @@ __device__ __forceinline__ void wide_barrier() { asm volatile("s_waitcnt lgkmcnt
 //
 // Two prompts of 4096 tokens, causal, 32 heads on 8 key heads: of 32 channels 133
 // us, of 64 173 (755 TFLOP/s); 20 heads of 192 on 5, 283 us (870), 16 of 256 on
-// 4, 294 (890), all in 4 bits.  Bound at few channels by vector instructions and products that
+// 4, 294 (890), all in 4 bits; in 8 bits, where these take 130, 165, 292 and 290, 137,
+// 176, 295 and 318.  Bound at few channels by vector instructions and products that
 // take turns, for the barrier keeps a SIMD's wavefronts in much the same phase: of
 // a SIMD's cycles the ones take 56% at 64 channels and the others 34%, 68 and 21%
 // at 32.  Of the vector work the exponentials are less than a third.  At 256
@@ -804,7 +805,7 @@ __global__ __launch_bounds__(512, D <= 64 ? 4 : 2) void attend_kv8_wide_kernel(A
 // step come by themselves.
 //
 // Two prompts of 4096 tokens, causal, 32 heads of 128 on 8 key heads: 268 us, 975
-// TFLOP/s (of 96: 229 us, 857); in 8 bits 283.  The matrix cores alone would take
+// TFLOP/s (of 96: 229 us, 857); in 8 bits 283 (241).  The matrix cores alone would take
 // 110 at full clock; with what each product has beside it a SIMD's product takes about 43
 // cycles in place of 32 in a loop without memory (measured with four
 // multiply-adds and two exponentials), which is 150, and the rest is barriers, LDS

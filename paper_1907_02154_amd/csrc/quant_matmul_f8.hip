@@ -265,9 +265,10 @@ using Number = std::integral_constant<int, N>;
 // lanes 64; LDS chunks are rotated so that both orders of rows are free of
 // conflicts.  Exponents come as four bytes a register, of which the instruction
 // picks one.
-// 8192 x 8192 outputs, K = 4096: 215 us, 2.55 PFLOP/s (the tile above: 255); K =
-// 8192, half the outputs: 206, 2.67 (246); the library's product of the first size
-// without exponents 224, its best, 8192 x 8192 x 8192, 2.75 PFLOP/s.  The
+// 8192 x 8192 outputs, K = 4096: 207 to 215 us, 2.55 to 2.66 PFLOP/s (the tile
+// above: 255); K = 8192, half the outputs: 196 to 206 (246).  The library's products
+// of these sizes without exponents took 180 and 168 on one card, 224 for the first
+// on another, and at its best, 8192 x 8192 x 8192, 3.3 and 2.75 PFLOP/s.  The
 // instruction alone, on such values in registers, reaches 3.7 to 4.5, as the
 // clock follows the power it takes; a product has a turn of 44 to 50 cycles
 // here, of which it takes 32.  Taking the next tile's first blocks while the last
@@ -434,11 +435,13 @@ __global__ __launch_bounds__(256) void matmul_f8_large_kernel(F8Args f)
     }
 }
 
-// Costs as measured for 8-bit integers, whose products take as long; the last
-// one's its own.  With every tile timed at K = 1024 and 4096, N = 1024, 4096 and
-// 11000, M from 1 to 2048 and both outputs, the cheapest by this rule is the
-// fastest or a few percent off; worst are 128 tokens, 1024 channels and K = 4096,
-// 6.0 us where tiles of 16 x 32 take 5.3.
+// Costs as measured for 8-bit integers, whose products take as long as those with
+// bf16 outputs; the last one's its own.  fp32 outputs take up to twice as long by
+// any tile, which leaves the order.  With every tile timed at K = 1024 to 4096, N =
+// 1000 to 11000, M from 1 to 8192 and both outputs, the cheapest by this rule is
+// the fastest or a few percent off (fp32 as bf16); worst are 128 tokens, 1024
+// channels and K = 4096, 6.0 us where tiles of 16 x 32 take 5.3, and 2048 tokens,
+// 11000 channels, 104 where the largest tile takes 95.
 constexpr Tile kTiles[] = {
     {16, 16, 1, 1, 4, 4, 2, 3.4f, 3.8f},    {16, 32, 1, 2, 4, 3, 2, 3.8f, 5.0f},    {32, 64, 1, 4, 4, 3, 1, 6.6f, 0.0f},
     {64, 32, 2, 2, 4, 3, 1, 6.6f, 0.0f},    {64, 64, 2, 2, 2, 4, 1, 9.3f, 0.0f},    {128, 64, 4, 2, 2, 3, 1, 13.8f, 0.0f},

@@ -990,7 +990,8 @@ __device__ __forceinline__ void Picker<T, NT, SHORT>::run(long r)
 // candidates by itself: 18 us without both.  Up to 4096 tokens take 256
 // threads, whose barriers are shorter, more of them 512: 256 rows in fp32 with
 // top_p .9, 2000 tokens 14 against 17 us, 4096 17 either way, 16000 32 against 27,
-// 32000 56 against 39.
+// 32000 56 against 39.  However few rows there are each has one work-group: one of
+// 128000 with top_p .9 takes 73 us, in bf16 (below) 47.
 template <typename T, int NT, bool SHORT>
 __global__ __launch_bounds__(NT) void sample_rows_kernel(SampleArgs a)
 {
@@ -1016,6 +1017,10 @@ __global__ __launch_bounds__(NT) void sample_rows_kernel(SampleArgs a)
 // are asked for, or the first, are not counted: they go through the search that
 // rows of fp32 use (top_k 50, 256 rows of 32000 18 against 28, of 128000 34
 // against 51; that search with 512 threads 17 and 36).
+// Tokens that are masked by the type's lowest value, not by minus infinity, lie
+// outside the counters' range: of more than 2048 of them the first pass is lost, and
+// the 256 rows take 163 us (without filters 121 where minus infinity takes 43; of
+// 32000 72 against 27; with top_k 50 as long, 34).
 // Measured beside it: the draw's run by one wavefront, unit by unit, 58 (11 of
 // them that run); six units in flight in place of three no change; twice as many
 // runs 1 us less in the draw and 2.5 more in the second pass.

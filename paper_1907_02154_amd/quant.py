@@ -532,8 +532,8 @@ def _read(slots, c, what: str, k, v, dtype, stream):
 
 class KV8Cache:
     """A paged cache of keys and values in 8-bit floats: e4m3 [pages][heads][page_size][head_dim] and exponent bytes uint8
-    [pages][heads][page_size / block] of each, `block` places of a page sharing one in each head (the format:
-    ``include/miquant.h``)."""
+    [pages][heads][page_size / block] of each, `block` places of a page sharing one in each head (the format, which tensors
+    that the caller fills keep to: ``include/miquant.h``)."""
 
     __slots__ = ("k_codes", "k_exps", "v_codes", "v_exps", "pages", "heads", "page_size", "head_dim", "block", "device",
                  "_desc")
